@@ -355,7 +355,7 @@ def _append(st):
 def _step(a):
     """2^e for the smallest e in -40 .. 40 with 127 * 2^e >= a."""
     m, x = torch.frexp(a)
-    return torch.exp2((x - 7 + (m > 127 / 128).int()).clamp(-40, 40).float())
+    return torch.exp2(torch.where(a > 0, x - 7 + (m > 127 / 128).int(), -40).clamp(-40, 40).float())
 
 
 def _finite(x):
