@@ -30,7 +30,9 @@ EXPORTS = ("icarus_create", "icarus_destroy", "icarus_last_error", "icarus_works
            "icarus_cache_create", "icarus_cache_destroy", "icarus_cache_last_error", "icarus_cache_acquire", "icarus_cache_extend",
            "icarus_cache_commit", "icarus_cache_release", "icarus_cache_get_stats", "icarus_set_full_decoders",
            "icarus_validate_block_tables", "icarus_set_attn_piece_limit", "icarus_attn_shared_kv_static", "icarus_bench_read",
-           "icarus_gemm_tile_order", "icarus_gemm_choice", "icarus_gemm_group_tile", "icarus_append_in_tiles", "icarus_prefill_plan", "icarus_row_order", "icarus_gemm")
+           "icarus_gemm_tile_order", "icarus_gemm_choice", "icarus_gemm_group_tile", "icarus_append_in_tiles", "icarus_prefill_plan", "icarus_row_order", "icarus_gemm",
+           "icarus_extend_sequences", "icarus_rope_append", "icarus_key_bounds", "icarus_select_workspace_bytes", "icarus_select_blocks",
+           "icarus_attn_blocks_workspace_bytes", "icarus_attn_blocks")
 
 PHASES = ("norm", "lora", "gemm_qkv", "rope_append", "attn", "attn_merge", "gemm_o", "gemm_gateup", "gemm_down",
           "elementwise")
@@ -168,6 +170,21 @@ def _load():
     lib.icarus_cache_release.argtypes = [vp, vp, i32]
     lib.icarus_set_full_decoders.restype = C.c_int
     lib.icarus_set_full_decoders.argtypes = [vp, C.POINTER(_Full)]
+    i64 = C.c_int64
+    lib.icarus_extend_sequences.restype = C.c_int
+    lib.icarus_extend_sequences.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.icarus_rope_append.restype = C.c_int
+    lib.icarus_rope_append.argtypes = [vp, vp, i64, i32, vp, vp, vp, vp, vp]
+    lib.icarus_key_bounds.restype = C.c_int
+    lib.icarus_key_bounds.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp]
+    lib.icarus_select_workspace_bytes.restype = sz
+    lib.icarus_select_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.icarus_select_blocks.restype = C.c_int
+    lib.icarus_select_blocks.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+    lib.icarus_attn_blocks_workspace_bytes.restype = sz
+    lib.icarus_attn_blocks_workspace_bytes.argtypes = [vp, i32, i32, i32]
+    lib.icarus_attn_blocks.restype = C.c_int
+    lib.icarus_attn_blocks.argtypes = [vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp]
     lib.icarus_cache_get_stats.restype = C.c_int
     lib.icarus_cache_get_stats.argtypes = [vp, C.POINTER(_CacheStats)]
     return lib
@@ -370,6 +387,35 @@ def gemm(x, w, tile, slices: int = 1, fused: bool = False, t=None, b=None, resid
     if rc != 0:
         raise IcarusError(rc, "icarus_gemm failed")
     return y
+
+
+class SequenceMap:
+    """Device arrays that IcarusLayer.extend_sequences fills, kept by the caller (a captured graph replays into the same ones): kv_lens [S],
+    row_start [S + 1], row_seq, row_pos, row_slot [max_rows], counts [2] (free ids taken, sequences refused); one allocation."""
+
+    def __init__(self, n_seqs: int, max_rows: int, device):
+        S, R = int(n_seqs), int(max_rows)
+        self.n_seqs, self.max_rows = S, R
+        self.row_slot = torch.empty(R, dtype=torch.int64, device=device)
+        ints = torch.empty(2 * S + 3 + 2 * R, dtype=torch.int32, device=device)
+        self.kv_lens, self.row_start, self.counts, self.row_seq, self.row_pos = ints.split([S, S + 1, 2, R, R])
+
+
+class _OnDevice:
+    """The device a call's tensors are on, made current while the library launches there."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.device.index not in (None, self.before):
+            torch.cuda.set_device(self.device)
+        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def __exit__(self, *exc):
+        if torch.cuda.current_device() != self.before:
+            torch.cuda.set_device(self.before)
 
 
 class IcarusLayer:
@@ -590,6 +636,134 @@ class IcarusLayer:
         self._check(_lib.icarus_attn_shared_kv(self._h, _ptr(q), _ptr(kv_pool), _ptr(block_tables), max_blocks, S,
                                                _ptr(kv_lens), R, _ptr(row_seq), _ptr(out), _ptr(ws), ws.numel(),
                                                self._stream(q.device)))
+        return out
+
+    # -- lengths on the device (include/icarus_blocks.h) -----------------------------
+    def _lens(self, S, device, **arrays):
+        for name, t in arrays.items():
+            if t is not None:
+                _want(t, name, torch.int32, (S,), device)
+
+    def _table(self, block_tables):
+        _want(block_tables, "block_tables", torch.int32)
+        if block_tables.dim() != 2:
+            raise ValueError(f"block_tables: need [S, max_blocks], got {tuple(block_tables.shape)}")
+        return block_tables.shape[0], block_tables.shape[1], block_tables.device
+
+    def _pool(self, kv_pool, device):
+        want = self.cfg.pool_shape()
+        _want(kv_pool, "kv_pool", self.cfg.pool_dtype, None, device)
+        if kv_pool.dim() != 4 or tuple(kv_pool.shape[1:]) != want[1:] or kv_pool.shape[0] < want[0]:
+            raise ValueError(f"kv_pool: shape {tuple(kv_pool.shape)}, expected at least {want[0]} blocks of {want[1:]}")
+
+    def _bounds(self, codes, scales, device):
+        c = self.cfg
+        _want(codes, "codes", torch.int8, (c.num_blocks, c.n_kv_heads, 2, c.head_dim), device)
+        _want(scales, "scales", torch.float32, (c.num_blocks, c.n_kv_heads), device)
+
+    def _queries(self, q, row_start, S, device):
+        c = self.cfg
+        _want(q, "q", c.torch_dtype, None, device)
+        if q.dim() != 3 or tuple(q.shape[1:]) != (c.n_q_heads, c.head_dim):
+            raise ValueError(f"q: shape {tuple(q.shape)}, expected [R, {c.n_q_heads}, {c.head_dim}]")
+        _want(row_start, "row_start", torch.int32, (S + 1,), device)
+
+    def new_key_bounds(self, device="cuda"):
+        """(codes, scales) for key_bounds and select_blocks, for all blocks of the pool."""
+        c = self.cfg
+        return (torch.zeros(c.num_blocks, c.n_kv_heads, 2, c.head_dim, dtype=torch.int8, device=device),
+                torch.ones(c.num_blocks, c.n_kv_heads, dtype=torch.float32, device=device))
+
+    def extend_sequences(self, seq_map, ctx_lens, new_lens, block_tables, free_ids, free_used, streams=None):
+        """Fills `seq_map` (a SequenceMap) and the new entries of block_tables; all arrays are device tensors.  Returns seq_map."""
+        S, max_blocks, dev = self._table(block_tables)
+        if seq_map.n_seqs != S:
+            raise ValueError(f"seq_map is for {seq_map.n_seqs} sequences, block_tables has {S}")
+        self._lens(S, dev, ctx_lens=ctx_lens, new_lens=new_lens, streams=streams, kv_lens=seq_map.kv_lens)
+        _want(free_ids, "free_ids", torch.int32, (free_ids.numel(),), dev)
+        _want(free_used, "free_used", torch.int32, (1,), dev)
+        m = seq_map
+        with _OnDevice(dev) as stream:
+            self._check(_lib.icarus_extend_sequences(
+                self._h, S, ctx_lens.data_ptr(), new_lens.data_ptr(), _ptr(streams), block_tables.data_ptr(), max_blocks, free_ids.data_ptr(),
+                free_ids.numel(), free_used.data_ptr(), m.max_rows, m.kv_lens.data_ptr(), m.row_start.data_ptr(), m.row_seq.data_ptr(),
+                m.row_pos.data_ptr(), m.row_slot.data_ptr(), m.counts.data_ptr(), stream))
+        return m
+
+    def rope_append(self, qkv, row_pos, row_slot, kv_pool, q_out=None):
+        """qkv [R, >= (Hq + 2 Hkv) * D], rows may be strided.  Returns q_out [R, Hq, D]; rows with a negative position are left as they were."""
+        c = self.cfg
+        if not isinstance(qkv, torch.Tensor):
+            raise TypeError(f"qkv: expected a torch tensor, got {type(qkv).__name__}")
+        width = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
+        if qkv.dim() != 2 or qkv.shape[1] < width or qkv.stride(1) != 1 or (qkv.shape[0] > 1 and qkv.stride(0) < width):
+            raise ValueError(f"qkv: shape {tuple(qkv.shape)} with strides {tuple(qkv.stride())}, expected rows of {width} contiguous elements")
+        if qkv.dtype != c.torch_dtype:
+            raise TypeError(f"qkv: dtype {qkv.dtype}, the library reads {c.torch_dtype}")
+        if not qkv.is_cuda:
+            raise ValueError("qkv: must be a device tensor")
+        R, dev = qkv.shape[0], qkv.device
+        _want(row_pos, "row_pos", torch.int32, (R,), dev)
+        _want(row_slot, "row_slot", torch.int64, (R,), dev)
+        self._pool(kv_pool, dev)
+        if q_out is None:
+            q_out = torch.zeros(R, c.n_q_heads, c.head_dim, dtype=c.torch_dtype, device=dev)
+        _want(q_out, "q_out", c.torch_dtype, (R, c.n_q_heads, c.head_dim), dev)
+        with _OnDevice(dev) as stream:
+            self._check(_lib.icarus_rope_append(self._h, qkv.data_ptr(), qkv.stride(0) if R > 1 else max(qkv.stride(0), width), R,
+                                                row_pos.data_ptr(), row_slot.data_ptr(), q_out.data_ptr(), kv_pool.data_ptr(), stream))
+        return q_out
+
+    def key_bounds(self, kv_pool, block_tables, from_lens, to_lens, codes, scales, max_new: int = 0):
+        """Bounds of the keys of the blocks that hold positions from_lens .. to_lens - 1, into codes and scales (new_key_bounds)."""
+        S, max_blocks, dev = self._table(block_tables)
+        self._pool(kv_pool, dev)
+        self._lens(S, dev, from_lens=from_lens, to_lens=to_lens)
+        self._bounds(codes, scales, dev)
+        with _OnDevice(dev) as stream:
+            self._check(_lib.icarus_key_bounds(self._h, kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S, from_lens.data_ptr(),
+                                               to_lens.data_ptr(), int(max_new), codes.data_ptr(), scales.data_ptr(), stream))
+
+    def select_blocks(self, q, codes, scales, block_tables, kv_lens, row_start, blocks, counts, first: int = 1, last: int = 2,
+                      seq_rows: int = 0, workspace=None):
+        """blocks [S, Hkv, top_k] and counts [S] receive each sequence's selected blocks."""
+        c = self.cfg
+        S, max_blocks, dev = self._table(block_tables)
+        self._queries(q, row_start, S, dev)
+        self._bounds(codes, scales, dev)
+        self._lens(S, dev, kv_lens=kv_lens, counts=counts)
+        if blocks.dim() != 3:
+            raise ValueError(f"blocks: need [S, Hkv, top_k], got {tuple(blocks.shape)}")
+        _want(blocks, "blocks", torch.int32, (S, c.n_kv_heads, blocks.shape[2]), dev)
+        if workspace is None:
+            workspace = torch.empty(_lib.icarus_select_workspace_bytes(self._h, S, max_blocks), dtype=torch.uint8, device=dev)
+        with _OnDevice(dev) as stream:
+            self._check(_lib.icarus_select_blocks(
+                self._h, q.data_ptr(), codes.data_ptr(), scales.data_ptr(), block_tables.data_ptr(), max_blocks, S, kv_lens.data_ptr(), q.shape[0],
+                row_start.data_ptr(), int(seq_rows), blocks.shape[2], int(first), int(last), blocks.data_ptr(), counts.data_ptr(),
+                workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
+        return blocks, counts
+
+    def attn_blocks(self, q, kv_pool, block_tables, kv_lens, row_start, blocks, counts, out=None, seq_rows: int = 0, workspace=None):
+        """Attention of the rows row_start[s] .. row_start[s + 1] - 1 over the listed blocks of sequence s; rows of no sequence are left as they were."""
+        c = self.cfg
+        S, max_blocks, dev = self._table(block_tables)
+        self._queries(q, row_start, S, dev)
+        self._pool(kv_pool, dev)
+        self._lens(S, dev, kv_lens=kv_lens, counts=counts)
+        if blocks.dim() != 3:
+            raise ValueError(f"blocks: need [S, Hkv, max_selected], got {tuple(blocks.shape)}")
+        _want(blocks, "blocks", torch.int32, (S, c.n_kv_heads, blocks.shape[2]), dev)
+        if out is None:
+            out = torch.zeros_like(q)
+        _want(out, "out", c.torch_dtype, tuple(q.shape), dev)
+        if workspace is None:
+            workspace = torch.empty(_lib.icarus_attn_blocks_workspace_bytes(self._h, S, q.shape[0], blocks.shape[2]), dtype=torch.uint8, device=dev)
+        with _OnDevice(dev) as stream:
+            self._check(_lib.icarus_attn_blocks(
+                self._h, q.data_ptr(), kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S, kv_lens.data_ptr(), q.shape[0],
+                row_start.data_ptr(), int(seq_rows), blocks.data_ptr(), counts.data_ptr(), blocks.shape[2], out.data_ptr(),
+                workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
         return out
 
 

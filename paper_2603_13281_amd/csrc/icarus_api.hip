@@ -13,8 +13,8 @@
 #include <new>
 #include <vector>
 
-#include "../../include/icarus.h"
-#include "kernels.h"
+#include "../../include/icarus_blocks.h"
+#include "block_ops.h"
 
 using namespace icarus;
 
@@ -1993,6 +1993,146 @@ icarus_status icarus_stack_decode(icarus_stack *st, void *const *kv_pools, const
     if (workspace_bytes < SL.total) return stack_fail(st, ICARUS_ERR_CAPACITY, "workspace too small");
     return run_stack(st, (char *)workspace, SL, pr, kv_pools, block_tables, max_blocks, R, true, seq_token, pr.rm.row_seq, nullptr, R,
                      row_next, pr.extra_dev, S, seq_next, logits, (hipStream_t)stream);
+}
+
+// ---- lengths on the device (icarus_blocks.h) ------------------------------------------------------------------------------
+
+namespace {
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool all_aligned(std::initializer_list<const void *> ps, size_t a) {
+    for (const void *p : ps)
+        if (!aligned(p, a)) return false;
+    return true;
+}
+bool any_null(std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if (!p) return true;
+    return false;
+}
+bool overlap(const void *a, size_t an, const void *b, size_t bn) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + bn && y < x + an;
+}
+constexpr int kBlockMaxSeqs = 65535, kBlockMaxRows = 1 << 30;
+}  // namespace
+
+icarus_status icarus_extend_sequences(icarus_ctx *ctx, int32_t S, const int32_t *ctx_lens, const int32_t *new_lens, const int32_t *streams,
+                                      int32_t *block_tables, int32_t max_blocks, const int32_t *free_ids, int32_t n_free,
+                                      const int32_t *free_used, int32_t max_rows, int32_t *kv_lens, int32_t *row_start,
+                                      int32_t *row_seq, int32_t *row_pos, int64_t *row_slot, int32_t *counts, void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (S < 0 || max_blocks < 0 || n_free < 0 || max_rows < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
+    if (S > kBlockMaxRows || max_rows > kBlockMaxRows || n_free > kBlockMaxRows)
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences, rows and free ids per call", kBlockMaxRows);
+    if (any_null({row_start, counts, free_used}) || (S && any_null({ctx_lens, new_lens, kv_lens})) || (S && max_blocks && !block_tables) ||
+        (n_free && !free_ids) || (max_rows && any_null({row_seq, row_pos, row_slot})))
+        return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({ctx_lens, new_lens, streams, block_tables, free_ids, free_used, kv_lens, row_start, row_seq, row_pos, counts}, 4) ||
+        !aligned(row_slot, 8))
+        return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays must be aligned to their element");
+    const size_t lens = (size_t)S * 4;
+    if (overlap(kv_lens, lens, ctx_lens, lens) || overlap(kv_lens, lens, new_lens, lens) || overlap(counts, 8, free_used, 4) ||
+        (streams && overlap(kv_lens, lens, streams, lens)))
+        return fail(ctx, ICARUS_ERR_INVALID_ARG, "kv_lens and counts must not share memory with the lengths and free_used that the call reads");
+    const icarus_layer_config &c = ctx->cfg;
+    ExtendArgs a{ctx_lens, new_lens, streams, block_tables, max_blocks, c.block_size, c.num_blocks, S, c.max_position, free_ids, free_used, n_free,
+                 max_rows, kv_lens, row_start, row_seq, row_pos, row_slot, counts};
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_extend(a, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+icarus_status icarus_rope_append(icarus_ctx *ctx, const void *qkv, int64_t ld, int32_t R, const int32_t *row_pos,
+                                 const int64_t *row_slot, void *q_out, void *kv_pool, void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    const icarus_layer_config &c = ctx->cfg;
+    if (R < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative number of rows");
+    if (R > kBlockMaxRows) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d rows per call", kBlockMaxRows);
+    if (ld < (int64_t)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim)
+        return fail(ctx, ICARUS_ERR_SHAPE, "rows of qkv are %lld elements apart, a row has %lld", (long long)ld,
+                    (long long)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim);
+    if (R == 0) return ICARUS_OK;
+    if (any_null({qkv, row_pos, row_slot, q_out, kv_pool})) return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({qkv, q_out, kv_pool}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "qkv, q_out and kv_pool must be 16-byte aligned");
+    if (!aligned(row_pos, 4) || !aligned(row_slot, 8)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays must be aligned to their element");
+    const size_t es = c.dtype == ICARUS_BF16 ? 2 : 4, head = (size_t)c.head_dim * es;
+    if (overlap(q_out, (size_t)R * c.n_q_heads * head, qkv, ((size_t)(R - 1) * ld) * es + (size_t)(c.n_q_heads + 2 * c.n_kv_heads) * head))
+        return fail(ctx, ICARUS_ERR_INVALID_ARG, "q_out must not share memory with qkv");
+    AppendArgs a{qkv, ld, R, row_pos, row_slot, q_out, kv_pool, (int64_t)c.num_blocks * c.block_size, ctx->base.q_norm, ctx->base.k_norm};
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ROPE_APPEND, launch_append(ctx->dm, a, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+icarus_status icarus_key_bounds(icarus_ctx *ctx, const void *kv_pool, const int32_t *block_tables, int32_t max_blocks, int32_t S,
+                                const int32_t *from_lens, const int32_t *to_lens, int32_t max_new, int8_t *codes, float *scales,
+                                void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (S < 0 || max_blocks < 0 || max_new < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
+    if (S > kBlockMaxSeqs) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences per call", kBlockMaxSeqs);
+    if (S == 0 || max_blocks == 0) return ICARUS_OK;
+    if (any_null({kv_pool, block_tables, from_lens, to_lens, codes, scales})) return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({kv_pool, codes}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "kv_pool and codes must be 16-byte aligned");
+    if (!all_aligned({block_tables, from_lens, to_lens, scales}, 4)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays and scales must be aligned to their element");
+    BoundsArgs a{kv_pool, block_tables, max_blocks, ctx->cfg.num_blocks, S, from_lens, to_lens, max_new, codes, scales};
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_bounds(ctx->dm, a, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+size_t icarus_select_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t max_blocks) {
+    if (!ctx || S < 0 || max_blocks < 0) return 0;
+    return align_up((size_t)S * ctx->cfg.n_kv_heads * max_blocks * 4, 256) + 256;
+}
+
+icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t *codes, const float *scales, const int32_t *block_tables,
+                                   int32_t max_blocks, int32_t S, const int32_t *kv_lens, int32_t R, const int32_t *row_start,
+                                   int32_t seq_rows, int32_t top_k, int32_t first, int32_t last, int32_t *blocks, int32_t *counts,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (S < 0 || max_blocks < 0 || R < 0 || seq_rows < 0 || first < 0 || last < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
+    if (top_k < 1 || (int64_t)first + last > top_k)
+        return fail(ctx, ICARUS_ERR_INVALID_ARG, "top_k %d must be positive and hold the first %d and the last %d blocks", top_k, first, last);
+    if (S > kBlockMaxSeqs) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences per call", kBlockMaxSeqs);
+    if (S == 0) return ICARUS_OK;
+    if (any_null({codes, scales, kv_lens, row_start, blocks, counts, workspace}) || (max_blocks && !block_tables) || (R && !q))
+        return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({q, codes, workspace}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "q, codes and workspace must be 16-byte aligned");
+    if (!all_aligned({scales, block_tables, kv_lens, row_start, blocks, counts}, 4))
+        return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays and scales must be aligned to their element");
+    const size_t need = icarus_select_workspace_bytes(ctx, S, max_blocks);
+    if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
+    SelectArgs a{q, codes, scales, block_tables, max_blocks, ctx->cfg.num_blocks, S, kv_lens, row_start, R, seq_rows, top_k, first, last, blocks, counts,
+                 (float *)workspace};
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_select(ctx->dm, a, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+size_t icarus_attn_blocks_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t R, int32_t max_selected) {
+    if (!ctx || S < 0 || R < 0 || max_selected < 0) return 0;
+    return 256;
+}
+
+icarus_status icarus_attn_blocks(icarus_ctx *ctx, const void *q, const void *kv_pool, const int32_t *block_tables, int32_t max_blocks,
+                                 int32_t S, const int32_t *kv_lens, int32_t R, const int32_t *row_start, int32_t seq_rows,
+                                 const int32_t *blocks, const int32_t *counts, int32_t max_selected, void *out, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (S < 0 || max_blocks < 0 || R < 0 || seq_rows < 0 || max_selected < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
+    if (S > kBlockMaxSeqs) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences per call", kBlockMaxSeqs);
+    if (S == 0 || R == 0) return ICARUS_OK;
+    if (any_null({q, kv_pool, kv_lens, row_start, counts, out, workspace}) || (max_blocks && !block_tables) || (max_selected && !blocks))
+        return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({q, kv_pool, out, workspace}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "q, kv_pool, out and workspace must be 16-byte aligned");
+    if (!all_aligned({block_tables, kv_lens, row_start, blocks, counts}, 4))
+        return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays must be aligned to their element");
+    const size_t need = icarus_attn_blocks_workspace_bytes(ctx, S, R, max_selected);
+    if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
+    BlockAttnArgs a{q, kv_pool, block_tables, max_blocks, ctx->cfg.num_blocks, S, kv_lens, row_start, R, seq_rows, blocks, counts, max_selected, out};
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ATTN, launch_block_attn_generic(ctx->dm, a, (hipStream_t)stream));
+    return ICARUS_OK;
 }
 
 }  // extern "C"
