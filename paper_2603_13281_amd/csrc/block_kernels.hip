@@ -266,11 +266,114 @@ __global__ void __launch_bounds__(256) k_bounds(BoundsArgs a, int Hkv, int D, in
 }
 
 // ---- choice of the blocks ---------------------------------------------------------------------------------------------------
-// A score as a number whose order is that of the floats; forced blocks above all of them.
-constexpr uint32_t kForced = 0xffffffffu;
+// A score as a number whose order is that of the floats.
 __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t u = __float_as_uint(x);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+// Blocks of a sequence that a choice is made from: [first, nb - last) of them compete, the others are taken.
+__device__ __forceinline__ int n_blocks_of(const SelectArgs &a, int s, int Bk) { return min(blocks_of(max(a.kv_lens[s], 0), Bk), a.max_blocks); }
+
+// Scores on the matrix cores, head sizes 64, 128, 192, 256: one wave to 16 * TB blocks, no other to wait for.  Codes of a block are the columns of 16x16x64 products in 8 bits, a
+// query's positive parts (as many as the largest keys) and negative parts (smallest keys) the rows.  In both operands a lane holds 16 bytes of one row or
+// column, which is how codes lie in memory and what a lane can quantise on its own: a query's 16 channels of one step, the same for both parts.
+// Bound by HBM and, with many queries to a sequence, by the quantising, which every wave does for itself (so that none waits for another): 64 sequences of
+// 1024-16384 tokens, 1-8 agents (73 MB) XXX us.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+template <typename T> __device__ __forceinline__ void load16(const T *p, float (&v)[16]) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint4 r = *(const uint4 *)(p + 8 * h);
+            const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[8 * h + 2 * i] = __uint_as_float(u[i] << 16);
+                v[8 * h + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const float4 r = *(const float4 *)(p + 4 * h);
+            v[4 * h] = r.x; v[4 * h + 1] = r.y; v[4 * h + 2] = r.z; v[4 * h + 3] = r.w;
+        }
+    }
+}
+template <typename T, int KS, int TB>
+__global__ void __launch_bounds__(256) k_scores_mfma(SelectArgs a, int Hq, int Hkv, int Bk) {
+    constexpr int D = KS * 32, H = KS / 2;  // steps of 64 of both parts, of one part
+    const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, g = Hq / Hkv;
+    const int lane = threadIdx.x & 63, m = lane & 15, q4 = lane >> 4;
+    const int b0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 16 * TB;
+    const int nb = n_blocks_of(a, s, Bk);
+    if (b0 >= nb - a.last || nb <= a.top_k) return;  // all of them are taken
+    const int row0 = min(max(a.row_start[s], 0), a.R), n = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
+    i32x4 code[TB][KS];
+    float scale[TB], best[TB];
+    bool good[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+        const int b = b0 + 16 * t + m, id = b < nb ? a.bt[(size_t)s * a.max_blocks + b] : -1;
+        good[t] = id >= 0 && id < a.num_blocks;
+        const size_t rec = good[t] ? (size_t)id * Hkv + c : 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) code[t][ks] = *(const i32x4 *)(a.codes + rec * 2 * D + 64 * ks + 16 * q4);
+        scale[t] = a.scales[rec];
+        best[t] = -INFINITY;
+    }
+    for (int j0 = 0; j0 < n; j0 += 16) {
+        const int j = min(j0 + m, n - 1);
+        const T *q = (const T *)a.q + ((size_t)(row0 + j / g) * Hq + c * g + j % g) * D + 16 * q4;
+        float v[H][16], most = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < H; ++ks) {
+            load16(q + 64 * ks, v[ks]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                v[ks][i] = finite_or_edge(v[ks][i]);
+                most = fmaxf(most, fabsf(v[ks][i]));
+            }
+        }
+        most = fmaxf(most, __shfl_xor(most, 16, 64));
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        const int e = step_exponent(most);
+        const float inv = ldexpf(1.f, -e), step = ldexpf(1.f, e);
+        i32x4 up[H], down[H];  // positive and negative parts
+#pragma unroll
+        for (int ks = 0; ks < H; ++ks)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                int u = 0, d = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int x = (int)fminf(fmaxf(rintf(v[ks][4 * i + k] * inv), -127.f), 127.f);
+                    u |= max(x, 0) << 8 * k;
+                    d |= (min(x, 0) & 255) << 8 * k;
+                }
+                up[ks][i] = u;
+                down[ks][i] = d;
+            }
+        float steps[4];  // of the queries whose sums this lane gets: rows 4 q4 .. + 3
+#pragma unroll
+        for (int i = 0; i < 4; ++i) steps[i] = __shfl(step, 4 * q4 + i, 64);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            i32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(ks < H ? up[ks] : down[ks - H], code[t][ks], sum, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) best[t] = fmaxf(best[t], (float)sum[i] * steps[i]);  // rows behind the last query repeat it
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+        float x = best[t];
+        x = fmaxf(x, __shfl_xor(x, 16, 64));
+        x = fmaxf(x, __shfl_xor(x, 32, 64));
+        const int b = b0 + 16 * t + m;
+        if (q4 == 0 && b < nb) ((uint32_t *)a.scores)[(size_t)pair * a.max_blocks + b] = order_key(good[t] ? (n ? x * scale[t] : 0.f) : -INFINITY);
+    }
 }
 
 // Any even head size: a thread to a block, the queries of a batch in LDS as codes [queries][2 D / 4 words], the positive parts before the negative ones.
@@ -280,8 +383,8 @@ __global__ void __launch_bounds__(256) k_scores(SelectArgs a, int Hq, int Hkv, i
     __shared__ int qs[kScoreBatch][128];
     __shared__ float qstep[kScoreBatch];
     const int s = blockIdx.x / Hkv, c = blockIdx.x % Hkv, g = Hq / Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int nb = min(blocks_of(max(a.kv_lens[s], 0), Bk), a.max_blocks);
-    if ((int)blockIdx.y * 256 >= nb) return;
+    const int nb = n_blocks_of(a, s, Bk);
+    if ((int)blockIdx.y * 256 >= nb || nb <= a.top_k) return;
     const int row0 = min(max(a.row_start[s], 0), a.R), n = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
     const int b = blockIdx.y * 256 + threadIdx.x;
     const int id = b < nb ? a.bt[(size_t)s * a.max_blocks + b] : -1;
@@ -321,70 +424,147 @@ __global__ void __launch_bounds__(256) k_scores(SelectArgs a, int Hq, int Hkv, i
             if (j < cnt) best = fmaxf(best, (float)acc[j] * qstep[j]);
     }
     if (b >= nb) return;
-    uint32_t key = order_key(good ? (n ? best * a.scales[rec] : 0.f) : -INFINITY);
-    if (b < a.first || b >= nb - a.last) key = kForced;
-    ((uint32_t *)a.scores)[((size_t)s * Hkv + c) * a.max_blocks + b] = key;
+    ((uint32_t *)a.scores)[((size_t)s * Hkv + c) * a.max_blocks + b] = order_key(good ? (n ? best * a.scales[rec] : 0.f) : -INFINITY);
 }
 
-// The top_k largest keys of a sequence and kv-head, lowest index first among equal ones: the k-th largest key is found eight bits at a
-// time from counts in LDS (whole numbers: their order does not matter), then one pass in the order of the blocks writes the list.
-__global__ void __launch_bounds__(256) k_pick(SelectArgs a, int Hkv, int Bk) {
-    __shared__ int hist[256], wave_gt[4], wave_eq[4], chosen[2];
-    const int s = blockIdx.x / Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int nb = min(blocks_of(max(a.kv_lens[s], 0), Bk), a.max_blocks), k = min(a.top_k, nb);
-    const uint32_t *keys = (const uint32_t *)a.scores + (size_t)blockIdx.x * a.max_blocks;
-    int32_t *out = a.blocks + (size_t)blockIdx.x * a.top_k;
-    if (threadIdx.x == 0 && blockIdx.x % Hkv == 0) a.counts[s] = k;
-    for (int i = k + threadIdx.x; i < a.top_k; i += 256) out[i] = -1;
+// The choice of a sequence and kv-head: of the keys that compete the k largest, lowest index first among equal ones.  The k-th largest is found eight bits at
+// a time from counts in LDS (whole numbers: their order does not matter), from the highest bit in which the keys differ at all on; then each thread
+// knows how many of its neighbouring blocks are taken, and one sum over the workgroup says where they go.  KPT: keys of a thread, in registers (0: read
+// again in every pass, for any number).
+template <int THREADS, int KPT>
+__global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ int hist[256], part[WAVES], chosen[2];
+    __shared__ uint32_t low[WAVES], high[WAVES];
+    const int pair = blockIdx.x, s = pair / Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int nb = n_blocks_of(a, s, Bk), k = min(a.top_k, nb);
+    const uint32_t *keys = (const uint32_t *)a.scores + (size_t)pair * a.max_blocks;
+    int32_t *out = a.blocks + (size_t)pair * a.top_k;
+    if (threadIdx.x == 0 && pair == s * Hkv) a.counts[s] = k;
+    for (int i = k + threadIdx.x; i < a.top_k; i += THREADS) out[i] = -1;
     if (nb <= a.top_k) {
-        for (int i = threadIdx.x; i < nb; i += 256) out[i] = i;
+        for (int i = threadIdx.x; i < nb; i += THREADS) out[i] = i;
         return;
     }
-    uint32_t prefix = 0;  // the bits of the k-th largest key found so far
-    int left = k;         // its rank among the keys that share them
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        hist[threadIdx.x] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < nb; i += 256) {
-            const uint32_t key = keys[i];
-            if (shift == 24 || (key >> (shift + 8)) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1);
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            int bin = 255, above = 0;
-            while (above + hist[bin] < left) above += hist[bin--];
-            chosen[0] = bin;
-            chosen[1] = above;
-        }
-        __syncthreads();
-        prefix = prefix << 8 | (uint32_t)chosen[0];
-        left -= chosen[1];
+    const int b_end = nb - a.last;  // [first, b_end) compete
+    const int per = KPT ? KPT : (nb + THREADS - 1) / THREADS, i0 = threadIdx.x * per;
+    uint32_t key[KPT ? KPT : 1], lo = 0xffffffffu, hi = 0;
+    auto competes = [&](int i) { return i >= a.first && i < b_end; };
+    auto key_at = [&](int j) { return KPT ? key[KPT ? j : 0] : keys[i0 + j]; };
+#pragma unroll
+    for (int j = 0; j < (KPT ? KPT : per); ++j) {
+        const int i = i0 + j;
+        if (!competes(i)) continue;
+        const uint32_t x = keys[i];
+        if (KPT) key[KPT ? j : 0] = x;
+        lo = min(lo, x);
+        hi = max(hi, x);
     }
-    // `left` of the keys equal to `prefix` are taken, and all larger ones
-    int at = 0, eq_before = 0;
-    for (int i0 = 0; i0 < nb; i0 += 256) {
-        const int i = i0 + threadIdx.x;
-        const uint32_t key = i < nb ? keys[i] : 0;
-        const bool gt = i < nb && key > prefix, eq = i < nb && key == prefix;
-        const unsigned long long m_gt = __ballot(gt), m_eq = __ballot(eq), below = (1ull << lane) - 1;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+    }
+    if (lane == 0) {
+        low[w] = lo;
+        high[w] = hi;
+    }
+    __syncthreads();
+    for (int i = 0; i < WAVES; ++i) {
+        lo = min(lo, low[i]);
+        hi = max(hi, high[i]);
+    }
+    int left = a.top_k - a.first - a.last;  // how many of the competing ones are taken; more than `left` compete
+    const int bits = lo == hi ? 0 : 32 - __clz((int)(lo ^ hi));
+    uint32_t prefix = bits == 32 ? 0 : hi >> bits;  // the bits of the key in question that are known, all above `shift`
+    for (int shift = bits; shift > 0 && left > 0;) {
+        const int take = min(8, shift);
+        for (int i = threadIdx.x; i < 256; i += THREADS) hist[i] = 0;
         __syncthreads();
-        if (lane == 0) {
-            wave_gt[w] = __popcll(m_gt);
-            wave_eq[w] = __popcll(m_eq);
+#pragma unroll
+        for (int j = 0; j < (KPT ? KPT : per); ++j) {
+            if (!competes(i0 + j)) continue;
+            const uint32_t x = key_at(j);
+            if (shift == 32 || x >> shift == prefix) atomicAdd(&hist[(x >> (shift - take)) & ((1 << take) - 1)], 1);
         }
         __syncthreads();
-        int gts = 0, eqs = 0, all_gt = 0, all_eq = 0;
-        for (int j = 0; j < 4; ++j) {
-            if (j < w) { gts += wave_gt[j]; eqs += wave_eq[j]; }
-            all_gt += wave_gt[j];
-            all_eq += wave_eq[j];
+        if (w == 0) {  // four bins to a lane, from the top: the bin in which the count passes `left`
+            int h[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                h[i] = hist[255 - 4 * lane - i];
+                sum += h[i];
+            }
+            int above = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(above, o, 64);
+                if (lane >= o) above += y;
+            }
+            above -= sum;  // in the lanes before
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (above < left && above + h[i] >= left) {
+                    chosen[0] = 255 - 4 * lane - i;
+                    chosen[1] = above;
+                }
+                above += h[i];
+            }
         }
-        gts += __popcll(m_gt & below);
-        eqs += __popcll(m_eq & below);
-        const int rank = eq_before + eqs;  // among the equal ones
-        if (gt || (eq && rank < left)) out[at + gts + min(rank, left) - min(eq_before, left)] = i;
-        at += all_gt + min(eq_before + all_eq, left) - min(eq_before, left);
-        eq_before += all_eq;
+        __syncthreads();
+        prefix = prefix << take | (uint32_t)chosen[0];
+        left -= chosen[1];
+        shift -= take;
+        __syncthreads();  // hist and chosen have been read
+    }
+    // With left > 0 `prefix` is the whole key of the last one taken: `left` of those equal to it are, and all larger ones.  With none to take, none is larger.
+    const bool any = a.top_k > a.first + a.last;
+    int gt = 0, eq = 0;
+#pragma unroll
+    for (int j = 0; j < (KPT ? KPT : per); ++j) {
+        const int i = i0 + j;
+        if (i >= nb) continue;
+        if (!competes(i)) ++gt;
+        else if (any) {
+            gt += key_at(j) > prefix;
+            eq += key_at(j) == prefix;
+        }
+    }
+    // both counts in one word: a workgroup has fewer than 65536 keys where they are in registers; else two sums
+    auto sum_before = [&](int v) {
+        int x = v;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(x, o, 64);
+            if (lane >= o) x += y;
+        }
+        __syncthreads();
+        if (lane == 63) part[w] = x;
+        __syncthreads();
+        for (int i = 0; i < w; ++i) x += part[i];
+        return x - v;
+    };
+    int at, eq_at;
+    if (KPT) {
+        const int both = sum_before(gt | eq << 16);
+        at = both & 0xffff;
+        eq_at = (int)((uint32_t)both >> 16);
+    } else {
+        at = sum_before(gt);
+        eq_at = sum_before(eq);
+    }
+    at += min(eq_at, left);
+#pragma unroll
+    for (int j = 0; j < (KPT ? KPT : per); ++j) {
+        const int i = i0 + j;
+        if (i >= nb) continue;
+        bool taken = !competes(i);
+        if (!taken && any) {
+            const uint32_t x = key_at(j);
+            taken = x > prefix || (x == prefix && eq_at < left);
+            eq_at += x == prefix;
+        }
+        if (taken) out[at++] = i;
     }
 }
 
@@ -412,11 +592,33 @@ hipError_t launch_bounds(const Dims &dm, const BoundsArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-hipError_t launch_select(const Dims &dm, const SelectArgs &a, hipStream_t st) {
-    DISPATCH_T(dm.bf16, hipLaunchKernelGGL(k_scores<T>, dim3(a.S * dm.Hkv, (a.max_blocks + 255) / 256), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D, dm.Bk));
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_pick, dim3(a.S * dm.Hkv), dim3(256), 0, st, a, dm.Hkv, dm.Bk);
+template <typename T, int TB>
+static bool scores_mfma(const Dims &dm, const SelectArgs &a, hipStream_t st) {
+    const dim3 grid(a.S * dm.Hkv, (a.max_blocks + 64 * TB - 1) / (64 * TB));
+    switch (dm.D) {
+    case 64: hipLaunchKernelGGL((k_scores_mfma<T, 2, TB>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.Bk); return true;
+    case 128: hipLaunchKernelGGL((k_scores_mfma<T, 4, TB>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.Bk); return true;
+    case 192: hipLaunchKernelGGL((k_scores_mfma<T, 6, TB>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.Bk); return true;
+    case 256: hipLaunchKernelGGL((k_scores_mfma<T, 8, TB>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.Bk); return true;
+    default: return false;
+    }
+}
+
+hipError_t launch_select(const Dims &dm, bool generic, const SelectArgs &a, hipStream_t st) {
+    bool done = false;
+    if (a.max_blocks > a.top_k) {  // else all blocks are taken
+        if (!generic) DISPATCH_T(dm.bf16, done = (scores_mfma<T, 2>(dm, a, st)));
+        if (!done)
+            DISPATCH_T(dm.bf16, hipLaunchKernelGGL(k_scores<T>, dim3(a.S * dm.Hkv, (a.max_blocks + 255) / 256), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D, dm.Bk));
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const dim3 grid(a.S * dm.Hkv);
+    if (a.max_blocks <= 1024) hipLaunchKernelGGL((k_pick<256, 4>), grid, dim3(256), 0, st, a, dm.Hkv, dm.Bk);
+    else if (a.max_blocks <= 2048) hipLaunchKernelGGL((k_pick<256, 8>), grid, dim3(256), 0, st, a, dm.Hkv, dm.Bk);
+    else if (a.max_blocks <= 8192) hipLaunchKernelGGL((k_pick<1024, 8>), grid, dim3(1024), 0, st, a, dm.Hkv, dm.Bk);
+    else if (a.max_blocks <= 32768) hipLaunchKernelGGL((k_pick<1024, 32>), grid, dim3(1024), 0, st, a, dm.Hkv, dm.Bk);
+    else hipLaunchKernelGGL((k_pick<1024, 0>), grid, dim3(1024), 0, st, a, dm.Hkv, dm.Bk);
     return hipGetLastError();
 }
 

@@ -35,7 +35,8 @@ struct SelectArgs {
     int32_t *blocks, *counts;
     float *scores;                                 // workspace [S, Hkv, max_blocks]
 };
-hipError_t launch_select(const Dims &dm, const SelectArgs &a, hipStream_t st);
+// generic: without the matrix cores
+hipError_t launch_select(const Dims &dm, bool generic, const SelectArgs &a, hipStream_t st);
 
 struct BlockAttnArgs {
     const void *q, *pool; const int32_t *bt; int max_blocks, num_blocks, S;

@@ -2105,7 +2105,7 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
     if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
     SelectArgs a{q, codes, scales, block_tables, max_blocks, ctx->cfg.num_blocks, S, kv_lens, row_start, R, seq_rows, top_k, first, last, blocks, counts,
                  (float *)workspace};
-    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_select(ctx->dm, a, (hipStream_t)stream));
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_select(ctx->dm, ctx->mode != 0, a, (hipStream_t)stream));
     return ICARUS_OK;
 }
 
