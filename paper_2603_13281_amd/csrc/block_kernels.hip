@@ -274,11 +274,10 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 // Blocks of a sequence that a choice is made from: [first, nb - last) of them compete, the others are taken.
 __device__ __forceinline__ int n_blocks_of(const SelectArgs &a, int s, int Bk) { return min(blocks_of(max(a.kv_lens[s], 0), Bk), a.max_blocks); }
 
-// Scores on the matrix cores, head sizes 64, 128, 192, 256: one wave to 16 * TB blocks, no other to wait for.  Codes of a block are the columns of 16x16x64 products in 8 bits, a
-// query's positive parts (as many as the largest keys) and negative parts (smallest keys) the rows.  In both operands a lane holds 16 bytes of one row or
-// column, which is how codes lie in memory and what a lane can quantise on its own: a query's 16 channels of one step, the same for both parts.
-// Bound by HBM and, with many queries to a sequence, by the quantising, which every wave does for itself (so that none waits for another): 64 sequences of
-// 1024-16384 tokens, 1-8 agents (73 MB) XXX us.
+// Scores on the matrix cores, head sizes 64, 128, 192, 256: a wave to 16 * TB blocks.  Codes of a block are the columns of 16x16x64 products in 8 bits, a query's positive
+// parts (as many as the largest keys) and negative parts (smallest keys) the rows.  In both operands a lane holds 16 bytes of one row or column,
+// which is how codes lie in memory and what a lane quantises by itself: a query's 16 channels of one step, the same for both parts.  The four waves
+// quantise a tile of 16 queries each and share them; their codes are on the way meanwhile.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 template <typename T> __device__ __forceinline__ void load16(const T *p, float (&v)[16]) {
     if constexpr (sizeof(T) == 2) {
@@ -300,14 +299,36 @@ template <typename T> __device__ __forceinline__ void load16(const T *p, float (
         }
     }
 }
+// Four rounded multiples of 2^-e: the bytes of their positive and of their negative parts.  The conversion to whole numbers makes 0 of a NaN and
+// saturates, so values need no looking at before.
+__device__ __forceinline__ void quantise4(const float *v, float inv, int *up, int *down) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    s16x2 h[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        int x, y;
+        asm("v_cvt_i32_f32 %0, %1" : "=v"(x) : "v"(rintf(v[2 * k] * inv)));
+        asm("v_cvt_i32_f32 %0, %1" : "=v"(y) : "v"(rintf(v[2 * k + 1] * inv)));
+        h[k] = __builtin_bit_cast(s16x2, __builtin_amdgcn_cvt_pk_i16(x, y));
+    }
+    const s16x2 most = {127, 127}, none = {0, 0}, least = {-127, -127};
+    const uint32_t u0 = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_elementwise_max(h[0], none), most));
+    const uint32_t u1 = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_elementwise_max(h[1], none), most));
+    const uint32_t d0 = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_min(h[0], none), least));
+    const uint32_t d1 = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_min(h[1], none), least));
+    *up = (int)__builtin_amdgcn_perm(u1, u0, 0x06040200);  // bytes 0 and 2 of both words
+    *down = (int)__builtin_amdgcn_perm(d1, d0, 0x06040200);
+}
 template <typename T, int KS, int TB>
 __global__ void __launch_bounds__(256) k_scores_mfma(SelectArgs a, int Hq, int Hkv, int Bk) {
     constexpr int D = KS * 32, H = KS / 2;  // steps of 64 of both parts, of one part
+    __shared__ i32x4 rows[4][KS][64];       // four tiles of queries: [tile][step][lane]
+    __shared__ __attribute__((aligned(16))) float steps[4][16];
     const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, g = Hq / Hkv;
-    const int lane = threadIdx.x & 63, m = lane & 15, q4 = lane >> 4;
-    const int b0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 16 * TB;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, q4 = lane >> 4;
     const int nb = n_blocks_of(a, s, Bk);
-    if (b0 >= nb - a.last || nb <= a.top_k) return;  // all of them are taken
+    if ((int)blockIdx.y * 64 * TB >= nb - a.last || nb <= a.top_k) return;  // all of them are taken
+    const int b0 = (blockIdx.y * 4 + w) * 16 * TB;
     const int row0 = min(max(a.row_start[s], 0), a.R), n = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
     i32x4 code[TB][KS];
     float scale[TB], best[TB];
@@ -322,49 +343,54 @@ __global__ void __launch_bounds__(256) k_scores_mfma(SelectArgs a, int Hq, int H
         scale[t] = a.scales[rec];
         best[t] = -INFINITY;
     }
-    for (int j0 = 0; j0 < n; j0 += 16) {
-        const int j = min(j0 + m, n - 1);
-        const T *q = (const T *)a.q + ((size_t)(row0 + j / g) * Hq + c * g + j % g) * D + 16 * q4;
-        float v[H][16], most = 0.f;
+    for (int j0 = 0; j0 < n; j0 += 64) {
+        if (j0 + 16 * w < n) {
+            const int j = min(j0 + 16 * w + m, n - 1);  // behind the last query: the last again
+            const T *q = (const T *)a.q + ((size_t)(row0 + j / g) * Hq + c * g + j % g) * D + 16 * q4;
+            float v[H][16], most = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < H; ++ks) {
-            load16(q + 64 * ks, v[ks]);
+            for (int ks = 0; ks < H; ++ks) load16(q + 64 * ks, v[ks]);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[ks][i] = finite_or_edge(v[ks][i]);
-                most = fmaxf(most, fabsf(v[ks][i]));
-            }
-        }
-        most = fmaxf(most, __shfl_xor(most, 16, 64));
-        most = fmaxf(most, __shfl_xor(most, 32, 64));
-        const int e = step_exponent(most);
-        const float inv = ldexpf(1.f, -e), step = ldexpf(1.f, e);
-        i32x4 up[H], down[H];  // positive and negative parts
+            for (int ks = 0; ks < H; ++ks)
 #pragma unroll
-        for (int ks = 0; ks < H; ++ks)
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(v[ks][i]));  // a NaN is passed over
+            most = fmaxf(most, __shfl_xor(most, 16, 64));
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const int e = step_exponent(fminf(most, 3.402823466e38f));
+            const float inv = ldexpf(1.f, -e);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                int u = 0, d = 0;
+            for (int ks = 0; ks < H; ++ks) {
+                i32x4 up, down;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int x = (int)fminf(fmaxf(rintf(v[ks][4 * i + k] * inv), -127.f), 127.f);
-                    u |= max(x, 0) << 8 * k;
-                    d |= (min(x, 0) & 255) << 8 * k;
+                for (int i = 0; i < 4; ++i) {
+                    int u, d;
+                    quantise4(v[ks] + 4 * i, inv, &u, &d);
+                    up[i] = u;
+                    down[i] = d;
                 }
-                up[ks][i] = u;
-                down[ks][i] = d;
+                rows[w][ks][lane] = up;
+                rows[w][ks + H][lane] = down;
             }
-        float steps[4];  // of the queries whose sums this lane gets: rows 4 q4 .. + 3
-#pragma unroll
-        for (int i = 0; i < 4; ++i) steps[i] = __shfl(step, 4 * q4 + i, 64);
-#pragma unroll
-        for (int t = 0; t < TB; ++t) {
-            i32x4 sum = {0, 0, 0, 0};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(ks < H ? up[ks] : down[ks - H], code[t][ks], sum, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) best[t] = fmaxf(best[t], (float)sum[i] * steps[i]);  // rows behind the last query repeat it
+            if (q4 == 0) steps[w][m] = ldexpf(1.f, e);
         }
+        __syncthreads();
+        const int tiles = min(4, (n - j0 + 15) / 16);
+        for (int j = 0; j < tiles; ++j) {
+            i32x4 sum[TB];
+#pragma unroll
+            for (int t = 0; t < TB; ++t) sum[t] = i32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const i32x4 r = rows[j][ks][lane];
+#pragma unroll
+                for (int t = 0; t < TB; ++t) sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(r, code[t][ks], sum[t], 0, 0, 0);
+            }
+            const float4 st = *(const float4 *)&steps[j][4 * q4];  // of the queries whose sums this lane has: rows 4 q4 .. + 3
+#pragma unroll
+            for (int t = 0; t < TB; ++t)
+                best[t] = fmaxf(fmaxf(fmaxf(best[t], (float)sum[t][0] * st.x), fmaxf((float)sum[t][1] * st.y, (float)sum[t][2] * st.z)), (float)sum[t][3] * st.w);
+        }
+        __syncthreads();
     }
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
