@@ -218,6 +218,169 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, i
     }
 }
 
+// Head sizes 64, 128 and 256, blocks of 16.  Bound by HBM where there are many rows, by the chain of its reads where there are few.
+// A workgroup takes a window of 16 rows and a part of their heads.  LPH = D / 8 lanes hold a head, four pairs to a lane, so that both halves of a
+// row of 128 bfloat16 are read and written as whole lines; a lane keeps its row's angles for all heads of the part.
+// V goes into the pool transposed: a run of rows that are consecutive places of one block is put together in LDS and written as one row of the block per
+// channel, 32 bytes at once where the run fills the block.  A run belongs to the window in which it starts, wherever it ends, so that prompts which begin
+// inside a block are written in whole blocks too.
+template <typename T> struct Four;  // four elements, as they lie in memory
+template <> struct Four<bf16_t> {
+    typedef uint2 raw;
+    static __device__ __forceinline__ void get(raw r, float (&v)[4]) {
+        v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);
+        v[2] = __uint_as_float(r.y << 16); v[3] = __uint_as_float(r.y & 0xffff0000u);
+    }
+    static __device__ __forceinline__ void put(bf16_t *p, const float (&v)[4], float) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
+};
+template <> struct Four<float> {
+    typedef float4 raw;
+    static __device__ __forceinline__ void get(raw r, float (&v)[4]) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
+    static __device__ __forceinline__ void put(float *p, const float (&v)[4], float) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <> struct Four<fp8_t> {
+    static __device__ __forceinline__ void put(fp8_t *p, const float (&v)[4], float scale) {
+        *(uint32_t *)p = f32_to_fp8(v[0] / scale) | f32_to_fp8(v[1] / scale) << 8 | f32_to_fp8(v[2] / scale) << 16 | f32_to_fp8(v[3] / scale) << 24;
+    }
+};
+
+constexpr int kWindow = 16;
+// What a wave wrote to LDS is what it reads next: an order for the compiler, the hardware keeps it anyway.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+template <typename T, typename KT, int D>
+__global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int Hkv, double log2_theta, float eps, int qk_norm, float k_scale, float v_scale) {
+    constexpr int Bk = 16, LPH = D / 8, HALF = D / 2, ROWS = 256 / LPH, VW = 16 / sizeof(T);  // ROWS: heads of a pass; VW: elements of 16 bytes
+    __shared__ double turns[HALF];
+    __shared__ __attribute__((aligned(16))) T tile[4][Bk][D];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = blockIdx.x * kWindow;
+    for (int i = threadIdx.x; i < HALF; i += 256) turns[i] = turns_per_position(i, D, log2_theta);
+    __syncthreads();
+    const int n_rot = Hq + Hkv;
+    // Rotated heads of this part, [h0, h1): with fewer than 16 lanes to a head the lanes of a row take neighbouring heads.
+    constexpr int HPR = ROWS > kWindow ? ROWS / kWindow : 1;  // heads of a row at a time
+    const int h0 = n_rot * blockIdx.y / gridDim.y, h1 = n_rot * (blockIdx.y + 1) / gridDim.y;
+    const int sub = threadIdx.x / LPH, i4 = 4 * (threadIdx.x % LPH);
+    for (int rr = sub / HPR; rr < kWindow; rr += ROWS / HPR) {
+        const int row = r0 + rr, pos = row < a.R ? a.row_pos[row] : -1;
+        if (pos < 0) continue;
+        const int64_t slot = a.row_slot[row];
+        const bool write = slot >= 0 && slot < a.n_slots;
+        float cs[4], sn[4], wq[2][4], wk[2][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) turn_of(pos, turns[i4 + e], &cs[e], &sn[e]);
+        if (qk_norm)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                Four<T>::get(*(const typename Four<T>::raw *)((const T *)a.q_norm + h * HALF + i4), wq[h]);
+                Four<T>::get(*(const typename Four<T>::raw *)((const T *)a.k_norm + h * HALF + i4), wk[h]);
+            }
+        const T *src = (const T *)a.qkv + (size_t)row * a.ld + i4;
+        KT *kdst = (KT *)a.pool + (write ? ((size_t)(slot / Bk) * Hkv * 2 * Bk + (size_t)(slot % Bk)) * D : 0) + i4;
+        const int end = write ? h1 : min(h1, Hq);  // a stream's key heads are not read
+#pragma unroll 4
+        for (int h = h0 + sub % HPR; h < end; h += HPR) {
+            float x[4], y[4], rx[4], ry[4];
+            Four<T>::get(*(const typename Four<T>::raw *)(src + (size_t)h * D), x);
+            Four<T>::get(*(const typename Four<T>::raw *)(src + (size_t)h * D + HALF), y);
+            if (qk_norm) {
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ss += x[e] * x[e] + y[e] * y[e];
+#pragma unroll
+                for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+                const float inv = rsqrtf(ss / (float)D + eps);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = x[e] * inv * (h < Hq ? wq[0][e] : wk[0][e]);
+                    y[e] = y[e] * inv * (h < Hq ? wq[1][e] : wk[1][e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rotate_pair(x[e], y[e], cs[e], sn[e], &rx[e], &ry[e]);
+            if (h < Hq) {
+                T *dst = (T *)a.q_out + ((size_t)row * Hq + h) * D + i4;
+                Four<T>::put(dst, rx, 1.f);
+                Four<T>::put(dst + HALF, ry, 1.f);
+            } else {
+                KT *dst = kdst + (size_t)(h - Hq) * 2 * Bk * D;
+                Four<KT>::put(dst, rx, k_scale);
+                Four<KT>::put(dst + HALF, ry, k_scale);
+            }
+        }
+    }
+    // V: lane l < 32 looks at row r0 + l; the rows behind the window matter for runs that start in it.
+    const int v0 = Hkv * blockIdx.y / gridDim.y, n_v = Hkv * (blockIdx.y + 1) / gridDim.y - v0;
+    if (n_v == 0) return;
+    int64_t slot = -1, before = -1;
+    if (lane < 32) {
+        auto place = [&](int row) {
+            if (row < 0 || row >= a.R || a.row_pos[row] < 0) return (int64_t)-1;
+            const int64_t x = a.row_slot[row];
+            return x < a.n_slots ? x : (int64_t)-1;
+        };
+        slot = place(r0 + lane);
+        before = place(r0 + lane - 1);
+    }
+    const bool there = slot >= 0, goes_on = there && before >= 0 && slot == before + 1 && slot % Bk != 0;
+    const uint32_t going = (uint32_t)__ballot(goes_on);
+    uint32_t starts = (uint32_t)__ballot(there && !goes_on) & 0xffffu;
+    const int n_runs = __popc(starts);
+    if (n_runs == 0) return;
+    int at = w;  // of the runs x heads of this part
+    for (int run = 0; run < n_runs; ++run, starts &= starts - 1) {
+        const int l = __ffs((int)starts) - 1, n = 1 + __builtin_ctz(~(going >> l >> 1));  // a run ends at a block's end: at most 16
+        const int64_t first = ((int64_t)__shfl((int)(slot >> 32), l, 64) << 32) | (uint32_t)__shfl((int)slot, l, 64);
+        const size_t blk = (size_t)(first / Bk);
+        const int off = (int)(first % Bk);
+        for (; at < (run + 1) * n_v; at += 4) {
+            const int c = v0 + at - run * n_v;
+            const T *src = (const T *)a.qkv + (size_t)(r0 + l) * a.ld + (size_t)(Hq + Hkv + c) * D;
+            KT *dst = (KT *)a.pool + ((blk * Hkv + c) * 2 + 1) * Bk * D;
+            if (n == 1) {
+                for (int d = lane; d < D; d += 64) KVElem<KT>::st(dst + d * Bk + off, Elem<T>::ld(src + d), v_scale);
+                continue;
+            }
+            constexpr int CH = D / VW;  // 16-byte pieces of a row
+#pragma unroll
+            for (int i = 0; i < Bk * CH / 64; ++i) {
+                const int t = (i * 64 + lane) / CH, d = (i * 64 + lane) % CH * VW;
+                if (t < n) *(uint4 *)&tile[w][t][d] = *(const uint4 *)(src + (size_t)t * a.ld + d);
+            }
+            wave_fence();  // the tile is this wave's own, and a wave's LDS accesses go in order
+            for (int d = lane; d < D; d += 64) {
+                if (n == Bk) {
+                    if constexpr (sizeof(KT) == 1) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            o[i] = 0;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[i] |= f32_to_fp8(Elem<T>::ld(&tile[w][4 * i + e][d]) / v_scale) << 8 * e;
+                        }
+                        *(uint4 *)(dst + d * Bk) = make_uint4(o[0], o[1], o[2], o[3]);
+                    } else {
+                        constexpr int PER = 4 / sizeof(KT);  // elements of a word: the same type on both sides, the bits are moved as they are
+                        uint32_t o[Bk / PER];
+#pragma unroll
+                        for (int i = 0; i < Bk / PER; ++i) {
+                            if constexpr (PER == 2) o[i] = (uint32_t)tile[w][2 * i][d] | (uint32_t)tile[w][2 * i + 1][d] << 16;
+                            else o[i] = __float_as_uint(tile[w][i][d]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < Bk / PER / 4; ++i) ((uint4 *)(dst + d * Bk))[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    }
+                } else {
+                    for (int t = 0; t < n; ++t) KVElem<KT>::st(dst + d * Bk + off + t, Elem<T>::ld(&tile[w][t][d]), v_scale);
+                }
+            }
+            wave_fence();
+        }
+    }
+}
+
 // ---- bounds of the keys ---------------------------------------------------------------------------------------------------
 // Exponent e of the smallest 2^e, -40 <= e <= 40, with 127 * 2^e >= x (x >= 0 and finite).  With both exponents of a score in this range
 // its value, a whole number below 2^23 times 2^(-80 .. 80), is an exact float.
@@ -603,9 +766,33 @@ hipError_t launch_extend(const ExtendArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-hipError_t launch_append(const Dims &dm, const AppendArgs &a, hipStream_t st) {
-    DISPATCH_TK(dm.bf16, dm.kv8, hipLaunchKernelGGL((k_append<T, KT>), dim3(a.R, (dm.Hq + 2 * dm.Hkv + 3) / 4), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D,
-                                                    dm.Bk, log2(dm.theta), dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale));
+template <typename T, typename KT>
+static bool append_window(const Dims &dm, const AppendArgs &a, hipStream_t st) {
+    if (dm.Bk != 16 || a.ld * (int64_t)sizeof(T) % 16) return false;
+    const int windows = (a.R + kWindow - 1) / kWindow;
+    int parts = 1;  // of the heads: two workgroups to a CU, as long as a part has a rotated head for every wave's turn
+    while (windows * parts < 512 && 2 * parts <= (dm.Hq + dm.Hkv + 3) / 4) parts *= 2;
+    const dim3 grid(windows, parts);
+    const double l2t = log2(dm.theta);
+    switch (dm.D) {
+    case 64: hipLaunchKernelGGL((k_append_window<T, KT, 64>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale); return true;
+    case 128: hipLaunchKernelGGL((k_append_window<T, KT, 128>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale); return true;
+    case 256:
+        if constexpr (sizeof(T) == 2) {  // four tiles of float32 pass what static LDS holds
+            hipLaunchKernelGGL((k_append_window<T, KT, 256>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale);
+            return true;
+        }
+        return false;
+    default: return false;
+    }
+}
+
+hipError_t launch_append(const Dims &dm, bool generic, const AppendArgs &a, hipStream_t st) {
+    bool done = false;
+    if (!generic) DISPATCH_TK(dm.bf16, dm.kv8, done = (append_window<T, KT>(dm, a, st)));
+    if (!done)
+        DISPATCH_TK(dm.bf16, dm.kv8, hipLaunchKernelGGL((k_append<T, KT>), dim3(a.R, (dm.Hq + 2 * dm.Hkv + 3) / 4), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D,
+                                                        dm.Bk, log2(dm.theta), dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale));
     return hipGetLastError();
 }
 

@@ -19,7 +19,8 @@ struct AppendArgs {
     void *q_out, *pool; int64_t n_slots;           // slots of the pool
     const void *q_norm, *k_norm;                   // read with Dims::qk_norm
 };
-hipError_t launch_append(const Dims &dm, const AppendArgs &a, hipStream_t st);
+// generic, here and below: only the kernels for any shape
+hipError_t launch_append(const Dims &dm, bool generic, const AppendArgs &a, hipStream_t st);
 
 struct BoundsArgs {
     const void *pool; const int32_t *bt; int max_blocks, num_blocks, S;
@@ -35,7 +36,6 @@ struct SelectArgs {
     int32_t *blocks, *counts;
     float *scores;                                 // workspace [S, Hkv, max_blocks]
 };
-// generic: without the matrix cores
 hipError_t launch_select(const Dims &dm, bool generic, const SelectArgs &a, hipStream_t st);
 
 struct BlockAttnArgs {

@@ -2060,7 +2060,7 @@ icarus_status icarus_rope_append(icarus_ctx *ctx, const void *qkv, int64_t ld, i
     if (overlap(q_out, (size_t)R * c.n_q_heads * head, qkv, ((size_t)(R - 1) * ld) * es + (size_t)(c.n_q_heads + 2 * c.n_kv_heads) * head))
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "q_out must not share memory with qkv");
     AppendArgs a{qkv, ld, R, row_pos, row_slot, q_out, kv_pool, (int64_t)c.num_blocks * c.block_size, ctx->base.q_norm, ctx->base.k_norm};
-    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ROPE_APPEND, launch_append(ctx->dm, a, (hipStream_t)stream));
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ROPE_APPEND, launch_append(ctx->dm, ctx->mode != 0, a, (hipStream_t)stream));
     return ICARUS_OK;
 }
 
