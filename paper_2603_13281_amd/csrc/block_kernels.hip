@@ -280,34 +280,46 @@ __global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int
         const T *src = (const T *)a.qkv + (size_t)row * a.ld + i4;
         KT *kdst = (KT *)a.pool + (write ? ((size_t)(slot / Bk) * Hkv * 2 * Bk + (size_t)(slot % Bk)) * D : 0) + i4;
         const int end = write ? h1 : min(h1, Hq);  // a stream's key heads are not read
-#pragma unroll 4
-        for (int h = h0 + sub % HPR; h < end; h += HPR) {
-            float x[4], y[4], rx[4], ry[4];
-            Four<T>::get(*(const typename Four<T>::raw *)(src + (size_t)h * D), x);
-            Four<T>::get(*(const typename Four<T>::raw *)(src + (size_t)h * D + HALF), y);
-            if (qk_norm) {
-                float ss = 0.f;
+        constexpr int U = 4;  // heads whose reads are under way together
+        for (int hu = h0 + sub % HPR; hu < end; hu += U * HPR) {
+            typename Four<T>::raw lo[U], up[U];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) ss += x[e] * x[e] + y[e] * y[e];
-#pragma unroll
-                for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-                const float inv = rsqrtf(ss / (float)D + eps);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = x[e] * inv * (h < Hq ? wq[0][e] : wk[0][e]);
-                    y[e] = y[e] * inv * (h < Hq ? wq[1][e] : wk[1][e]);
-                }
+            for (int u = 0; u < U; ++u) {
+                const T *p = src + (size_t)min(hu + u * HPR, end - 1) * D;
+                lo[u] = *(const typename Four<T>::raw *)p;
+                up[u] = *(const typename Four<T>::raw *)(p + HALF);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) rotate_pair(x[e], y[e], cs[e], sn[e], &rx[e], &ry[e]);
-            if (h < Hq) {
-                T *dst = (T *)a.q_out + ((size_t)row * Hq + h) * D + i4;
-                Four<T>::put(dst, rx, 1.f);
-                Four<T>::put(dst + HALF, ry, 1.f);
-            } else {
-                KT *dst = kdst + (size_t)(h - Hq) * 2 * Bk * D;
-                Four<KT>::put(dst, rx, k_scale);
-                Four<KT>::put(dst + HALF, ry, k_scale);
+            for (int u = 0; u < U; ++u) {
+                const int h = hu + u * HPR;
+                if (h >= end) break;
+                float x[4], y[4], rx[4], ry[4];
+                Four<T>::get(lo[u], x);
+                Four<T>::get(up[u], y);
+                if (qk_norm) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ss += x[e] * x[e] + y[e] * y[e];
+#pragma unroll
+                    for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+                    const float inv = rsqrtf(ss / (float)D + eps);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = x[e] * inv * (h < Hq ? wq[0][e] : wk[0][e]);
+                        y[e] = y[e] * inv * (h < Hq ? wq[1][e] : wk[1][e]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) rotate_pair(x[e], y[e], cs[e], sn[e], &rx[e], &ry[e]);
+                if (h < Hq) {
+                    T *dst = (T *)a.q_out + ((size_t)row * Hq + h) * D + i4;
+                    Four<T>::put(dst, rx, 1.f);
+                    Four<T>::put(dst + HALF, ry, 1.f);
+                } else {
+                    KT *dst = kdst + (size_t)(h - Hq) * 2 * Bk * D;
+                    Four<KT>::put(dst, rx, k_scale);
+                    Four<KT>::put(dst + HALF, ry, k_scale);
+                }
             }
         }
     }
@@ -770,8 +782,8 @@ template <typename T, typename KT>
 static bool append_window(const Dims &dm, const AppendArgs &a, hipStream_t st) {
     if (dm.Bk != 16 || a.ld * (int64_t)sizeof(T) % 16) return false;
     const int windows = (a.R + kWindow - 1) / kWindow;
-    int parts = 1;  // of the heads: two workgroups to a CU, as long as a part has a rotated head for every wave's turn
-    while (windows * parts < 512 && 2 * parts <= (dm.Hq + dm.Hkv + 3) / 4) parts *= 2;
+    int parts = 1;  // of the heads: eight workgroups to a CU, as long as a part has a rotated head for every wave's turn
+    while (windows * parts < 2048 && 2 * parts <= (dm.Hq + dm.Hkv + 3) / 4) parts *= 2;
     const dim3 grid(windows, parts);
     const double l2t = log2(dm.theta);
     switch (dm.D) {
