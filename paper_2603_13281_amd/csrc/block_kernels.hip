@@ -4,6 +4,8 @@
 #include "block_ops.h"
 #include "device_util.h"
 
+#include <algorithm>
+
 namespace icarus {
 namespace {
 
@@ -440,6 +442,161 @@ __global__ void __launch_bounds__(256) k_bounds(BoundsArgs a, int Hkv, int D, in
     }
 }
 
+// Blocks of 16, a token's keys in 8 to 64 pieces of 16 bytes: a wave to the keys of a block and kv-head, which it reads as they lie, a piece to a lane; the pieces of
+// the same channels meet by exchanges between lanes.  Bound by HBM.  bfloat16 pairs stay pairs: as whole numbers of 16 bits whose order is that of the values
+// two at a time are compared (the float way, with a look at each value for NaN, took the vector units longer than the reads).
+template <typename KT> struct Piece;  // 16 bytes
+template <> struct Piece<bf16_t> {
+    static __device__ __forceinline__ void get(uint4 r, float (&v)[8]) {
+        const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(u[i] << 16);
+            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        }
+    }
+};
+template <> struct Piece<float> {
+    static __device__ __forceinline__ void get(uint4 r, float (&v)[4]) {
+        v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    }
+};
+template <> struct Piece<fp8_t> {
+    static __device__ __forceinline__ void get(uint4 r, float (&v)[16]) {
+        const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2_t p = __builtin_amdgcn_cvt_pk_f32_fp8(u[i], false), q = __builtin_amdgcn_cvt_pk_f32_fp8(u[i], true);
+            v[4 * i] = p[0]; v[4 * i + 1] = p[1]; v[4 * i + 2] = q[0]; v[4 * i + 3] = q[1];
+        }
+    }
+};
+typedef short s16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ s16x2_t ordered(uint32_t u) {  // two bfloat16 -> whole numbers in their order; its own inverse
+    const s16x2_t x = __builtin_bit_cast(s16x2_t, u);
+    return x ^ ((x >> 15) & s16x2_t{0x7fff, 0x7fff});
+}
+
+template <typename KT, int D>
+__global__ void __launch_bounds__(256) k_bounds_wave(BoundsArgs a, int Hkv) {
+    constexpr int Bk = 16, VW = 16 / sizeof(KT), LPT = D / VW, TPI = 64 / LPT, NI = Bk / TPI;  // channels of a piece, lanes of a token, tokens of a read, reads
+    const int s = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, t0 = lane / LPT, d0 = lane % LPT * VW;
+    const int from = max(a.from_lens[s], 0), to = (int)min((int64_t)max(a.to_lens[s], 0), (int64_t)a.max_blocks * Bk);
+    if (from >= to) return;
+    const int b_end = (to - 1) / Bk + 1;
+    const int32_t *bt = a.bt + (size_t)s * a.max_blocks;
+    int b = from / Bk + blockIdx.y, id = b < b_end ? bt[b] : -1;
+    for (; b < b_end; b += gridDim.y) {
+        const int here = id, n = min(Bk, to - b * Bk);
+        if (b + (int)gridDim.y < b_end) id = bt[b + gridDim.y];
+        if (here < 0 || here >= a.num_blocks) continue;
+        for (int c = w; c < Hkv; c += 4) {
+            const size_t rec = (size_t)here * Hkv + c;
+            const uint4 *src = (const uint4 *)((const KT *)a.pool + rec * 2 * Bk * D) + lane;
+            uint4 r[NI];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) r[i] = src[i * 64];
+            float hi[VW], lo[VW];
+            auto by_value = [&] {
+#pragma unroll
+                for (int e = 0; e < VW; ++e) {
+                    hi[e] = -INFINITY;
+                    lo[e] = INFINITY;
+                }
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    float v[VW];
+                    Piece<KT>::get(r[i], v);
+                    if (i * TPI + t0 < n)
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) {
+                            const float x = finite_or_edge(v[e]);
+                            hi[e] = fmaxf(hi[e], x);
+                            lo[e] = fminf(lo[e], x);
+                        }
+                }
+#pragma unroll
+                for (int o = LPT; o < 64; o <<= 1)
+#pragma unroll
+                    for (int e = 0; e < VW; ++e) {
+                        hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], o, 64));
+                        lo[e] = fminf(lo[e], __shfl_xor(lo[e], o, 64));
+                    }
+            };
+            if constexpr (sizeof(KT) == 2) {
+                s16x2_t h[4], l[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    h[e] = s16x2_t{-32768, -32768};
+                    l[e] = s16x2_t{32767, 32767};
+                }
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const uint32_t u[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+                    if (i * TPI + t0 < n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const s16x2_t x = ordered(u[e]);
+                            h[e] = __builtin_elementwise_max(h[e], x);
+                            l[e] = __builtin_elementwise_min(l[e], x);
+                        }
+                }
+                bool nan = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                    for (int o = LPT; o < 64; o <<= 1) {
+                        h[e] = __builtin_elementwise_max(h[e], __builtin_bit_cast(s16x2_t, __shfl_xor(__builtin_bit_cast(int, h[e]), o, 64)));
+                        l[e] = __builtin_elementwise_min(l[e], __builtin_bit_cast(s16x2_t, __shfl_xor(__builtin_bit_cast(int, l[e]), o, 64)));
+                    }
+                    nan |= h[e][0] > 0x7f80 || h[e][1] > 0x7f80 || l[e][0] < -0x7f81 || l[e][1] < -0x7f81;  // beyond the infinities
+                }
+                if (__any(nan)) {
+                    by_value();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t x = __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, h[e])));
+                        const uint32_t y = __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, l[e])));
+                        hi[2 * e] = finite_or_edge(__uint_as_float(x << 16));
+                        hi[2 * e + 1] = finite_or_edge(__uint_as_float(x & 0xffff0000u));
+                        lo[2 * e] = finite_or_edge(__uint_as_float(y << 16));
+                        lo[2 * e + 1] = finite_or_edge(__uint_as_float(y & 0xffff0000u));
+                    }
+                }
+            } else {
+                by_value();
+            }
+            float most = 0.f;
+#pragma unroll
+            for (int e = 0; e < VW; ++e) most = fmaxf(most, fmaxf(fabsf(hi[e]), fabsf(lo[e])));
+#pragma unroll
+            for (int o = 1; o < LPT; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+            const int e2 = step_exponent(most);
+            const float inv = ldexpf(1.f, -e2);
+            int8_t *dst = a.codes + rec * 2 * D + d0;
+            auto put = [&](int8_t *p, const float (&v)[VW], bool up) {
+                uint32_t word[VW / 4];
+#pragma unroll
+                for (int i = 0; i < VW / 4; ++i) {
+                    word[i] = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float x = v[4 * i + k] * inv;
+                        word[i] |= (uint32_t)(uint8_t)code_of(up ? ceilf(x) : floorf(x)) << 8 * k;
+                    }
+                }
+                if constexpr (VW == 4) *(uint32_t *)p = word[0];
+                else if constexpr (VW == 8) *(uint2 *)p = make_uint2(word[0], word[1]);
+                else *(uint4 *)p = make_uint4(word[0], word[1], word[2], word[3]);
+            };
+            if (t0 == 0) put(dst, hi, true);
+            if (t0 == (TPI > 1 ? 1 : 0)) put(dst + D, lo, false);
+            if (lane == 0) a.scales[rec] = ldexpf(1.f, e2);
+        }
+    }
+}
+
 // ---- choice of the blocks ---------------------------------------------------------------------------------------------------
 // A score as a number whose order is that of the floats.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -808,12 +965,29 @@ hipError_t launch_append(const Dims &dm, bool generic, const AppendArgs &a, hipS
     return hipGetLastError();
 }
 
-hipError_t launch_bounds(const Dims &dm, const BoundsArgs &a, hipStream_t st) {
-    const int most = a.max_new > 0 ? min(a.max_blocks, (a.max_new - 1) / dm.Bk + 2) : a.max_blocks;
-    DISPATCH_TK(dm.bf16, dm.kv8, {
-        (void)sizeof(T);
-        hipLaunchKernelGGL(k_bounds<KT>, dim3(a.S, min(most, 65535), (dm.Hkv + 3) / 4), dim3(256), 0, st, a, dm.Hkv, dm.D, dm.Bk);
-    });
+constexpr int kBoundsWgs = 4096;
+template <typename KT>
+static bool bounds_wave(const Dims &dm, const BoundsArgs &a, dim3 grid, hipStream_t st) {
+    if (dm.Bk != 16) return false;
+    switch (dm.D) {
+    case 64: hipLaunchKernelGGL((k_bounds_wave<KT, 64>), grid, dim3(256), 0, st, a, dm.Hkv); return true;
+    case 128: hipLaunchKernelGGL((k_bounds_wave<KT, 128>), grid, dim3(256), 0, st, a, dm.Hkv); return true;
+    case 256: hipLaunchKernelGGL((k_bounds_wave<KT, 256>), grid, dim3(256), 0, st, a, dm.Hkv); return true;
+    default: return false;
+    }
+}
+
+hipError_t launch_bounds(const Dims &dm, bool generic, const BoundsArgs &a, hipStream_t st) {
+    const int64_t most = a.max_new > 0 ? std::min<int64_t>(a.max_blocks, (a.max_new - 1) / dm.Bk + 2) : a.max_blocks;  // blocks of a sequence, about
+    // workgroups to a sequence: a block to each, until there are 16 to a CU; what is left goes round
+    const int per_seq = (int)std::min<int64_t>(most, std::max<int64_t>(1, (kBoundsWgs + a.S - 1) / a.S));
+    bool done = false;
+    if (!generic) DISPATCH_TK(dm.bf16, dm.kv8, { (void)sizeof(T); done = bounds_wave<KT>(dm, a, dim3(a.S, per_seq), st); });
+    if (!done)
+        DISPATCH_TK(dm.bf16, dm.kv8, {
+            (void)sizeof(T);
+            hipLaunchKernelGGL(k_bounds<KT>, dim3(a.S, per_seq, (dm.Hkv + 3) / 4), dim3(256), 0, st, a, dm.Hkv, dm.D, dm.Bk);
+        });
     return hipGetLastError();
 }
 

@@ -27,7 +27,7 @@ struct BoundsArgs {
     const int32_t *from_lens, *to_lens; int max_new;
     int8_t *codes; float *scales;
 };
-hipError_t launch_bounds(const Dims &dm, const BoundsArgs &a, hipStream_t st);
+hipError_t launch_bounds(const Dims &dm, bool generic, const BoundsArgs &a, hipStream_t st);
 
 struct SelectArgs {
     const void *q; const int8_t *codes; const float *scales;

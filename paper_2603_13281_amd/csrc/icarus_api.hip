@@ -2076,7 +2076,7 @@ icarus_status icarus_key_bounds(icarus_ctx *ctx, const void *kv_pool, const int3
     if (!all_aligned({kv_pool, codes}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "kv_pool and codes must be 16-byte aligned");
     if (!all_aligned({block_tables, from_lens, to_lens, scales}, 4)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays and scales must be aligned to their element");
     BoundsArgs a{kv_pool, block_tables, max_blocks, ctx->cfg.num_blocks, S, from_lens, to_lens, max_new, codes, scales};
-    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_bounds(ctx->dm, a, (hipStream_t)stream));
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_bounds(ctx->dm, ctx->mode != 0, a, (hipStream_t)stream));
     return ICARUS_OK;
 }
 
