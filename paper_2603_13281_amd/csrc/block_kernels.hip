@@ -5,6 +5,7 @@
 #include "device_util.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace icarus {
 namespace {
@@ -442,33 +443,27 @@ __global__ void __launch_bounds__(256) k_bounds(BoundsArgs a, int Hkv, int D, in
     }
 }
 
-// Blocks of 16, a token's keys in 8 to 64 pieces of 16 bytes: a wave to the keys of a block and kv-head, which it reads as they lie, a piece to a lane; the pieces of
-// the same channels meet by exchanges between lanes.  Bound by HBM.  bfloat16 pairs stay pairs: as whole numbers of 16 bits whose order is that of the values
-// two at a time are compared (the float way, with a look at each value for NaN, took the vector units longer than the reads).
-template <typename KT> struct Piece;  // 16 bytes
-template <> struct Piece<bf16_t> {
-    static __device__ __forceinline__ void get(uint4 r, float (&v)[8]) {
-        const uint32_t u[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-        }
+// Blocks of 16, head sizes 64, 128 and 256: a wave to the keys of a block and kv-head, which it reads as they lie, four channels of a token to a lane; a lane sees 4 to 16 of
+// the tokens, and lanes of the same channels meet by exchanges in registers.  Bound by HBM (half of a block's lines), with the vector units close behind: with
+// 16 bytes to a lane there were twice the exchanges and the reads waited for them.  bfloat16 pairs stay pairs: as whole numbers of 16 bits whose order is that of the values two
+// are compared at a time.
+template <typename KT> struct Quad;  // four elements as they lie
+template <> struct Quad<bf16_t> {
+    typedef uint2 raw;
+    static __device__ __forceinline__ void get(raw r, float (&v)[4]) {
+        v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);
+        v[2] = __uint_as_float(r.y << 16); v[3] = __uint_as_float(r.y & 0xffff0000u);
     }
 };
-template <> struct Piece<float> {
-    static __device__ __forceinline__ void get(uint4 r, float (&v)[4]) {
-        v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
-    }
+template <> struct Quad<float> {
+    typedef float4 raw;
+    static __device__ __forceinline__ void get(raw r, float (&v)[4]) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
 };
-template <> struct Piece<fp8_t> {
-    static __device__ __forceinline__ void get(uint4 r, float (&v)[16]) {
-        const uint32_t u[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x2_t p = __builtin_amdgcn_cvt_pk_f32_fp8(u[i], false), q = __builtin_amdgcn_cvt_pk_f32_fp8(u[i], true);
-            v[4 * i] = p[0]; v[4 * i + 1] = p[1]; v[4 * i + 2] = q[0]; v[4 * i + 3] = q[1];
-        }
+template <> struct Quad<fp8_t> {
+    typedef uint32_t raw;
+    static __device__ __forceinline__ void get(raw r, float (&v)[4]) {
+        const f32x2_t p = __builtin_amdgcn_cvt_pk_f32_fp8(r, false), q = __builtin_amdgcn_cvt_pk_f32_fp8(r, true);
+        v[0] = p[0]; v[1] = p[1]; v[2] = q[0]; v[3] = q[1];
     }
 };
 typedef short s16x2_t __attribute__((ext_vector_type(2)));
@@ -477,10 +472,33 @@ __device__ __forceinline__ s16x2_t ordered(uint32_t u) {  // two bfloat16 -> who
     return x ^ ((x >> 15) & s16x2_t{0x7fff, 0x7fff});
 }
 
+// op over lanes that are O apart, O = 16 or 32, in both of them.
+template <int O, typename V, typename Op> __device__ __forceinline__ V with_lane(V x, Op op) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    if constexpr (O == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return op(__builtin_bit_cast(V, (uint32_t)r[0]), __builtin_bit_cast(V, (uint32_t)r[1]));
+    } else {
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        return op(__builtin_bit_cast(V, (uint32_t)r[0]), __builtin_bit_cast(V, (uint32_t)r[1]));
+    }
+}
+// The largest of the wave's lanes, in each of them; inside 16 lanes as operands of the maximum itself.
+__device__ __forceinline__ float max_of_lanes(float x) {
+    auto step = [&](auto ctrl) { x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true))); };
+    step(std::integral_constant<int, 0xb1>());   // quad 1 0 3 2
+    step(std::integral_constant<int, 0x4e>());   // quad 2 3 0 1
+    step(std::integral_constant<int, 0x141>());  // mirrored in 8
+    step(std::integral_constant<int, 0x140>());  // mirrored in 16
+    auto most = [](float a, float b) { return fmaxf(a, b); };
+    return with_lane<32>(with_lane<16>(x, most), most);
+}
+
 template <typename KT, int D>
 __global__ void __launch_bounds__(256) k_bounds_wave(BoundsArgs a, int Hkv) {
-    constexpr int Bk = 16, VW = 16 / sizeof(KT), LPT = D / VW, TPI = 64 / LPT, NI = Bk / TPI;  // channels of a piece, lanes of a token, tokens of a read, reads
-    const int s = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, t0 = lane / LPT, d0 = lane % LPT * VW;
+    constexpr int Bk = 16, LPT = D / 4, TPI = 64 / LPT, NI = Bk / TPI;  // lanes of a token, tokens of a read, reads
+    typedef typename Quad<KT>::raw raw;
+    const int s = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, t0 = lane / LPT;
     const int from = max(a.from_lens[s], 0), to = (int)min((int64_t)max(a.to_lens[s], 0), (int64_t)a.max_blocks * Bk);
     if (from >= to) return;
     const int b_end = (to - 1) / Bk + 1;
@@ -492,106 +510,105 @@ __global__ void __launch_bounds__(256) k_bounds_wave(BoundsArgs a, int Hkv) {
         if (here < 0 || here >= a.num_blocks) continue;
         for (int c = w; c < Hkv; c += 4) {
             const size_t rec = (size_t)here * Hkv + c;
-            const uint4 *src = (const uint4 *)((const KT *)a.pool + rec * 2 * Bk * D) + lane;
-            uint4 r[NI];
+            const raw *src = (const raw *)((const KT *)a.pool + rec * 2 * Bk * D) + lane % LPT;
+            raw r[NI];  // behind the last token: the last again
 #pragma unroll
-            for (int i = 0; i < NI; ++i) r[i] = src[i * 64];
-            float hi[VW], lo[VW];
+            for (int i = 0; i < NI; ++i) r[i] = src[min(i * TPI + t0, n - 1) * LPT];
+            float hi[4], lo[4];
             auto by_value = [&] {
 #pragma unroll
-                for (int e = 0; e < VW; ++e) {
+                for (int e = 0; e < 4; ++e) {
                     hi[e] = -INFINITY;
                     lo[e] = INFINITY;
                 }
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
-                    float v[VW];
-                    Piece<KT>::get(r[i], v);
-                    if (i * TPI + t0 < n)
+                    float v[4];
+                    Quad<KT>::get(r[i], v);
 #pragma unroll
-                        for (int e = 0; e < VW; ++e) {
-                            const float x = finite_or_edge(v[e]);
-                            hi[e] = fmaxf(hi[e], x);
-                            lo[e] = fminf(lo[e], x);
-                        }
-                }
-#pragma unroll
-                for (int o = LPT; o < 64; o <<= 1)
-#pragma unroll
-                    for (int e = 0; e < VW; ++e) {
-                        hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], o, 64));
-                        lo[e] = fminf(lo[e], __shfl_xor(lo[e], o, 64));
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = finite_or_edge(v[e]);
+                        hi[e] = fmaxf(hi[e], x);
+                        lo[e] = fminf(lo[e], x);
                     }
-            };
-            if constexpr (sizeof(KT) == 2) {
-                s16x2_t h[4], l[4];
+                }
+                auto most = [](float x, float y) { return fmaxf(x, y); };
+                auto least = [](float x, float y) { return fminf(x, y); };
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                    if constexpr (LPT <= 16) {
+                        hi[e] = with_lane<16>(hi[e], most);
+                        lo[e] = with_lane<16>(lo[e], least);
+                    }
+                    if constexpr (LPT <= 32) {
+                        hi[e] = with_lane<32>(hi[e], most);
+                        lo[e] = with_lane<32>(lo[e], least);
+                    }
+                }
+            };
+            if constexpr (sizeof(KT) == 2) {
+                s16x2_t h[2], l[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
                     h[e] = s16x2_t{-32768, -32768};
                     l[e] = s16x2_t{32767, 32767};
                 }
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const uint32_t u[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
-                    if (i * TPI + t0 < n)
+                for (int i = 0; i < NI; ++i)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const s16x2_t x = ordered(u[e]);
-                            h[e] = __builtin_elementwise_max(h[e], x);
-                            l[e] = __builtin_elementwise_min(l[e], x);
-                        }
-                }
-                bool nan = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-#pragma unroll
-                    for (int o = LPT; o < 64; o <<= 1) {
-                        h[e] = __builtin_elementwise_max(h[e], __builtin_bit_cast(s16x2_t, __shfl_xor(__builtin_bit_cast(int, h[e]), o, 64)));
-                        l[e] = __builtin_elementwise_min(l[e], __builtin_bit_cast(s16x2_t, __shfl_xor(__builtin_bit_cast(int, l[e]), o, 64)));
+                    for (int e = 0; e < 2; ++e) {
+                        const s16x2_t x = ordered(e ? r[i].y : r[i].x);
+                        h[e] = __builtin_elementwise_max(h[e], x);
+                        l[e] = __builtin_elementwise_min(l[e], x);
                     }
-                    nan |= h[e][0] > 0x7f80 || h[e][1] > 0x7f80 || l[e][0] < -0x7f81 || l[e][1] < -0x7f81;  // beyond the infinities
+                auto most = [](s16x2_t x, s16x2_t y) { return __builtin_elementwise_max(x, y); };
+                auto least = [](s16x2_t x, s16x2_t y) { return __builtin_elementwise_min(x, y); };
+                bool odd = false;  // an infinity or a NaN
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if constexpr (LPT <= 16) {
+                        h[e] = with_lane<16>(h[e], most);
+                        l[e] = with_lane<16>(l[e], least);
+                    }
+                    if constexpr (LPT <= 32) {
+                        h[e] = with_lane<32>(h[e], most);
+                        l[e] = with_lane<32>(l[e], least);
+                    }
+                    odd |= max(h[e][0], h[e][1]) >= 0x7f80 || min(l[e][0], l[e][1]) <= -0x7f81;
                 }
-                if (__any(nan)) {
+                if (__any(odd)) {
                     by_value();
                 } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t x = __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, h[e])));
-                        const uint32_t y = __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, l[e])));
-                        hi[2 * e] = finite_or_edge(__uint_as_float(x << 16));
-                        hi[2 * e + 1] = finite_or_edge(__uint_as_float(x & 0xffff0000u));
-                        lo[2 * e] = finite_or_edge(__uint_as_float(y << 16));
-                        lo[2 * e + 1] = finite_or_edge(__uint_as_float(y & 0xffff0000u));
-                    }
+                    Quad<bf16_t>::get(make_uint2(__builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, h[0]))),
+                                                 __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, h[1])))), hi);
+                    Quad<bf16_t>::get(make_uint2(__builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, l[0]))),
+                                                 __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, l[1])))), lo);
                 }
             } else {
                 by_value();
             }
             float most = 0.f;
 #pragma unroll
-            for (int e = 0; e < VW; ++e) most = fmaxf(most, fmaxf(fabsf(hi[e]), fabsf(lo[e])));
-#pragma unroll
-            for (int o = 1; o < LPT; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-            const int e2 = step_exponent(most);
+            for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(hi[e]), fabsf(lo[e])));
+            const int e2 = step_exponent(max_of_lanes(most));
             const float inv = ldexpf(1.f, -e2);
-            int8_t *dst = a.codes + rec * 2 * D + d0;
-            auto put = [&](int8_t *p, const float (&v)[VW], bool up) {
-                uint32_t word[VW / 4];
+            // The first token's lanes write the largest, the second's the smallest: floor(x) = -ceil(-x), so that one way serves both.
+            auto put = [&](bool low) {
+                const float turn = low ? -inv : inv;
+                uint32_t word = 0;
 #pragma unroll
-                for (int i = 0; i < VW / 4; ++i) {
-                    word[i] = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float x = v[4 * i + k] * inv;
-                        word[i] |= (uint32_t)(uint8_t)code_of(up ? ceilf(x) : floorf(x)) << 8 * k;
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const int x = (int)fminf(fmaxf(ceilf((low ? lo : hi)[e] * turn), -127.f), 127.f);
+                    word |= (uint32_t)(uint8_t)(low ? -x : x) << 8 * e;
                 }
-                if constexpr (VW == 4) *(uint32_t *)p = word[0];
-                else if constexpr (VW == 8) *(uint2 *)p = make_uint2(word[0], word[1]);
-                else *(uint4 *)p = make_uint4(word[0], word[1], word[2], word[3]);
+                ((uint32_t *)(a.codes + rec * 2 * D))[(low ? LPT : 0) + lane % LPT] = word;
             };
-            if (t0 == 0) put(dst, hi, true);
-            if (t0 == (TPI > 1 ? 1 : 0)) put(dst + D, lo, false);
+            if constexpr (TPI > 1) {
+                if (t0 < 2) put(t0 == 1);
+            } else {
+                put(false);
+                put(true);
+            }
             if (lane == 0) a.scales[rec] = ldexpf(1.f, e2);
         }
     }
