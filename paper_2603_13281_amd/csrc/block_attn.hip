@@ -1,23 +1,12 @@
 // Attention of single-token rows over the blocks that were selected for their sequence and kv-head.
 #include "attn_tile.h"
 #include "block_ops.h"
+#include "block_util.h"
 
 #include <algorithm>
 
 namespace icarus {
 namespace {
-
-#define DISPATCH_T(bf16, ...)                                        \
-    do {                                                             \
-        if (bf16) { typedef bf16_t T; __VA_ARGS__; }                 \
-        else { typedef float T; __VA_ARGS__; }                       \
-    } while (0)
-#define DISPATCH_TK(bf16, kv8, ...)                                   \
-    do {                                                              \
-        if (kv8) { typedef fp8_t KT; DISPATCH_T(bf16, __VA_ARGS__); } \
-        else if (bf16) { typedef bf16_t T; typedef bf16_t KT; __VA_ARGS__; } \
-        else { typedef float T; typedef float KT; __VA_ARGS__; }      \
-    } while (0)
 
 // Any shape: a workgroup to a query head of a row; a thread to a position for the scores, to a channel for the sum of the values.
 // Running maximum and sum in float32, rounds of kChunk positions.
@@ -352,48 +341,221 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
     }
 }
 
-// The splits of a row's head joined, in their order: a wave to a head, two channels to a lane.
-__global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitOut part, int Hq) {
+bool on_matrix_cores(const Dims &dm) { return dm.bf16 && dm.D == kD && dm.Bk == kBk; }
+
+// ---- blocks of 16, head sizes that are multiples of 16: vector units -----------------------------------------------------------
+// For float32 and head sizes other than 128.  A workgroup takes a sequence, kv-head and range of the list, NQ of its stacked queries at a time; a wave takes
+// blocks in turn, whose ids it reads 64 at a time.  Scores: lane t + 16 p has a quarter p of token t's key, the queries lie in LDS; values: a lane has
+// channels d, d + 64, .. of all tokens, a row of the transposed block, and the weights lie in LDS.  Each block is read once for NQ queries.
+template <typename T, typename KT, int ND, int NQ>  // ND: channels of a lane, D <= 64 ND; NQ: a multiple of 4
+__global__ void __launch_bounds__(256) k_block_attn_vec(BlockAttnArgs a, SplitOut part, int Hq, int Hkv, int D, float scale_log2, float v_scale) {
+    constexpr int Bk = 16;
+    __shared__ __attribute__((aligned(16))) float qs[NQ][64 * ND], weight[4][NQ][Bk], image[4][NQ][64 * ND];
+    __shared__ float image_m[4][NQ], image_l[4][NQ];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, quarter = lane >> 4, g = Hq / Hkv;
+    const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, split = blockIdx.y;
+    const int row0 = min(max(a.row_start[s], 0), a.R), G = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
+    const int len = max(a.kv_lens[s], 0), n_sel = min(max(a.counts[s], 0), a.max_selected);
+    const int e_begin = split * part.per, e_end = min(n_sel, e_begin + part.per);
+    const int32_t *list = a.blocks + (size_t)pair * a.max_selected, *bt = a.bt + (size_t)s * a.max_blocks;
+    const int PD = D / 4;
+    for (int j0 = 0; j0 < G; j0 += NQ) {
+        const int nq = min(NQ, G - j0);
+        __syncthreads();
+        for (int i = threadIdx.x; i < NQ * D; i += 256) {
+            const int j = j0 + min(i / D, nq - 1);
+            qs[i / D][i % D] = Elem<T>::ld((const T *)a.q + ((size_t)(row0 + j / g) * Hq + c * g + j % g) * D + i % D);
+        }
+        __syncthreads();
+        float m[NQ], l[NQ], acc[NQ][ND];
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            m[j] = -INFINITY;
+            l[j] = 0.f;
+#pragma unroll
+            for (int k = 0; k < ND; ++k) acc[j][k] = 0.f;
+        }
+        for (int e0 = e_begin + w; e0 < e_end; e0 += 256) {
+            int my_id = -1, my_n = 0;  // block of entry e0 + 4 lane, and its tokens
+            if (e0 + 4 * lane < e_end) {
+                const int b = list[e0 + 4 * lane];
+                if (b >= 0 && b < a.max_blocks) {
+                    my_n = (int)min((int64_t)Bk, (int64_t)len - (int64_t)b * Bk);
+                    if (my_n > 0) my_id = bt[b];
+                }
+            }
+            const int some = min(64, (e_end - e0 + 3) / 4);
+            for (int i0 = 0; i0 < some; ++i0) {
+                const int id = __builtin_amdgcn_readlane(my_id, i0), n = __builtin_amdgcn_readlane(my_n, i0);
+                if (id < 0 || id >= a.num_blocks) continue;
+                const KT *blk = (const KT *)a.pool + ((size_t)id * Hkv + c) * 2 * Bk * D;
+                typename Quad<KT>::raw vr[ND][4];
+#pragma unroll
+                for (int k = 0; k < ND; ++k)
+                    if (lane + 64 * k < D)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) vr[k][i] = ((const typename Quad<KT>::raw *)(blk + Bk * D + (lane + 64 * k) * Bk))[i];
+                const typename Quad<KT>::raw *kr = (const typename Quad<KT>::raw *)(blk + min(t, n - 1) * D + quarter * PD);
+                float dot[NQ];
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) dot[j] = 0.f;
+                for (int i0 = 0; i0 < PD / 4; i0 += 4) {
+                    typename Quad<KT>::raw kq[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) kq[u] = kr[min(i0 + u, PD / 4 - 1)];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if (i0 + u >= PD / 4) continue;
+                        float k[4];
+                        Quad<KT>::get(kq[u], k);
+#pragma unroll
+                        for (int jj = 0; jj < NQ; jj += 4) {
+                            if (jj >= nq) continue;
+#pragma unroll
+                            for (int j = jj; j < jj + 4; ++j) {
+                                const float4 qv = *(const float4 *)&qs[j][quarter * PD + 4 * (i0 + u)];
+                                dot[j] += qv.x * k[0];
+                                dot[j] += qv.y * k[1];
+                                dot[j] += qv.z * k[2];
+                                dot[j] += qv.w * k[3];
+                            }
+                        }
+                    }
+                }
+                auto weigh = [&](int j) {
+                    float x = dot[j];
+                    x += __shfl_xor(x, 16, 64);
+                    x += __shfl_xor(x, 32, 64);
+                    x = t < n ? x * scale_log2 : -INFINITY;
+                    if (__any(x > m[j] + kSlack)) {  // see compute_group: the reference moves rarely
+                        const float m_new = fmaxf(m[j], wave_max(x)), f = __builtin_amdgcn_exp2f(m[j] - m_new);
+                        m[j] = m_new;
+                        l[j] *= f;
+#pragma unroll
+                        for (int k = 0; k < ND; ++k) acc[j][k] *= f;
+                    }
+                    const float p = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - m[j]);
+                    l[j] += p;  // of token t, in all four quarters
+                    if (quarter == 0) weight[w][j][t] = p;
+                };
+#pragma unroll
+                for (int j = 0; j < NQ; ++j)
+                    if (j < nq) weigh(j);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int k = 0; k < ND; ++k) {
+                    if (lane + 64 * k >= D) continue;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float v[4];
+                        Quad<KT>::get(vr[k][i], v);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) v[u] = 4 * i + u < n ? v[u] : 0.f;  // places behind the last token may hold anything
+#pragma unroll
+                        for (int jj = 0; jj < NQ; jj += 4) {
+                            if (jj >= nq) continue;
+#pragma unroll
+                            for (int j = jj; j < jj + 4; ++j) {
+                                const float4 p = *(const float4 *)&weight[w][j][4 * i];
+                                acc[j][k] += p.x * v[0];
+                                acc[j][k] += p.y * v[1];
+                                acc[j][k] += p.z * v[2];
+                                acc[j][k] += p.w * v[3];
+                            }
+                        }
+                    }
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            float x = l[j];  // over the 16 tokens
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) x += __shfl_xor(x, o, 64);
+            if (lane == 0) {
+                image_m[w][j] = m[j];
+                image_l[w][j] = x;
+            }
+#pragma unroll
+            for (int k = 0; k < ND; ++k) image[w][j][lane + 64 * k] = acc[j][k];
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < nq * D; i += 256) {
+            const int j = i / D, d = i % D;
+            const float mx = fmaxf(fmaxf(image_m[0][j], image_m[1][j]), fmaxf(image_m[2][j], image_m[3][j]));
+            float o = 0.f, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = image_m[k][j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(image_m[k][j] - mx);
+                sum += f * image_l[k][j];
+                o += f * image[k][j][d];
+            }
+            const size_t at = (size_t)(row0 + (j0 + j) / g) * Hq + c * g + (j0 + j) % g;
+            if (part.splits == 1) {
+                Elem<T>::st((T *)a.out + at * D + d, sum > 0.f ? o * v_scale / sum : 0.f);
+            } else {
+                const size_t ps = (size_t)split * a.R * Hq + at;
+                part.o[ps * D + d] = o * v_scale;
+                if (d == 0) part.ml[ps] = make_float2(mx, sum);
+            }
+        }
+    }
+}
+
+// The splits of a row's head joined, in their order: a wave to a head, two channels at a time to a lane.
+template <typename T>
+__global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitOut part, int Hq, int D) {
     const int s = blockIdx.x, h = blockIdx.z * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (h >= Hq) return;
     const int row0 = min(max(a.row_start[s], 0), a.R), row1 = min(max(a.row_start[s + 1], row0), a.R);
     for (int row = row0 + blockIdx.y; row < row1; row += gridDim.y) {
         const size_t at = (size_t)row * Hq + h, step = (size_t)a.R * Hq;
-        float mx = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
-        for (int k0 = 0; k0 < part.splits; k0 += 64) {
-            const int cnt = min(64, part.splits - k0);
-            const float2 mine = lane < cnt ? part.ml[at + (k0 + lane) * step] : make_float2(-INFINITY, 0.f);
-            const float m_new = fmaxf(mx, wave_max(mine.x));
-            const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine.x - m_new), old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m_new);
-            l = l * old + wave_sum(f * mine.y);
-            x *= old;
-            y *= old;
-            for (int k = 0; k < cnt; k += 8) {  // eight loads in flight; behind the last split: the last again, with weight 0
-                float2 o[8];
+        for (int d0 = 0; d0 < D; d0 += 128) {
+            const int d = min(d0 + 2 * lane, D - 2);
+            float mx = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
+            for (int k0 = 0; k0 < part.splits; k0 += 64) {
+                const int cnt = min(64, part.splits - k0);
+                const float2 mine = lane < cnt ? part.ml[at + (k0 + lane) * step] : make_float2(-INFINITY, 0.f);
+                const float m_new = fmaxf(mx, wave_max(mine.x));
+                const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine.x - m_new), old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m_new);
+                l = l * old + wave_sum(f * mine.y);
+                x *= old;
+                y *= old;
+                for (int k = 0; k < cnt; k += 8) {  // eight loads in flight; behind the last split: the last again, with weight 0
+                    float2 o[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = *(const float2 *)(part.o + (at + (k0 + min(k + e, cnt - 1)) * step) * kD + 2 * lane);
+                    for (int e = 0; e < 8; ++e) o[e] = *(const float2 *)(part.o + (at + (k0 + min(k + e, cnt - 1)) * step) * D + d);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float fk = k + e < cnt ? __shfl(f, (k + e) & 63, 64) : 0.f;
-                    x += fk * o[e].x;
-                    y += fk * o[e].y;
+                    for (int e = 0; e < 8; ++e) {
+                        const float fk = k + e < cnt ? __shfl(f, (k + e) & 63, 64) : 0.f;
+                        x += fk * o[e].x;
+                        y += fk * o[e].y;
+                    }
                 }
+                mx = m_new;
             }
-            mx = m_new;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            if (d0 + 2 * lane < D) {
+                if constexpr (sizeof(T) == 2) *(uint32_t *)((T *)a.out + at * D + d) = pack_bf16(x * inv, y * inv);
+                else *(float2 *)((T *)a.out + at * D + d) = make_float2(x * inv, y * inv);
+            }
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        ((uint32_t *)a.out)[at * (kD / 2) + lane] = pack_bf16(x * inv, y * inv);
     }
 }
 
-// Splits of the lists, at most `most`.  Items go over 256 workgroups in rounds; a round costs the blocks of its items and as much as kItemCost blocks on top, joining kJoinCost.
+// Splits of the lists, at most `most`.  Items go over the workgroups that the chip holds (1 to a CU on the matrix cores, 4 on the vector units) in rounds; a round costs the blocks
+// of its items and as much as kItemCost blocks on top, joining kJoinCost.
 constexpr int kWgs = 256, kItemCost = 12, kJoinCost = 24, kMaxSplits = 32;
-int splits_for(int64_t pairs, int max_selected, int most = kMaxSplits) {
+int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxSplits) {
     const int least = (max_selected + kItemBlocks - 1) / kItemBlocks;
+    const int64_t wgs = on_matrix_cores(dm) ? kWgs : 4 * kWgs;
     int best = 0;
     int64_t cost = 0;
     for (int n = std::max(1, least); n <= std::max(least, std::min(most, (max_selected + 7) / 8)) || !best; ++n) {  // 8 blocks: a group to a wave
-        const int64_t rounds = (pairs * n + kWgs - 1) / kWgs, blocks = (max_selected + n - 1) / n;
+        const int64_t rounds = (pairs * n + wgs - 1) / wgs, blocks = (max_selected + n - 1) / n;
         const int64_t t = rounds * (blocks + kItemCost) + (n > 1 ? kJoinCost : 0);
         if (!best || t < cost) {
             best = n;
@@ -419,33 +581,48 @@ hipError_t launch_mfma(const Dims &dm, const BlockAttnArgs &a, const SplitOut &p
 
 }  // namespace
 
-bool block_attn_mfma_supported(const Dims &dm) { return dm.bf16 && dm.D == kD && dm.Bk == kBk; }
+bool block_attn_fast(const Dims &dm) { return dm.Bk == kBk && dm.D % 16 == 0; }
 
 size_t block_attn_workspace(const Dims &dm, int S, int R, int max_selected) {
-    if (!block_attn_mfma_supported(dm) || S == 0) return 256;
-    const int splits = splits_for((int64_t)S * dm.Hkv, max_selected);
-    return splits > 1 ? (size_t)splits * R * dm.Hq * (kD + 2) * 4 + 512 : 256;
+    if (!block_attn_fast(dm) || S == 0) return 256;
+    const int splits = splits_for(dm, (int64_t)S * dm.Hkv, max_selected);
+    return splits > 1 ? (size_t)splits * R * dm.Hq * (dm.D + 2) * 4 + 512 : 256;
+}
+
+template <typename T, typename KT>
+static hipError_t launch_vec(const Dims &dm, const BlockAttnArgs &a, const SplitOut &part, hipStream_t st) {
+    const dim3 grid(a.S * dm.Hkv, part.splits);
+    const float scale_log2 = kLog2e / sqrtf((float)dm.D) * (sizeof(KT) == 1 ? dm.k_scale : 1.f), v_scale = sizeof(KT) == 1 ? dm.v_scale : 1.f;
+    switch ((dm.D + 63) / 64) {
+    case 1: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 1, 16>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
+    case 2: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 2, 8>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
+    case 3: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 3, 8>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
+    default: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 4, 8>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
+    }
+    return hipGetLastError();
 }
 
 hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *workspace, hipStream_t st) {
     const int g = dm.Hq / dm.Hkv;
     const int64_t pairs = (int64_t)a.S * dm.Hkv;
     const int rows = a.seq_rows ? std::min(a.seq_rows, a.R) : a.R;  // of a sequence, at most
+    const bool mfma = on_matrix_cores(dm);
     const int64_t tiles = ((int64_t)rows * g + 15) / 16;
     const int nt = (int)std::min<int64_t>(tiles, 3);
     SplitOut part;
-    part.tile_groups = (int)((tiles + nt - 1) / nt);
-    part.splits = splits_for(pairs * part.tile_groups, a.max_selected, splits_for(pairs, a.max_selected));  // no more than the workspace was sized for
+    part.tile_groups = mfma ? (int)((tiles + nt - 1) / nt) : 1;
+    part.splits = splits_for(dm, pairs * part.tile_groups, a.max_selected, splits_for(dm, pairs, a.max_selected));  // no more than the workspace was sized for
     part.per = std::max(2, ((a.max_selected + part.splits - 1) / part.splits + 1) & ~1);
     part.o = (float *)workspace;
-    part.ml = (float2 *)(part.o + (size_t)part.splits * a.R * dm.Hq * kD);
+    part.ml = (float2 *)(part.o + (size_t)part.splits * a.R * dm.Hq * dm.D);
     part.n_items = (int)((pairs + 7) / 8 * 8 * part.splits * part.tile_groups);
-    hipError_t e;
-    if (nt == 1) e = dm.kv8 ? launch_mfma<1, true>(dm, a, part, st) : launch_mfma<1, false>(dm, a, part, st);
+    hipError_t e = hipSuccess;
+    if (!mfma) DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_vec<T, KT>(dm, a, part, st)));
+    else if (nt == 1) e = dm.kv8 ? launch_mfma<1, true>(dm, a, part, st) : launch_mfma<1, false>(dm, a, part, st);
     else if (nt == 2) e = dm.kv8 ? launch_mfma<2, true>(dm, a, part, st) : launch_mfma<2, false>(dm, a, part, st);
     else e = dm.kv8 ? launch_mfma<3, true>(dm, a, part, st) : launch_mfma<3, false>(dm, a, part, st);
     if (e != hipSuccess || part.splits == 1) return e;
-    hipLaunchKernelGGL(k_block_attn_join, dim3(a.S, std::min(std::max(rows, 1), 64), (dm.Hq + 3) / 4), dim3(256), 0, st, a, part, dm.Hq);
+    DISPATCH_T(dm.bf16, hipLaunchKernelGGL(k_block_attn_join<T>, dim3(a.S, std::min(std::max(rows, 1), 64), (dm.Hq + 3) / 4), dim3(256), 0, st, a, part, dm.Hq, dm.D));
     return hipGetLastError();
 }
 

@@ -2,25 +2,13 @@
 // blocks.  Everything a kernel indexes with -- lengths, slots, block ids -- comes from device memory and is checked
 // where it is used.
 #include "block_ops.h"
-#include "device_util.h"
+#include "block_util.h"
 
 #include <algorithm>
 #include <type_traits>
 
 namespace icarus {
 namespace {
-
-#define DISPATCH_T(bf16, ...)                                        \
-    do {                                                             \
-        if (bf16) { typedef bf16_t T; __VA_ARGS__; }                 \
-        else { typedef float T; __VA_ARGS__; }                       \
-    } while (0)
-#define DISPATCH_TK(bf16, kv8, ...)                                   \
-    do {                                                              \
-        if (kv8) { typedef fp8_t KT; DISPATCH_T(bf16, __VA_ARGS__); } \
-        else if (bf16) { typedef bf16_t T; typedef bf16_t KT; __VA_ARGS__; } \
-        else { typedef float T; typedef float KT; __VA_ARGS__; }      \
-    } while (0)
 
 // ---- growth of the sequences ------------------------------------------------------------------------------------------
 // Two sums over the sequences decide everything: rows before a sequence, and blocks taken before it.  Every workgroup
@@ -227,25 +215,12 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, i
 // V goes into the pool transposed: a run of rows that are consecutive places of one block is put together in LDS and written as one row of the block per
 // channel, 32 bytes at once where the run fills the block.  A run belongs to the window in which it starts, wherever it ends, so that prompts which begin
 // inside a block are written in whole blocks too.
-template <typename T> struct Four;  // four elements, as they lie in memory
-template <> struct Four<bf16_t> {
-    typedef uint2 raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[4]) {
-        v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);
-        v[2] = __uint_as_float(r.y << 16); v[3] = __uint_as_float(r.y & 0xffff0000u);
-    }
-    static __device__ __forceinline__ void put(bf16_t *p, const float (&v)[4], float) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
-};
-template <> struct Four<float> {
-    typedef float4 raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[4]) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
-    static __device__ __forceinline__ void put(float *p, const float (&v)[4], float) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
-};
-template <> struct Four<fp8_t> {
-    static __device__ __forceinline__ void put(fp8_t *p, const float (&v)[4], float scale) {
-        *(uint32_t *)p = f32_to_fp8(v[0] / scale) | f32_to_fp8(v[1] / scale) << 8 | f32_to_fp8(v[2] / scale) << 16 | f32_to_fp8(v[3] / scale) << 24;
-    }
-};
+template <typename KT> __device__ __forceinline__ void put4(KT *p, const float (&v)[4], float scale);
+template <> __device__ __forceinline__ void put4(bf16_t *p, const float (&v)[4], float) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
+template <> __device__ __forceinline__ void put4(float *p, const float (&v)[4], float) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
+template <> __device__ __forceinline__ void put4(fp8_t *p, const float (&v)[4], float scale) {
+    *(uint32_t *)p = f32_to_fp8(v[0] / scale) | f32_to_fp8(v[1] / scale) << 8 | f32_to_fp8(v[2] / scale) << 16 | f32_to_fp8(v[3] / scale) << 24;
+}
 
 constexpr int kWindow = 16;
 // What a wave wrote to LDS is what it reads next: an order for the compiler, the hardware keeps it anyway.
@@ -277,28 +252,28 @@ __global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int
         if (qk_norm)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                Four<T>::get(*(const typename Four<T>::raw *)((const T *)a.q_norm + h * HALF + i4), wq[h]);
-                Four<T>::get(*(const typename Four<T>::raw *)((const T *)a.k_norm + h * HALF + i4), wk[h]);
+                Quad<T>::get(*(const typename Quad<T>::raw *)((const T *)a.q_norm + h * HALF + i4), wq[h]);
+                Quad<T>::get(*(const typename Quad<T>::raw *)((const T *)a.k_norm + h * HALF + i4), wk[h]);
             }
         const T *src = (const T *)a.qkv + (size_t)row * a.ld + i4;
         KT *kdst = (KT *)a.pool + (write ? ((size_t)(slot / Bk) * Hkv * 2 * Bk + (size_t)(slot % Bk)) * D : 0) + i4;
         const int end = write ? h1 : min(h1, Hq);  // a stream's key heads are not read
         constexpr int U = 4;  // heads whose reads are under way together
         for (int hu = h0 + sub % HPR; hu < end; hu += U * HPR) {
-            typename Four<T>::raw lo[U], up[U];
+            typename Quad<T>::raw lo[U], up[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const T *p = src + (size_t)min(hu + u * HPR, end - 1) * D;
-                lo[u] = *(const typename Four<T>::raw *)p;
-                up[u] = *(const typename Four<T>::raw *)(p + HALF);
+                lo[u] = *(const typename Quad<T>::raw *)p;
+                up[u] = *(const typename Quad<T>::raw *)(p + HALF);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int h = hu + u * HPR;
                 if (h >= end) break;
                 float x[4], y[4], rx[4], ry[4];
-                Four<T>::get(lo[u], x);
-                Four<T>::get(up[u], y);
+                Quad<T>::get(lo[u], x);
+                Quad<T>::get(up[u], y);
                 if (qk_norm) {
                     float ss = 0.f;
 #pragma unroll
@@ -316,12 +291,12 @@ __global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int
                 for (int e = 0; e < 4; ++e) rotate_pair(x[e], y[e], cs[e], sn[e], &rx[e], &ry[e]);
                 if (h < Hq) {
                     T *dst = (T *)a.q_out + ((size_t)row * Hq + h) * D + i4;
-                    Four<T>::put(dst, rx, 1.f);
-                    Four<T>::put(dst + HALF, ry, 1.f);
+                    put4(dst, rx, 1.f);
+                    put4(dst + HALF, ry, 1.f);
                 } else {
                     KT *dst = kdst + (size_t)(h - Hq) * 2 * Bk * D;
-                    Four<KT>::put(dst, rx, k_scale);
-                    Four<KT>::put(dst + HALF, ry, k_scale);
+                    put4(dst, rx, k_scale);
+                    put4(dst + HALF, ry, k_scale);
                 }
             }
         }
@@ -447,25 +422,6 @@ __global__ void __launch_bounds__(256) k_bounds(BoundsArgs a, int Hkv, int D, in
 // the tokens, and lanes of the same channels meet by exchanges in registers.  Bound by HBM (half of a block's lines), with the vector units close behind: with
 // 16 bytes to a lane there were twice the exchanges and the reads waited for them.  bfloat16 pairs stay pairs: as whole numbers of 16 bits whose order is that of the values two
 // are compared at a time.
-template <typename KT> struct Quad;  // four elements as they lie
-template <> struct Quad<bf16_t> {
-    typedef uint2 raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[4]) {
-        v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);
-        v[2] = __uint_as_float(r.y << 16); v[3] = __uint_as_float(r.y & 0xffff0000u);
-    }
-};
-template <> struct Quad<float> {
-    typedef float4 raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[4]) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
-};
-template <> struct Quad<fp8_t> {
-    typedef uint32_t raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[4]) {
-        const f32x2_t p = __builtin_amdgcn_cvt_pk_f32_fp8(r, false), q = __builtin_amdgcn_cvt_pk_f32_fp8(r, true);
-        v[0] = p[0]; v[1] = p[1]; v[2] = q[0]; v[3] = q[1];
-    }
-};
 typedef short s16x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ s16x2_t ordered(uint32_t u) {  // two bfloat16 -> whole numbers in their order; its own inverse
     const s16x2_t x = __builtin_bit_cast(s16x2_t, u);

@@ -44,8 +44,8 @@ struct BlockAttnArgs {
     const int32_t *blocks, *counts; int max_selected;
     void *out;
 };
-// Matrix cores.  Workspace: 16-byte aligned, block_attn_workspace bytes.
-bool block_attn_mfma_supported(const Dims &dm);
+// Shapes that block_attn_fast names: matrix cores or vector units.  Workspace: 16-byte aligned, block_attn_workspace bytes.
+bool block_attn_fast(const Dims &dm);
 size_t block_attn_workspace(const Dims &dm, int S, int R, int max_selected);
 hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *workspace, hipStream_t st);
 hipError_t launch_block_attn_generic(const Dims &dm, const BlockAttnArgs &a, hipStream_t st);

@@ -2131,9 +2131,9 @@ icarus_status icarus_attn_blocks(icarus_ctx *ctx, const void *q, const void *kv_
     const size_t need = icarus_attn_blocks_workspace_bytes(ctx, S, R, max_selected);
     if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
     BlockAttnArgs a{q, kv_pool, block_tables, max_blocks, ctx->cfg.num_blocks, S, kv_lens, row_start, R, seq_rows, blocks, counts, max_selected, out};
-    const bool mfma = ctx->mode == 0 && block_attn_mfma_supported(ctx->dm);
+    const bool fast = ctx->mode == 0 && block_attn_fast(ctx->dm);
     PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ATTN,
-          mfma ? launch_block_attn(ctx->dm, a, workspace, (hipStream_t)stream) : launch_block_attn_generic(ctx->dm, a, (hipStream_t)stream));
+          fast ? launch_block_attn(ctx->dm, a, workspace, (hipStream_t)stream) : launch_block_attn_generic(ctx->dm, a, (hipStream_t)stream));
     return ICARUS_OK;
 }
 
