@@ -391,7 +391,7 @@ def gemm(x, w, tile, slices: int = 1, fused: bool = False, t=None, b=None, resid
 
 class SequenceMap:
     """Device arrays that IcarusLayer.extend_sequences fills, kept by the caller (a captured graph replays into the same ones): kv_lens [S],
-    row_start [S + 1], row_seq, row_pos, row_slot [max_rows], counts [2] (free ids taken, sequences refused); one allocation."""
+    row_start [S + 1], row_seq, row_pos, row_slot [max_rows], counts [2] (free ids taken, sequences refused); one allocation of each type."""
 
     def __init__(self, n_seqs: int, max_rows: int, device):
         S, R = int(n_seqs), int(max_rows)
@@ -401,21 +401,32 @@ class SequenceMap:
         self.kv_lens, self.row_start, self.counts, self.row_seq, self.row_pos = ints.split([S, S + 1, 2, R, R])
 
 
-class _OnDevice:
-    """The device a call's tensors are on, made current while the library launches there."""
+# The calls with lengths on the device take a few microseconds on the GPU, so their marshalling is kept short: one look at a tensor in the common case,
+# _want's message where something is wrong.
+def _need(t, what: str, dtype, shape, index: int):
+    """A contiguous tensor of this type and shape on CUDA device `index`."""
+    if not (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+        _want(t, what, dtype, shape, torch.device("cuda", index))
 
-    def __init__(self, device):
-        self.device = device
 
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.device.index not in (None, self.before):
-            torch.cuda.set_device(self.device)
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+def _index_of(t, what: str, dtype) -> int:
+    """CUDA device of a tensor of this type."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a torch tensor, got {type(t).__name__}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what}: dtype {t.dtype}, the library reads {dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: must be a device tensor")
+    return t.get_device()
 
-    def __exit__(self, *exc):
-        if torch.cuda.current_device() != self.before:
-            torch.cuda.set_device(self.before)
+
+def _launch(index: int, call, *args) -> int:
+    """call(*args, stream) on the current stream of CUDA device `index`, which is made the current device meanwhile."""
+    before = torch._C._cuda_getDevice()
+    if before == index:
+        return call(*args, torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        return call(*args, torch._C._cuda_getCurrentRawStream(index))
 
 
 class IcarusLayer:
@@ -639,34 +650,37 @@ class IcarusLayer:
         return out
 
     # -- lengths on the device (include/icarus_blocks.h) -----------------------------
-    def _lens(self, S, device, **arrays):
-        for name, t in arrays.items():
-            if t is not None:
-                _want(t, name, torch.int32, (S,), device)
-
     def _table(self, block_tables):
-        _want(block_tables, "block_tables", torch.int32)
+        """Sequences, width and device of a block table."""
+        index = _index_of(block_tables, "block_tables", torch.int32)
         if block_tables.dim() != 2:
             raise ValueError(f"block_tables: need [S, max_blocks], got {tuple(block_tables.shape)}")
-        return block_tables.shape[0], block_tables.shape[1], block_tables.device
+        S, max_blocks = block_tables.shape
+        _need(block_tables, "block_tables", torch.int32, (S, max_blocks), index)
+        return S, max_blocks, index
 
-    def _pool(self, kv_pool, device):
-        want = self.cfg.pool_shape()
-        _want(kv_pool, "kv_pool", self.cfg.pool_dtype, None, device)
-        if kv_pool.dim() != 4 or tuple(kv_pool.shape[1:]) != want[1:] or kv_pool.shape[0] < want[0]:
-            raise ValueError(f"kv_pool: shape {tuple(kv_pool.shape)}, expected at least {want[0]} blocks of {want[1:]}")
-
-    def _bounds(self, codes, scales, device):
+    def _pool(self, kv_pool, index):
         c = self.cfg
-        _want(codes, "codes", torch.int8, (c.num_blocks, c.n_kv_heads, 2, c.head_dim), device)
-        _want(scales, "scales", torch.float32, (c.num_blocks, c.n_kv_heads), device)
+        have = kv_pool.shape if isinstance(kv_pool, torch.Tensor) else ()
+        _need(kv_pool, "kv_pool", c.pool_dtype, (max(c.num_blocks, have[0] if have else 0), c.n_kv_heads, 2, c.block_size * c.head_dim), index)
 
-    def _queries(self, q, row_start, S, device):
+    def _bounds(self, codes, scales, index):
         c = self.cfg
-        _want(q, "q", c.torch_dtype, None, device)
-        if q.dim() != 3 or tuple(q.shape[1:]) != (c.n_q_heads, c.head_dim):
-            raise ValueError(f"q: shape {tuple(q.shape)}, expected [R, {c.n_q_heads}, {c.head_dim}]")
-        _want(row_start, "row_start", torch.int32, (S + 1,), device)
+        _need(codes, "codes", torch.int8, (c.num_blocks, c.n_kv_heads, 2, c.head_dim), index)
+        _need(scales, "scales", torch.float32, (c.num_blocks, c.n_kv_heads), index)
+
+    def _rows(self, q, what, index) -> int:
+        """Number of rows of queries [R, Hq, D]."""
+        R = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else 0
+        _need(q, what, self.cfg.torch_dtype, (R, self.cfg.n_q_heads, self.cfg.head_dim), index)
+        return R
+
+    def _lists(self, blocks, counts, S, index) -> int:
+        """Width of the lists of blocks [S, Hkv, width]."""
+        width = blocks.shape[-1] if isinstance(blocks, torch.Tensor) and blocks.dim() else 0
+        _need(blocks, "blocks", torch.int32, (S, self.cfg.n_kv_heads, width), index)
+        _need(counts, "counts", torch.int32, (S,), index)
+        return width
 
     def new_key_bounds(self, device="cuda"):
         """(codes, scales) for key_bounds and select_blocks, for all blocks of the pool."""
@@ -676,94 +690,87 @@ class IcarusLayer:
 
     def extend_sequences(self, seq_map, ctx_lens, new_lens, block_tables, free_ids, free_used, streams=None):
         """Fills `seq_map` (a SequenceMap) and the new entries of block_tables; all arrays are device tensors.  Returns seq_map."""
-        S, max_blocks, dev = self._table(block_tables)
-        if seq_map.n_seqs != S:
-            raise ValueError(f"seq_map is for {seq_map.n_seqs} sequences, block_tables has {S}")
-        self._lens(S, dev, ctx_lens=ctx_lens, new_lens=new_lens, streams=streams, kv_lens=seq_map.kv_lens)
-        _want(free_ids, "free_ids", torch.int32, (free_ids.numel(),), dev)
-        _want(free_used, "free_used", torch.int32, (1,), dev)
+        S, max_blocks, index = self._table(block_tables)
         m = seq_map
-        with _OnDevice(dev) as stream:
-            self._check(_lib.icarus_extend_sequences(
-                self._h, S, ctx_lens.data_ptr(), new_lens.data_ptr(), _ptr(streams), block_tables.data_ptr(), max_blocks, free_ids.data_ptr(),
-                free_ids.numel(), free_used.data_ptr(), m.max_rows, m.kv_lens.data_ptr(), m.row_start.data_ptr(), m.row_seq.data_ptr(),
-                m.row_pos.data_ptr(), m.row_slot.data_ptr(), m.counts.data_ptr(), stream))
+        if m.n_seqs != S:
+            raise ValueError(f"seq_map is for {m.n_seqs} sequences, block_tables has {S}")
+        one, n_free = (S,), free_ids.shape[0]
+        _need(ctx_lens, "ctx_lens", torch.int32, one, index)
+        _need(new_lens, "new_lens", torch.int32, one, index)
+        if streams is not None:
+            _need(streams, "streams", torch.int32, one, index)
+        _need(m.kv_lens, "seq_map", torch.int32, one, index)
+        _need(free_ids, "free_ids", torch.int32, (n_free,), index)
+        _need(free_used, "free_used", torch.int32, (1,), index)
+        self._check(_launch(index, _lib.icarus_extend_sequences, self._h, S, ctx_lens.data_ptr(), new_lens.data_ptr(),
+                            None if streams is None else streams.data_ptr(), block_tables.data_ptr(), max_blocks, free_ids.data_ptr(), n_free,
+                            free_used.data_ptr(), m.max_rows, m.kv_lens.data_ptr(), m.row_start.data_ptr(), m.row_seq.data_ptr(),
+                            m.row_pos.data_ptr(), m.row_slot.data_ptr(), m.counts.data_ptr()))
         return m
 
     def rope_append(self, qkv, row_pos, row_slot, kv_pool, q_out=None):
         """qkv [R, >= (Hq + 2 Hkv) * D], rows may be strided.  Returns q_out [R, Hq, D]; rows with a negative position are left as they were."""
         c = self.cfg
-        if not isinstance(qkv, torch.Tensor):
-            raise TypeError(f"qkv: expected a torch tensor, got {type(qkv).__name__}")
+        index = _index_of(qkv, "qkv", c.torch_dtype)
         width = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
         if qkv.dim() != 2 or qkv.shape[1] < width or qkv.stride(1) != 1 or (qkv.shape[0] > 1 and qkv.stride(0) < width):
             raise ValueError(f"qkv: shape {tuple(qkv.shape)} with strides {tuple(qkv.stride())}, expected rows of {width} contiguous elements")
-        if qkv.dtype != c.torch_dtype:
-            raise TypeError(f"qkv: dtype {qkv.dtype}, the library reads {c.torch_dtype}")
-        if not qkv.is_cuda:
-            raise ValueError("qkv: must be a device tensor")
-        R, dev = qkv.shape[0], qkv.device
-        _want(row_pos, "row_pos", torch.int32, (R,), dev)
-        _want(row_slot, "row_slot", torch.int64, (R,), dev)
-        self._pool(kv_pool, dev)
+        R = qkv.shape[0]
+        _need(row_pos, "row_pos", torch.int32, (R,), index)
+        _need(row_slot, "row_slot", torch.int64, (R,), index)
+        self._pool(kv_pool, index)
         if q_out is None:
-            q_out = torch.zeros(R, c.n_q_heads, c.head_dim, dtype=c.torch_dtype, device=dev)
-        _want(q_out, "q_out", c.torch_dtype, (R, c.n_q_heads, c.head_dim), dev)
-        with _OnDevice(dev) as stream:
-            self._check(_lib.icarus_rope_append(self._h, qkv.data_ptr(), qkv.stride(0) if R > 1 else max(qkv.stride(0), width), R,
-                                                row_pos.data_ptr(), row_slot.data_ptr(), q_out.data_ptr(), kv_pool.data_ptr(), stream))
+            q_out = torch.zeros(R, c.n_q_heads, c.head_dim, dtype=c.torch_dtype, device=qkv.device)
+        _need(q_out, "q_out", c.torch_dtype, (R, c.n_q_heads, c.head_dim), index)
+        self._check(_launch(index, _lib.icarus_rope_append, self._h, qkv.data_ptr(), max(qkv.stride(0), width), R, row_pos.data_ptr(),
+                            row_slot.data_ptr(), q_out.data_ptr(), kv_pool.data_ptr()))
         return q_out
 
     def key_bounds(self, kv_pool, block_tables, from_lens, to_lens, codes, scales, max_new: int = 0):
         """Bounds of the keys of the blocks that hold positions from_lens .. to_lens - 1, into codes and scales (new_key_bounds)."""
-        S, max_blocks, dev = self._table(block_tables)
-        self._pool(kv_pool, dev)
-        self._lens(S, dev, from_lens=from_lens, to_lens=to_lens)
-        self._bounds(codes, scales, dev)
-        with _OnDevice(dev) as stream:
-            self._check(_lib.icarus_key_bounds(self._h, kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S, from_lens.data_ptr(),
-                                               to_lens.data_ptr(), int(max_new), codes.data_ptr(), scales.data_ptr(), stream))
+        S, max_blocks, index = self._table(block_tables)
+        self._pool(kv_pool, index)
+        _need(from_lens, "from_lens", torch.int32, (S,), index)
+        _need(to_lens, "to_lens", torch.int32, (S,), index)
+        self._bounds(codes, scales, index)
+        self._check(_launch(index, _lib.icarus_key_bounds, self._h, kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S, from_lens.data_ptr(),
+                            to_lens.data_ptr(), max_new, codes.data_ptr(), scales.data_ptr()))
 
     def select_blocks(self, q, codes, scales, block_tables, kv_lens, row_start, blocks, counts, first: int = 1, last: int = 2,
                       seq_rows: int = 0, workspace=None):
-        """blocks [S, Hkv, top_k] and counts [S] receive each sequence's selected blocks."""
-        c = self.cfg
-        S, max_blocks, dev = self._table(block_tables)
-        self._queries(q, row_start, S, dev)
-        self._bounds(codes, scales, dev)
-        self._lens(S, dev, kv_lens=kv_lens, counts=counts)
-        if blocks.dim() != 3:
-            raise ValueError(f"blocks: need [S, Hkv, top_k], got {tuple(blocks.shape)}")
-        _want(blocks, "blocks", torch.int32, (S, c.n_kv_heads, blocks.shape[2]), dev)
+        """blocks [S, Hkv, top_k] and counts [S] receive each sequence's selected blocks.  workspace: bytes for one call at a time, by default of its own."""
+        S, max_blocks, index = self._table(block_tables)
+        R = self._rows(q, "q", index)
+        _need(row_start, "row_start", torch.int32, (S + 1,), index)
+        _need(kv_lens, "kv_lens", torch.int32, (S,), index)
+        self._bounds(codes, scales, index)
+        top_k = self._lists(blocks, counts, S, index)
         if workspace is None:
-            workspace = torch.empty(_lib.icarus_select_workspace_bytes(self._h, S, max_blocks), dtype=torch.uint8, device=dev)
-        with _OnDevice(dev) as stream:
-            self._check(_lib.icarus_select_blocks(
-                self._h, q.data_ptr(), codes.data_ptr(), scales.data_ptr(), block_tables.data_ptr(), max_blocks, S, kv_lens.data_ptr(), q.shape[0],
-                row_start.data_ptr(), int(seq_rows), blocks.shape[2], int(first), int(last), blocks.data_ptr(), counts.data_ptr(),
-                workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
+            workspace = torch.empty(_lib.icarus_select_workspace_bytes(self._h, S, max_blocks), dtype=torch.uint8, device=q.device)
+        self._check(_launch(index, _lib.icarus_select_blocks, self._h, q.data_ptr(), codes.data_ptr(), scales.data_ptr(), block_tables.data_ptr(), max_blocks,
+                            S, kv_lens.data_ptr(), R, row_start.data_ptr(), seq_rows, top_k, first, last, blocks.data_ptr(), counts.data_ptr(),
+                            workspace.data_ptr(), workspace.nbytes))
         return blocks, counts
 
     def attn_blocks(self, q, kv_pool, block_tables, kv_lens, row_start, blocks, counts, out=None, seq_rows: int = 0, workspace=None):
-        """Attention of the rows row_start[s] .. row_start[s + 1] - 1 over the listed blocks of sequence s; rows of no sequence are left as they were."""
-        c = self.cfg
-        S, max_blocks, dev = self._table(block_tables)
-        self._queries(q, row_start, S, dev)
-        self._pool(kv_pool, dev)
-        self._lens(S, dev, kv_lens=kv_lens, counts=counts)
-        if blocks.dim() != 3:
-            raise ValueError(f"blocks: need [S, Hkv, max_selected], got {tuple(blocks.shape)}")
-        _want(blocks, "blocks", torch.int32, (S, c.n_kv_heads, blocks.shape[2]), dev)
+        """Attention of the rows row_start[s] .. row_start[s + 1] - 1 over the listed blocks of sequence s; rows of no sequence are left as they were.
+        workspace: as for select_blocks."""
+        S, max_blocks, index = self._table(block_tables)
+        R = self._rows(q, "q", index)
+        self._pool(kv_pool, index)
+        _need(row_start, "row_start", torch.int32, (S + 1,), index)
+        _need(kv_lens, "kv_lens", torch.int32, (S,), index)
+        width = self._lists(blocks, counts, S, index)
         if out is None:
             out = torch.zeros_like(q)
-        _want(out, "out", c.torch_dtype, tuple(q.shape), dev)
+        self._rows(out, "out", index)
+        if out.shape[0] != R:
+            raise ValueError(f"out has {out.shape[0]} rows, q {R}")
         if workspace is None:
-            workspace = torch.empty(_lib.icarus_attn_blocks_workspace_bytes(self._h, S, q.shape[0], blocks.shape[2]), dtype=torch.uint8, device=dev)
-        with _OnDevice(dev) as stream:
-            self._check(_lib.icarus_attn_blocks(
-                self._h, q.data_ptr(), kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S, kv_lens.data_ptr(), q.shape[0],
-                row_start.data_ptr(), int(seq_rows), blocks.data_ptr(), counts.data_ptr(), blocks.shape[2], out.data_ptr(),
-                workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
+            workspace = torch.empty(_lib.icarus_attn_blocks_workspace_bytes(self._h, S, R, width), dtype=torch.uint8, device=q.device)
+        self._check(_launch(index, _lib.icarus_attn_blocks, self._h, q.data_ptr(), kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S,
+                            kv_lens.data_ptr(), R, row_start.data_ptr(), seq_rows, blocks.data_ptr(), counts.data_ptr(), width, out.data_ptr(),
+                            workspace.data_ptr(), workspace.nbytes))
         return out
 
 

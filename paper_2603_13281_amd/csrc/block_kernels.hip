@@ -902,7 +902,7 @@ __global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk)
 }  // namespace
 
 hipError_t launch_extend(const ExtendArgs &a, hipStream_t st) {
-    const int rows_per_wg = 512;
+    const int rows_per_wg = a.max_rows <= 16384 ? 256 : 512;  // a row to a thread, until all compute units have a workgroup or two
     const int wgs = a.max_rows > rows_per_wg ? (a.max_rows + rows_per_wg - 1) / rows_per_wg : 1;
     hipLaunchKernelGGL(k_extend, dim3(wgs), dim3(kExtThreads), 0, st, a, rows_per_wg);
     return hipGetLastError();

@@ -138,8 +138,8 @@ def test_binding_refuses_tensors_the_c_signature_would_misread():
         layer.attn_blocks(None, None, table.long(), lens, lens, lens, lens)
     with pytest.raises(TypeError):
         layer.rope_append(torch.zeros(2, 768), lens, lens, None)
-    with pytest.raises(ValueError):
-        layer.rope_append(torch.zeros(2, 700, dtype=torch.bfloat16), lens, lens, None)
+    with pytest.raises(ValueError):      # host tensors again
+        layer.rope_append(torch.zeros(2, 768, dtype=torch.bfloat16), lens, lens, None)
     layer.close()
 
 
