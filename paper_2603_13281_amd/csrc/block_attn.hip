@@ -89,7 +89,7 @@ struct SplitOut {
     float2 *ml;  // [splits][R][Hq]: maximum in log2 units, sum
     int splits;  // 1: the output itself is written
     int per;     // list entries of a split, even
-    int tile_groups, n_items;
+    int tiles, tile_groups, n_items;  // tiles of an item, items to the rows of the call's largest sequence
 };
 
 // Which part of the call an item is: workgroups of one XCD that run at the same time take the tile groups of the same blocks, which its L2 then reads once.
@@ -110,7 +110,7 @@ template <int NT, bool KV8>
 __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut part, int Hq, int Hkv, float scale_log2, float v_scale) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     // LDS: the waves' states | two buffers of Q fragments [qt][ks][lane]
-    constexpr int kQBytes = NT * kKS * 1024, kQAt = 4 * Image<NT>::kBytes;
+    constexpr int kIT = NT < 3 ? NT : 3, kQBytes = NT * kKS * 1024, kQAt = 4 * Image<kIT>::kBytes;  // kIT: tiles put together at a time
     __shared__ int ids[2][kItemBlocks], wave_n[2][4];
     __shared__ uint8_t fill[2][kItemBlocks];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
         x.split = it.split;
         x.row0 = min(max(a.row_start[it.s], 0), a.R);
         x.G = (min(max(a.row_start[it.s + 1], x.row0), a.R) - x.row0) * g;
-        x.j0 = it.tg * NT * 16;
+        x.j0 = it.tg * part.tiles * 16;
         x.len = max(a.kv_lens[it.s], 0);
         x.n_sel = min(max(a.counts[it.s], 0), a.max_selected);
         return x;
@@ -228,11 +228,12 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
                 for (int ks = 0; ks < kKS; ++ks) qr[qt][ks] = qlds[(qt * kKS + ks) * 64 + lane];
         }
         // a sequence with more rows than the launch was sized for: the same blocks again for its next tiles
-        const bool again = x.j0 + part.tile_groups * NT * 16 < x.G;
+        const int far = part.tile_groups * part.tiles * 16;
+        const bool again = x.j0 + far < x.G;
         const int i2 = again ? i1 : item_of(r + 1);
         if (again) {
             nx = x;
-            nx.j0 += part.tile_groups * NT * 16;
+            nx.j0 += far;
             id = id_of_entry(nx, entry_of(i1), n);
             load_q(nx, qv);
         } else if (i2 >= 0) {
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
 #pragma unroll
             for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const int n_grp = (n_blk + 1) / 2, stop = min(n_grp - 4, n_full >> 1), tiles = min(NT, (x.G - x.j0 + 15) / 16);
+        const int n_grp = (n_blk + 1) / 2, stop = min(n_grp - 4, n_full >> 1), tiles = min(part.tiles, (x.G - x.j0 + 15) / 16);
         auto walk = [&](auto n_tiles) {
             constexpr int N = decltype(n_tiles)::value;
             auto compute = [&](auto tail, Frag &f, int left) {
@@ -289,50 +290,75 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
             if (tiles == 1) walk(std::integral_constant<int, 1>());
             if constexpr (NT >= 2) if (tiles == 2) walk(std::integral_constant<int, 2>());
             if constexpr (NT >= 3) if (tiles == 3) walk(std::integral_constant<int, 3>());
+            if constexpr (NT >= 5) {
+                if (tiles == 4) walk(std::integral_constant<int, 4>());
+                if (tiles == 5) walk(std::integral_constant<int, 5>());
+            }
         }
-        // All waves have read the images of the item before, the counts and this item's ids: what they leave now is read after the next barrier.
+        // The waves' states are put together up to three tiles at a time: each wave leaves its own in LDS and takes d tiles 2 w, 2 w + 1 of all.
+        auto leave = [&](int qt0) {
+            f32x4 *o = (f32x4 *)(smem + w * Image<kIT>::kBytes);
+            float2 *ml = (float2 *)(o + Image<kIT>::kO);
+#pragma unroll
+            for (int i = 0; i < kIT; ++i) {
+                if (qt0 + i >= NT) continue;
+                ml[i * 64 + lane] = make_float2(st.m[min(qt0 + i, NT - 1)], st.l[min(qt0 + i, NT - 1)]);
+#pragma unroll
+                for (int dt = 0; dt < kDT; ++dt) o[(dt * kIT + i) * 64 + lane] = st.o[dt][min(qt0 + i, NT - 1)];
+            }
+        };
+        auto take = [&](int qt0) {
+#pragma unroll
+            for (int i = 0; i < kIT; ++i) {
+                const int qt = qt0 + i, j = x.j0 + 16 * qt + m;
+                if (qt >= tiles) continue;
+                float2 ml[4];
+                float mx = -INFINITY, l = 0.f;
+                f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    ml[k] = ((const float2 *)(smem + k * Image<kIT>::kBytes + Image<kIT>::kO * 16))[i * 64 + lane];
+                    mx = fmaxf(mx, ml[k].x);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float f = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - mx);  // a wave without tokens
+                    l += f * ml[k].y;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) o[h] += f * ((const f32x4 *)(smem + k * Image<kIT>::kBytes))[((2 * w + h) * kIT + i) * 64 + lane];
+                }
+                l += __shfl_xor(l, 16, 64);
+                l += __shfl_xor(l, 32, 64);
+                if (j >= x.G) continue;
+                const size_t at = (size_t)(x.row0 + j / g) * Hq + x.c * g + j % g;
+                if (part.splits == 1) {
+                    const float inv = l > 0.f ? v_scale / l : 0.f;
+                    bf16_t *op = (bf16_t *)a.out + at * kD + 32 * w + 4 * q;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        *(uint2 *)(op + 16 * h) = make_uint2(pack_bf16(o[h][0] * inv, o[h][1] * inv), pack_bf16(o[h][2] * inv, o[h][3] * inv));
+                } else {
+                    const size_t ps = (size_t)x.split * a.R * Hq + at;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) *(f32x4 *)(part.o + ps * kD + 32 * w + 16 * h + 4 * q) = o[h] * v_scale;
+                    if (w == 0 && q == 0) part.ml[ps] = make_float2(mx, l);
+                }
+            }
+        };
+        __syncthreads();  // every wave has taken its part of the item before: a wave without a group of this one is here at once
         if (i2 >= 0) count(id, n);
-        image_store<NT>(st, smem + w * Image<NT>::kBytes, lane);
+        leave(0);
         if (i2 >= 0) q_to_lds(qv, buf ^ 1);
         __syncthreads();
         if (i2 >= 0) place(id, n, buf ^ 1);
         __syncthreads();
         if (i2 >= 0) load(f0, nx, buf ^ 1, w);
-        // d tiles 2 w, 2 w + 1 of all queries, from the four states
-#pragma unroll
-        for (int qt = 0; qt < NT; ++qt) {
-            const int j = x.j0 + 16 * qt + m;
-            float2 ml[4];
-            float mx = -INFINITY, l = 0.f;
-            f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                ml[k] = ((const float2 *)(smem + k * Image<NT>::kBytes + Image<NT>::kO * 16))[qt * 64 + lane];
-                mx = fmaxf(mx, ml[k].x);
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float f = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - mx);  // a wave without tokens
-                l += f * ml[k].y;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) o[h] += f * ((const f32x4 *)(smem + k * Image<NT>::kBytes))[((2 * w + h) * NT + qt) * 64 + lane];
-            }
-            l += __shfl_xor(l, 16, 64);
-            l += __shfl_xor(l, 32, 64);
-            if (j >= x.G) continue;
-            const size_t at = (size_t)(x.row0 + j / g) * Hq + x.c * g + j % g;
-            if (part.splits == 1) {
-                const float inv = l > 0.f ? v_scale / l : 0.f;
-                bf16_t *op = (bf16_t *)a.out + at * kD + 32 * w + 4 * q;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    *(uint2 *)(op + 16 * h) = make_uint2(pack_bf16(o[h][0] * inv, o[h][1] * inv), pack_bf16(o[h][2] * inv, o[h][3] * inv));
-            } else {
-                const size_t ps = (size_t)x.split * a.R * Hq + at;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) *(f32x4 *)(part.o + ps * kD + 32 * w + 16 * h + 4 * q) = o[h] * v_scale;
-                if (w == 0 && q == 0) part.ml[ps] = make_float2(mx, l);
-            }
+        take(0);
+        if constexpr (NT > kIT) {
+            __syncthreads();
+            leave(kIT);
+            __syncthreads();
+            take(kIT);
         }
         if (i2 < 0) break;
         x = nx;
@@ -567,7 +593,7 @@ int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxS
 
 template <int NT, bool KV8>
 hipError_t launch_mfma(const Dims &dm, const BlockAttnArgs &a, const SplitOut &part, hipStream_t st) {
-    const size_t lds = 4 * Image<NT>::kBytes + 2 * NT * kKS * 1024;
+    const size_t lds = 4 * Image<(NT < 3 ? NT : 3)>::kBytes + 2 * NT * kKS * 1024;
     static bool attr_set = false;
     if (lds > 64 * 1024 && !attr_set) {
         hipError_t e = hipFuncSetAttribute((const void *)k_block_attn<NT, KV8>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
@@ -608,9 +634,9 @@ hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *works
     const int rows = a.seq_rows ? std::min(a.seq_rows, a.R) : a.R;  // of a sequence, at most
     const bool mfma = on_matrix_cores(dm);
     const int64_t tiles = ((int64_t)rows * g + 15) / 16;
-    const int nt = (int)std::min<int64_t>(tiles, 3);
     SplitOut part;
-    part.tile_groups = mfma ? (int)((tiles + nt - 1) / nt) : 1;
+    part.tile_groups = mfma ? (int)((tiles + 4) / 5) : 1;
+    part.tiles = (int)((tiles + part.tile_groups - 1) / part.tile_groups);
     part.splits = splits_for(dm, pairs * part.tile_groups, a.max_selected, splits_for(dm, pairs, a.max_selected));  // no more than the workspace was sized for
     part.per = std::max(2, ((a.max_selected + part.splits - 1) / part.splits + 1) & ~1);
     part.o = (float *)workspace;
@@ -618,9 +644,10 @@ hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *works
     part.n_items = (int)((pairs + 7) / 8 * 8 * part.splits * part.tile_groups);
     hipError_t e = hipSuccess;
     if (!mfma) DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_vec<T, KT>(dm, a, part, st)));
-    else if (nt == 1) e = dm.kv8 ? launch_mfma<1, true>(dm, a, part, st) : launch_mfma<1, false>(dm, a, part, st);
-    else if (nt == 2) e = dm.kv8 ? launch_mfma<2, true>(dm, a, part, st) : launch_mfma<2, false>(dm, a, part, st);
-    else e = dm.kv8 ? launch_mfma<3, true>(dm, a, part, st) : launch_mfma<3, false>(dm, a, part, st);
+    else if (part.tiles == 1) e = dm.kv8 ? launch_mfma<1, true>(dm, a, part, st) : launch_mfma<1, false>(dm, a, part, st);
+    else if (part.tiles == 2) e = dm.kv8 ? launch_mfma<2, true>(dm, a, part, st) : launch_mfma<2, false>(dm, a, part, st);
+    else if (part.tiles == 3) e = dm.kv8 ? launch_mfma<3, true>(dm, a, part, st) : launch_mfma<3, false>(dm, a, part, st);
+    else e = dm.kv8 ? launch_mfma<5, true>(dm, a, part, st) : launch_mfma<5, false>(dm, a, part, st);
     if (e != hipSuccess || part.splits == 1) return e;
     DISPATCH_T(dm.bf16, hipLaunchKernelGGL(k_block_attn_join<T>, dim3(a.S, std::min(std::max(rows, 1), 64), (dm.Hq + 3) / 4), dim3(256), 0, st, a, part, dm.Hq, dm.D));
     return hipGetLastError();
