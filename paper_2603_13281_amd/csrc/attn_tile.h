@@ -68,9 +68,9 @@ __device__ __forceinline__ void load_group(KVFrag &f, const bf16_t *__restrict__
 // Where the decode walks keep the wave's Q fragments: in registers when the wave has two or three query tiles (a
 // wave issues in order and is alone on its SIMD, so a fragment read in front of the MFMAs that need it stalls it for
 // the read's whole latency, up to twelve times per group); with one tile they stay in LDS, which keeps that
-// instantiation at two workgroups per CU, and with five, whose accumulators and fragments would not fit the registers.
+// instantiation at two workgroups per CU.
 template <int NT>
-constexpr bool kQInRegs = NT > 1 && NT != 5;
+constexpr bool kQInRegs = NT > 1;
 
 // Per-wave running state for NT query tiles.
 template <int NT>

@@ -106,11 +106,97 @@ struct Item {
     }
 };
 
+// One group of two blocks for N query tiles: scores of all of them, one look whether any softmax reference has to move (rare: see compute_group), and then straight-line code in
+// which the weights of one tile and the products of the tile before can be under way together -- with a branch to a tile, as compute_group has it, a wave
+// that is alone on its SIMD waits out every step of every tile.  there: tokens of this lane's block (masked only).
+template <int NT, int N, bool KV8, bool masked, typename Frag>
+__device__ __forceinline__ void group_of(State<NT> &st, const Frag &f, const bf16x8 (&qr)[NT][kKS], const bf16x8 *__restrict__ qlds, int there, float scale_log2, int lane) {
+    const int t0 = 8 * ((lane >> 4) & 1);
+    f32x4 sc[N][2];
+    bf16x8 v[kDT];
+#pragma unroll
+    for (int qt = 0; qt < N; ++qt) sc[qt][0] = sc[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < kKS; ++ks) {
+        bf16x8 k[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if constexpr (KV8) {
+                const uint4 r = f.k[t][ks >> 1];
+                k[t] = (ks & 1) ? cvt8(r.z, r.w) : cvt8(r.x, r.y);
+            } else {
+                k[t] = f.k[t][ks];
+            }
+        }
+#pragma unroll
+        for (int qt = 0; qt < N; ++qt) {
+            const bf16x8 qv = kQInRegs<NT> ? qr[qt][ks] : qlds[(qt * kKS + ks) * 64 + lane];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) sc[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t], qv, sc[qt][t], 0, 0, 0);
+        }
+    }
+    uint32_t keep[4];  // places behind the last token may hold anything
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keep[i] = (t0 + 2 * i < there ? 0xffffu : 0u) | (t0 + 2 * i + 1 < there ? 0xffff0000u : 0u);
+    }
+#pragma unroll
+    for (int dt = 0; dt < kDT; ++dt) {
+        if constexpr (KV8) v[dt] = cvt8(f.v[dt].x, f.v[dt].y);
+        else v[dt] = f.v[dt];
+        if (masked) {
+            const uint4 r = __builtin_bit_cast(uint4, v[dt]);
+            v[dt] = __builtin_bit_cast(bf16x8, make_uint4(r.x & keep[0], r.y & keep[1], r.z & keep[2], r.w & keep[3]));
+        }
+    }
+    float mx[N];
+    bool move = false;
+#pragma unroll
+    for (int qt = 0; qt < N; ++qt) {
+        if (masked)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (t0 + i >= there) sc[qt][i >> 2][i & 3] = -INFINITY;
+        const f32x4 a = sc[qt][0], b = sc[qt][1];
+        mx[qt] = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]))) * scale_log2;
+        move |= mx[qt] > st.m[qt] + kSlack;
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) ICARUS_IN_ACC(st.o[dt][qt]);
+    }
+    if (__any(move)) {
+#pragma unroll
+        for (int qt = 0; qt < N; ++qt) {
+            float m_new = fmaxf(mx[qt], __shfl_xor(mx[qt], 16, 64));
+            m_new = fmaxf(st.m[qt], fmaxf(m_new, __shfl_xor(m_new, 32, 64)));
+            const float c = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[qt] - m_new);
+            st.m[qt] = m_new;
+            st.l[qt] *= c;
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) {
+                st.o[dt][qt][0] *= c; st.o[dt][qt][1] *= c; st.o[dt][qt][2] *= c; st.o[dt][qt][3] *= c;
+                ICARUS_IN_ACC(st.o[dt][qt]);
+            }
+        }
+    }
+#pragma unroll
+    for (int qt = 0; qt < N; ++qt) {
+        const float m_ref = masked && st.m[qt] == -INFINITY ? 0.f : st.m[qt];  // nothing yet: every weight 0
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 2][i & 3], scale_log2, -m_ref));
+        // rounded to bfloat16 for the matrix cores (half a step, 2^-8, each); the sum takes them as they are
+        const uint4 p = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+        st.l[qt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[dt], __builtin_bit_cast(bf16x8, p), st.o[dt][qt], 0, 0, 0);
+    }
+}
+
 template <int NT, bool KV8>
 __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut part, int Hq, int Hkv, float scale_log2, float v_scale) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     // LDS: the waves' states | two buffers of Q fragments [qt][ks][lane]
-    constexpr int kIT = NT < 3 ? NT : 3, kQBytes = NT * kKS * 1024, kQAt = 4 * Image<kIT>::kBytes;  // kIT: tiles put together at a time
+    constexpr int kQBytes = NT * kKS * 1024, kQAt = 4 * Image<NT>::kBytes;
     __shared__ int ids[2][kItemBlocks], wave_n[2][4];
     __shared__ uint8_t fill[2][kItemBlocks];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -243,44 +329,39 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
             entry = entry_of(item_of(r + 2));
         }
         State<NT> st;
-        int stag[NT];
 #pragma unroll
         for (int qt = 0; qt < NT; ++qt) {
             st.m[qt] = -INFINITY;
             st.l[qt] = 0.f;
-            stag[qt] = 0;
 #pragma unroll
             for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         const int n_grp = (n_blk + 1) / 2, stop = min(n_grp - 4, n_full >> 1), tiles = min(part.tiles, (x.G - x.j0 + 15) / 16);
         auto walk = [&](auto n_tiles) {
             constexpr int N = decltype(n_tiles)::value;
-            auto compute = [&](auto tail, Frag &f, int left) {
-                constexpr bool masked = decltype(tail)::value;
-                if constexpr (KV8) compute_group8<NT, N, masked>(st, f, qr, qlds, left, stag, scale_log2, lane);
-                else compute_group<NT, N, masked>(st, f, qr, qlds, left, stag, scale_log2, lane);
+            auto compute = [&](auto masked, const Frag &f, int there) {
+                group_of<NT, N, KV8, decltype(masked)::value>(st, f, qr, qlds, there, scale_log2, lane);
             };
             Frag f1;
             int grp = w;
 #pragma nounroll
             for (; grp + 4 < stop; grp += 8) {
                 load(f1, x, buf, grp + 4);
-                compute(std::false_type(), f0, kGrp);
+                compute(std::false_type(), f0, kBk);
                 load(f0, x, buf, grp + 8);
-                compute(std::false_type(), f1, kGrp);
+                compute(std::false_type(), f1, kBk);
             }
             if (grp < stop) {
                 load(f1, x, buf, grp + 4);
-                compute(std::false_type(), f0, kGrp);
+                compute(std::false_type(), f0, kBk);
                 f0 = f1;
                 grp += 4;
             }
-            // the wave's last group, and any before it with a block that ends early.  A mask compares 16 * (a lane's block) + token with
-            // `left`, so each lane gives its own block's.
+            // the wave's last group, and any before it with a block that ends early
 #pragma nounroll
             for (;;) {
-                const int b = 2 * grp + (q >> 1), there = b < n_full ? kBk : b < n_blk ? (int)fill[buf][b] : 0;
-                compute(std::true_type(), f0, 16 * (q >> 1) + there);
+                const int b = 2 * grp + (q >> 1);  // this lane's block
+                compute(std::true_type(), f0, b < n_full ? kBk : b < n_blk ? (int)fill[buf][b] : 0);
                 grp += 4;
                 if (grp >= n_grp) break;
                 load(f0, x, buf, grp);
@@ -290,34 +371,29 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
             if (tiles == 1) walk(std::integral_constant<int, 1>());
             if constexpr (NT >= 2) if (tiles == 2) walk(std::integral_constant<int, 2>());
             if constexpr (NT >= 3) if (tiles == 3) walk(std::integral_constant<int, 3>());
-            if constexpr (NT >= 5) {
-                if (tiles == 4) walk(std::integral_constant<int, 4>());
-                if (tiles == 5) walk(std::integral_constant<int, 5>());
-            }
         }
-        // The waves' states are put together up to three tiles at a time: each wave leaves its own in LDS and takes d tiles 2 w, 2 w + 1 of all.
-        auto leave = [&](int qt0) {
-            f32x4 *o = (f32x4 *)(smem + w * Image<kIT>::kBytes);
-            float2 *ml = (float2 *)(o + Image<kIT>::kO);
+        // The waves' states are put together: each wave leaves its own in LDS and takes d tiles 2 w, 2 w + 1 of all queries.
+        auto leave = [&] {
+            f32x4 *o = (f32x4 *)(smem + w * Image<NT>::kBytes);
+            float2 *ml = (float2 *)(o + Image<NT>::kO);
 #pragma unroll
-            for (int i = 0; i < kIT; ++i) {
-                if (qt0 + i >= NT) continue;
-                ml[i * 64 + lane] = make_float2(st.m[min(qt0 + i, NT - 1)], st.l[min(qt0 + i, NT - 1)]);
+            for (int qt = 0; qt < NT; ++qt) {
+                ml[qt * 64 + lane] = make_float2(st.m[qt], st.l[qt]);
 #pragma unroll
-                for (int dt = 0; dt < kDT; ++dt) o[(dt * kIT + i) * 64 + lane] = st.o[dt][min(qt0 + i, NT - 1)];
+                for (int dt = 0; dt < kDT; ++dt) o[(dt * NT + qt) * 64 + lane] = st.o[dt][qt];
             }
         };
-        auto take = [&](int qt0) {
+        auto take = [&] {
 #pragma unroll
-            for (int i = 0; i < kIT; ++i) {
-                const int qt = qt0 + i, j = x.j0 + 16 * qt + m;
+            for (int qt = 0; qt < NT; ++qt) {
+                const int j = x.j0 + 16 * qt + m;
                 if (qt >= tiles) continue;
                 float2 ml[4];
                 float mx = -INFINITY, l = 0.f;
                 f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    ml[k] = ((const float2 *)(smem + k * Image<kIT>::kBytes + Image<kIT>::kO * 16))[i * 64 + lane];
+                    ml[k] = ((const float2 *)(smem + k * Image<NT>::kBytes + Image<NT>::kO * 16))[qt * 64 + lane];
                     mx = fmaxf(mx, ml[k].x);
                 }
 #pragma unroll
@@ -325,7 +401,7 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
                     const float f = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - mx);  // a wave without tokens
                     l += f * ml[k].y;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) o[h] += f * ((const f32x4 *)(smem + k * Image<kIT>::kBytes))[((2 * w + h) * kIT + i) * 64 + lane];
+                    for (int h = 0; h < 2; ++h) o[h] += f * ((const f32x4 *)(smem + k * Image<NT>::kBytes))[((2 * w + h) * NT + qt) * 64 + lane];
                 }
                 l += __shfl_xor(l, 16, 64);
                 l += __shfl_xor(l, 32, 64);
@@ -347,19 +423,13 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
         };
         __syncthreads();  // every wave has taken its part of the item before: a wave without a group of this one is here at once
         if (i2 >= 0) count(id, n);
-        leave(0);
+        leave();
         if (i2 >= 0) q_to_lds(qv, buf ^ 1);
         __syncthreads();
         if (i2 >= 0) place(id, n, buf ^ 1);
         __syncthreads();
         if (i2 >= 0) load(f0, nx, buf ^ 1, w);
-        take(0);
-        if constexpr (NT > kIT) {
-            __syncthreads();
-            leave(kIT);
-            __syncthreads();
-            take(kIT);
-        }
+        take();
         if (i2 < 0) break;
         x = nx;
         i1 = i2;
@@ -593,7 +663,7 @@ int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxS
 
 template <int NT, bool KV8>
 hipError_t launch_mfma(const Dims &dm, const BlockAttnArgs &a, const SplitOut &part, hipStream_t st) {
-    const size_t lds = 4 * Image<(NT < 3 ? NT : 3)>::kBytes + 2 * NT * kKS * 1024;
+    const size_t lds = 4 * Image<NT>::kBytes + 2 * NT * kKS * 1024;
     static bool attr_set = false;
     if (lds > 64 * 1024 && !attr_set) {
         hipError_t e = hipFuncSetAttribute((const void *)k_block_attn<NT, KV8>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
@@ -635,7 +705,7 @@ hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *works
     const bool mfma = on_matrix_cores(dm);
     const int64_t tiles = ((int64_t)rows * g + 15) / 16;
     SplitOut part;
-    part.tile_groups = mfma ? (int)((tiles + 4) / 5) : 1;
+    part.tile_groups = mfma ? (int)((tiles + 2) / 3) : 1;
     part.tiles = (int)((tiles + part.tile_groups - 1) / part.tile_groups);
     part.splits = splits_for(dm, pairs * part.tile_groups, a.max_selected, splits_for(dm, pairs, a.max_selected));  // no more than the workspace was sized for
     part.per = std::max(2, ((a.max_selected + part.splits - 1) / part.splits + 1) & ~1);
@@ -646,8 +716,7 @@ hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *works
     if (!mfma) DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_vec<T, KT>(dm, a, part, st)));
     else if (part.tiles == 1) e = dm.kv8 ? launch_mfma<1, true>(dm, a, part, st) : launch_mfma<1, false>(dm, a, part, st);
     else if (part.tiles == 2) e = dm.kv8 ? launch_mfma<2, true>(dm, a, part, st) : launch_mfma<2, false>(dm, a, part, st);
-    else if (part.tiles == 3) e = dm.kv8 ? launch_mfma<3, true>(dm, a, part, st) : launch_mfma<3, false>(dm, a, part, st);
-    else e = dm.kv8 ? launch_mfma<5, true>(dm, a, part, st) : launch_mfma<5, false>(dm, a, part, st);
+    else e = dm.kv8 ? launch_mfma<3, true>(dm, a, part, st) : launch_mfma<3, false>(dm, a, part, st);
     if (e != hipSuccess || part.splits == 1) return e;
     DISPATCH_T(dm.bf16, hipLaunchKernelGGL(k_block_attn_join<T>, dim3(a.S, std::min(std::max(rows, 1), 64), (dm.Hq + 3) / 4), dim3(256), 0, st, a, part, dm.Hq, dm.D));
     return hipGetLastError();
