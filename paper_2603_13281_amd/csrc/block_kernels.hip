@@ -582,7 +582,9 @@ __device__ __forceinline__ int n_blocks_of(const SelectArgs &a, int s, int Bk) {
 // Scores on the matrix cores, head sizes 64, 128, 192, 256: a wave to 16 * TB blocks.  Codes of a block are the columns of 16x16x64 products in 8 bits, a query's positive
 // parts (as many as the largest keys) and negative parts (smallest keys) the rows.  In both operands a lane holds 16 bytes of one row or column,
 // which is how codes lie in memory and what a lane quantises by itself: a query's 16 channels of one step, the same for both parts.  The four waves
-// quantise a tile of 16 queries each and share them; their codes are on the way meanwhile.
+// quantise a tile of 16 queries each and share them; their codes are on the way meanwhile.  Each workgroup is one chain of reads (length, ids, codes), so many small ones at a
+// time do best: 64 sequences of 1024-16384 tokens, 1-8 agents (73 MB) 19 us with five waves to a SIMD, 21 with four, 28 with six (the registers do not hold the codes);
+// 23 us where a workgroup goes on to further blocks with the next codes on their way.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 template <typename T> __device__ __forceinline__ void load16(const T *p, float (&v)[16]) {
     if constexpr (sizeof(T) == 2) {
@@ -625,7 +627,7 @@ __device__ __forceinline__ void quantise4(const float *v, float inv, int *up, in
     *down = (int)__builtin_amdgcn_perm(d1, d0, 0x06040200);
 }
 template <typename T, int KS, int TB>
-__global__ void __launch_bounds__(256) k_scores_mfma(SelectArgs a, int Hq, int Hkv, int Bk) {
+__global__ void __launch_bounds__(256, KS <= 4 ? 5 : 1) k_scores_mfma(SelectArgs a, int Hq, int Hkv, int Bk) {
     constexpr int D = KS * 32, H = KS / 2;  // steps of 64 of both parts, of one part
     __shared__ i32x4 rows[4][KS][64];       // four tiles of queries: [tile][step][lane]
     __shared__ __attribute__((aligned(16))) float steps[4][16];
