@@ -67,8 +67,9 @@ icarus_status icarus_rope_append(icarus_ctx *ctx, const void *qkv, int64_t ld, i
  * below to_lens[s].  hi[d], lo[d]: largest and smallest k[d] (a NaN counts as 0, an infinity as the largest finite value; FP8 cache:
  * of the codes' values, without k_scale).  With 2^e the smallest power of two, -40 <= e <= 40, with 127 * 2^e >= every |hi[d]| and |lo[d]|:
  *   codes[block][kv-head][0][d] = ceil(hi[d] / 2^e), codes[..][1][d] = floor(lo[d] / 2^e), at most 127 in size; scales[block][kv-head] = 2^e
- * so that code * scale bounds the keys (wherever e = 40 suffices).  Blocks outside the pool are left out.  After icarus_prefill_kv
- * or icarus_decode_step: from_lens = the lengths before, to_lens = after.
+ * so that code * scale bounds the keys (wherever e = 40 suffices).  Blocks outside the pool are left out.  A block of two sequences (a common
+ * cached prefix) has to hold as many tokens for one as for the other.  After icarus_prefill_kv or icarus_decode_step: from_lens = the
+ * lengths before, to_lens = after.
  *   block_tables          device int32 [S, max_blocks]
  *   from_lens, to_lens    device int32 [S]
  *   max_new               about the largest to_lens - from_lens, 0 if unknown: sizes the launch
@@ -102,6 +103,8 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
  * left out; a block named twice counts twice.  A row that has nothing to attend to becomes zeros; rows of no sequence keep
  * what out holds.
  *   blocks, counts   device int32 [S, Hkv, max_selected] and [S], as icarus_select_blocks gives them (in any order)
+ *   seq_rows         about the most rows of a sequence, 0 if unknown: sizes the launch
+ *   out              device [R, Hq, D], no memory of q
  *   workspace        at least icarus_attn_blocks_workspace_bytes(ctx, S, R, max_selected) */
 size_t icarus_attn_blocks_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t R, int32_t max_selected);
 icarus_status icarus_attn_blocks(icarus_ctx *ctx, const void *q, const void *kv_pool, const int32_t *block_tables, int32_t max_blocks,

@@ -4,6 +4,7 @@
 #include "block_util.h"
 
 #include <algorithm>
+#include <atomic>
 
 namespace icarus {
 namespace {
@@ -14,7 +15,7 @@ constexpr int kChunk = 512;
 template <typename T, typename KT>
 __global__ void __launch_bounds__(256) k_block_attn_generic(BlockAttnArgs a, int Hq, int Hkv, int D, int Bk, float scale, float k_scale, float v_scale) {
     __shared__ float qs[256], sc[kChunk], red[16];
-    __shared__ int64_t where[kChunk];  // element of a position's key block, with its place in the block in the low bits; -1: masked
+    __shared__ int64_t where[kChunk];  // a position's element of channel 0 of the values, -1: masked
     const int s = blockIdx.y, h = blockIdx.x, c = h / (Hq / Hkv);
     const int row0 = min(max(a.row_start[s], 0), a.R), row1 = min(max(a.row_start[s + 1], row0), a.R);
     const int len = max(a.kv_lens[s], 0), n_sel = min(max(a.counts[s], 0), a.max_selected);
@@ -77,8 +78,9 @@ __global__ void __launch_bounds__(256) k_block_attn_generic(BlockAttnArgs a, int
 // Items are short -- a list of 64 blocks is 8 groups to a wave -- and what an item waits for before its first key is a chain of reads: its list entry, the block id of the
 // entry, the block.  So while item i is walked, the ids of item i + 1 and its queries, and the list entries of item i + 2 are on their way, and the first blocks of item i + 1
 // are requested before the waves' states of item i are put together.
-// Two workgroups of 8 waves to a CU instead, a buffer of keys and one of values each: 64 sequences, 1-8 agents, 64 blocks (268 MB) 75 us, each item from
-// nothing with two buffers 70-75 us, this 58 us.
+// 64 sequences, 1-8 agents, 64 blocks (268 MB): 57.5 us, 4.7 TB/s, of which about 10 us are the first item's start and the last one's end.  Two workgroups to a CU, a buffer of
+// keys and one of values each: 75 us; one with two buffers, each item from nothing: 70-75 us.  More than three tiles: the queries are dealt to
+// workgroups three tiles at a time (16 sequences over an FP8 cache, 72 queries, 256 blocks 39 us; five tiles to a workgroup and half the list 51 us).
 //
 // The ids of an item stand in LDS, full blocks first, then blocks that end behind the sequence's last token, entries that name nothing dropped: the loop over full
 // blocks needs no masks and loads without conditions.
@@ -644,7 +646,7 @@ __global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitO
 
 // Splits of the lists, at most `most`.  Items go over the workgroups that the chip holds (1 to a CU on the matrix cores, 4 on the vector units) in rounds; a round costs the blocks
 // of its items and as much as kItemCost blocks on top, joining kJoinCost.
-constexpr int kWgs = 256, kItemCost = 12, kJoinCost = 24, kMaxSplits = 32;
+constexpr int kWgs = 256, kItemCost = 12, kJoinCost = 24, kMaxSplits = 32, kMaxTileGroups = 64;
 int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxSplits) {
     const int least = (max_selected + kItemBlocks - 1) / kItemBlocks;
     const int64_t wgs = on_matrix_cores(dm) ? kWgs : 4 * kWgs;
@@ -664,11 +666,17 @@ int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxS
 template <int NT, bool KV8>
 hipError_t launch_mfma(const Dims &dm, const BlockAttnArgs &a, const SplitOut &part, hipStream_t st) {
     const size_t lds = 4 * Image<NT>::kBytes + 2 * NT * kKS * 1024;
-    static bool attr_set = false;
-    if (lds > 64 * 1024 && !attr_set) {
-        hipError_t e = hipFuncSetAttribute((const void *)k_block_attn<NT, KV8>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
+    if (lds > 64 * 1024) {  // each device has its own copy of the kernel
+        static std::atomic<uint64_t> set{0};
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
-        attr_set = true;
+        const uint64_t bit = 1ull << (dev & 63);
+        if (dev > 63 || !(set.load() & bit)) {
+            e = hipFuncSetAttribute((const void *)k_block_attn<NT, KV8>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
+            if (e != hipSuccess) return e;
+            if (dev <= 63) set.fetch_or(bit);
+        }
     }
     const float scale_log2 = kLog2e / sqrtf((float)kD) * (KV8 ? dm.k_scale : 1.f);
     hipLaunchKernelGGL((k_block_attn<NT, KV8>), dim3(std::min(part.n_items, kWgs)), dim3(256), lds, st, a, part, dm.Hq, dm.Hkv, scale_log2, KV8 ? dm.v_scale : 1.f);
@@ -701,12 +709,12 @@ static hipError_t launch_vec(const Dims &dm, const BlockAttnArgs &a, const Split
 hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *workspace, hipStream_t st) {
     const int g = dm.Hq / dm.Hkv;
     const int64_t pairs = (int64_t)a.S * dm.Hkv;
-    const int rows = a.seq_rows ? std::min(a.seq_rows, a.R) : a.R;  // of a sequence, at most
+    const int rows = std::min(a.R, a.seq_rows ? a.seq_rows : 2 * ((a.R + a.S - 1) / a.S));  // of a sequence, about: the kernels go on where there are more
     const bool mfma = on_matrix_cores(dm);
     const int64_t tiles = ((int64_t)rows * g + 15) / 16;
     SplitOut part;
-    part.tile_groups = mfma ? (int)((tiles + 2) / 3) : 1;
-    part.tiles = (int)((tiles + part.tile_groups - 1) / part.tile_groups);
+    part.tile_groups = mfma ? (int)std::min<int64_t>((tiles + 2) / 3, kMaxTileGroups) : 1;
+    part.tiles = (int)std::min<int64_t>((tiles + part.tile_groups - 1) / part.tile_groups, 3);
     part.splits = splits_for(dm, pairs * part.tile_groups, a.max_selected, splits_for(dm, pairs, a.max_selected));  // no more than the workspace was sized for
     part.per = std::max(2, ((a.max_selected + part.splits - 1) / part.splits + 1) & ~1);
     part.o = (float *)workspace;

@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kExtThreads) k_extend(ExtendArgs a, int rows_p
             at = min(at + n[j], row_cap);
             row_end[i] = at;
             ok[j] = ok[j] && (n[j] == 0 || at <= a.max_rows);
-            need[j] = ok[j] ? blocks_of(c[j] + nw[j], a.Bk) - blocks_of(c[j], a.Bk) : 0;
+            need[j] = ok[j] ? min(blocks_of(c[j] + nw[j], a.Bk) - blocks_of(c[j], a.Bk), id_cap) : 0;
             sum = min(sum + need[j], id_cap);
         }
         int id = min(ids_before + scan_sat(sum, id_cap, red, &total), id_cap);

@@ -2013,7 +2013,8 @@ bool overlap(const void *a, size_t an, const void *b, size_t bn) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return x < y + bn && y < x + an;
 }
-constexpr int kBlockMaxSeqs = 65535, kBlockMaxRows = 1 << 30;
+constexpr int kBlockMaxSeqs = 65535, kBlockMaxRows = 1 << 29;  // sums of two counts stay in 32 bits
+constexpr int kBlockMaxTable = 1 << 22;                        // blocks of a sequence, entries of a list
 }  // namespace
 
 icarus_status icarus_extend_sequences(icarus_ctx *ctx, int32_t S, const int32_t *ctx_lens, const int32_t *new_lens, const int32_t *streams,
@@ -2094,7 +2095,8 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
     if (S < 0 || max_blocks < 0 || R < 0 || seq_rows < 0 || first < 0 || last < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
     if (top_k < 1 || (int64_t)first + last > top_k)
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "top_k %d must be positive and hold the first %d and the last %d blocks", top_k, first, last);
-    if (S > kBlockMaxSeqs) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences per call", kBlockMaxSeqs);
+    if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_blocks > kBlockMaxTable || top_k > kBlockMaxTable)
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences, %d rows and %d blocks of a sequence per call", kBlockMaxSeqs, kBlockMaxRows, kBlockMaxTable);
     if (S == 0) return ICARUS_OK;
     if (any_null({codes, scales, kv_lens, row_start, blocks, counts, workspace}) || (max_blocks && !block_tables) || (R && !q))
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
@@ -2121,13 +2123,18 @@ icarus_status icarus_attn_blocks(icarus_ctx *ctx, const void *q, const void *kv_
     if (!ctx) return ICARUS_ERR_INVALID_ARG;
     std::lock_guard<std::mutex> lk(ctx->mu);
     if (S < 0 || max_blocks < 0 || R < 0 || seq_rows < 0 || max_selected < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
-    if (S > kBlockMaxSeqs) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences per call", kBlockMaxSeqs);
+    const icarus_layer_config &c = ctx->cfg;
+    if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_selected > kBlockMaxTable || (int64_t)S * c.n_kv_heads * (max_selected / 256 + 1) > 1 << 20)
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d sequences, %d kv-heads, %d rows, lists of %d blocks: at most %d sequences and %d rows per call, and 2^20 times 256 entries in all lists",
+                    S, c.n_kv_heads, R, max_selected, kBlockMaxSeqs, kBlockMaxRows);
     if (S == 0 || R == 0) return ICARUS_OK;
     if (any_null({q, kv_pool, kv_lens, row_start, counts, out, workspace}) || (max_blocks && !block_tables) || (max_selected && !blocks))
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
     if (!all_aligned({q, kv_pool, out, workspace}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "q, kv_pool, out and workspace must be 16-byte aligned");
     if (!all_aligned({block_tables, kv_lens, row_start, blocks, counts}, 4))
         return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays must be aligned to their element");
+    const size_t q_bytes = (size_t)R * c.n_q_heads * c.head_dim * (c.dtype == ICARUS_BF16 ? 2 : 4);
+    if (overlap(out, q_bytes, q, q_bytes)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "out must not share memory with q");
     const size_t need = icarus_attn_blocks_workspace_bytes(ctx, S, R, max_selected);
     if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
     BlockAttnArgs a{q, kv_pool, block_tables, max_blocks, ctx->cfg.num_blocks, S, kv_lens, row_start, R, seq_rows, blocks, counts, max_selected, out};

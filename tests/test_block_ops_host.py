@@ -101,6 +101,7 @@ def test_select_and_attend_refusals():
         run("INVALID_ARG", **{name: None})
         run("ALIGNMENT", **{name: A + 2})
     run("CAPACITY", wsb=lib.icarus_select_workspace_bytes(layer._h, 2, 8) - 1)
+    run("UNSUPPORTED", mb=(1 << 22) + 1)
     good = dict(q=A, pool=A, bt=A, mb=8, S=2, kv=A, R=3, start=A, hint=0, blocks=A, counts=A, k=4, out=A + (1 << 20), ws=A, wsb=1 << 30)
 
     def run(status, **kw):  # noqa: F811
@@ -116,6 +117,8 @@ def test_select_and_attend_refusals():
         run("INVALID_ARG", **{name: None})
         run("ALIGNMENT", **{name: good[name] + 2})
     run("CAPACITY", wsb=lib.icarus_attn_blocks_workspace_bytes(layer._h, 2, 3, 4) - 1)
+    run("INVALID_ARG", out=good["q"] + 2 * 3 * 8 * 64 - 16)
+    run("UNSUPPORTED", S=60000, k=100000)
     layer.close()
 
 

@@ -185,7 +185,8 @@ def run_append(layer, rows, seed, ld=None, slots=None, pos=None):
 
 SHAPES = [dict(), dict(qk_norm=True), dict(Hq=4, Hkv=4, D=64, bf16=False, theta=1e4), dict(Hq=64, Hkv=8, qk_norm=True, fp8=True, k_scale=0.02, v_scale=0.013),
           dict(Hq=6, Hkv=1, D=256, bk=8), dict(Hq=3, Hkv=3, D=36, bk=5, qk_norm=True), dict(Hq=2, Hkv=1, D=2, bk=1, bf16=False), dict(Hq=4, Hkv=2, D=96, bk=32, fp8=True),
-          dict(Hq=4, Hkv=2, D=64, bk=16, fp8=True, bf16=False, qk_norm=True), dict(Hq=5, Hkv=5, D=254, bk=3)]
+          dict(Hq=4, Hkv=2, D=64, bk=16, fp8=True, bf16=False, qk_norm=True), dict(Hq=5, Hkv=5, D=254, bk=3), dict(mode=1, qk_norm=True), dict(Hq=6, Hkv=2, D=192),
+          dict(Hq=2, Hkv=2, D=256, bf16=False, qk_norm=True), dict(Hq=4, Hkv=2, D=64, qk_norm=True), dict(Hq=6, Hkv=3, D=16, bf16=False), dict(Hq=4, Hkv=4, D=128, bf16=False)]
 
 
 @pytest.mark.parametrize("kw", SHAPES, ids=str)
@@ -454,6 +455,95 @@ def test_attend_large_scores(kw):
     q = torch.tensor(rng.standard_normal((3, 4, 128)) * 30, dtype=torch.float32).to(c.torch_dtype).to(DEV)
     for order in (np.arange(40), np.arange(40)[::-1], rng.permutation(40)):
         run_attend(layer, q, pool, table, [640], np.array([0, 3]), order.reshape(1, 1, 40).copy(), [40])
+    layer.close()
+
+
+def test_attend_lists_in_many_parts():
+    """Lists longer than a workgroup holds, of few sequences among many without rows; and of no entry at all."""
+    for kw, S, top in ((dict(), 300, 700), (dict(Hq=4, Hkv=4, D=64, bf16=False), 300, 600), (dict(), 2, 2600), (dict(Hq=4, Hkv=2, D=64, bf16=False), 1, 2600), (dict(), 3, 0)):
+        print("case:", kw, S, top, flush=True)
+        layer = make(num_blocks=64, **kw)
+        c, rng = layer.cfg, np.random.default_rng(top)
+        pool = random_pool(layer, rng)
+        table = rng.integers(0, 64, (S, 64))
+        kv = rng.integers(900, 1025, S)
+        rows = np.zeros(S, dtype=int)
+        rows[[0, S // 2, S - 1]] = (2, 5, 1) if S > 2 else (3, 3, 3)
+        start = np.concatenate([[0], np.cumsum(rows)])
+        q = torch.tensor(rng.standard_normal((start[-1], c.n_q_heads, c.head_dim)), dtype=torch.float32).to(c.torch_dtype).to(DEV)
+        blocks = rng.integers(0, 64, (S, c.n_kv_heads, top))
+        for counts in (np.full(S, top), rng.integers(0, top + 1, S)):
+            run_attend(layer, q, pool, table, kv, start, blocks, counts)
+        layer.close()
+
+
+def test_blocks_beyond_32_bits():
+    """A pool of 9.2 GB, elements beyond 2^32: the same bits as from a small pool that holds the same blocks."""
+    n_big, n_small = 140000, 48
+    rng = np.random.default_rng(0)
+    high = np.sort(rng.choice(np.arange(n_big - 8000, n_big), n_small, replace=False))
+    high[-1] = n_big - 1
+    results = []
+    qkv = torch.tensor(rng.standard_normal((40, 48 * 128)), dtype=torch.float32).to(torch.bfloat16).to(DEV)
+    small_pool = None
+    for n, ids in ((n_small, np.arange(n_small)), (n_big, high)):
+        layer = make(Hq=32, Hkv=8, num_blocks=n, qk_norm=True)
+        pool = torch.empty(layer.cfg.pool_shape(), dtype=torch.bfloat16, device=DEV)
+        where = torch.tensor(ids, device=DEV)
+        if small_pool is None:
+            small_pool = random_pool(layer, np.random.default_rng(1)).clone()
+        pool[where] = small_pool
+        table = ids[np.random.default_rng(2).permutation(n_small)].reshape(3, 16)
+        kv = np.array([256, 255, 130])
+        slots = np.concatenate([table[0, 15] * 16 + np.arange(3), table[1, 14] * 16 + np.arange(16), table[2, 8] * 16 + np.arange(2), np.full(19, -1)])
+        q = torch.zeros(40, 32, 128, dtype=torch.bfloat16, device=DEV)
+        layer.rope_append(qkv, i32(np.arange(40) * 7), torch.tensor(slots, dtype=torch.int64, device=DEV), pool, q)
+        codes, scales = layer.new_key_bounds(DEV)
+        layer.key_bounds(pool, i32(table), i32([0, 0, 0]), i32(kv), codes, scales)
+        blocks, counts = torch.zeros(3, 8, 6, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+        start = i32([0, 9, 30, 40])
+        layer.select_blocks(q, codes, scales, i32(table), i32(kv), start, blocks, counts)
+        out = layer.attn_blocks(q, pool, i32(table), i32(kv), start, blocks, counts)
+        fresh = i32(ids[:6] if n == n_small else high[:6])
+        m = binding.SequenceMap(1, 70, DEV)
+        grown = torch.full((1, 5), -1, dtype=torch.int32, device=DEV)
+        layer.extend_sequences(m, i32([0]), i32([70]), grown, fresh, i32([0]))
+        slot = m.row_slot.clone()
+        at = torch.searchsorted(where, slot // 16) * 16 + slot % 16  # as the small pool counts
+        results.append([q, pool[where], codes[where], scales[where], blocks, counts, out, at])
+        assert int(slot.max()) // 16 == int(ids[:5].max())
+        torch.cuda.synchronize()
+        layer.close()
+        del pool
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(*results))
+
+
+def test_integer_arrays_need_only_their_own_alignment():
+    layer = make(num_blocks=64)
+    c, rng = layer.cfg, np.random.default_rng(0)
+    off = lambda a: torch.cat([i32([0]), i32(a).reshape(-1)])[1:].reshape(np.shape(a))  # noqa: E731: four bytes behind an aligned address
+    pool = random_pool(layer, rng)
+    table, kv, start = rng.permutation(64)[:60].reshape(3, 20), np.array([320, 77, 300]), np.array([0, 1, 4, 6])
+    codes, scales = layer.new_key_bounds(DEV)
+    scales = torch.ones(scales.numel() + 1, device=DEV)[1:].view(scales.shape)
+    layer.key_bounds(pool, off(table), off([0, 0, 0]), off(kv), codes, scales)
+    q = torch.tensor(rng.standard_normal((6, 8, 128)), dtype=torch.float32).to(torch.bfloat16).to(DEV)
+    blocks, counts = off(np.zeros((3, 2, 7), dtype=int)), off([0, 0, 0])
+    layer.select_blocks(q, codes, scales, off(table), off(kv), off(start), blocks, counts)
+    want = ref.select(host(q), host(codes).astype(np.int64), host(scales), table, kv, start, 7, 1, 2, 16)
+    assert np.array_equal(blocks.cpu().numpy(), want[0])
+    out = layer.attn_blocks(q, pool, off(table), off(kv), off(start), blocks, counts)
+    again = layer.attn_blocks(q, pool, i32(table), i32(kv), i32(start), blocks.clone(), counts.clone())
+    assert torch.equal(out, again)
+    new, used = off([1, 0, 17]), off([2])
+    m, free = binding.SequenceMap(3, 21, DEV), off(np.arange(40))
+    t2 = off(np.concatenate([table, np.full((3, 2), -1)], 1))
+    wide = t2.cpu().numpy().copy()
+    layer.extend_sequences(m, off(kv), new, t2, free, used, streams=off([2, 1, 1]))
+    want = ref.extend(kv, [1, 0, 17], [2, 1, 1], wide, np.arange(40), 2, 21, 16, 64, 1 << 20)
+    for name in ("kv_lens", "row_start", "row_seq", "row_pos", "row_slot", "counts"):
+        assert np.array_equal(getattr(m, name).cpu().numpy(), want[name]), name
+    assert np.array_equal(t2.cpu().numpy(), want["block_tables"])
     layer.close()
 
 
