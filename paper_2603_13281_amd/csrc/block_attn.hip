@@ -441,164 +441,151 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
 
 bool on_matrix_cores(const Dims &dm) { return dm.bf16 && dm.D == kD && dm.Bk == kBk; }
 
-// ---- blocks of 16, head sizes that are multiples of 16: vector units -----------------------------------------------------------
-// For float32 and head sizes other than 128.  A workgroup takes a sequence, kv-head and range of the list, NQ of its stacked queries at a time; a wave takes
-// blocks in turn, whose ids it reads 64 at a time.  Scores: lane t + 16 p has a quarter p of token t's key, the queries lie in LDS; values: a lane has
-// channels d, d + 64, .. of all tokens, a row of the transposed block, and the weights lie in LDS.  Each block is read once for NQ queries.
-template <typename T, typename KT, int ND, int NQ>  // ND: channels of a lane, D <= 64 ND; NQ: a multiple of 4
-__global__ void __launch_bounds__(256) k_block_attn_vec(BlockAttnArgs a, SplitOut part, int Hq, int Hkv, int D, float scale_log2, float v_scale) {
+// ---- blocks of 16, head sizes that are multiples of 16: matrix cores in float32 ----------------------------------------------
+// For float32 and head sizes other than 128.  A workgroup takes a sequence, kv-head, range of the list and a tile of 16 stacked queries; a wave takes
+// blocks in turn (with the next one on its way: no faster).  Products of 16 x 16 x 4 with the transposed operands: scores are keys [token][channel] times
+// queries [channel][query], which leaves lane t + 16 p query t's scores of tokens 4 p .. 4 p + 3, and these are at once the right operand of the values'
+// product [channel][token] x [token][query], whose left operand is a row piece of the transposed block.  So nothing passes through LDS until the waves join, and
+// a query's reference, sum and sums of values lie in its own four lanes.  float32, 4 heads of 64, 25 sequences x 9 rows x up to 190 blocks (147 MB): 29 us, 5.1 TB/s;
+// the same on the vector units with the queries in LDS took 76 us, bound by LDS.  Rows beyond 16 / g read the blocks again, from the caches: float32, 8 heads of 128 for
+// 32 queries, 32 x up to 9 rows x 64 blocks (268 MB) 85 us; two tiles of queries to a workgroup halve the reads and took 121 us, for want of waves.  bfloat16 keys and
+// values become float32 here: 8 heads of 64 (134 MB) 61 us, bound by the products, a sixteenth of the rate of 16-bit ones.
+template <typename T, typename KT, int DT, bool EXACT>  // tiles of 16 channels: at most DT, or DT exactly
+__global__ void __launch_bounds__(256) k_block_attn_f32(BlockAttnArgs a, SplitOut part, int Hq, int Hkv, int D_, float scale_log2, float v_scale) {
     constexpr int Bk = 16;
-    __shared__ __attribute__((aligned(16))) float qs[NQ][64 * ND], weight[4][NQ][Bk], image[4][NQ][64 * ND];
-    __shared__ float image_m[4][NQ], image_l[4][NQ];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, quarter = lane >> 4, g = Hq / Hkv;
+    typedef typename Quad<KT>::raw Raw;
+    __shared__ f32x4 image[2][DT][64];
+    __shared__ float image_m[4][16], image_l[4][16];
+    const int D = EXACT ? 16 * DT : D_, d16 = D / 16;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, p4 = 4 * (lane >> 4), g = Hq / Hkv;
     const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, split = blockIdx.y;
     const int row0 = min(max(a.row_start[s], 0), a.R), G = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
     const int len = max(a.kv_lens[s], 0), n_sel = min(max(a.counts[s], 0), a.max_selected);
-    const int e_begin = split * part.per, e_end = min(n_sel, e_begin + part.per);
-    const int32_t *list = a.blocks + (size_t)pair * a.max_selected, *bt = a.bt + (size_t)s * a.max_blocks;
-    const int PD = D / 4;
-    for (int j0 = 0; j0 < G; j0 += NQ) {
-        const int nq = min(NQ, G - j0);
-        __syncthreads();
-        for (int i = threadIdx.x; i < NQ * D; i += 256) {
-            const int j = j0 + min(i / D, nq - 1);
-            qs[i / D][i % D] = Elem<T>::ld((const T *)a.q + ((size_t)(row0 + j / g) * Hq + c * g + j % g) * D + i % D);
+    const int e0 = split * part.per + w, e_end = min(n_sel, (split + 1) * part.per), some = max(0, e_end - e0 + 3) / 4;  // entries e0, e0 + 4, ..: at most 64
+    int my_id = 0, my_n = 0;  // block of entry e0 + 4 lane, and its tokens
+    if (lane < some) {
+        const int b = a.blocks[(size_t)pair * a.max_selected + e0 + 4 * lane];
+        if (b >= 0 && b < a.max_blocks && (int64_t)b * Bk < len) {
+            const int id = a.bt[(size_t)s * a.max_blocks + b];
+            if (id >= 0 && id < a.num_blocks) {
+                my_id = id;
+                my_n = min(Bk, len - b * Bk);
+            }
         }
-        __syncthreads();
-        float m[NQ], l[NQ], acc[NQ][ND];
+    }
+    for (int j0 = 16 * blockIdx.z; j0 < G; j0 += 16 * gridDim.z) {
+        const int j = min(j0 + t, G - 1);
+        const size_t at = (size_t)(row0 + j / g) * Hq + c * g + j % g;
+        float q[DT][4];
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            m[j] = -INFINITY;
-            l[j] = 0.f;
+        for (int x = 0; x < DT; ++x)
+            if (EXACT || x < d16) Quad<T>::get(*(const typename Quad<T>::raw *)((const T *)a.q + at * D + 16 * x + p4), q[x]);
+        f32x4 o[DT];
+        float m = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int k = 0; k < ND; ++k) acc[j][k] = 0.f;
-        }
-        for (int e0 = e_begin + w; e0 < e_end; e0 += 256) {
-            int my_id = -1, my_n = 0;  // block of entry e0 + 4 lane, and its tokens
-            if (e0 + 4 * lane < e_end) {
-                const int b = list[e0 + 4 * lane];
-                if (b >= 0 && b < a.max_blocks) {
-                    my_n = (int)min((int64_t)Bk, (int64_t)len - (int64_t)b * Bk);
-                    if (my_n > 0) my_id = bt[b];
+        for (int x = 0; x < DT; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const auto add = [&](int id, int n) {
+            const KT *blk = (const KT *)a.pool + ((size_t)id * Hkv + c) * 2 * Bk * D;
+            const KT *kr = blk + min(t, n - 1) * D + p4, *vr = blk + Bk * D + t * Bk + p4;  // behind the last token: the last again
+            Raw k[DT], v[DT];
+#pragma unroll
+            for (int x = 0; x < DT; ++x)
+                if (EXACT || x < d16) k[x] = *(const Raw *)(kr + 16 * x);
+#pragma unroll
+            for (int x = 0; x < DT; ++x)
+                if (EXACT || x < d16) v[x] = *(const Raw *)(vr + 16 * Bk * x);
+            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < DT; ++x) {
+                if (!EXACT && x >= d16) continue;
+                float kf[4];
+                Quad<KT>::get(k[x], kf);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u], q[x][u], sc, 0, 0, 0);
+            }
+            float most = -INFINITY, p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                sc[u] = p4 + u < n ? sc[u] * scale_log2 : -INFINITY;
+                most = fmaxf(most, sc[u]);
+            }
+            if (__any(most > m + kSlack)) {  // see compute_group: the reference moves rarely
+                most = fmaxf(most, __shfl_xor(most, 16, 64));
+                most = fmaxf(most, __shfl_xor(most, 32, 64));
+                const float m_new = fmaxf(m, most), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+                m = m_new;
+                l *= f;
+#pragma unroll
+                for (int x = 0; x < DT; ++x) o[x] *= f;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                p[u] = sc[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sc[u] - m);
+                l += p[u];
+            }
+#pragma unroll
+            for (int x = 0; x < DT; ++x) {
+                if (!EXACT && x >= d16) continue;
+                float vf[4];
+                Quad<KT>::get(v[x], vf);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (n < Bk) vf[u] = p4 + u < n ? vf[u] : 0.f;  // places behind the last token may hold anything
+                    o[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[u], p[u], o[x], 0, 0, 0);
                 }
             }
-            const int some = min(64, (e_end - e0 + 3) / 4);
-            for (int i0 = 0; i0 < some; ++i0) {
-                const int id = __builtin_amdgcn_readlane(my_id, i0), n = __builtin_amdgcn_readlane(my_n, i0);
-                if (id < 0 || id >= a.num_blocks) continue;
-                const KT *blk = (const KT *)a.pool + ((size_t)id * Hkv + c) * 2 * Bk * D;
-                typename Quad<KT>::raw vr[ND][4];
-#pragma unroll
-                for (int k = 0; k < ND; ++k)
-                    if (lane + 64 * k < D)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) vr[k][i] = ((const typename Quad<KT>::raw *)(blk + Bk * D + (lane + 64 * k) * Bk))[i];
-                const typename Quad<KT>::raw *kr = (const typename Quad<KT>::raw *)(blk + min(t, n - 1) * D + quarter * PD);
-                float dot[NQ];
-#pragma unroll
-                for (int j = 0; j < NQ; ++j) dot[j] = 0.f;
-                for (int i0 = 0; i0 < PD / 4; i0 += 4) {
-                    typename Quad<KT>::raw kq[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) kq[u] = kr[min(i0 + u, PD / 4 - 1)];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if (i0 + u >= PD / 4) continue;
-                        float k[4];
-                        Quad<KT>::get(kq[u], k);
-#pragma unroll
-                        for (int jj = 0; jj < NQ; jj += 4) {
-                            if (jj >= nq) continue;
-#pragma unroll
-                            for (int j = jj; j < jj + 4; ++j) {
-                                const float4 qv = *(const float4 *)&qs[j][quarter * PD + 4 * (i0 + u)];
-                                dot[j] += qv.x * k[0];
-                                dot[j] += qv.y * k[1];
-                                dot[j] += qv.z * k[2];
-                                dot[j] += qv.w * k[3];
-                            }
-                        }
-                    }
-                }
-                auto weigh = [&](int j) {
-                    float x = dot[j];
-                    x += __shfl_xor(x, 16, 64);
-                    x += __shfl_xor(x, 32, 64);
-                    x = t < n ? x * scale_log2 : -INFINITY;
-                    if (__any(x > m[j] + kSlack)) {  // see compute_group: the reference moves rarely
-                        const float m_new = fmaxf(m[j], wave_max(x)), f = __builtin_amdgcn_exp2f(m[j] - m_new);
-                        m[j] = m_new;
-                        l[j] *= f;
-#pragma unroll
-                        for (int k = 0; k < ND; ++k) acc[j][k] *= f;
-                    }
-                    const float p = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - m[j]);
-                    l[j] += p;  // of token t, in all four quarters
-                    if (quarter == 0) weight[w][j][t] = p;
-                };
-#pragma unroll
-                for (int j = 0; j < NQ; ++j)
-                    if (j < nq) weigh(j);
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int k = 0; k < ND; ++k) {
-                    if (lane + 64 * k >= D) continue;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float v[4];
-                        Quad<KT>::get(vr[k][i], v);
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) v[u] = 4 * i + u < n ? v[u] : 0.f;  // places behind the last token may hold anything
-#pragma unroll
-                        for (int jj = 0; jj < NQ; jj += 4) {
-                            if (jj >= nq) continue;
-#pragma unroll
-                            for (int j = jj; j < jj + 4; ++j) {
-                                const float4 p = *(const float4 *)&weight[w][j][4 * i];
-                                acc[j][k] += p.x * v[0];
-                                acc[j][k] += p.y * v[1];
-                                acc[j][k] += p.z * v[2];
-                                acc[j][k] += p.w * v[3];
-                            }
-                        }
-                    }
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
+        };
+        for (int i = 0; i < some; ++i) {
+            const int id = __builtin_amdgcn_readlane(my_id, i), n = __builtin_amdgcn_readlane(my_n, i);
+            if (n > 0) add(id, n);
         }
-#pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            float x = l[j];  // over the 16 tokens
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) x += __shfl_xor(x, o, 64);
-            if (lane == 0) {
-                image_m[w][j] = m[j];
-                image_l[w][j] = x;
-            }
-#pragma unroll
-            for (int k = 0; k < ND; ++k) image[w][j][lane + 64 * k] = acc[j][k];
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (lane < 16) {
+            image_m[w][t] = m;
+            image_l[w][t] = l;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < nq * D; i += 256) {
-            const int j = i / D, d = i % D;
-            const float mx = fmaxf(fmaxf(image_m[0][j], image_m[1][j]), fmaxf(image_m[2][j], image_m[3][j]));
-            float o = 0.f, sum = 0.f;
+        const float mx = fmaxf(fmaxf(image_m[0][t], image_m[1][t]), fmaxf(image_m[2][t], image_m[3][t]));
+        float sum = 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float f = image_m[k][j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(image_m[k][j] - mx);
-                sum += f * image_l[k][j];
-                o += f * image[k][j][d];
+        for (int k = 0; k < 4; ++k) sum += (image_m[k][t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(image_m[k][t] - mx)) * image_l[k][t];
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
+#pragma unroll
+        for (int x = 0; x < DT; ++x) o[x] *= f;
+        const auto give = [&](int at) {
+#pragma unroll
+            for (int x = 0; x < DT; ++x)
+                if (EXACT || x < d16) image[at][x][lane] = o[x];
+        };
+        const auto take = [&](int at) {
+#pragma unroll
+            for (int x = 0; x < DT; ++x)
+                if (EXACT || x < d16) o[x] += image[at][x][lane];
+        };
+        if (w >= 2) give(w - 2);
+        __syncthreads();
+        if (w < 2) take(w);
+        if (w == 1) give(1);  // its own place
+        __syncthreads();
+        if (w != 0) continue;
+        take(1);
+        if (j0 + t >= G) continue;
+        if (part.splits == 1) {
+            const float inv = sum == 0.f ? 0.f : v_scale / sum;
+#pragma unroll
+            for (int x = 0; x < DT; ++x) {
+                if (!EXACT && x >= d16) continue;
+                T *out = (T *)a.out + at * D + 16 * x + p4;
+                if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(pack_bf16(o[x][0] * inv, o[x][1] * inv), pack_bf16(o[x][2] * inv, o[x][3] * inv));
+                else *(f32x4 *)out = o[x] * inv;
             }
-            const size_t at = (size_t)(row0 + (j0 + j) / g) * Hq + c * g + (j0 + j) % g;
-            if (part.splits == 1) {
-                Elem<T>::st((T *)a.out + at * D + d, sum > 0.f ? o * v_scale / sum : 0.f);
-            } else {
-                const size_t ps = (size_t)split * a.R * Hq + at;
-                part.o[ps * D + d] = o * v_scale;
-                if (d == 0) part.ml[ps] = make_float2(mx, sum);
-            }
+        } else {
+            const size_t ps = (size_t)split * a.R * Hq + at;
+#pragma unroll
+            for (int x = 0; x < DT; ++x)
+                if (EXACT || x < d16) *(f32x4 *)(part.o + ps * D + 16 * x + p4) = o[x] * v_scale;
+            if (p4 == 0) part.ml[ps] = make_float2(mx, sum);
         }
     }
 }
@@ -644,12 +631,12 @@ __global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitO
     }
 }
 
-// Splits of the lists, at most `most`.  Items go over the workgroups that the chip holds (1 to a CU on the matrix cores, 4 on the vector units) in rounds; a round costs the blocks
+// Splits of the lists, at most `most`.  Items go over the workgroups that the chip holds (1 to a CU of the 128 kernel, 3 of the float32 one: with 4 the 25 sequences above took 33 us, with 8 35) in rounds; a round costs the blocks
 // of its items and as much as kItemCost blocks on top, joining kJoinCost.
 constexpr int kWgs = 256, kItemCost = 12, kJoinCost = 24, kMaxSplits = 32, kMaxTileGroups = 64;
 int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxSplits) {
     const int least = (max_selected + kItemBlocks - 1) / kItemBlocks;
-    const int64_t wgs = on_matrix_cores(dm) ? kWgs : 4 * kWgs;
+    const int64_t wgs = on_matrix_cores(dm) ? kWgs : 3 * kWgs;
     int best = 0;
     int64_t cost = 0;
     for (int n = std::max(1, least); n <= std::max(least, std::min(most, (max_selected + 7) / 8)) || !best; ++n) {  // 8 blocks: a group to a wave
@@ -694,15 +681,15 @@ size_t block_attn_workspace(const Dims &dm, int S, int R, int max_selected) {
 }
 
 template <typename T, typename KT>
-static hipError_t launch_vec(const Dims &dm, const BlockAttnArgs &a, const SplitOut &part, hipStream_t st) {
-    const dim3 grid(a.S * dm.Hkv, part.splits);
+static hipError_t launch_f32(const Dims &dm, const BlockAttnArgs &a, const SplitOut &part, hipStream_t st) {
+    const dim3 grid(a.S * dm.Hkv, part.splits, part.tile_groups);
     const float scale_log2 = kLog2e / sqrtf((float)dm.D) * (sizeof(KT) == 1 ? dm.k_scale : 1.f), v_scale = sizeof(KT) == 1 ? dm.v_scale : 1.f;
-    switch ((dm.D + 63) / 64) {
-    case 1: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 1, 16>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
-    case 2: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 2, 8>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
-    case 3: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 3, 8>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
-    default: hipLaunchKernelGGL((k_block_attn_vec<T, KT, 4, 8>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale); break;
-    }
+#define BLOCK_ATTN_F32(DT, EXACT) hipLaunchKernelGGL((k_block_attn_f32<T, KT, DT, EXACT>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale)
+    if (dm.D == 64) BLOCK_ATTN_F32(4, true);
+    else if (dm.D == 128) BLOCK_ATTN_F32(8, true);
+    else if (dm.D < 128) BLOCK_ATTN_F32(8, false);
+    else BLOCK_ATTN_F32(16, false);
+#undef BLOCK_ATTN_F32
     return hipGetLastError();
 }
 
@@ -713,7 +700,7 @@ hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *works
     const bool mfma = on_matrix_cores(dm);
     const int64_t tiles = ((int64_t)rows * g + 15) / 16;
     SplitOut part;
-    part.tile_groups = mfma ? (int)std::min<int64_t>((tiles + 2) / 3, kMaxTileGroups) : 1;
+    part.tile_groups = (int)std::min<int64_t>(mfma ? (tiles + 2) / 3 : tiles, kMaxTileGroups);
     part.tiles = (int)std::min<int64_t>((tiles + part.tile_groups - 1) / part.tile_groups, 3);
     part.splits = splits_for(dm, pairs * part.tile_groups, a.max_selected, splits_for(dm, pairs, a.max_selected));  // no more than the workspace was sized for
     part.per = std::max(2, ((a.max_selected + part.splits - 1) / part.splits + 1) & ~1);
@@ -721,7 +708,7 @@ hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *works
     part.ml = (float2 *)(part.o + (size_t)part.splits * a.R * dm.Hq * dm.D);
     part.n_items = (int)((pairs + 7) / 8 * 8 * part.splits * part.tile_groups);
     hipError_t e = hipSuccess;
-    if (!mfma) DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_vec<T, KT>(dm, a, part, st)));
+    if (!mfma) DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_f32<T, KT>(dm, a, part, st)));
     else if (part.tiles == 1) e = dm.kv8 ? launch_mfma<1, true>(dm, a, part, st) : launch_mfma<1, false>(dm, a, part, st);
     else if (part.tiles == 2) e = dm.kv8 ? launch_mfma<2, true>(dm, a, part, st) : launch_mfma<2, false>(dm, a, part, st);
     else e = dm.kv8 ? launch_mfma<3, true>(dm, a, part, st) : launch_mfma<3, false>(dm, a, part, st);
