@@ -40,10 +40,10 @@ __device__ __forceinline__ int scan_sat(int v, int cap, int *red, int *total) {
     return min(before + (lane ? up : 0), cap);
 }
 
-__global__ void __launch_bounds__(kExtThreads) k_extend(ExtendArgs a, int rows_per_wg) {
+__global__ void __launch_bounds__(kExtThreads) k_extend(ExtendArgs a) {
     __shared__ int row_begin[kExtSeg], row_end[kExtSeg], first_id[kExtSeg], ctx[kExtSeg], fresh[kExtSeg], red[kExtThreads / 64];
     const int row_cap = a.max_rows + 1, id_cap = a.n_free + 1;
-    const int r0 = blockIdx.x * rows_per_wg, r1 = min(a.max_rows, r0 + rows_per_wg);
+    const int r0 = blockIdx.x * kExtThreads, r1 = min(a.max_rows, r0 + kExtThreads);
     const bool lead = blockIdx.x == 0;
     const int head = min(max(*a.free_used, 0), a.n_free);
     int rows_before = 0, ids_before = head, used = head, refused = 0;
@@ -705,7 +705,7 @@ __global__ void __launch_bounds__(256, KS <= 4 ? 5 : 1) k_scores_mfma(SelectArgs
         x = fmaxf(x, __shfl_xor(x, 16, 64));
         x = fmaxf(x, __shfl_xor(x, 32, 64));
         const int b = b0 + 16 * t + m;
-        if (q4 == 0 && b < nb) ((uint32_t *)a.scores)[(size_t)pair * a.max_blocks + b] = order_key(good[t] ? (n ? x * scale[t] : 0.f) : -INFINITY);
+        if (q4 == 0 && b < nb) ((uint32_t *)a.scores)[(size_t)pair * key_pitch(a.max_blocks) + b] = order_key(good[t] ? (n ? x * scale[t] : 0.f) : -INFINITY);
     }
 }
 
@@ -757,21 +757,22 @@ __global__ void __launch_bounds__(256) k_scores(SelectArgs a, int Hq, int Hkv, i
             if (j < cnt) best = fmaxf(best, (float)acc[j] * qstep[j]);
     }
     if (b >= nb) return;
-    ((uint32_t *)a.scores)[((size_t)s * Hkv + c) * a.max_blocks + b] = order_key(good ? (n ? best * a.scales[rec] : 0.f) : -INFINITY);
+    ((uint32_t *)a.scores)[((size_t)s * Hkv + c) * key_pitch(a.max_blocks) + b] = order_key(good ? (n ? best * a.scales[rec] : 0.f) : -INFINITY);
 }
 
 // The choice of a sequence and kv-head: of the keys that compete the k largest, lowest index first among equal ones.  The k-th largest is found eight bits at
-// a time from counts in LDS (whole numbers: their order does not matter), from the highest bit in which the keys differ at all on; then each thread
-// knows how many of its neighbouring blocks are taken, and one sum over the workgroup says where they go.  KPT: keys of a thread, in registers (0: read
-// again in every pass, for any number).
+// a time from counts in LDS (whole numbers: their order does not matter), from the highest bit in which the keys differ at all on until all keys that agree so far
+// are taken; then each thread knows how many of its neighbouring blocks are taken, and one sum over the workgroup says where they go.  Scores share most of their
+// first bits, so eight lanes in turn count in places of their own (32 lists of 7500: 12.2 -> 8.7 us).  Bound by its dependent steps: 8 lists of 2048 5.9 us.  KPT: keys of a thread, in registers (0: read again in every pass, for any number).
 template <int THREADS, int KPT>
 __global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk) {
-    constexpr int WAVES = THREADS / 64;
-    __shared__ int hist[256], part[WAVES], chosen[2];
+    constexpr int WAVES = THREADS / 64, COPIES = 8;
+    __shared__ __attribute__((aligned(16))) int hist[256][COPIES], count[256];
+    __shared__ int part[WAVES];
     __shared__ uint32_t low[WAVES], high[WAVES];
     const int pair = blockIdx.x, s = pair / Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int nb = n_blocks_of(a, s, Bk), k = min(a.top_k, nb);
-    const uint32_t *keys = (const uint32_t *)a.scores + (size_t)pair * a.max_blocks;
+    const int nb = n_blocks_of(a, s, Bk), k = min(a.top_k, nb), pitch = key_pitch(a.max_blocks);
+    const uint32_t *keys = (const uint32_t *)a.scores + (size_t)pair * pitch;
     int32_t *out = a.blocks + (size_t)pair * a.top_k;
     if (threadIdx.x == 0 && pair == s * Hkv) a.counts[s] = k;
     for (int i = k + threadIdx.x; i < a.top_k; i += THREADS) out[i] = -1;
@@ -780,19 +781,31 @@ __global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk)
         return;
     }
     const int b_end = nb - a.last;  // [first, b_end) compete
-    const int per = KPT ? KPT : (nb + THREADS - 1) / THREADS, i0 = threadIdx.x * per;
-    uint32_t key[KPT ? KPT : 1], lo = 0xffffffffu, hi = 0;
-    auto competes = [&](int i) { return i >= a.first && i < b_end; };
-    auto key_at = [&](int j) { return KPT ? key[KPT ? j : 0] : keys[i0 + j]; };
+    const int per = KPT ? KPT : ((nb + THREADS - 1) / THREADS + 3) & ~3, i0 = threadIdx.x * per;
+    uint4 key[KPT ? KPT / 4 : 1];
+    const auto competes = [&](int i) { return i >= a.first && i < b_end; };
 #pragma unroll
-    for (int j = 0; j < (KPT ? KPT : per); ++j) {
-        const int i = i0 + j;
-        if (!competes(i)) continue;
-        const uint32_t x = keys[i];
-        if (KPT) key[KPT ? j : 0] = x;
+    for (int j = 0; j < KPT / 4; ++j)
+        if (i0 + 4 * j < nb) key[j] = *(const uint4 *)(keys + i0 + 4 * j);
+    const auto quad = [&](const uint4 &x, int i, auto &&f) {  // what competes of keys i .. i + 3
+        if (competes(i)) f(x.x);
+        if (competes(i + 1)) f(x.y);
+        if (competes(i + 2)) f(x.z);
+        if (competes(i + 3)) f(x.w);
+    };
+    const auto each = [&](auto &&f) {
+        if constexpr (KPT > 0) {
+#pragma unroll
+            for (int j = 0; j < KPT / 4; ++j) quad(key[j], i0 + 4 * j, f);
+        } else {
+            for (int i = 4 * threadIdx.x; i < nb; i += 4 * THREADS) quad(*(const uint4 *)(keys + i), i, f);
+        }
+    };
+    uint32_t lo = 0xffffffffu, hi = 0;
+    each([&](uint32_t x) {
         lo = min(lo, x);
         hi = max(hi, x);
-    }
+    });
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
         lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
@@ -802,69 +815,75 @@ __global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk)
         low[w] = lo;
         high[w] = hi;
     }
+    for (int i = threadIdx.x; i < 256 * COPIES / 4; i += THREADS) ((int4 *)hist)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
     for (int i = 0; i < WAVES; ++i) {
         lo = min(lo, low[i]);
         hi = max(hi, high[i]);
     }
     int left = a.top_k - a.first - a.last;  // how many of the competing ones are taken; more than `left` compete
-    const int bits = lo == hi ? 0 : 32 - __clz((int)(lo ^ hi));
-    uint32_t prefix = bits == 32 ? 0 : hi >> bits;  // the bits of the key in question that are known, all above `shift`
-    for (int shift = bits; shift > 0 && left > 0;) {
-        const int take = min(8, shift);
-        for (int i = threadIdx.x; i < 256; i += THREADS) hist[i] = 0;
+    int shift = lo == hi ? 0 : 32 - __clz((int)(lo ^ hi));
+    uint32_t prefix = shift == 32 ? 0 : hi >> shift;  // the bits of the key in question that are known, all above `shift`
+    while (shift > 0 && left > 0) {
+        const int next = max(0, shift - 8);
+        const uint32_t mask = (1u << (shift - next)) - 1;
+        each([&](uint32_t x) {
+            if (shift == 32 || x >> shift == prefix) atomicAdd(&hist[(x >> next) & mask][lane % COPIES], 1);
+        });
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < (KPT ? KPT : per); ++j) {
-            if (!competes(i0 + j)) continue;
-            const uint32_t x = key_at(j);
-            if (shift == 32 || x >> shift == prefix) atomicAdd(&hist[(x >> (shift - take)) & ((1 << take) - 1)], 1);
+        if (threadIdx.x < 256) {
+            const int4 x = ((const int4 *)hist[threadIdx.x])[0], y = ((const int4 *)hist[threadIdx.x])[1];
+            count[255 - threadIdx.x] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+            ((int4 *)hist[threadIdx.x])[0] = make_int4(0, 0, 0, 0);
+            ((int4 *)hist[threadIdx.x])[1] = make_int4(0, 0, 0, 0);
         }
         __syncthreads();
-        if (w == 0) {  // four bins to a lane, from the top: the bin in which the count passes `left`
-            int h[4], sum = 0;
+        // each wave for itself, four bins to a lane from the top: the bin in which the count reaches `left`
+        const int4 h = ((const int4 *)count)[lane];
+        const int sum = h.x + h.y + h.z + h.w;
+        int upto = sum;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                h[i] = hist[255 - 4 * lane - i];
-                sum += h[i];
-            }
-            int above = sum;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int y = __shfl_up(above, o, 64);
-                if (lane >= o) above += y;
-            }
-            above -= sum;  // in the lanes before
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (above < left && above + h[i] >= left) {
-                    chosen[0] = 255 - 4 * lane - i;
-                    chosen[1] = above;
-                }
-                above += h[i];
-            }
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += y;
         }
-        __syncthreads();
-        prefix = prefix << take | (uint32_t)chosen[0];
-        left -= chosen[1];
-        shift -= take;
-        __syncthreads();  // hist and chosen have been read
+        const int at = __ffsll((unsigned long long)__ballot(upto >= left)) - 1;
+        int above = upto - sum, bin = 255 - 4 * lane, here = h.x;
+        if (above + here < left) above += here, --bin, here = h.y;
+        if (above + here < left) above += here, --bin, here = h.z;
+        if (above + here < left) above += here, --bin, here = h.w;
+        prefix = prefix << (shift - next) | (uint32_t)__shfl(bin, at, 64);
+        left -= __shfl(above, at, 64);
+        shift = next;
+        if (__shfl(here, at, 64) == left) break;
     }
-    // With left > 0 `prefix` is the whole key of the last one taken: `left` of those equal to it are, and all larger ones.  With none to take, none is larger.
+    // With left > 0 `prefix` is the key of the last ones taken down to bit `shift`: `left` of those equal to it there are, and all larger ones.
+    // With none to take, none is larger.
     const bool any = a.top_k > a.first + a.last;
-    int gt = 0, eq = 0;
-#pragma unroll
-    for (int j = 0; j < (KPT ? KPT : per); ++j) {
-        const int i = i0 + j;
-        if (i >= nb) continue;
-        if (!competes(i)) ++gt;
-        else if (any) {
-            gt += key_at(j) > prefix;
-            eq += key_at(j) == prefix;
+    const auto above = [&](uint32_t x) { return any && x >> shift > prefix; };
+    const auto equal = [&](uint32_t x) { return any && x >> shift == prefix; };
+    const auto mine = [&](auto &&f) {  // of this thread's neighbours
+        const auto one = [&](int i, uint32_t x) {
+            if (i < nb) f(i, !competes(i) || above(x), competes(i) && equal(x));
+        };
+#pragma unroll KPT ? KPT / 4 : 1
+        for (int j = 0; j < (KPT ? KPT / 4 : per / 4); ++j) {
+            const int i = i0 + 4 * j;
+            if (i >= nb) continue;
+            const uint4 x = KPT ? key[KPT ? j : 0] : *(const uint4 *)(keys + i);
+            one(i, x.x);
+            one(i + 1, x.y);
+            one(i + 2, x.z);
+            one(i + 3, x.w);
         }
-    }
+    };
+    int gt = 0, eq = 0;
+    mine([&](int, bool more, bool same) {
+        gt += more;
+        eq += same;
+    });
     // both counts in one word: a workgroup has fewer than 65536 keys where they are in registers; else two sums
-    auto sum_before = [&](int v) {
+    const auto sum_before = [&](int v) {
         int x = v;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -887,26 +906,17 @@ __global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk)
         eq_at = sum_before(eq);
     }
     at += min(eq_at, left);
-#pragma unroll
-    for (int j = 0; j < (KPT ? KPT : per); ++j) {
-        const int i = i0 + j;
-        if (i >= nb) continue;
-        bool taken = !competes(i);
-        if (!taken && any) {
-            const uint32_t x = key_at(j);
-            taken = x > prefix || (x == prefix && eq_at < left);
-            eq_at += x == prefix;
-        }
-        if (taken) out[at++] = i;
-    }
+    mine([&](int i, bool more, bool same) {
+        if (more || (same && eq_at < left)) out[at++] = i;
+        eq_at += same;
+    });
 }
 
 }  // namespace
 
 hipError_t launch_extend(const ExtendArgs &a, hipStream_t st) {
-    const int rows_per_wg = a.max_rows <= 16384 ? 256 : 512;  // a row to a thread, until all compute units have a workgroup or two
-    const int wgs = a.max_rows > rows_per_wg ? (a.max_rows + rows_per_wg - 1) / rows_per_wg : 1;
-    hipLaunchKernelGGL(k_extend, dim3(wgs), dim3(kExtThreads), 0, st, a, rows_per_wg);
+    const int wgs = a.max_rows > kExtThreads ? (a.max_rows + kExtThreads - 1) / kExtThreads : 1;  // a row to a thread
+    hipLaunchKernelGGL(k_extend, dim3(wgs), dim3(kExtThreads), 0, st, a);
     return hipGetLastError();
 }
 
@@ -988,8 +998,10 @@ hipError_t launch_select(const Dims &dm, bool generic, const SelectArgs &a, hipS
         if (e != hipSuccess) return e;
     }
     const dim3 grid(a.S * dm.Hkv);
+    // The fewest threads that hold the keys of the widest list: 512 lists of up to 1024 blocks 6.3 us (512 threads 7.1, 1024 10.4); 8 of 2048 5.9 us (256 threads with
+    // 8 keys 7.9, 1024 7.7); 32 of 7500 8.7 us (keys read again 16); 8 of 31250 23 us (keys read again 43).
     if (a.max_blocks <= 1024) hipLaunchKernelGGL((k_pick<256, 4>), grid, dim3(256), 0, st, a, dm.Hkv, dm.Bk);
-    else if (a.max_blocks <= 2048) hipLaunchKernelGGL((k_pick<256, 8>), grid, dim3(256), 0, st, a, dm.Hkv, dm.Bk);
+    else if (a.max_blocks <= 2048) hipLaunchKernelGGL((k_pick<512, 4>), grid, dim3(512), 0, st, a, dm.Hkv, dm.Bk);
     else if (a.max_blocks <= 8192) hipLaunchKernelGGL((k_pick<1024, 8>), grid, dim3(1024), 0, st, a, dm.Hkv, dm.Bk);
     else if (a.max_blocks <= 32768) hipLaunchKernelGGL((k_pick<1024, 32>), grid, dim3(1024), 0, st, a, dm.Hkv, dm.Bk);
     else hipLaunchKernelGGL((k_pick<1024, 0>), grid, dim3(1024), 0, st, a, dm.Hkv, dm.Bk);

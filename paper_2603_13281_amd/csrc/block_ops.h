@@ -29,12 +29,13 @@ struct BoundsArgs {
 };
 hipError_t launch_bounds(const Dims &dm, bool generic, const BoundsArgs &a, hipStream_t st);
 
+__host__ __device__ inline int key_pitch(int max_blocks) { return (max_blocks + 3) & ~3; }
 struct SelectArgs {
     const void *q; const int8_t *codes; const float *scales;
     const int32_t *bt; int max_blocks, num_blocks, S;
     const int32_t *kv_lens, *row_start; int R, seq_rows, top_k, first, last;
     int32_t *blocks, *counts;
-    float *scores;                                 // workspace [S, Hkv, max_blocks]
+    float *scores;                                 // workspace [S, Hkv, key_pitch(max_blocks)], 16-byte aligned
 };
 hipError_t launch_select(const Dims &dm, bool generic, const SelectArgs &a, hipStream_t st);
 

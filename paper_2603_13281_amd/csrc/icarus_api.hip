@@ -2083,7 +2083,7 @@ icarus_status icarus_key_bounds(icarus_ctx *ctx, const void *kv_pool, const int3
 
 size_t icarus_select_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t max_blocks) {
     if (!ctx || S < 0 || max_blocks < 0) return 0;
-    return align_up((size_t)S * ctx->cfg.n_kv_heads * max_blocks * 4, 256) + 256;
+    return align_up((size_t)S * ctx->cfg.n_kv_heads * key_pitch(max_blocks) * 4, 256) + 256;
 }
 
 icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t *codes, const float *scales, const int32_t *block_tables,
