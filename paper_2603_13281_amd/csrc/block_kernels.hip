@@ -14,6 +14,7 @@ namespace {
 // Two sums over the sequences decide everything: rows before a sequence, and blocks taken before it.  Every workgroup
 // forms both over all sequences (8-12 bytes each, from L2) and writes its own range of rows, so that one launch does and no
 // workgroup waits for another.  Sums saturate just past the largest value that is told apart (max_rows, n_free), so that no length overflows them.
+// Bound by its chain of reads, sums and barriers: 64 sequences, 374 rows 5.3 us; 256 sequences, 62208 rows 6.2 us (two rows to a thread 7.1, four 8.8).
 constexpr int kExtThreads = 256, kExtPer = 4, kExtSeg = kExtThreads * kExtPer;  // sequences of a round
 
 __host__ __device__ __forceinline__ int blocks_of(int tokens, int Bk) { return tokens / Bk + (tokens % Bk != 0); }
@@ -163,7 +164,8 @@ __device__ __forceinline__ double turns_per_position(int i, int D, double log2_t
     return exp2(-(2.0 * (double)i / (double)D) * log2_theta) * 0.15915494309189533577;
 }
 
-// Any head size: a wave to a head of a row, a pair to a lane.
+// Any head size and block size, rows at any distance: a wave to a head of a row, a pair to a lane, V written element by element (16384 rows of 48 heads of 128,
+// 402 MB: 339 us; 356 rows of them 7.9 us).
 template <typename T, typename KT>
 __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, int D, int Bk, double log2_theta, float eps, int qk_norm,
                                                 float k_scale, float v_scale) {
@@ -215,6 +217,7 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, i
 // V goes into the pool transposed: a run of rows that are consecutive places of one block is put together in LDS and written as one row of the block per
 // channel, 32 bytes at once where the run fills the block.  A run belongs to the window in which it starts, wherever it ends, so that prompts which begin
 // inside a block are written in whole blocks too.
+// 16384 rows of 48 heads of 128 (402 MB): 96 us, 4.2 TB/s (339 us a wave to a head); 1145 rows of 80 heads into an FP8 cache (44 MB): 18 us (46); 356 rows: 7 us (7.9).
 template <typename KT> __device__ __forceinline__ void put4(KT *p, const float (&v)[4], float scale);
 template <> __device__ __forceinline__ void put4(bf16_t *p, const float (&v)[4], float) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
 template <> __device__ __forceinline__ void put4(float *p, const float (&v)[4], float) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
@@ -385,7 +388,7 @@ __device__ __forceinline__ float finite_or_edge(float x) {
 __device__ __forceinline__ int8_t code_of(float rounded) { return (int8_t)(int)fminf(fmaxf(rounded, -127.f), 127.f); }
 template <typename KT> __device__ __forceinline__ float key_value(const KT *p) { return finite_or_edge(KVElem<KT>::ld(p, 1.f)); }
 
-// Any shape: a wave to a block and kv-head, a channel to a lane.
+// Any shape: a wave to a block and kv-head, a channel to a lane (16384 blocks of 8 heads of 128, 571 MB: 338 us).
 template <typename KT>
 __global__ void __launch_bounds__(256) k_bounds(BoundsArgs a, int Hkv, int D, int Bk) {
     const int s = blockIdx.x, c = blockIdx.z * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -421,7 +424,7 @@ __global__ void __launch_bounds__(256) k_bounds(BoundsArgs a, int Hkv, int D, in
 // Blocks of 16, head sizes 64, 128 and 256: a wave to the keys of a block and kv-head, which it reads as they lie, four channels of a token to a lane; a lane sees 4 to 16 of
 // the tokens, and lanes of the same channels meet by exchanges in registers.  Bound by HBM (half of a block's lines), with the vector units close behind: with
 // 16 bytes to a lane there were twice the exchanges and the reads waited for them.  bfloat16 pairs stay pairs: as whole numbers of 16 bits whose order is that of the values two
-// are compared at a time.
+// are compared at a time.  16384 blocks of 8 heads of 128 (537 MB of keys, 4 KB of every 8 KB, and 34 MB out): 121 us, 4.7 TB/s (16 bytes to a lane: 129).
 typedef short s16x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ s16x2_t ordered(uint32_t u) {  // two bfloat16 -> whole numbers in their order; its own inverse
     const s16x2_t x = __builtin_bit_cast(s16x2_t, u);
@@ -709,7 +712,8 @@ __global__ void __launch_bounds__(256, KS <= 4 ? 5 : 1) k_scores_mfma(SelectArgs
     }
 }
 
-// Any even head size: a thread to a block, the queries of a batch in LDS as codes [queries][2 D / 4 words], the positive parts before the negative ones.
+// Any even head size: a thread to a block, the queries of a batch in LDS as codes [queries][2 D / 4 words], the positive parts before the negative ones
+// (64 sequences as above: 114 us).
 constexpr int kScoreBatch = 16;
 template <typename T>
 __global__ void __launch_bounds__(256) k_scores(SelectArgs a, int Hq, int Hkv, int D, int Bk) {
@@ -763,7 +767,8 @@ __global__ void __launch_bounds__(256) k_scores(SelectArgs a, int Hq, int Hkv, i
 // The choice of a sequence and kv-head: of the keys that compete the k largest, lowest index first among equal ones.  The k-th largest is found eight bits at
 // a time from counts in LDS (whole numbers: their order does not matter), from the highest bit in which the keys differ at all on until all keys that agree so far
 // are taken; then each thread knows how many of its neighbouring blocks are taken, and one sum over the workgroup says where they go.  Scores share most of their
-// first bits, so eight lanes in turn count in places of their own (32 lists of 7500: 12.2 -> 8.7 us).  Bound by its dependent steps: 8 lists of 2048 5.9 us.  KPT: keys of a thread, in registers (0: read again in every pass, for any number).
+// first bits, so eight lanes in turn count in places of their own (32 lists of 7500: 12.2 -> 8.7 us).  Bound by its dependent steps: 8 lists of 2048 5.9 us.
+// KPT: keys of a thread, in registers (0: read again in every pass, for any number).
 template <int THREADS, int KPT>
 __global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk) {
     constexpr int WAVES = THREADS / 64, COPIES = 8;
@@ -924,7 +929,8 @@ template <typename T, typename KT>
 static bool append_window(const Dims &dm, const AppendArgs &a, hipStream_t st) {
     if (dm.Bk != 16 || a.ld * (int64_t)sizeof(T) % 16) return false;
     const int windows = (a.R + kWindow - 1) / kWindow;
-    int parts = 1;  // of the heads: eight workgroups to a CU, as long as a part has a rotated head for every wave's turn
+    // of the heads: eight workgroups to a CU, as long as a part has a rotated head for every wave's turn (1145 rows of 80 heads: 18 us; two to a CU 20)
+    int parts = 1;
     while (windows * parts < 2048 && 2 * parts <= (dm.Hq + dm.Hkv + 3) / 4) parts *= 2;
     const dim3 grid(windows, parts);
     const double l2t = log2(dm.theta);
@@ -964,7 +970,7 @@ static bool bounds_wave(const Dims &dm, const BoundsArgs &a, dim3 grid, hipStrea
 
 hipError_t launch_bounds(const Dims &dm, bool generic, const BoundsArgs &a, hipStream_t st) {
     const int64_t most = a.max_new > 0 ? std::min<int64_t>(a.max_blocks, (a.max_new - 1) / dm.Bk + 2) : a.max_blocks;  // blocks of a sequence, about
-    // workgroups to a sequence: a block to each, until there are 16 to a CU; what is left goes round
+    // workgroups to a sequence: a block to each, until there are 16 to a CU; what is left goes round (4 to a CU: 124 us for the above, 32: 119)
     const int per_seq = (int)std::min<int64_t>(most, std::max<int64_t>(1, (kBoundsWgs + a.S - 1) / a.S));
     bool done = false;
     if (!generic) DISPATCH_TK(dm.bf16, dm.kv8, { (void)sizeof(T); done = bounds_wave<KT>(dm, a, dim3(a.S, per_seq), st); });
