@@ -21,7 +21,7 @@ def _refused(layer, rc, status):
 
 def test_extend_refusals():
     layer, call = _layer(), binding._lib.icarus_extend_sequences
-    good = dict(S=4, ctx=A, new=A + 64, streams=None, bt=A + 256, mb=8, free=A + 512, nf=10, used=A + 1024, rows=16, kv=A + 2048, start=A + 3072 + 64,
+    good = dict(S=4, ctx=A, new=A + 64, streams=None, bt=A + 256, mb=8, free=A + 512, nf=10, used=A + 1024, rows=16, kv=A + 2048, start=A + 3136,
                 seq=A + 4096, pos=A + 5120, slot=A + 6144, counts=A + 7168)
 
     def run(status, **kw):
