@@ -18,6 +18,9 @@
  * memory may overlap; a workspace belongs to one call at a time.
  * Pointers: float and code arrays, pool and workspace 16-byte aligned; integer arrays and scales aligned to their element.
  *
+ * A call takes up to 65535 sequences (icarus_extend_sequences: 2^29), 2^29 rows, 2^30 queries of a kv-head, 2^22 blocks of a sequence and in the
+ * lists of icarus_attn_blocks 2^20 parts of 256 entries over sequences and kv-heads; more is ICARUS_ERR_UNSUPPORTED.
+ *
  * What the device finds out of range is not followed: a block id outside the pool, a position beyond the table, a slot outside
  * the pool or a negative length are skipped as each call says.  Results never depend on max_new and seq_rows, which
  * only size a launch.
@@ -57,7 +60,7 @@ icarus_status icarus_extend_sequences(icarus_ctx *ctx, int32_t S, const int32_t 
 /* Row r of qkv holds the projections of one token: Hq query, Hkv key, Hkv value heads.  Query and key heads go through
  * RMSNorm (qk_norm) and are rotated to position row_pos[r]; q_out [R, Hq, D] receives the queries, the pool K and V at slot
  * row_slot[r].  Rows with a negative position are left out, q_out with them; with a slot outside the pool only the append
- * is left out and the row's K and V are not read.  Slots that are not named keep every byte.  A slot named twice holds the K and V of either row.
+ * is left out and the row's K and V are not read.  Slots that are not named keep every byte.  Of a slot that is named twice each element is one of its rows'.
  *   qkv                 device, dtype elements, rows ld elements apart (ld >= (Hq + 2 Hkv) * D)
  *   row_pos, row_slot   device int32, int64 [R] */
 icarus_status icarus_rope_append(icarus_ctx *ctx, const void *qkv, int64_t ld, int32_t R, const int32_t *row_pos,

@@ -747,6 +747,8 @@ class IcarusLayer:
         top_k = self._lists(blocks, counts, S, index)
         if workspace is None:
             workspace = torch.empty(_lib.icarus_select_workspace_bytes(self._h, S, max_blocks), dtype=torch.uint8, device=q.device)
+        elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace: need a contiguous tensor on the device of the others")
         self._check(_launch(index, _lib.icarus_select_blocks, self._h, q.data_ptr(), codes.data_ptr(), scales.data_ptr(), block_tables.data_ptr(), max_blocks,
                             S, kv_lens.data_ptr(), R, row_start.data_ptr(), seq_rows, top_k, first, last, blocks.data_ptr(), counts.data_ptr(),
                             workspace.data_ptr(), workspace.nbytes))
@@ -768,6 +770,8 @@ class IcarusLayer:
             raise ValueError(f"out has {out.shape[0]} rows, q {R}")
         if workspace is None:
             workspace = torch.empty(_lib.icarus_attn_blocks_workspace_bytes(self._h, S, R, width), dtype=torch.uint8, device=q.device)
+        elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace: need a contiguous tensor on the device of the others")
         self._check(_launch(index, _lib.icarus_attn_blocks, self._h, q.data_ptr(), kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S,
                             kv_lens.data_ptr(), R, row_start.data_ptr(), seq_rows, blocks.data_ptr(), counts.data_ptr(), width, out.data_ptr(),
                             workspace.data_ptr(), workspace.nbytes))

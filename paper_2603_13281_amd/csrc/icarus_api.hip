@@ -2015,6 +2015,7 @@ bool overlap(const void *a, size_t an, const void *b, size_t bn) {
 }
 constexpr int kBlockMaxSeqs = 65535, kBlockMaxRows = 1 << 29;  // sums of two counts stay in 32 bits
 constexpr int kBlockMaxTable = 1 << 22;                        // blocks of a sequence, entries of a list
+bool too_many_queries(const icarus_ctx *ctx, int R) { return (int64_t)R * (ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads) > 1 << 30; }  // counted in 32 bits
 }  // namespace
 
 icarus_status icarus_extend_sequences(icarus_ctx *ctx, int32_t S, const int32_t *ctx_lens, const int32_t *new_lens, const int32_t *streams,
@@ -2097,6 +2098,7 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "top_k %d must be positive and hold the first %d and the last %d blocks", top_k, first, last);
     if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_blocks > kBlockMaxTable || top_k > kBlockMaxTable)
         return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences, %d rows and %d blocks of a sequence per call", kBlockMaxSeqs, kBlockMaxRows, kBlockMaxTable);
+    if (too_many_queries(ctx, R)) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d rows: at most 2^30 queries of a kv-head per call", R);
     if (S == 0) return ICARUS_OK;
     if (any_null({codes, scales, kv_lens, row_start, blocks, counts, workspace}) || (max_blocks && !block_tables) || (R && !q))
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
@@ -2127,6 +2129,7 @@ icarus_status icarus_attn_blocks(icarus_ctx *ctx, const void *q, const void *kv_
     if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_selected > kBlockMaxTable || (int64_t)S * c.n_kv_heads * (max_selected / 256 + 1) > 1 << 20)
         return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d sequences, %d kv-heads, %d rows, lists of %d blocks: at most %d sequences and %d rows per call, and 2^20 times 256 entries in all lists",
                     S, c.n_kv_heads, R, max_selected, kBlockMaxSeqs, kBlockMaxRows);
+    if (too_many_queries(ctx, R)) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d rows: at most 2^30 queries of a kv-head per call", R);
     if (S == 0 || R == 0) return ICARUS_OK;
     if (any_null({q, kv_pool, kv_lens, row_start, counts, out, workspace}) || (max_blocks && !block_tables) || (max_selected && !blocks))
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");

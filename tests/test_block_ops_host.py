@@ -102,6 +102,7 @@ def test_select_and_attend_refusals():
         run("ALIGNMENT", **{name: A + 2})
     run("CAPACITY", wsb=lib.icarus_select_workspace_bytes(layer._h, 2, 8) - 1)
     run("UNSUPPORTED", mb=(1 << 22) + 1)
+    run("UNSUPPORTED", R=1 << 29)                 # rows x heads of a kv-head beyond 2^30
     good = dict(q=A, pool=A, bt=A, mb=8, S=2, kv=A, R=3, start=A, hint=0, blocks=A, counts=A, k=4, out=A + (1 << 20), ws=A, wsb=1 << 30)
 
     def run(status, **kw):  # noqa: F811
@@ -119,6 +120,7 @@ def test_select_and_attend_refusals():
     run("CAPACITY", wsb=lib.icarus_attn_blocks_workspace_bytes(layer._h, 2, 3, 4) - 1)
     run("INVALID_ARG", out=good["q"] + 2 * 3 * 8 * 64 - 16)
     run("UNSUPPORTED", S=60000, k=100000)
+    run("UNSUPPORTED", R=1 << 29)
     layer.close()
 
 

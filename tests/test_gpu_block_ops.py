@@ -573,6 +573,21 @@ def test_integer_arrays_need_only_their_own_alignment():
 
 # ---- together -------------------------------------------------------------------------------------------------------------------
 
+def test_workspaces_elsewhere_are_refused():
+    layer = make(num_blocks=8)
+    q, pool, table = torch.zeros(1, 8, 128, dtype=torch.bfloat16, device=DEV), random_pool(layer, np.random.default_rng(0)), i32([[0, 1]])
+    codes, scales = layer.new_key_bounds(DEV)
+    blocks, counts = torch.zeros(1, 2, 3, dtype=torch.int32, device=DEV), i32([0])
+    for ws in (torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(1 << 20, 2, dtype=torch.uint8, device=DEV)[:, 0], 5):
+        with pytest.raises(ValueError):
+            layer.select_blocks(q, codes, scales, table, i32([20]), i32([0, 1]), blocks, counts, workspace=ws)
+        with pytest.raises(ValueError):
+            layer.attn_blocks(q, pool, table, i32([20]), i32([0, 1]), blocks, counts, workspace=ws)
+    with pytest.raises(binding.IcarusError):
+        layer.attn_blocks(q, pool, table, i32([20]), i32([0, 1]), blocks, counts, workspace=torch.zeros(16, dtype=torch.uint8, device=DEV))
+    layer.close()
+
+
 def test_a_step_is_the_layers_attention():
     """Growth, append, bounds, choice of all blocks, attention over them: what icarus_attn_shared_kv gives on the same cache."""
     for kw in (dict(Hq=8, Hkv=2), dict(Hq=8, Hkv=2, fp8=True, k_scale=0.02, v_scale=0.02), dict(Hq=4, Hkv=4, D=64, bf16=False)):
