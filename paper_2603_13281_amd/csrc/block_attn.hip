@@ -10,7 +10,7 @@ namespace icarus {
 namespace {
 
 // Any shape: a workgroup to a query head of a row; a thread to a position for the scores, to a channel for the sum of the values.
-// Running maximum and sum in float32, rounds of kChunk positions.  Right for every block and head size, and slow: 64 sequences, 1-8 agents, 64 blocks 13.6 ms.
+// Running maximum and sum in float32, rounds of kChunk positions.  Right for every block and head size, and slow: see k_block_attn_f32.
 constexpr int kChunk = 512;
 template <typename T, typename KT>
 __global__ void __launch_bounds__(256) k_block_attn_generic(BlockAttnArgs a, int Hq, int Hkv, int D, int Bk, float scale, float k_scale, float v_scale) {
@@ -90,7 +90,7 @@ struct SplitOut {
     float *o;    // [splits][R][Hq][D]
     float2 *ml;  // [splits][R][Hq]: maximum in log2 units, sum
     int splits;  // 1: the output itself is written
-    int per;     // list entries of a split, even
+    int per;     // list entries of a split, even on the 128 kernel
     int tiles, tile_groups, n_items;  // tiles of an item, items to the rows of the call's largest sequence
 };
 
@@ -441,38 +441,39 @@ __global__ void __launch_bounds__(256) k_block_attn(BlockAttnArgs a, SplitOut pa
 
 bool on_matrix_cores(const Dims &dm) { return dm.bf16 && dm.D == kD && dm.Bk == kBk; }
 
-// ---- blocks of 16, head sizes that are multiples of 16: matrix cores in float32 ----------------------------------------------
-// For float32 and head sizes other than 128.  A workgroup takes a sequence, kv-head, range of the list and a tile of 16 stacked queries; a wave takes
-// blocks in turn (with the next one on its way: no faster).  Products of 16 x 16 x 4 with the transposed operands: scores are keys [token][channel] times
+// ---- block and head sizes that are multiples of 16: matrix cores in float32 ------------------------------------------------------
+// For float32, head sizes other than 128 and blocks of more than 16 tokens.  A workgroup takes a sequence, kv-head, range of the list and a tile of 16 stacked queries; a wave takes
+// sixteen tokens of a block in turn (with the next ones on their way: no faster).  Products of 16 x 16 x 4 with the transposed operands: scores are keys [token][channel] times
 // queries [channel][query], which leaves lane t + 16 p query t's scores of tokens 4 p .. 4 p + 3, and these are at once the right operand of the values'
 // product [channel][token] x [token][query], whose left operand is a row piece of the transposed block.  So nothing passes through LDS until the waves join, and
 // a query's reference, sum and sums of values lie in its own four lanes.  float32, 4 heads of 64, 25 sequences x 9 rows x up to 190 blocks (147 MB): 29 us, 5.1 TB/s;
 // the same on the vector units with the queries in LDS took 76 us, bound by LDS.  Rows beyond 16 / g read the blocks again, from the caches: float32, 8 heads of 128 for
 // 32 queries, 32 x up to 9 rows x 64 blocks (268 MB) 85 us; two tiles of queries to a workgroup halve the reads and took 121 us, for want of waves.  bfloat16 keys and
-// values become float32 here: 8 heads of 64 (134 MB) 61 us, bound by the products, a sixteenth of the rate of 16-bit ones.
+// values become float32 here: 8 heads of 64 (134 MB) 63 us, bound by the products, a sixteenth of the rate of 16-bit ones; blocks of 64 tokens, 64 sequences of 4 rows
+// x 32 heads over 1024 tokens of 8 heads of 128 (268 MB) 77 us, in blocks of 16 (k_block_attn) 45, a thread to a position (below 16 tokens or with odd sizes) 13.9 ms.
 template <typename T, typename KT, int DT, bool EXACT>  // tiles of 16 channels: at most DT, or DT exactly
-__global__ void __launch_bounds__(256) k_block_attn_f32(BlockAttnArgs a, SplitOut part, int Hq, int Hkv, int D_, float scale_log2, float v_scale) {
-    constexpr int Bk = 16;
+__global__ void __launch_bounds__(256) k_block_attn_f32(BlockAttnArgs a, SplitOut part, int Hq, int Hkv, int D_, int Bk, float scale_log2, float v_scale) {
     typedef typename Quad<KT>::raw Raw;
     __shared__ f32x4 image[2][DT][64];
+    __shared__ int2 ids[kItemBlocks];  // of the list's entries: block of the pool, and its tokens
     __shared__ float image_m[4][16], image_l[4][16];
     const int D = EXACT ? 16 * DT : D_, d16 = D / 16;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, p4 = 4 * (lane >> 4), g = Hq / Hkv;
     const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, split = blockIdx.y;
     const int row0 = min(max(a.row_start[s], 0), a.R), G = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
     const int len = max(a.kv_lens[s], 0), n_sel = min(max(a.counts[s], 0), a.max_selected);
-    const int e0 = split * part.per + w, e_end = min(n_sel, (split + 1) * part.per), some = max(0, e_end - e0 + 3) / 4;  // entries e0, e0 + 4, ..: at most 64
-    int my_id = 0, my_n = 0;  // block of entry e0 + 4 lane, and its tokens
-    if (lane < some) {
-        const int b = a.blocks[(size_t)pair * a.max_selected + e0 + 4 * lane];
+    const int e0 = split * part.per, entries = max(0, min(part.per, n_sel - e0));
+    const int parts = Bk / 16, units = entries * parts, step = 4 / parts, step_parts = 4 % parts;  // sixteen tokens of a block are a unit
+    if ((int)threadIdx.x < entries) {
+        int2 x = make_int2(0, 0);
+        const int b = a.blocks[(size_t)pair * a.max_selected + e0 + threadIdx.x];
         if (b >= 0 && b < a.max_blocks && (int64_t)b * Bk < len) {
             const int id = a.bt[(size_t)s * a.max_blocks + b];
-            if (id >= 0 && id < a.num_blocks) {
-                my_id = id;
-                my_n = min(Bk, len - b * Bk);
-            }
+            if (id >= 0 && id < a.num_blocks) x = make_int2(id, min(Bk, len - b * Bk));
         }
+        ids[threadIdx.x] = x;
     }
+    __syncthreads();
     for (int j0 = 16 * blockIdx.z; j0 < G; j0 += 16 * gridDim.z) {
         const int j = min(j0 + t, G - 1);
         const size_t at = (size_t)(row0 + j / g) * Hq + c * g + j % g;
@@ -484,16 +485,16 @@ __global__ void __launch_bounds__(256) k_block_attn_f32(BlockAttnArgs a, SplitOu
         float m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int x = 0; x < DT; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const auto add = [&](int id, int n) {
+        const auto add = [&](int id, int first, int n) {  // n of the block's tokens, from `first` on
             const KT *blk = (const KT *)a.pool + ((size_t)id * Hkv + c) * 2 * Bk * D;
-            const KT *kr = blk + min(t, n - 1) * D + p4, *vr = blk + Bk * D + t * Bk + p4;  // behind the last token: the last again
+            const KT *kr = blk + (first + min(t, n - 1)) * D + p4, *vr = blk + (D + t) * Bk + first + p4;  // behind the last token: the last again
             Raw k[DT], v[DT];
 #pragma unroll
             for (int x = 0; x < DT; ++x)
                 if (EXACT || x < d16) k[x] = *(const Raw *)(kr + 16 * x);
 #pragma unroll
             for (int x = 0; x < DT; ++x)
-                if (EXACT || x < d16) v[x] = *(const Raw *)(vr + 16 * Bk * x);
+                if (EXACT || x < d16) v[x] = *(const Raw *)(vr + (size_t)16 * Bk * x);
             f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int x = 0; x < DT; ++x) {
@@ -530,14 +531,18 @@ __global__ void __launch_bounds__(256) k_block_attn_f32(BlockAttnArgs a, SplitOu
                 Quad<KT>::get(v[x], vf);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    if (n < Bk) vf[u] = p4 + u < n ? vf[u] : 0.f;  // places behind the last token may hold anything
+                    if (n < 16) vf[u] = p4 + u < n ? vf[u] : 0.f;  // places behind the last token may hold anything
                     o[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[u], p[u], o[x], 0, 0, 0);
                 }
             }
         };
-        for (int i = 0; i < some; ++i) {
-            const int id = __builtin_amdgcn_readlane(my_id, i), n = __builtin_amdgcn_readlane(my_n, i);
-            if (n > 0) add(id, n);
+        int e = w / parts, part_of = w % parts;
+        for (int u = w; u < units; u += 4) {
+            const int id = __builtin_amdgcn_readfirstlane(ids[e].x), n = __builtin_amdgcn_readfirstlane(ids[e].y) - 16 * part_of;
+            if (n > 0) add(id, 16 * part_of, min(16, n));
+            e += step;
+            part_of += step_parts;
+            if (part_of >= parts) part_of -= parts, ++e;
         }
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
@@ -633,15 +638,17 @@ __global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitO
 }
 
 // Splits of the lists, at most `most`.  Items go over the workgroups that the chip holds in rounds (1 to a CU of the 128 kernel, 3 of the float32 one: with 4 its 25
-// sequences above took 33 us, with 8 35); a round costs the blocks of its items and as much as kItemCost blocks on top, joining kJoinCost.
+// sequences above took 33 us, with 8 35); a round costs the blocks of its items and as much as kItemCost blocks of 16 tokens on top, joining kJoinCost.
 constexpr int kWgs = 256, kItemCost = 12, kJoinCost = 24, kMaxSplits = 32, kMaxTileGroups = 64;
 int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxSplits) {
     const int least = (max_selected + kItemBlocks - 1) / kItemBlocks;
     const int64_t wgs = on_matrix_cores(dm) ? kWgs : 3 * kWgs;
     int best = 0;
     int64_t cost = 0;
-    for (int n = std::max(1, least); n <= std::max(least, std::min(most, (max_selected + 7) / 8)) || !best; ++n) {  // 8 blocks: a group to a wave
-        const int64_t rounds = (pairs * n + wgs - 1) / wgs, blocks = (max_selected + n - 1) / n;
+    const int parts = on_matrix_cores(dm) ? 1 : dm.Bk / 16;
+    const int limit = (int)std::min<int64_t>({most, max_selected, ((int64_t)max_selected * parts + 7) / 8});  // 8 times 16 tokens: a group of two or two units to a wave
+    for (int n = std::max(1, least); n <= std::max(least, limit) || !best; ++n) {
+        const int64_t rounds = (pairs * n + wgs - 1) / wgs, blocks = (int64_t)((max_selected + n - 1) / n) * parts;
         const int64_t t = rounds * (blocks + kItemCost) + (n > 1 ? kJoinCost : 0);
         if (!best || t < cost) {
             best = n;
@@ -673,7 +680,7 @@ hipError_t launch_mfma(const Dims &dm, const BlockAttnArgs &a, const SplitOut &p
 
 }  // namespace
 
-bool block_attn_fast(const Dims &dm) { return dm.Bk == kBk && dm.D % 16 == 0; }
+bool block_attn_fast(const Dims &dm) { return dm.Bk % 16 == 0 && dm.D % 16 == 0; }
 
 size_t block_attn_workspace(const Dims &dm, int S, int R, int max_selected) {
     if (!block_attn_fast(dm) || S == 0) return 256;
@@ -685,7 +692,7 @@ template <typename T, typename KT>
 static hipError_t launch_f32(const Dims &dm, const BlockAttnArgs &a, const SplitOut &part, hipStream_t st) {
     const dim3 grid(a.S * dm.Hkv, part.splits, part.tile_groups);
     const float scale_log2 = kLog2e / sqrtf((float)dm.D) * (sizeof(KT) == 1 ? dm.k_scale : 1.f), v_scale = sizeof(KT) == 1 ? dm.v_scale : 1.f;
-#define BLOCK_ATTN_F32(DT, EXACT) hipLaunchKernelGGL((k_block_attn_f32<T, KT, DT, EXACT>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, scale_log2, v_scale)
+#define BLOCK_ATTN_F32(DT, EXACT) hipLaunchKernelGGL((k_block_attn_f32<T, KT, DT, EXACT>), grid, dim3(256), 0, st, a, part, dm.Hq, dm.Hkv, dm.D, dm.Bk, scale_log2, v_scale)
     if (dm.D == 64) BLOCK_ATTN_F32(4, true);
     else if (dm.D == 128) BLOCK_ATTN_F32(8, true);
     else if (dm.D < 128) BLOCK_ATTN_F32(8, false);
@@ -706,7 +713,8 @@ hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *works
     while (mfma && part.tile_groups < std::min<int64_t>(tiles, 3) && pairs * (part.tile_groups + 1) * 8 <= kWgs) ++part.tile_groups;
     part.tiles = (int)std::min<int64_t>((tiles + part.tile_groups - 1) / part.tile_groups, 3);
     part.splits = splits_for(dm, pairs * part.tile_groups, a.max_selected, splits_for(dm, pairs, a.max_selected));  // no more than the workspace was sized for
-    part.per = std::max(2, ((a.max_selected + part.splits - 1) / part.splits + 1) & ~1);
+    part.per = (a.max_selected + part.splits - 1) / part.splits;
+    if (mfma) part.per = std::max(2, (part.per + 1) & ~1);
     part.o = (float *)workspace;
     part.ml = (float2 *)(part.o + (size_t)part.splits * a.R * dm.Hq * dm.D);
     part.n_items = (int)((pairs + 7) / 8 * 8 * part.splits * part.tile_groups);

@@ -45,7 +45,7 @@ struct BlockAttnArgs {
     const int32_t *blocks, *counts; int max_selected;
     void *out;
 };
-// Shapes that block_attn_fast names: matrix cores or vector units.  Workspace: 16-byte aligned, block_attn_workspace bytes.
+// Shapes that block_attn_fast names.  Workspace: 16-byte aligned, block_attn_workspace bytes.
 bool block_attn_fast(const Dims &dm);
 size_t block_attn_workspace(const Dims &dm, int S, int R, int max_selected);
 hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *workspace, hipStream_t st);

@@ -422,7 +422,8 @@ def run_attend(layer, q, pool, table, kv, row_start, blocks, counts, hint=0):
 
 ATTN = SHAPES + [dict(Hq=32, Hkv=8), dict(Hq=8, Hkv=8), dict(Hq=16, Hkv=2, fp8=True, k_scale=0.05, v_scale=0.03), dict(mode=1), dict(Hq=40, Hkv=2),
                dict(D=80), dict(D=128, bf16=False, fp8=True, v_scale=0.5), dict(D=112, bf16=False), dict(Hq=24, Hkv=1, D=96, fp8=True), dict(D=64, fp8=True, k_scale=2.0),
-               dict(D=240, fp8=True), dict(D=256), dict(D=256, bf16=False, fp8=True), dict(D=208, bf16=False), dict(Hq=34, Hkv=2, D=48, bf16=False, fp8=True)]
+               dict(D=240, fp8=True), dict(D=256), dict(D=256, bf16=False, fp8=True), dict(D=208, bf16=False), dict(Hq=34, Hkv=2, D=48, bf16=False, fp8=True),
+               dict(bk=32), dict(bk=48, fp8=True, k_scale=0.3), dict(bk=64, bf16=False), dict(bk=128, D=64), dict(bk=80, D=48, fp8=True, bf16=False)]
 
 
 @pytest.mark.parametrize("kw", ATTN, ids=str)
