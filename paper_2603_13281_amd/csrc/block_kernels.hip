@@ -629,86 +629,111 @@ __device__ __forceinline__ void quantise4(const float *v, float inv, int *up, in
     *up = (int)__builtin_amdgcn_perm(u1, u0, 0x06040200);  // bytes 0 and 2 of both words
     *down = (int)__builtin_amdgcn_perm(d1, d0, 0x06040200);
 }
+// A sequence's queries of one kv-head: n of them, query j in row row0 + j / g, head c * g + j % g.
+template <typename T> struct Stack {
+    const T *q;
+    int row0, n, g, c, Hq;
+    __device__ __forceinline__ Stack(const SelectArgs &a, int s, int c_, int Hq_, int Hkv) : q((const T *)a.q), g(Hq_ / Hkv), c(c_), Hq(Hq_) {
+        row0 = min(max(a.row_start[s], 0), a.R);
+        n = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
+    }
+};
+// Queries j0 .. j0 + 15 (behind the last: the last again) as rows of the products: rows[step][lane], steps[query].
+template <typename T, int KS>
+__device__ __forceinline__ void quantise_tile(const Stack<T> &x, int j0, i32x4 (*rows)[64], float *steps, int lane) {
+    constexpr int D = KS * 32, H = KS / 2;
+    const int m = lane & 15, q4 = lane >> 4, j = min(j0 + m, x.n - 1);
+    const T *q = x.q + ((size_t)(x.row0 + j / x.g) * x.Hq + x.c * x.g + j % x.g) * D + 16 * q4;
+    float v[H][16], most = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < H; ++ks) load16(q + 64 * ks, v[ks]);
+#pragma unroll
+    for (int ks = 0; ks < H; ++ks)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(v[ks][i]));  // a NaN is passed over
+    most = fmaxf(most, __shfl_xor(most, 16, 64));
+    most = fmaxf(most, __shfl_xor(most, 32, 64));
+    const int e = step_exponent(fminf(most, 3.402823466e38f));
+    const float inv = ldexpf(1.f, -e);
+#pragma unroll
+    for (int ks = 0; ks < H; ++ks) {
+        i32x4 up, down;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            int u, d;
+            quantise4(v[ks] + 4 * i, inv, &u, &d);
+            up[i] = u;
+            down[i] = d;
+        }
+        rows[ks][lane] = up;
+        rows[ks + H][lane] = down;
+    }
+    if (q4 == 0) steps[m] = ldexpf(1.f, e);
+}
+// Codes of blocks b0 .. b0 + 16 TB - 1, a column to a lane; scale 0: no such block in the pool.
+template <int KS, int TB> struct Codes {
+    i32x4 code[TB][KS];
+    float scale[TB];
+    __device__ __forceinline__ void load(const SelectArgs &a, int s, int c, int Hkv, int b0, int nb, int lane) {
+        constexpr int D = KS * 32;
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            const int b = b0 + 16 * t + (lane & 15), id = b < nb ? a.bt[(size_t)s * a.max_blocks + b] : -1;
+            const bool good = id >= 0 && id < a.num_blocks;
+            const size_t rec = good ? (size_t)id * Hkv + c : 0;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) code[t][ks] = *(const i32x4 *)(a.codes + rec * 2 * D + 64 * ks + 16 * (lane >> 4));
+            scale[t] = good ? a.scales[rec] : 0.f;
+        }
+    }
+    // the largest of a tile's scores, so far; lanes 16 apart have other queries of the same block
+    __device__ __forceinline__ void score(float (&best)[TB], const i32x4 (*rows)[64], const float *steps, int lane) const {
+        i32x4 sum[TB];
+#pragma unroll
+        for (int t = 0; t < TB; ++t) sum[t] = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const i32x4 r = rows[ks][lane];
+#pragma unroll
+            for (int t = 0; t < TB; ++t) sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(r, code[t][ks], sum[t], 0, 0, 0);
+        }
+        const float4 st = *(const float4 *)(steps + 4 * (lane >> 4));
+#pragma unroll
+        for (int t = 0; t < TB; ++t)
+            best[t] = fmaxf(fmaxf(fmaxf(best[t], (float)sum[t][0] * st.x), fmaxf((float)sum[t][1] * st.y, (float)sum[t][2] * st.z)), (float)sum[t][3] * st.w);
+    }
+    __device__ __forceinline__ uint32_t key(int t, float best, int n) const {
+        best = fmaxf(best, __shfl_xor(best, 16, 64));
+        best = fmaxf(best, __shfl_xor(best, 32, 64));
+        return order_key(scale[t] > 0.f ? (n ? best * scale[t] : 0.f) : -INFINITY);
+    }
+};
+
 template <typename T, int KS, int TB>
 __global__ void __launch_bounds__(256, KS <= 4 ? 5 : 1) k_scores_mfma(SelectArgs a, int Hq, int Hkv, int Bk) {
-    constexpr int D = KS * 32, H = KS / 2;  // steps of 64 of both parts, of one part
-    __shared__ i32x4 rows[4][KS][64];       // four tiles of queries: [tile][step][lane]
+    __shared__ i32x4 rows[4][KS][64];  // four tiles of queries
     __shared__ __attribute__((aligned(16))) float steps[4][16];
-    const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, g = Hq / Hkv;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, q4 = lane >> 4;
+    const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int nb = n_blocks_of(a, s, Bk);
     if ((int)blockIdx.y * 64 * TB >= nb - a.last || nb <= a.top_k) return;  // all of them are taken
     const int b0 = (blockIdx.y * 4 + w) * 16 * TB;
-    const int row0 = min(max(a.row_start[s], 0), a.R), n = (min(max(a.row_start[s + 1], row0), a.R) - row0) * g;
-    i32x4 code[TB][KS];
-    float scale[TB], best[TB];
-    bool good[TB];
+    const Stack<T> x(a, s, c, Hq, Hkv);
+    Codes<KS, TB> codes;
+    codes.load(a, s, c, Hkv, b0, nb, lane);
+    float best[TB];
 #pragma unroll
-    for (int t = 0; t < TB; ++t) {
-        const int b = b0 + 16 * t + m, id = b < nb ? a.bt[(size_t)s * a.max_blocks + b] : -1;
-        good[t] = id >= 0 && id < a.num_blocks;
-        const size_t rec = good[t] ? (size_t)id * Hkv + c : 0;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) code[t][ks] = *(const i32x4 *)(a.codes + rec * 2 * D + 64 * ks + 16 * q4);
-        scale[t] = a.scales[rec];
-        best[t] = -INFINITY;
-    }
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        if (j0 + 16 * w < n) {
-            const int j = min(j0 + 16 * w + m, n - 1);  // behind the last query: the last again
-            const T *q = (const T *)a.q + ((size_t)(row0 + j / g) * Hq + c * g + j % g) * D + 16 * q4;
-            float v[H][16], most = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < H; ++ks) load16(q + 64 * ks, v[ks]);
-#pragma unroll
-            for (int ks = 0; ks < H; ++ks)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(v[ks][i]));  // a NaN is passed over
-            most = fmaxf(most, __shfl_xor(most, 16, 64));
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
-            const int e = step_exponent(fminf(most, 3.402823466e38f));
-            const float inv = ldexpf(1.f, -e);
-#pragma unroll
-            for (int ks = 0; ks < H; ++ks) {
-                i32x4 up, down;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    int u, d;
-                    quantise4(v[ks] + 4 * i, inv, &u, &d);
-                    up[i] = u;
-                    down[i] = d;
-                }
-                rows[w][ks][lane] = up;
-                rows[w][ks + H][lane] = down;
-            }
-            if (q4 == 0) steps[w][m] = ldexpf(1.f, e);
-        }
+    for (int t = 0; t < TB; ++t) best[t] = -INFINITY;
+    for (int j0 = 0; j0 < x.n; j0 += 64) {
+        if (j0 + 16 * w < x.n) quantise_tile<T, KS>(x, j0 + 16 * w, rows[w], steps[w], lane);
         __syncthreads();
-        const int tiles = min(4, (n - j0 + 15) / 16);
-        for (int j = 0; j < tiles; ++j) {
-            i32x4 sum[TB];
-#pragma unroll
-            for (int t = 0; t < TB; ++t) sum[t] = i32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const i32x4 r = rows[j][ks][lane];
-#pragma unroll
-                for (int t = 0; t < TB; ++t) sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(r, code[t][ks], sum[t], 0, 0, 0);
-            }
-            const float4 st = *(const float4 *)&steps[j][4 * q4];  // of the queries whose sums this lane has: rows 4 q4 .. + 3
-#pragma unroll
-            for (int t = 0; t < TB; ++t)
-                best[t] = fmaxf(fmaxf(fmaxf(best[t], (float)sum[t][0] * st.x), fmaxf((float)sum[t][1] * st.y, (float)sum[t][2] * st.z)), (float)sum[t][3] * st.w);
-        }
+        for (int j = 0; j < min(4, (x.n - j0 + 15) / 16); ++j) codes.score(best, rows[j], steps[j], lane);
         __syncthreads();
     }
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
-        float x = best[t];
-        x = fmaxf(x, __shfl_xor(x, 16, 64));
-        x = fmaxf(x, __shfl_xor(x, 32, 64));
-        const int b = b0 + 16 * t + m;
-        if (q4 == 0 && b < nb) ((uint32_t *)a.scores)[(size_t)pair * key_pitch(a.max_blocks) + b] = order_key(good[t] ? (n ? x * scale[t] : 0.f) : -INFINITY);
+        const uint32_t key = codes.key(t, best[t], x.n);
+        const int b = b0 + 16 * t + lane;
+        if (lane < 16 && b < nb) ((uint32_t *)a.scores)[(size_t)pair * key_pitch(a.max_blocks) + b] = key;
     }
 }
 
@@ -770,21 +795,12 @@ __global__ void __launch_bounds__(256) k_scores(SelectArgs a, int Hq, int Hkv, i
 // first bits, so eight lanes in turn count in places of their own (32 lists of 7500: 12.2 -> 8.7 us).  Bound by its dependent steps: 8 lists of 2048 5.9 us.
 // KPT: keys of a thread, in registers (0: read again in every pass, for any number).
 template <int THREADS, int KPT>
-__global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk) {
+__device__ __forceinline__ void pick(const SelectArgs &a, int nb, const uint32_t *keys, int32_t *out) {
     constexpr int WAVES = THREADS / 64, COPIES = 8;
     __shared__ __attribute__((aligned(16))) int hist[256][COPIES], count[256];
     __shared__ int part[WAVES];
     __shared__ uint32_t low[WAVES], high[WAVES];
-    const int pair = blockIdx.x, s = pair / Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int nb = n_blocks_of(a, s, Bk), k = min(a.top_k, nb), pitch = key_pitch(a.max_blocks);
-    const uint32_t *keys = (const uint32_t *)a.scores + (size_t)pair * pitch;
-    int32_t *out = a.blocks + (size_t)pair * a.top_k;
-    if (threadIdx.x == 0 && pair == s * Hkv) a.counts[s] = k;
-    for (int i = k + threadIdx.x; i < a.top_k; i += THREADS) out[i] = -1;
-    if (nb <= a.top_k) {
-        for (int i = threadIdx.x; i < nb; i += THREADS) out[i] = i;
-        return;
-    }
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int b_end = nb - a.last;  // [first, b_end) compete
     const int per = KPT ? KPT : ((nb + THREADS - 1) / THREADS + 3) & ~3, i0 = threadIdx.x * per;
     uint4 key[KPT ? KPT / 4 : 1];
@@ -917,6 +933,66 @@ __global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk)
     });
 }
 
+// What needs no choice: the length of the list, its end, and a list of all blocks.  True: done.
+template <int THREADS>
+__device__ __forceinline__ bool all_taken(const SelectArgs &a, int pair, int s, int Hkv, int nb, int32_t *out) {
+    const int k = min(a.top_k, nb);
+    if (threadIdx.x == 0 && pair == s * Hkv) a.counts[s] = k;
+    for (int i = k + threadIdx.x; i < a.top_k; i += THREADS) out[i] = -1;
+    if (nb > a.top_k) return false;
+    for (int i = threadIdx.x; i < nb; i += THREADS) out[i] = i;
+    return true;
+}
+
+template <int THREADS, int KPT>
+__global__ void __launch_bounds__(THREADS) k_pick(SelectArgs a, int Hkv, int Bk) {
+    const int pair = blockIdx.x, s = pair / Hkv, nb = n_blocks_of(a, s, Bk);
+    int32_t *out = a.blocks + (size_t)pair * a.top_k;
+    if (all_taken<THREADS>(a, pair, s, Hkv, nb, out)) return;
+    pick<THREADS, KPT>(a, nb, (const uint32_t *)a.scores + (size_t)pair * key_pitch(a.max_blocks), out);
+}
+
+// Both at once where a sequence has few blocks, head sizes 64 and 128: a workgroup to a sequence and kv-head, keys in LDS.  Replayed from a graph, 8 heads of 128, up to
+// 9 rows x 4 heads: 1 sequence of 125 blocks 7.3 us, of 250 8.0 (two kernels 8.1 and 8.4), 64 of 250 12.7 (15.9), 64 of 506 17.9 (21.8); but 1 of 506 11.3 (9.2), one
+// workgroup's reads of all its codes, and 64 of 1012 26.4 (25.4).
+constexpr int kOnceThreads = 512, kOnceBlocks = 512, kOnceTiles = 5;
+template <typename T, int KS>
+__global__ void __launch_bounds__(kOnceThreads) k_select(SelectArgs a, int Hq, int Hkv, int Bk) {
+    constexpr int TB = 2, STEP = kOnceThreads / 64 * 16 * TB;
+    __shared__ i32x4 rows[kOnceTiles][KS][64];
+    __shared__ __attribute__((aligned(16))) float steps[kOnceTiles][16];
+    __shared__ __attribute__((aligned(16))) uint32_t keys[kOnceBlocks];
+    const int pair = blockIdx.x, s = pair / Hkv, c = pair - s * Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int nb = n_blocks_of(a, s, Bk);
+    int32_t *out = a.blocks + (size_t)pair * a.top_k;
+    if (all_taken<kOnceThreads>(a, pair, s, Hkv, nb, out)) return;
+    const Stack<T> x(a, s, c, Hq, Hkv);
+    for (int j0 = 0; j0 == 0 || j0 < x.n; j0 += 16 * kOnceTiles) {  // without queries once too: the keys say which blocks there are
+        const int tiles = max(0, min(kOnceTiles, (x.n - j0 + 15) / 16));
+        int b0 = w * 16 * TB;
+        Codes<KS, TB> codes;
+        codes.load(a, s, c, Hkv, b0, nb, lane);
+        if (j0) __syncthreads();
+        for (int t = w; t < tiles; t += kOnceThreads / 64) quantise_tile<T, KS>(x, j0 + 16 * t, rows[t], steps[t], lane);
+        __syncthreads();
+        for (; b0 < nb - a.last; b0 += STEP) {
+            float best[TB];
+#pragma unroll
+            for (int t = 0; t < TB; ++t) best[t] = -INFINITY;
+            for (int j = 0; j < tiles; ++j) codes.score(best, rows[j], steps[j], lane);
+#pragma unroll
+            for (int t = 0; t < TB; ++t) {
+                const uint32_t key = codes.key(t, best[t], x.n);
+                const int b = b0 + 16 * t + lane;
+                if (lane < 16 && b < nb) keys[b] = j0 ? max(keys[b], key) : key;
+            }
+            if (b0 + STEP < nb - a.last) codes.load(a, s, c, Hkv, b0 + STEP, nb, lane);
+        }
+    }
+    __syncthreads();
+    pick<kOnceThreads, 4>(a, nb, keys, out);
+}
+
 }  // namespace
 
 hipError_t launch_extend(const ExtendArgs &a, hipStream_t st) {
@@ -994,11 +1070,26 @@ static bool scores_mfma(const Dims &dm, const SelectArgs &a, hipStream_t st) {
     }
 }
 
+template <typename T>
+static bool select_at_once(const Dims &dm, const SelectArgs &a, hipStream_t st) {
+    const dim3 grid(a.S * dm.Hkv), threads(kOnceThreads);
+    switch (dm.D) {
+    case 64: hipLaunchKernelGGL((k_select<T, 2>), grid, threads, 0, st, a, dm.Hq, dm.Hkv, dm.Bk); return true;
+    case 128: hipLaunchKernelGGL((k_select<T, 4>), grid, threads, 0, st, a, dm.Hq, dm.Hkv, dm.Bk); return true;
+    default: return false;
+    }
+}
+
 hipError_t launch_select(const Dims &dm, bool generic, const SelectArgs &a, hipStream_t st) {
     bool done = false;
+    const int64_t pairs = (int64_t)a.S * dm.Hkv;
+    if (!generic && a.max_blocks <= (pairs < 128 ? kOnceBlocks / 2 : kOnceBlocks)) {  // few lists: two kernels spread the codes of each over the chip
+        DISPATCH_T(dm.bf16, done = (select_at_once<T>(dm, a, st)));
+        if (done) return hipGetLastError();
+    }
     if (a.max_blocks > a.top_k) {  // else all blocks are taken
         // 128 blocks to a workgroup share its queries, 64 fill the chip sooner: 1 sequence, 8 kv-heads, 2048 blocks 6.6 and 5.7 us; 64 sequences 18.6 and 20.7
-        const bool few = (int64_t)a.S * dm.Hkv * ((a.max_blocks + 127) / 128) <= 256;
+        const bool few = pairs * ((a.max_blocks + 127) / 128) <= 256;
         if (!generic) DISPATCH_T(dm.bf16, done = (few ? scores_mfma<T, 1>(dm, a, st) : scores_mfma<T, 2>(dm, a, st)));
         if (!done)
             DISPATCH_T(dm.bf16, hipLaunchKernelGGL(k_scores<T>, dim3(a.S * dm.Hkv, (a.max_blocks + 255) / 256), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D, dm.Bk));

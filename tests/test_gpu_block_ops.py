@@ -371,13 +371,15 @@ def test_select_extremes():
 
 @pytest.mark.parametrize("kw", [dict(Hq=16), dict(Hq=8, D=64), dict(Hq=8, D=192), dict(Hq=16, D=256), dict(bf16=False), dict(D=64, bf16=False), dict(D=192, bf16=False),
                                 dict(D=256, bf16=False), dict(D=128, mode=1)], ids=str)
-def test_select_many_sequences(kw):
-    print("case:", kw, flush=True)
+@pytest.mark.parametrize("max_blocks", [140, 500, 600])
+def test_select_many_sequences(kw, max_blocks):
+    print("case:", kw, max_blocks, flush=True)
     layer = make(num_blocks=300, **{"Hq": 8, "Hkv": 8, **kw})
     c, rng = layer.cfg, np.random.default_rng(5)
-    S, max_blocks = 33, 140
+    S = 33
     codes, scales = random_bounds(layer, rng, True)
     rows = rng.integers(0, 5, S)
+    rows[5] = 90                                                          # more queries than are held at a time
     start = np.concatenate([[0], np.cumsum(rows)])
     q = torch.tensor(rng.standard_normal((start[-1], c.n_q_heads, c.head_dim)), dtype=torch.float32).to(c.torch_dtype).to(DEV)
     table, kv = rng.integers(0, 300, (S, max_blocks)), rng.integers(0, max_blocks * 16 + 1, S)
