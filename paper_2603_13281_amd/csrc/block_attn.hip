@@ -637,19 +637,22 @@ __global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitO
     }
 }
 
-// Splits of the lists, at most `most`.  Items go over the workgroups that the chip holds in rounds (1 to a CU of the 128 kernel, 3 of the float32 one: with 4 its 25
-// sequences above took 33 us, with 8 35); a round costs the blocks of its items and as much as kItemCost blocks of 16 tokens on top, joining kJoinCost.
-constexpr int kWgs = 256, kItemCost = 12, kJoinCost = 24, kMaxSplits = 32, kMaxTileGroups = 64;
+// Splits of the lists, at most `most`: the number whose rounds of workgroups cost least.  Unit: what 16 tokens take a workgroup that is alone, 0.15 us on the 128 kernel
+// and 0.25 on the float32 one; an item costs kItemCost besides, a join 4 us.  Next to others HBM is shared: 256 blocks of 192 lists take the 128 kernel 76 us in one
+// part (twice the unit; in four parts, three rounds, 88), of 96 lists 47 (two parts 42), of 8 lists 39 (eight parts 11); 32 blocks of 96 lists the float32 one 15 us (four
+// parts 12).  The chip holds 1 workgroup to a CU of the 128 kernel and 3 of the float32 one (counted on 4: 33 for 29 us on its 25 sequences above, on 8 35).
+constexpr int kWgs = 256, kItemCost = 12, kMaxSplits = 32, kMaxTileGroups = 64;
 int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxSplits) {
-    const int least = (max_selected + kItemBlocks - 1) / kItemBlocks;
-    const int64_t wgs = on_matrix_cores(dm) ? kWgs : 3 * kWgs;
+    const bool mfma = on_matrix_cores(dm);
+    const int least = (max_selected + kItemBlocks - 1) / kItemBlocks, parts = mfma ? 1 : dm.Bk / 16;
+    const int limit = (int)std::min<int64_t>({most, max_selected, ((int64_t)max_selected * parts + 7) / 8});  // 8 times 16 tokens: a group of two or two units to a wave
+    const int64_t wgs = mfma ? kWgs : 3 * kWgs;
+    const auto round = [&](int64_t running, int64_t blocks) { return 128 * kItemCost + blocks * (128 + (mfma ? std::max<int64_t>(running - 64, 0) : running * 5 / 8)); };
     int best = 0;
     int64_t cost = 0;
-    const int parts = on_matrix_cores(dm) ? 1 : dm.Bk / 16;
-    const int limit = (int)std::min<int64_t>({most, max_selected, ((int64_t)max_selected * parts + 7) / 8});  // 8 times 16 tokens: a group of two or two units to a wave
     for (int n = std::max(1, least); n <= std::max(least, limit) || !best; ++n) {
-        const int64_t rounds = (pairs * n + wgs - 1) / wgs, blocks = (int64_t)((max_selected + n - 1) / n) * parts;
-        const int64_t t = rounds * (blocks + kItemCost) + (n > 1 ? kJoinCost : 0);
+        const int64_t items = pairs * n, blocks = (int64_t)((max_selected + n - 1) / n) * parts;
+        const int64_t t = items / wgs * round(wgs, blocks) + (items % wgs ? round(items % wgs, blocks) : 0) + (n > 1 ? 128 * (mfma ? 24 : 16) : 0);
         if (!best || t < cost) {
             best = n;
             cost = t;
