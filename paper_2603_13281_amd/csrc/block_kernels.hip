@@ -212,12 +212,13 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, i
 }
 
 // Head sizes 64, 128 and 256, blocks of 16.  Bound by HBM where there are many rows, by the chain of its reads where there are few.
-// A workgroup takes a window of 16 rows and a part of their heads.  LPH = D / 8 lanes hold a head, four pairs to a lane, so that both halves of a
+// A workgroup takes a window of 16 rows and a part of their rotated heads or of their values.  LPH = D / 8 lanes hold a head, four pairs to a lane, so that both halves of a
 // row of 128 bfloat16 are read and written as whole lines; a lane keeps its row's angles for all heads of the part.
 // V goes into the pool transposed: a run of rows that are consecutive places of one block is put together in LDS and written as one row of the block per
 // channel, 32 bytes at once where the run fills the block.  A run belongs to the window in which it starts, wherever it ends, so that prompts which begin
 // inside a block are written in whole blocks too.
-// 16384 rows of 48 heads of 128 (402 MB): 96 us, 4.2 TB/s (339 us a wave to a head); 1145 rows of 80 heads into an FP8 cache (44 MB): 18 us (46); 356 rows: 7 us (7.9).
+// The values have workgroups of their own, whose chain of reads runs beside the other.  16384 rows of 48 heads of 128 (402 MB): 92 us, 4.4 TB/s (values after the
+// rotation in one workgroup 97; a wave to a head 339); 1145 rows of 80 heads into an FP8 cache (44 MB): 14.6 us (18; 46); 356 rows of 48 heads 5.2 us (6.9; 7.9).
 template <typename KT> __device__ __forceinline__ void put4(KT *p, const float (&v)[4], float scale);
 template <> __device__ __forceinline__ void put4(bf16_t *p, const float (&v)[4], float) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
 template <> __device__ __forceinline__ void put4(float *p, const float (&v)[4], float) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
@@ -232,81 +233,83 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_wave_barrier();
 }
 template <typename T, typename KT, int D>
-__global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int Hkv, double log2_theta, float eps, int qk_norm, float k_scale, float v_scale) {
+__global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int Hkv, int parts, double log2_theta, float eps, int qk_norm, float k_scale, float v_scale) {
     constexpr int Bk = 16, LPH = D / 8, HALF = D / 2, ROWS = 256 / LPH, VW = 16 / sizeof(T);  // ROWS: heads of a pass; VW: elements of 16 bytes
     __shared__ double turns[HALF];
     __shared__ __attribute__((aligned(16))) T tile[4][Bk][D];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = blockIdx.x * kWindow;
-    for (int i = threadIdx.x; i < HALF; i += 256) turns[i] = turns_per_position(i, D, log2_theta);
-    __syncthreads();
     const int n_rot = Hq + Hkv;
-    // Rotated heads of this part, [h0, h1): with fewer than 16 lanes to a head the lanes of a row take neighbouring heads.
-    constexpr int HPR = ROWS > kWindow ? ROWS / kWindow : 1;  // heads of a row at a time
-    const int h0 = n_rot * blockIdx.y / gridDim.y, h1 = n_rot * (blockIdx.y + 1) / gridDim.y;
-    const int sub = threadIdx.x / LPH, i4 = 4 * (threadIdx.x % LPH);
-    for (int rr = sub / HPR; rr < kWindow; rr += ROWS / HPR) {
-        const int row = r0 + rr, pos = row < a.R ? a.row_pos[row] : -1;
-        if (pos < 0) continue;
-        const int64_t slot = a.row_slot[row];
-        const bool write = slot >= 0 && slot < a.n_slots;
-        float cs[4], sn[4], wq[2][4], wk[2][4];
+    if ((int)blockIdx.y < parts) {
+        for (int i = threadIdx.x; i < HALF; i += 256) turns[i] = turns_per_position(i, D, log2_theta);
+        __syncthreads();
+        // Rotated heads of this part, [h0, h1): with fewer than 16 lanes to a head the lanes of a row take neighbouring heads.
+        constexpr int HPR = ROWS > kWindow ? ROWS / kWindow : 1;  // heads of a row at a time
+        const int h0 = n_rot * blockIdx.y / parts, h1 = n_rot * (blockIdx.y + 1) / parts;
+        const int sub = threadIdx.x / LPH, i4 = 4 * (threadIdx.x % LPH);
+        for (int rr = sub / HPR; rr < kWindow; rr += ROWS / HPR) {
+            const int row = r0 + rr, pos = row < a.R ? a.row_pos[row] : -1;
+            if (pos < 0) continue;
+            const int64_t slot = a.row_slot[row];
+            const bool write = slot >= 0 && slot < a.n_slots;
+            float cs[4], sn[4], wq[2][4], wk[2][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) turn_of(pos, turns[i4 + e], &cs[e], &sn[e]);
-        if (qk_norm)
+            for (int e = 0; e < 4; ++e) turn_of(pos, turns[i4 + e], &cs[e], &sn[e]);
+            if (qk_norm)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                Quad<T>::get(*(const typename Quad<T>::raw *)((const T *)a.q_norm + h * HALF + i4), wq[h]);
-                Quad<T>::get(*(const typename Quad<T>::raw *)((const T *)a.k_norm + h * HALF + i4), wk[h]);
-            }
-        const T *src = (const T *)a.qkv + (size_t)row * a.ld + i4;
-        KT *kdst = (KT *)a.pool + (write ? ((size_t)(slot / Bk) * Hkv * 2 * Bk + (size_t)(slot % Bk)) * D : 0) + i4;
-        const int end = write ? h1 : min(h1, Hq);  // a stream's key heads are not read
-        constexpr int U = 4;  // heads whose reads are under way together
-        for (int hu = h0 + sub % HPR; hu < end; hu += U * HPR) {
-            typename Quad<T>::raw lo[U], up[U];
+                for (int h = 0; h < 2; ++h) {
+                    Quad<T>::get(*(const typename Quad<T>::raw *)((const T *)a.q_norm + h * HALF + i4), wq[h]);
+                    Quad<T>::get(*(const typename Quad<T>::raw *)((const T *)a.k_norm + h * HALF + i4), wk[h]);
+                }
+            const T *src = (const T *)a.qkv + (size_t)row * a.ld + i4;
+            KT *kdst = (KT *)a.pool + (write ? ((size_t)(slot / Bk) * Hkv * 2 * Bk + (size_t)(slot % Bk)) * D : 0) + i4;
+            const int end = write ? h1 : min(h1, Hq);  // a stream's key heads are not read
+            constexpr int U = 4;  // heads whose reads are under way together
+            for (int hu = h0 + sub % HPR; hu < end; hu += U * HPR) {
+                typename Quad<T>::raw lo[U], up[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const T *p = src + (size_t)min(hu + u * HPR, end - 1) * D;
-                lo[u] = *(const typename Quad<T>::raw *)p;
-                up[u] = *(const typename Quad<T>::raw *)(p + HALF);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = hu + u * HPR;
-                if (h >= end) break;
-                float x[4], y[4], rx[4], ry[4];
-                Quad<T>::get(lo[u], x);
-                Quad<T>::get(up[u], y);
-                if (qk_norm) {
-                    float ss = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) ss += x[e] * x[e] + y[e] * y[e];
-#pragma unroll
-                    for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-                    const float inv = rsqrtf(ss / (float)D + eps);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[e] = x[e] * inv * (h < Hq ? wq[0][e] : wk[0][e]);
-                        y[e] = y[e] * inv * (h < Hq ? wq[1][e] : wk[1][e]);
-                    }
+                for (int u = 0; u < U; ++u) {
+                    const T *p = src + (size_t)min(hu + u * HPR, end - 1) * D;
+                    lo[u] = *(const typename Quad<T>::raw *)p;
+                    up[u] = *(const typename Quad<T>::raw *)(p + HALF);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) rotate_pair(x[e], y[e], cs[e], sn[e], &rx[e], &ry[e]);
-                if (h < Hq) {
-                    T *dst = (T *)a.q_out + ((size_t)row * Hq + h) * D + i4;
-                    put4(dst, rx, 1.f);
-                    put4(dst + HALF, ry, 1.f);
-                } else {
-                    KT *dst = kdst + (size_t)(h - Hq) * 2 * Bk * D;
-                    put4(dst, rx, k_scale);
-                    put4(dst + HALF, ry, k_scale);
+                for (int u = 0; u < U; ++u) {
+                    const int h = hu + u * HPR;
+                    if (h >= end) break;
+                    float x[4], y[4], rx[4], ry[4];
+                    Quad<T>::get(lo[u], x);
+                    Quad<T>::get(up[u], y);
+                    if (qk_norm) {
+                        float ss = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) ss += x[e] * x[e] + y[e] * y[e];
+#pragma unroll
+                        for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+                        const float inv = rsqrtf(ss / (float)D + eps);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[e] = x[e] * inv * (h < Hq ? wq[0][e] : wk[0][e]);
+                            y[e] = y[e] * inv * (h < Hq ? wq[1][e] : wk[1][e]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) rotate_pair(x[e], y[e], cs[e], sn[e], &rx[e], &ry[e]);
+                    if (h < Hq) {
+                        T *dst = (T *)a.q_out + ((size_t)row * Hq + h) * D + i4;
+                        put4(dst, rx, 1.f);
+                        put4(dst + HALF, ry, 1.f);
+                    } else {
+                        KT *dst = kdst + (size_t)(h - Hq) * 2 * Bk * D;
+                        put4(dst, rx, k_scale);
+                        put4(dst + HALF, ry, k_scale);
+                    }
                 }
             }
         }
+        return;
     }
     // V: lane l < 32 looks at row r0 + l; the rows behind the window matter for runs that start in it.
-    const int v0 = Hkv * blockIdx.y / gridDim.y, n_v = Hkv * (blockIdx.y + 1) / gridDim.y - v0;
-    if (n_v == 0) return;
+    const int v_part = blockIdx.y - parts, v_parts = gridDim.y - parts, v0 = Hkv * v_part / v_parts, n_v = Hkv * (v_part + 1) / v_parts - v0;
     int64_t slot = -1, before = -1;
     if (lane < 32) {
         auto place = [&](int row) {
@@ -1005,17 +1008,18 @@ template <typename T, typename KT>
 static bool append_window(const Dims &dm, const AppendArgs &a, hipStream_t st) {
     if (dm.Bk != 16 || a.ld * (int64_t)sizeof(T) % 16) return false;
     const int windows = (a.R + kWindow - 1) / kWindow;
-    // of the heads: eight workgroups to a CU, as long as a part has a rotated head for every wave's turn (1145 rows of 80 heads: 18 us; two to a CU 20)
+    // Of the heads: four workgroups to a CU, as long as a part has a rotated head for every wave's turn.  5300 rows of 80 heads 53 us (1 to a CU 66, 16 to a CU 56),
+    // 1145 rows 14.6 (1 to a CU 18.6), 16384 rows of 48 heads 92 (16 to a CU 98).
     int parts = 1;
-    while (windows * parts < 2048 && 2 * parts <= (dm.Hq + dm.Hkv + 3) / 4) parts *= 2;
-    const dim3 grid(windows, parts);
+    while (windows * parts < 1024 && 2 * parts <= (dm.Hq + dm.Hkv + 3) / 4) parts *= 2;
+    const dim3 grid(windows, parts + std::min(parts, dm.Hkv));
     const double l2t = log2(dm.theta);
     switch (dm.D) {
-    case 64: hipLaunchKernelGGL((k_append_window<T, KT, 64>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale); return true;
-    case 128: hipLaunchKernelGGL((k_append_window<T, KT, 128>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale); return true;
+    case 64: hipLaunchKernelGGL((k_append_window<T, KT, 64>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, parts, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale); return true;
+    case 128: hipLaunchKernelGGL((k_append_window<T, KT, 128>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, parts, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale); return true;
     case 256:
         if constexpr (sizeof(T) == 2) {  // four tiles of float32 pass what static LDS holds
-            hipLaunchKernelGGL((k_append_window<T, KT, 256>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale);
+            hipLaunchKernelGGL((k_append_window<T, KT, 256>), grid, dim3(256), 0, st, a, dm.Hq, dm.Hkv, parts, l2t, dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale);
             return true;
         }
         return false;
