@@ -170,6 +170,7 @@ __device__ __forceinline__ void group_of(State<NT> &st, const Frag &f, const bf1
         for (int qt = 0; qt < N; ++qt) {
             float m_new = fmaxf(mx[qt], __shfl_xor(mx[qt], 16, 64));
             m_new = fmaxf(st.m[qt], fmaxf(m_new, __shfl_xor(m_new, 32, 64)));
+            if (!__any(mx[qt] > st.m[qt] + kSlack)) m_new = st.m[qt];  // a tile's results must not depend on the tiles beside it
             const float c = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[qt] - m_new);
             st.m[qt] = m_new;
             st.l[qt] *= c;
@@ -637,15 +638,28 @@ __global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitO
     }
 }
 
-// Splits of the lists, at most `most`: the number whose rounds of workgroups cost least.  Unit: what 16 tokens take a workgroup that is alone, 0.15 us on the 128 kernel
+// Tiles of 16 queries of `rows` rows, and in how many groups an item each takes them.
+struct TileGroups { int64_t tiles; int groups; };
+constexpr int kWgs = 256, kItemCost = 12, kMaxSplits = 32, kMaxTileGroups = 64;
+TileGroups tile_groups_for(const Dims &dm, int64_t pairs, int64_t rows) {
+    const bool mfma = on_matrix_cores(dm);
+    const int64_t tiles = std::max<int64_t>(1, (rows * (dm.Hq / dm.Hkv) + 15) / 16);
+    int groups = (int)std::min<int64_t>(mfma ? (tiles + 2) / 3 : tiles, kMaxTileGroups);
+    // few lists: tiles apart while their items and 8 splits fit on the chip at once (1 sequence, 8 kv-heads, 3 tiles, 128 blocks: 11.5 -> 8.5 us; 2 of 2 tiles, 64 blocks: 9.2 -> 8.3)
+    while (mfma && groups < std::min<int64_t>(tiles, 3) && pairs * (groups + 1) * 8 <= kWgs) ++groups;
+    return {tiles, groups};
+}
+
+// Splits of the lists: the number whose rounds of workgroups cost least.  Unit: what 16 tokens take a workgroup that is alone, 0.15 us on the 128 kernel
 // and 0.25 on the float32 one; an item costs kItemCost besides, a join 4 us.  Next to others HBM is shared: 256 blocks of 192 lists take the 128 kernel 76 us in one
 // part (twice the unit; in four parts, three rounds, 88), of 96 lists 47 (two parts 42), of 8 lists 39 (eight parts 11); 32 blocks of 96 lists the float32 one 15 us (four
 // parts 12).  The chip holds 1 workgroup to a CU of the 128 kernel and 3 of the float32 one (counted on 4: 33 for 29 us on its 25 sequences above, on 8 35).
-constexpr int kWgs = 256, kItemCost = 12, kMaxSplits = 32, kMaxTileGroups = 64;
-int splits_for(const Dims &dm, int64_t pairs, int max_selected, int most = kMaxSplits) {
+// A sum's order goes by the splits, so they go by the arrays' sizes alone: the rows are taken to be spread evenly over the sequences, whatever seq_rows says.
+int splits_for(const Dims &dm, int S, int R, int max_selected) {
     const bool mfma = on_matrix_cores(dm);
+    const int64_t lists = (int64_t)S * dm.Hkv, pairs = lists * tile_groups_for(dm, lists, ((int64_t)R + S - 1) / S).groups;
     const int least = (max_selected + kItemBlocks - 1) / kItemBlocks, parts = mfma ? 1 : dm.Bk / 16;
-    const int limit = (int)std::min<int64_t>({most, max_selected, ((int64_t)max_selected * parts + 7) / 8});  // 8 times 16 tokens: a group of two or two units to a wave
+    const int limit = (int)std::min<int64_t>({kMaxSplits, max_selected, ((int64_t)max_selected * parts + 7) / 8});  // 8 times 16 tokens: a group of two or two units to a wave
     const int64_t wgs = mfma ? kWgs : 3 * kWgs;
     const auto round = [&](int64_t running, int64_t blocks) { return 128 * kItemCost + blocks * (128 + (mfma ? std::max<int64_t>(running - 64, 0) : running * 5 / 8)); };
     int best = 0;
@@ -687,7 +701,7 @@ bool block_attn_fast(const Dims &dm) { return dm.Bk % 16 == 0 && dm.D % 16 == 0;
 
 size_t block_attn_workspace(const Dims &dm, int S, int R, int max_selected) {
     if (!block_attn_fast(dm) || S == 0) return 256;
-    const int splits = splits_for(dm, (int64_t)S * dm.Hkv, max_selected);
+    const int splits = splits_for(dm, S, R, max_selected);
     return splits > 1 ? (size_t)splits * R * dm.Hq * (dm.D + 2) * 4 + 512 : 256;
 }
 
@@ -705,17 +719,14 @@ static hipError_t launch_f32(const Dims &dm, const BlockAttnArgs &a, const Split
 }
 
 hipError_t launch_block_attn(const Dims &dm, const BlockAttnArgs &a, void *workspace, hipStream_t st) {
-    const int g = dm.Hq / dm.Hkv;
     const int64_t pairs = (int64_t)a.S * dm.Hkv;
     const int rows = std::min(a.R, a.seq_rows ? a.seq_rows : 2 * ((a.R + a.S - 1) / a.S));  // of a sequence, about: the kernels go on where there are more
     const bool mfma = on_matrix_cores(dm);
-    const int64_t tiles = ((int64_t)rows * g + 15) / 16;
+    const TileGroups of = tile_groups_for(dm, pairs, rows);
     SplitOut part;
-    part.tile_groups = (int)std::min<int64_t>(mfma ? (tiles + 2) / 3 : tiles, kMaxTileGroups);
-    // few lists: tiles apart while their items and 8 splits fit on the chip at once (1 sequence, 8 kv-heads, 3 tiles, 128 blocks: 11.5 -> 8.5 us; 2 of 2 tiles, 64 blocks: 9.2 -> 8.3)
-    while (mfma && part.tile_groups < std::min<int64_t>(tiles, 3) && pairs * (part.tile_groups + 1) * 8 <= kWgs) ++part.tile_groups;
-    part.tiles = (int)std::min<int64_t>((tiles + part.tile_groups - 1) / part.tile_groups, 3);
-    part.splits = splits_for(dm, pairs * part.tile_groups, a.max_selected, splits_for(dm, pairs, a.max_selected));  // no more than the workspace was sized for
+    part.tile_groups = of.groups;
+    part.tiles = (int)std::min<int64_t>((of.tiles + of.groups - 1) / of.groups, 3);
+    part.splits = splits_for(dm, a.S, a.R, a.max_selected);
     part.per = (a.max_selected + part.splits - 1) / part.splits;
     if (mfma) part.per = std::max(2, (part.per + 1) & ~1);
     part.o = (float *)workspace;
