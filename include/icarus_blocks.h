@@ -60,7 +60,8 @@ icarus_status icarus_extend_sequences(icarus_ctx *ctx, int32_t S, const int32_t 
 /* Row r of qkv holds the projections of one token: Hq query, Hkv key, Hkv value heads.  Query and key heads go through
  * RMSNorm (qk_norm) and are rotated to position row_pos[r]; q_out [R, Hq, D] receives the queries, the pool K and V at slot
  * row_slot[r].  Rows with a negative position are left out, q_out with them; with a slot outside the pool only the append
- * is left out and the row's K and V are not read.  Slots that are not named keep every byte.  Of a slot that is named twice each element is one of its rows'.
+ * is left out and the row's K and V are not read.  The entries are those that icarus_prefill_kv and icarus_decode_step write, bit for bit, where their
+ * projections (float32) are the same numbers.  Slots that are not named keep every byte.  Of a slot that is named twice each element is one of its rows'.
  *   qkv                 device, dtype elements, rows ld elements apart (ld >= (Hq + 2 Hkv) * D)
  *   row_pos, row_slot   device int32, int64 [R] */
 icarus_status icarus_rope_append(icarus_ctx *ctx, const void *qkv, int64_t ld, int32_t R, const int32_t *row_pos,

@@ -153,26 +153,30 @@ __global__ void __launch_bounds__(kExtThreads) k_extend(ExtendArgs a) {
 }
 
 // ---- rotation and append ------------------------------------------------------------------------------------------------
-// Turns of pair i at a position, pos * theta^(-2i/D) / 2 pi, in float64: a far position keeps the fraction of its last turn.
-__device__ __forceinline__ void turn_of(int pos, double turns_per_pos, float *cs, float *sn) {
-    const double t = (double)pos * turns_per_pos;
-    const float half_turns = (float)(2.0 * (t - rint(t)));  // -1 .. 1, rounded last
-    *cs = cospif(half_turns);
-    *sn = sinpif(half_turns);
-}
-__device__ __forceinline__ double turns_per_position(int i, int D, double log2_theta) {
-    return exp2(-(2.0 * (double)i / (double)D) * log2_theta) * 0.15915494309189533577;
+// Cosine and sine of pos * theta^(-2i/D), in float64 and rounded once: a far position keeps the fraction of its last turn.  A cache entry must not depend on which
+// call appended it, so the angles, and the order in which a norm's squares are summed, are those of the kernels behind icarus_prefill_kv and icarus_decode_step.
+__device__ __forceinline__ double frequency_of(int i, int D, double log2_theta) { return exp2(-(2.0 * (double)i / (double)D) * log2_theta); }
+__device__ __forceinline__ void angle_of(int pos, double frequency, float *cs, float *sn) {
+    double s, c;
+    sincos((double)pos * frequency, &s, &c);
+    *cs = (float)c;
+    *sn = (float)s;
 }
 
 // Any head size and block size, rows at any distance: a wave to a head of a row, a pair to a lane, V written element by element (16384 rows of 48 heads of 128,
-// 402 MB: 339 us; 356 rows of them 7.9 us).
+// 402 MB: 366 us; 356 rows of them 7.8 us; angles taken by every wave for itself 455 and 9.8).
 template <typename T, typename KT>
 __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, int D, int Bk, double log2_theta, float eps, int qk_norm,
                                                 float k_scale, float v_scale) {
+    __shared__ float cos_t[128], sin_t[128];
     const int row = blockIdx.x, h = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, half = D >> 1;
-    if (h >= Hq + 2 * Hkv) return;
     const int pos = a.row_pos[row];
     if (pos < 0) return;
+    if ((int)blockIdx.y * 4 < Hq + Hkv) {  // the row's angles, for the four heads
+        for (int i = threadIdx.x; i < half; i += 256) angle_of(pos, frequency_of(i, D, log2_theta), cos_t + i, sin_t + i);
+        __syncthreads();
+    }
+    if (h >= Hq + 2 * Hkv) return;
     const int64_t slot = a.row_slot[row];
     const bool write = slot >= 0 && slot < a.n_slots;
     if (h >= Hq && !write) return;
@@ -191,14 +195,13 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, i
         inv = rsqrtf(wave_sum(ss) / (float)D + eps);
     }
     for (int i = lane; i < half; i += 64) {
-        float x = Elem<T>::ld(src + i), y = Elem<T>::ld(src + i + half), cs, sn, rx, ry;
+        float x = Elem<T>::ld(src + i), y = Elem<T>::ld(src + i + half), rx, ry;
         if (qk_norm) {
             const T *w = (const T *)(h < Hq ? a.q_norm : a.k_norm);
             x = x * inv * Elem<T>::ld(w + i);
             y = y * inv * Elem<T>::ld(w + i + half);
         }
-        turn_of(pos, turns_per_position(i, D, log2_theta), &cs, &sn);
-        rotate_pair(x, y, cs, sn, &rx, &ry);
+        rotate_pair(x, y, cos_t[i], sin_t[i], &rx, &ry);
         if (h < Hq) {
             T *dst = (T *)a.q_out + ((size_t)row * Hq + h) * D;
             Elem<T>::st(dst + i, rx);
@@ -217,8 +220,9 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, i
 // V goes into the pool transposed: a run of rows that are consecutive places of one block is put together in LDS and written as one row of the block per
 // channel, 32 bytes at once where the run fills the block.  A run belongs to the window in which it starts, wherever it ends, so that prompts which begin
 // inside a block are written in whole blocks too.
-// The values have workgroups of their own, whose chain of reads runs beside the other.  16384 rows of 48 heads of 128 (402 MB): 92 us, 4.4 TB/s (values after the
-// rotation in one workgroup 97; a wave to a head 339); 1145 rows of 80 heads into an FP8 cache (44 MB): 14.6 us (18; 46); 356 rows of 48 heads 5.2 us (6.9; 7.9).
+// The values have workgroups of their own, whose chain of reads runs beside the other.  16384 rows of 48 heads of 128 (402 MB): 92 us, 4.4 TB/s (a wave to a head
+// 366); 1145 rows of 80 heads into an FP8 cache (44 MB): 15.4 us (48); 356 rows of 48 heads 5.6 us (7.8).  With angles in float32 half turns, which differ from the other
+// kernels' in the last bit, 92, 14.5 and 5.3, and then with the values after the rotation in one workgroup 97, 18 and 6.9.
 template <typename KT> __device__ __forceinline__ void put4(KT *p, const float (&v)[4], float scale);
 template <> __device__ __forceinline__ void put4(bf16_t *p, const float (&v)[4], float) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
 template <> __device__ __forceinline__ void put4(float *p, const float (&v)[4], float) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
@@ -232,15 +236,39 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
+// Squares of a head whose pairs (x, y) 4 l .. 4 l + 3 lane l of its D / 8 holds, in the order of a wave that adds elements i, i + 64, .. in lane i and then lanes 32, 16, .. 1 apart.
+template <int D> __device__ __forceinline__ float sum_of_squares(const float (&x)[4], const float (&y)[4]) {
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (D == 64) {  // two lanes' squares: each is rounded
+            float a = x[e] * x[e], b = y[e] * y[e];
+            asm("" : "+v"(a), "+v"(b));
+            p[e] = a + b;
+        } else if constexpr (D == 128) {
+            p[e] = __builtin_fmaf(y[e], y[e], x[e] * x[e]);
+        } else {  // pairs i and i + 64 of one lane, whose values lie 16 lanes apart here: both lanes add them in the order of i
+            static_assert(D == 256, "");
+            const bool up = threadIdx.x & 16;
+            const float x2 = __shfl_xor(x[e], 16, 64), y2 = __shfl_xor(y[e], 16, 64);
+            const float a = up ? x2 : x[e], b = up ? x[e] : x2, c = up ? y2 : y[e], d = up ? y[e] : y2;
+            p[e] = __builtin_fmaf(d, d, __builtin_fmaf(c, c, __builtin_fmaf(b, b, a * a)));
+        }
+#pragma unroll
+        for (int o = D == 64 ? 4 : 8; o > 0; o >>= 1) p[e] += __shfl_xor(p[e], o, 64);
+    }
+    return (p[0] + p[2]) + (p[1] + p[3]);
+}
+
 template <typename T, typename KT, int D>
 __global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int Hkv, int parts, double log2_theta, float eps, int qk_norm, float k_scale, float v_scale) {
     constexpr int Bk = 16, LPH = D / 8, HALF = D / 2, ROWS = 256 / LPH, VW = 16 / sizeof(T);  // ROWS: heads of a pass; VW: elements of 16 bytes
-    __shared__ double turns[HALF];
+    __shared__ double frequency[HALF];
     __shared__ __attribute__((aligned(16))) T tile[4][Bk][D];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = blockIdx.x * kWindow;
     const int n_rot = Hq + Hkv;
     if ((int)blockIdx.y < parts) {
-        for (int i = threadIdx.x; i < HALF; i += 256) turns[i] = turns_per_position(i, D, log2_theta);
+        for (int i = threadIdx.x; i < HALF; i += 256) frequency[i] = frequency_of(i, D, log2_theta);
         __syncthreads();
         // Rotated heads of this part, [h0, h1): with fewer than 16 lanes to a head the lanes of a row take neighbouring heads.
         constexpr int HPR = ROWS > kWindow ? ROWS / kWindow : 1;  // heads of a row at a time
@@ -253,7 +281,7 @@ __global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int
             const bool write = slot >= 0 && slot < a.n_slots;
             float cs[4], sn[4], wq[2][4], wk[2][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) turn_of(pos, turns[i4 + e], &cs[e], &sn[e]);
+            for (int e = 0; e < 4; ++e) angle_of(pos, frequency[i4 + e], &cs[e], &sn[e]);
             if (qk_norm)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -280,12 +308,7 @@ __global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int
                     Quad<T>::get(lo[u], x);
                     Quad<T>::get(up[u], y);
                     if (qk_norm) {
-                        float ss = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) ss += x[e] * x[e] + y[e] * y[e];
-#pragma unroll
-                        for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-                        const float inv = rsqrtf(ss / (float)D + eps);
+                        const float inv = rsqrtf(sum_of_squares<D>(x, y) / (float)D + eps);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             x[e] = x[e] * inv * (h < Hq ? wq[0][e] : wk[0][e]);
@@ -1008,8 +1031,8 @@ template <typename T, typename KT>
 static bool append_window(const Dims &dm, const AppendArgs &a, hipStream_t st) {
     if (dm.Bk != 16 || a.ld * (int64_t)sizeof(T) % 16) return false;
     const int windows = (a.R + kWindow - 1) / kWindow;
-    // Of the heads: four workgroups to a CU, as long as a part has a rotated head for every wave's turn.  5300 rows of 80 heads 53 us (1 to a CU 66, 16 to a CU 56),
-    // 1145 rows 14.6 (1 to a CU 18.6), 16384 rows of 48 heads 92 (16 to a CU 98).
+    // Of the heads: four workgroups to a CU, as long as a part has a rotated head for every wave's turn.  5300 rows of 80 heads 54 us (1 to a CU 68, 16 to a CU 58),
+    // 1145 rows 15.4 (1 to a CU 19.7), 16384 rows of 48 heads 92 (16 to a CU 98).
     int parts = 1;
     while (windows * parts < 1024 && 2 * parts <= (dm.Hq + dm.Hkv + 3) / 4) parts *= 2;
     const dim3 grid(windows, parts + std::min(parts, dm.Hkv));

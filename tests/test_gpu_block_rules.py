@@ -1,9 +1,12 @@
-"""What include/icarus_blocks.h promises beyond each operator's values."""
+"""What include/icarus_blocks.h promises beyond each operator's values: results that do not go by hints, cache entries that do not go by the call that
+wrote them."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_block_ops import DEV, i32, make, random_pool
+import block_reference as ref
+from paper_2603_13281_amd import binding
+from test_gpu_block_ops import DEV, host, i32, make, random_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -31,4 +34,72 @@ def test_attention_does_not_go_by_the_hint(kw, rows, top, unit):
     want = layer.attn_blocks(q, pool, table, kv, i32(start), blocks, counts)
     for hint in (1, 2, 4, 9, 25, 1000):
         assert same_bits(layer.attn_blocks(q, pool, table, kv, i32(start), blocks, counts, seq_rows=hint), want), hint
+    layer.close()
+
+
+# ---- one cache ------------------------------------------------------------------------------------------------------------
+
+def _projecting(seed, Hq, Hkv, D, bk, num_blocks, bf16, fp8=False, qk_norm=False, scale=1.0, mode=0):
+    """A layer whose keys and values are known before the cache: each row of W_k and W_v has one element, and hidden states of 1 and -1 stay what they
+    are under the norm, so that every projection is an element or its negative, exactly."""
+    dt = torch.bfloat16 if bf16 else torch.float32
+    gen = torch.Generator().manual_seed(seed)
+    d = 256
+    column = {p: torch.randint(0, d, (Hkv * D,), generator=gen) for p in "kv"}
+    element = {p: torch.randn(Hkv * D, generator=gen).to(dt) for p in "kv"}
+    w = {p: torch.zeros(n, m, dtype=dt) for p, n, m in (("q", Hq * D, d), ("k", Hkv * D, d), ("v", Hkv * D, d), ("o", d, Hq * D), ("gate", d, d), ("up", d, d), ("down", d, d))}
+    for p in "kv":
+        w[p][torch.arange(Hkv * D), column[p]] = element[p]
+    w["norm_attn"], w["norm_ffn"] = torch.ones(d, dtype=dt), torch.ones(d, dtype=dt)
+    if qk_norm:
+        w["q_norm"], w["k_norm"] = ((1 + 0.2 * torch.randn(D, generator=gen)).to(dt) for _ in range(2))
+    cfg = binding.LayerConfig(d_model=d, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=D, d_ffn=d, block_size=bk, num_blocks=num_blocks, bf16=bf16, qk_norm=qk_norm, max_position=1 << 20,
+                              rope_theta=5e5, rms_eps=0.0, kv_fp8=fp8, k_scale=scale, v_scale=scale)
+    layer = binding.IcarusLayer(cfg, {n: t.to(DEV) for n, t in w.items()})
+    layer.set_kernel_mode(mode)
+    return layer, column, element
+
+
+@pytest.mark.parametrize("kw", [dict(Hq=8, Hkv=8, D=128, bk=16, bf16=True), dict(Hq=8, Hkv=8, D=128, bk=16, bf16=True, qk_norm=True),
+                                dict(Hq=64, Hkv=8, D=128, bk=16, bf16=True, qk_norm=True),
+                                dict(Hq=8, Hkv=4, D=128, bk=16, bf16=True, qk_norm=True, fp8=True, scale=0.02), dict(Hq=4, Hkv=4, D=128, bk=16, bf16=False, qk_norm=True),
+                                dict(Hq=4, Hkv=4, D=64, bk=16, bf16=False), dict(Hq=4, Hkv=4, D=64, bk=16, bf16=False, qk_norm=True), dict(Hq=4, Hkv=4, D=64, bk=16, bf16=True, qk_norm=True),
+                                dict(Hq=4, Hkv=2, D=256, bk=16, bf16=True, qk_norm=True), dict(Hq=4, Hkv=2, D=256, bk=16, bf16=False, qk_norm=True),
+                                dict(Hq=4, Hkv=2, D=192, bk=16, bf16=False, qk_norm=True), dict(Hq=6, Hkv=2, D=36, bk=5, bf16=False, qk_norm=True),
+                                dict(Hq=8, Hkv=8, D=128, bk=16, bf16=False, qk_norm=True, mode=1), dict(Hq=4, Hkv=4, D=64, bk=16, bf16=False, fp8=True, qk_norm=True)], ids=str)
+def test_appended_entries_are_prefills(kw):
+    """The same projections at the same positions, appended here and by icarus_prefill_kv and icarus_decode_step: the same cache, bit for bit."""
+    print("case:", kw, flush=True)
+    ctx, new = [0, 99990, 131, 5000], [40, 300, 17, 1]
+    bk = kw["bk"]
+    used = [ref.blocks_of(c + n + 1, bk) - c // bk for c, n in zip(ctx, new)]
+    layer, column, element = _projecting(3, num_blocks=1 + sum(used), **kw)
+    c, rng = layer.cfg, np.random.default_rng(4)
+    table = np.zeros((4, max(ref.blocks_of(a + n + 1, bk) for a, n in zip(ctx, new))), dtype=np.int64)  # earlier positions: block 0, which holds zeros
+    ids, at = 1 + rng.permutation(sum(used)), 0
+    for s in range(4):
+        table[s, ctx[s] // bk: ctx[s] // bk + used[s]] = ids[at:at + used[s]]
+        at += used[s]
+    pools = [torch.zeros(c.pool_shape(), dtype=c.pool_dtype, device=DEV) for _ in range(2)]
+
+    def both(starts, counts, decode):
+        x = torch.tensor(rng.integers(0, 2, (sum(counts), c.d_model)) * 2 - 1, dtype=torch.float32).to(c.torch_dtype)
+        pos = np.concatenate([np.arange(a, a + n) for a, n in zip(starts, counts)])
+        seq = np.repeat(np.arange(4), counts)
+        if decode:
+            layer.decode_step(pools[0], i32(table), starts, seq, [-1] * len(seq), x.to(DEV))
+        else:
+            layer.prefill_kv(pools[0], i32(table), starts, counts, x.to(DEV), want_out=False)
+        kv = [x[:, column[p]] * element[p] for p in "kv"]
+        qkv = torch.cat([torch.zeros(len(pos), c.n_q_heads * c.head_dim, dtype=c.torch_dtype), *kv], 1).to(DEV)
+        slot = table[seq, pos // bk] * bk + pos % bk
+        layer.rope_append(qkv, i32(pos), torch.tensor(slot, dtype=torch.int64, device=DEV), pools[1])
+
+    both(ctx, new, False)
+    both([a + n for a, n in zip(ctx, new)], [1] * 4, True)
+    torch.cuda.synchronize()
+    a, b = (host(p.view(torch.float8_e4m3fn) if c.kv_fp8 else p) for p in pools)
+    assert np.abs(a[1:]).max() > 0 and np.array_equal(a[:, :, 1], b[:, :, 1])      # values: the projections are what they were made to be
+    assert np.array_equal(a[:, :, 0], b[:, :, 0]), ((a != b).mean(), np.abs(a - b).max())
+    assert same_bits(*pools)
     layer.close()
