@@ -104,8 +104,8 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
 
 /* out[r, h] = softmax(q[r, h] K^T / sqrt(D)) V over the positions below kv_lens[s] of the blocks that blocks[s][kv-head of h][0 .. counts[s]) names, for
  * the rows r of each sequence s.  S, R, the kv-heads and max_selected say how the sums of a list are split: calls that differ in one of them agree up to rounding.  Entries outside the table, blocks outside the pool and positions from kv_lens[s] on are
- * left out; a block named twice counts twice.  A row that has nothing to attend to becomes zeros; rows of no sequence keep
- * what out holds.
+ * left out; a block named twice counts twice.  A row that has nothing to attend to, or
+ * only scores of minus infinity, becomes zeros; a NaN or a score of plus infinity makes NaN, as in the formula; rows of no sequence keep what out holds.
  *   blocks, counts   device int32 [S, Hkv, max_selected] and [S], as icarus_select_blocks gives them (in any order)
  *   seq_rows         about the most rows of a sequence, 0 if unknown: sizes the launch
  *   out              device [R, Hq, D], no memory of q

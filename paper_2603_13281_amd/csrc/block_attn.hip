@@ -50,14 +50,15 @@ __global__ void __launch_bounds__(256) k_block_attn_generic(BlockAttnArgs a, int
                 most = fmaxf(most, dot);
             }
             const float m_new = fmaxf(m, block_max(most, red));
-            if (m_new == -INFINITY) continue;  // nothing yet
+            const float m_ref = m_new == -INFINITY ? 0.f : m_new;  // nothing yet, or nothing but NaN, which the maximum passes over
             float sum = 0.f;
             for (int t = threadIdx.x; t < cnt; t += 256) {
-                const float p = __expf(sc[t] - m_new);
+                const float p = __expf(sc[t] - m_ref);
                 sc[t] = p;
                 sum += p;
             }
             sum = block_sum(sum, red);
+            if (m_new == -INFINITY && sum == 0.f) continue;
             const float alpha = m == -INFINITY ? 0.f : __expf(m - m_new);
             l = l * alpha + sum;
             acc *= alpha;
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(256) k_block_attn_generic(BlockAttnArgs a, int
                 for (int t = 0; t < cnt; ++t)
                     if (where[t] >= 0) acc += sc[t] * KVElem<KT>::ld(pool + where[t] + (size_t)threadIdx.x * Bk, v_scale);
         }
-        if (threadIdx.x < D) Elem<T>::st((T *)a.out + ((size_t)row * Hq + h) * D + threadIdx.x, l > 0.f ? acc / l : 0.f);
+        if (threadIdx.x < D) Elem<T>::st((T *)a.out + ((size_t)row * Hq + h) * D + threadIdx.x, l == 0.f ? 0.f : acc / l);  // a NaN stays one
     }
 }
 

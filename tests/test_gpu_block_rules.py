@@ -1,12 +1,12 @@
 """What include/icarus_blocks.h promises beyond each operator's values: results that do not go by hints, cache entries that do not go by the call that
-wrote them."""
+wrote them, NaN that is not hidden."""
 import numpy as np
 import pytest
 import torch
 
 import block_reference as ref
 from paper_2603_13281_amd import binding
-from test_gpu_block_ops import DEV, host, i32, make, random_pool
+from test_gpu_block_ops import DEV, E24, host, i32, make, pool_values, random_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -102,4 +102,46 @@ def test_appended_entries_are_prefills(kw):
     assert np.abs(a[1:]).max() > 0 and np.array_equal(a[:, :, 1], b[:, :, 1])      # values: the projections are what they were made to be
     assert np.array_equal(a[:, :, 0], b[:, :, 0]), ((a != b).mean(), np.abs(a - b).max())
     assert same_bits(*pools)
+    layer.close()
+
+
+# ---- NaN and infinities in what is read -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(Hq=40, Hkv=2), dict(D=64), dict(D=64, bf16=False), dict(bf16=False), dict(bk=32), dict(bk=8), dict(D=36, bk=5),
+                                dict(D=36, bk=5, fp8=True), dict(mode=1), dict(mode=1, bf16=False)], ids=str)
+@pytest.mark.parametrize("top", [7, 120])
+def test_attention_does_not_hide_nan(kw, top):
+    """A NaN or an infinite score where it counts gives NaN, as the formula does, in these rows and heads alone; 120 entries of few sequences: in parts that are joined."""
+    print("case:", kw, top, flush=True)
+    layer = make(num_blocks=200, **kw)
+    c, rng = layer.cfg, np.random.default_rng(top)
+    bk, D, Hkv, g = c.block_size, c.head_dim, c.n_kv_heads, c.n_q_heads // c.n_kv_heads
+    pool = random_pool(layer, rng)
+    nan = torch.tensor(float("nan")).to(torch.float8_e4m3fn).view(torch.uint8).item() if c.kv_fp8 else float("nan")
+    table = rng.permutation(195).reshape(5, 39)
+    kv, rows = np.full(5, 39 * bk), [3, 2, 2, 1, 2]
+    start = np.concatenate([[0], np.cumsum(rows)])
+    blocks = rng.integers(0, 38, (5, Hkv, top))
+    blocks[1, :, top // 2] = 38                                          # listed, with a NaN key for one kv-head
+    pool.view(200, Hkv, 2, bk, D)[table[1, 38], Hkv - 1, 0, 1, 2] = nan
+    for b in table[2]:                                                   # nothing but NaN keys for one kv-head
+        pool.view(200, Hkv, 2, bk, D)[b, 0, 0, :, 0] = nan
+    pool.view(200, Hkv, 2, D, bk)[table[3, blocks[3, 0, 0]], 0, 1, 3, bk - 1] = nan  # a NaN value: of one channel
+    q = torch.tensor(rng.standard_normal((start[-1], c.n_q_heads, D)), dtype=torch.float32).to(c.torch_dtype).to(DEV)
+    q[0, 1, 5] = float("nan")                                            # a query
+    q[1, c.n_q_heads - 1, 0] = float("inf")                              # scores of both infinities
+    q[2, 0] = float("nan")
+    out = torch.full(q.shape, 7.0, dtype=c.torch_dtype, device=DEV)
+    layer.attn_blocks(q, pool, i32(table), i32(kv), i32(start), i32(blocks), i32([top] * 5), out)
+    got = host(out)
+    with np.errstate(invalid="ignore"):
+        want, weight, size = ref.attend(host(q), pool_values(layer, pool), table, kv, start, blocks, [top] * 5, bk, np.zeros(q.shape))
+    bad = np.isnan(want)
+    heads = bad.any(-1)                                                  # what the above says, of the oracle
+    assert heads[0, 1] and heads[1, -1] and heads[2, 0] and heads[3:5, -g:].all() and heads[5:7, :g].all() and heads[7, :g].all() and not heads[8:].any()
+    assert bad[7, :g].sum() == g and heads.sum() == 3 + 2 * g + 2 * g + g
+    assert np.array_equal(np.isnan(got), bad)
+    ds = (D + 3) * E24 * size                                            # run_attend's bound
+    tol = (2.0 ** -8 if c.bf16 else E24) * np.abs(want) + weight * (2 * ds + 2.0 ** -17 + top * bk * E24 + (2.0 ** -8 if c.bf16 else 0.0))
+    assert (np.abs(got - want) <= tol)[~bad].all()
     layer.close()
