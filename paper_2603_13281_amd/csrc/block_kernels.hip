@@ -169,7 +169,7 @@ template <typename T, typename KT>
 __global__ void __launch_bounds__(256) k_append(AppendArgs a, int Hq, int Hkv, int D, int Bk, double log2_theta, float eps, int qk_norm,
                                                 float k_scale, float v_scale) {
     __shared__ float cos_t[128], sin_t[128];
-    const int row = blockIdx.x, h = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, half = D >> 1;
+    const int row = a.first + blockIdx.x, h = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, half = D >> 1;
     const int pos = a.row_pos[row];
     if (pos < 0) return;
     if ((int)blockIdx.y * 4 < Hq + Hkv) {  // the row's angles, for the four heads
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(256) k_append_window(AppendArgs a, int Hq, int
     constexpr int Bk = 16, LPH = D / 8, HALF = D / 2, ROWS = 256 / LPH, VW = 16 / sizeof(T);  // ROWS: heads of a pass; VW: elements of 16 bytes
     __shared__ double frequency[HALF];
     __shared__ __attribute__((aligned(16))) T tile[4][Bk][D];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = blockIdx.x * kWindow;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = a.first + blockIdx.x * kWindow;
     const int n_rot = Hq + Hkv;
     if ((int)blockIdx.y < parts) {
         for (int i = threadIdx.x; i < HALF; i += 256) frequency[i] = frequency_of(i, D, log2_theta);
@@ -1028,9 +1028,9 @@ hipError_t launch_extend(const ExtendArgs &a, hipStream_t st) {
 }
 
 template <typename T, typename KT>
-static bool append_window(const Dims &dm, const AppendArgs &a, hipStream_t st) {
+static bool append_window(const Dims &dm, const AppendArgs &a, int rows, hipStream_t st) {
     if (dm.Bk != 16 || a.ld * (int64_t)sizeof(T) % 16) return false;
-    const int windows = (a.R + kWindow - 1) / kWindow;
+    const int windows = (rows + kWindow - 1) / kWindow;
     // Of the heads: four workgroups to a CU, as long as a part has a rotated head for every wave's turn.  5300 rows of 80 heads 54 us (1 to a CU 68, 16 to a CU 58),
     // 1145 rows 15.4 (1 to a CU 19.7), 16384 rows of 48 heads 92 (16 to a CU 98).
     int parts = 1;
@@ -1050,13 +1050,19 @@ static bool append_window(const Dims &dm, const AppendArgs &a, hipStream_t st) {
     }
 }
 
-hipError_t launch_append(const Dims &dm, bool generic, const AppendArgs &a, hipStream_t st) {
-    bool done = false;
-    if (!generic) DISPATCH_TK(dm.bf16, dm.kv8, done = (append_window<T, KT>(dm, a, st)));
-    if (!done)
-        DISPATCH_TK(dm.bf16, dm.kv8, hipLaunchKernelGGL((k_append<T, KT>), dim3(a.R, (dm.Hq + 2 * dm.Hkv + 3) / 4), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D,
-                                                        dm.Bk, log2(dm.theta), dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale));
-    return hipGetLastError();
+hipError_t launch_append(const Dims &dm, bool generic, AppendArgs a, hipStream_t st) {
+    constexpr int kRows = 1 << 23;  // of a launch, whole windows: its work items in one direction have to be fewer than 2^32
+    for (a.first = 0; a.first < a.R; a.first += kRows) {
+        const int rows = std::min(kRows, a.R - a.first);
+        bool done = false;
+        if (!generic) DISPATCH_TK(dm.bf16, dm.kv8, done = (append_window<T, KT>(dm, a, rows, st)));
+        if (!done)
+            DISPATCH_TK(dm.bf16, dm.kv8, hipLaunchKernelGGL((k_append<T, KT>), dim3(rows, (dm.Hq + 2 * dm.Hkv + 3) / 4), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D,
+                                                            dm.Bk, log2(dm.theta), dm.eps, dm.qk_norm, dm.k_scale, dm.v_scale));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 constexpr int kBoundsWgs = 4096;

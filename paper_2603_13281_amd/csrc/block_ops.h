@@ -18,9 +18,10 @@ struct AppendArgs {
     const int32_t *row_pos; const int64_t *row_slot;
     void *q_out, *pool; int64_t n_slots;           // slots of the pool
     const void *q_norm, *k_norm;                   // read with Dims::qk_norm
+    int first;                                     // row that the launch begins with
 };
 // generic, here and below: only the kernels for any shape
-hipError_t launch_append(const Dims &dm, bool generic, const AppendArgs &a, hipStream_t st);
+hipError_t launch_append(const Dims &dm, bool generic, AppendArgs a, hipStream_t st);
 
 struct BoundsArgs {
     const void *pool; const int32_t *bt; int max_blocks, num_blocks, S;

@@ -145,3 +145,28 @@ def test_attention_does_not_hide_nan(kw, top):
     tol = (2.0 ** -8 if c.bf16 else E24) * np.abs(want) + weight * (2 * ds + 2.0 ** -17 + top * bk * E24 + (2.0 ** -8 if c.bf16 else 0.0))
     assert (np.abs(got - want) <= tol)[~bad].all()
     layer.close()
+
+
+# ---- sizes ------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw,rows", [(dict(Hq=1, Hkv=1, D=64), (1 << 23) + 237), (dict(Hq=1, Hkv=1, D=2, bk=5, bf16=False), (1 << 24) + 37)], ids=str)
+def test_append_of_more_rows_than_a_launch_holds(kw, rows):
+    """Every row is there, and those around the borders, with blocks that go on across one, are the rows of a small call."""
+    print("case:", kw, rows, flush=True)
+    layer = make(num_blocks=100, **kw)
+    c, edge = layer.cfg, 1 << 23
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    qkv = torch.randn(rows, 3 * c.head_dim, generator=gen, device=DEV).to(c.torch_dtype)
+    pos = (torch.arange(rows, device=DEV) % 100000).int()
+    slot = torch.full((rows,), -1, dtype=torch.int64, device=DEV)
+    parts = [slice(0, 64), slice(edge - 40, edge + 40), slice(rows - 150, rows)]
+    for part, at in zip(parts, (3, 101, 250)):
+        slot[part] = at + torch.arange(part.stop - part.start, device=DEV)
+    q = torch.full((rows, 1, c.head_dim), float("nan"), dtype=c.torch_dtype, device=DEV)
+    pools = [torch.zeros(c.pool_shape(), dtype=c.pool_dtype, device=DEV) for _ in range(2)]
+    layer.rope_append(qkv, pos, slot, pools[0], q)
+    assert not bool(torch.isnan(q).any())
+    for part in parts:
+        assert same_bits(layer.rope_append(qkv[part].clone(), pos[part].clone(), slot[part].clone(), pools[1]), q[part])
+    assert same_bits(*pools) and int((pools[1] != 0).sum()) >= 280 * 2 * c.head_dim
+    layer.close()
