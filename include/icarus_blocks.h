@@ -18,8 +18,9 @@
  * memory may overlap; a workspace belongs to one call at a time.
  * Pointers: float and code arrays, pool and workspace 16-byte aligned; integer arrays and scales aligned to their element.
  *
- * A call takes up to 65535 sequences (icarus_extend_sequences: 2^29), 2^29 rows, 2^30 queries of a kv-head, 2^22 blocks of a sequence and in the
- * lists of icarus_attn_blocks 2^20 parts of 256 entries over sequences and kv-heads; more is ICARUS_ERR_UNSUPPORTED.
+ * A call takes up to 65535 sequences (icarus_extend_sequences: 2^29, as many free ids), 2^29 rows and 2^30 queries of a kv-head; a table that
+ * icarus_select_blocks chooses from up to 2^22 blocks of a sequence, and it makes up to 2^22 - 1 lists (sequences x kv-heads) of 2^22 entries; icarus_attn_blocks takes
+ * lists of 2^22 entries, and 2^20 parts of 256 entries (an empty list: one) over all of them.  More is ICARUS_ERR_UNSUPPORTED, and a workspace for more has size 0.
  *
  * What the device finds out of range is not followed: a block id outside the pool, a position beyond the table, a slot outside
  * the pool or a negative length are skipped as each call says.  Results never depend on max_new and seq_rows, which

@@ -2014,7 +2014,12 @@ bool overlap(const void *a, size_t an, const void *b, size_t bn) {
     return x < y + bn && y < x + an;
 }
 constexpr int kBlockMaxSeqs = 65535, kBlockMaxRows = 1 << 29;  // sums of two counts stay in 32 bits
-constexpr int kBlockMaxTable = 1 << 22;                        // blocks of a sequence, entries of a list
+constexpr int kBlockMaxTable = 1 << 22;                        // blocks of a sequence that is chosen from, entries of a list
+constexpr int kBlockMaxLists = (1 << 22) - 1;                  // to choose: a workgroup of 1024 each, and a launch has fewer than 2^32 work items
+// Parts of 256 entries in all lists, an empty one counts as one: they are counted in 32 bits, times the splits and tiles of a launch.
+bool too_many_parts(const icarus_ctx *ctx, int S, int max_selected) {
+    return (int64_t)S * ctx->cfg.n_kv_heads * std::max(1, (int)(((int64_t)max_selected + 255) / 256)) > 1 << 20;
+}
 bool too_many_queries(const icarus_ctx *ctx, int R) { return (int64_t)R * (ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads) > 1 << 30; }  // counted in 32 bits
 }  // namespace
 
@@ -2061,7 +2066,7 @@ icarus_status icarus_rope_append(icarus_ctx *ctx, const void *qkv, int64_t ld, i
     const size_t es = c.dtype == ICARUS_BF16 ? 2 : 4, head = (size_t)c.head_dim * es;
     if (overlap(q_out, (size_t)R * c.n_q_heads * head, qkv, ((size_t)(R - 1) * ld) * es + (size_t)(c.n_q_heads + 2 * c.n_kv_heads) * head))
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "q_out must not share memory with qkv");
-    AppendArgs a{qkv, ld, R, row_pos, row_slot, q_out, kv_pool, (int64_t)c.num_blocks * c.block_size, ctx->base.q_norm, ctx->base.k_norm};
+    AppendArgs a{qkv, ld, R, row_pos, row_slot, q_out, kv_pool, (int64_t)c.num_blocks * c.block_size, ctx->base.q_norm, ctx->base.k_norm, 0};
     PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ROPE_APPEND, launch_append(ctx->dm, ctx->mode != 0, a, (hipStream_t)stream));
     return ICARUS_OK;
 }
@@ -2083,7 +2088,7 @@ icarus_status icarus_key_bounds(icarus_ctx *ctx, const void *kv_pool, const int3
 }
 
 size_t icarus_select_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t max_blocks) {
-    if (!ctx || S < 0 || max_blocks < 0) return 0;
+    if (!ctx || S < 0 || max_blocks < 0 || S > kBlockMaxSeqs || max_blocks > kBlockMaxTable) return 0;
     return align_up((size_t)S * ctx->cfg.n_kv_heads * key_pitch(max_blocks) * 4, 256) + 256;
 }
 
@@ -2096,8 +2101,9 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
     if (S < 0 || max_blocks < 0 || R < 0 || seq_rows < 0 || first < 0 || last < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
     if (top_k < 1 || (int64_t)first + last > top_k)
         return fail(ctx, ICARUS_ERR_INVALID_ARG, "top_k %d must be positive and hold the first %d and the last %d blocks", top_k, first, last);
-    if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_blocks > kBlockMaxTable || top_k > kBlockMaxTable)
-        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "at most %d sequences, %d rows and %d blocks of a sequence per call", kBlockMaxSeqs, kBlockMaxRows, kBlockMaxTable);
+    if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_blocks > kBlockMaxTable || top_k > kBlockMaxTable || (int64_t)S * ctx->cfg.n_kv_heads > kBlockMaxLists)
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d sequences of %d kv-heads, %d rows, %d blocks of a sequence, lists of %d: at most %d sequences, %d lists, %d rows and %d blocks and entries per call",
+                    S, ctx->cfg.n_kv_heads, R, max_blocks, top_k, kBlockMaxSeqs, kBlockMaxLists, kBlockMaxRows, kBlockMaxTable);
     if (too_many_queries(ctx, R)) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d rows: at most 2^30 queries of a kv-head per call", R);
     if (S == 0) return ICARUS_OK;
     if (any_null({codes, scales, kv_lens, row_start, blocks, counts, workspace}) || (max_blocks && !block_tables) || (R && !q))
@@ -2114,7 +2120,7 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
 }
 
 size_t icarus_attn_blocks_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t R, int32_t max_selected) {
-    if (!ctx || S < 0 || R < 0 || max_selected < 0) return 0;
+    if (!ctx || S < 0 || R < 0 || max_selected < 0 || S > kBlockMaxSeqs || R > kBlockMaxRows || max_selected > kBlockMaxTable || too_many_parts(ctx, S, max_selected)) return 0;
     return block_attn_workspace(ctx->dm, S, R, max_selected);
 }
 
@@ -2126,7 +2132,7 @@ icarus_status icarus_attn_blocks(icarus_ctx *ctx, const void *q, const void *kv_
     std::lock_guard<std::mutex> lk(ctx->mu);
     if (S < 0 || max_blocks < 0 || R < 0 || seq_rows < 0 || max_selected < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
     const icarus_layer_config &c = ctx->cfg;
-    if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_selected > kBlockMaxTable || (int64_t)S * c.n_kv_heads * (max_selected / 256 + 1) > 1 << 20)
+    if (S > kBlockMaxSeqs || R > kBlockMaxRows || max_selected > kBlockMaxTable || too_many_parts(ctx, S, max_selected))
         return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d sequences, %d kv-heads, %d rows, lists of %d blocks: at most %d sequences and %d rows per call, and 2^20 times 256 entries in all lists",
                     S, c.n_kv_heads, R, max_selected, kBlockMaxSeqs, kBlockMaxRows);
     if (too_many_queries(ctx, R)) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d rows: at most 2^30 queries of a kv-head per call", R);

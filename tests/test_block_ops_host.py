@@ -189,3 +189,48 @@ def test_reference_attend_is_softmax():
     v = np.concatenate([pool[3, 0, 1].reshape(D, bk).T, pool[1, 0, 1].reshape(D, bk).T[:2]])
     w = np.exp(q[0] @ k.T / np.sqrt(D))
     assert np.allclose(out[0], w @ v / w.sum(-1, keepdims=True), atol=1e-14)
+
+
+# ---- limits -----------------------------------------------------------------------------------------------------------
+
+def test_limits_are_the_stated_ones():
+    """Each limit of the header: one more is refused as unsupported, and at the limit the call goes on to look at its arrays (null here)."""
+    lib, big = binding._lib, 1 << 29
+    layer = _layer()
+
+    def extend(S=1, free=1, rows=1):
+        return lib.icarus_extend_sequences(layer._h, S, None, None, None, None, 1, None, free, None, rows, *[None] * 7)
+
+    def append(R):
+        return lib.icarus_rope_append(layer._h, None, 768, R, None, None, None, None, None)
+
+    def bounds(S):
+        return lib.icarus_key_bounds(layer._h, None, None, 1 << 30, S, None, None, 0, None, None, None)
+
+    def select(S=1, mb=1, R=1, k=1):
+        return lib.icarus_select_blocks(layer._h, None, None, None, None, mb, S, None, R, None, 0, k, 0, 0, None, None, None, 0, None)
+
+    def attend(S=1, R=1, k=1, mb=1 << 30):
+        return lib.icarus_attn_blocks(layer._h, None, None, None, mb, S, None, R, None, 0, None, None, k, None, None, 0, None)
+
+    cases = [(extend, "S", big), (extend, "free", big), (extend, "rows", big), (append, "R", big), (bounds, "S", 65535), (select, "S", 65535), (select, "mb", 1 << 22),
+             (select, "k", 1 << 22), (select, "R", 1 << 28), (attend, "S", 65535), (attend, "R", 1 << 28), (attend, "k", 1 << 22)]   # 4 heads share a kv-head: 2^30 queries
+    for call, name, most in cases:
+        _refused(layer, call(**{name: most}), "INVALID_ARG")
+        _refused(layer, call(**{name: most + 1}), "UNSUPPORTED")
+    layer.close()
+    layer = _layer(n_q_heads=32, n_kv_heads=32, head_dim=2)
+    for S, k in ((1 << 15, 0), (1 << 15, 256), (1 << 14, 257), (1 << 14, 512), (1, 1 << 22)):
+        _refused(layer, attend(S=S, k=k), "INVALID_ARG")
+        assert lib.icarus_attn_blocks_workspace_bytes(layer._h, S, 1, k) > 0
+    for S, k in (((1 << 15) + 1, 0), ((1 << 15) + 1, 256), (1 << 15, 257), ((1 << 14) + 1, 512), (3, 1 << 22)):
+        _refused(layer, attend(S=S, k=k), "UNSUPPORTED")
+        assert lib.icarus_attn_blocks_workspace_bytes(layer._h, S, 1, k) == 0
+    layer.close()
+    layer = _layer(n_q_heads=65, n_kv_heads=65, head_dim=2)
+    _refused(layer, select(S=((1 << 22) - 1) // 65), "INVALID_ARG")
+    _refused(layer, select(S=((1 << 22) - 1) // 65 + 1), "UNSUPPORTED")
+    assert lib.icarus_select_workspace_bytes(layer._h, 1, 1 << 22) > 0
+    for S, mb in ((1, (1 << 22) + 1), (1, 2 ** 31 - 1), (65536, 1)):
+        assert lib.icarus_select_workspace_bytes(layer._h, S, mb) == 0
+    layer.close()
