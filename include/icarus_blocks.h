@@ -24,7 +24,7 @@
  *
  * What the device finds out of range is not followed: a block id outside the pool, a position beyond the table, a slot outside
  * the pool or a negative length are skipped as each call says.  Results never depend on max_new and seq_rows, which
- * only size a launch.
+ * at most size a launch.
  */
 #ifndef ICARUS_BLOCKS_H
 #define ICARUS_BLOCKS_H
@@ -95,7 +95,7 @@ icarus_status icarus_key_bounds(icarus_ctx *ctx, const void *kv_pool, const int3
  *   row_start  device int32 [S + 1], not decreasing, within 0 .. R
  *   blocks     device int32 [S, Hkv, top_k]: indexes into the sequence's row of the table, ascending, -1 behind the last
  *   counts     device int32 [S]: how many, min(top_k, number of blocks)
- *   seq_rows   about the most rows of a sequence, 0 if unknown: sizes the launch
+ *   seq_rows   as icarus_attn_blocks takes it, not negative; the launches here go by S and max_blocks alone
  *   workspace  at least icarus_select_workspace_bytes(ctx, S, max_blocks) */
 size_t icarus_select_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t max_blocks);
 icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t *codes, const float *scales, const int32_t *block_tables,

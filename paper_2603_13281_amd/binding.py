@@ -738,7 +738,7 @@ class IcarusLayer:
 
     def select_blocks(self, q, codes, scales, block_tables, kv_lens, row_start, blocks, counts, first: int = 1, last: int = 2,
                       seq_rows: int = 0, workspace=None):
-        """blocks [S, Hkv, top_k] and counts [S] receive each sequence's selected blocks.  workspace: bytes for one call at a time, by default of its own."""
+        """blocks [S, Hkv, top_k] and counts [S] receive each sequence's selected blocks.  seq_rows: as for attn_blocks, not needed here.  workspace: bytes for one call at a time, by default of its own."""
         S, max_blocks, index = self._table(block_tables)
         R = self._rows(q, "q", index)
         _need(row_start, "row_start", torch.int32, (S + 1,), index)

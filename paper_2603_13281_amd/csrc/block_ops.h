@@ -34,7 +34,7 @@ __host__ __device__ inline int key_pitch(int max_blocks) { return (max_blocks + 
 struct SelectArgs {
     const void *q; const int8_t *codes; const float *scales;
     const int32_t *bt; int max_blocks, num_blocks, S;
-    const int32_t *kv_lens, *row_start; int R, seq_rows, top_k, first, last;
+    const int32_t *kv_lens, *row_start; int R, top_k, first, last;
     int32_t *blocks, *counts;
     float *scores;                                 // workspace [S, Hkv, key_pitch(max_blocks)], 16-byte aligned
 };

@@ -2113,7 +2113,7 @@ icarus_status icarus_select_blocks(icarus_ctx *ctx, const void *q, const int8_t 
         return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays and scales must be aligned to their element");
     const size_t need = icarus_select_workspace_bytes(ctx, S, max_blocks);
     if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
-    SelectArgs a{q, codes, scales, block_tables, max_blocks, ctx->cfg.num_blocks, S, kv_lens, row_start, R, seq_rows, top_k, first, last, blocks, counts,
+    SelectArgs a{q, codes, scales, block_tables, max_blocks, ctx->cfg.num_blocks, S, kv_lens, row_start, R, top_k, first, last, blocks, counts,
                  (float *)workspace};
     PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_select(ctx->dm, ctx->mode != 0, a, (hipStream_t)stream));
     return ICARUS_OK;
