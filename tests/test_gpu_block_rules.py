@@ -6,7 +6,7 @@ import torch
 
 import block_reference as ref
 from paper_2603_13281_amd import binding
-from test_gpu_block_ops import DEV, E24, host, i32, make, pool_values, random_pool
+from test_gpu_block_ops import DEV, E24, _loop, _state, _step, host, i32, make, pool_values, random_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -105,6 +105,30 @@ def test_appended_entries_are_prefills(kw):
     layer.close()
 
 
+@pytest.mark.parametrize("kw", [dict(Hq=8, Hkv=2, qk_norm=True), dict(Hq=8, Hkv=2, fp8=True, qk_norm=True), dict(Hq=4, Hkv=4, D=64, bf16=False), dict(Hq=4, Hkv=2, D=36, bk=5, qk_norm=True),
+                                dict(Hq=4, Hkv=2, D=256), dict(Hq=8, Hkv=2, qk_norm=True, mode=1)], ids=str)
+def test_append_does_not_go_by_what_it_leaves_out(kw):
+    """K and V of rows whose slot is outside the pool, and whole rows with a negative position, hold NaN: the same bits as with anything else there."""
+    print("case:", kw, flush=True)
+    layer = make(num_blocks=64, **kw)
+    c, rng = layer.cfg, np.random.default_rng(6)
+    rows, n_slots, first_k = 75, c.num_blocks * c.block_size, c.n_q_heads * c.head_dim
+    pos, slot = rng.integers(0, 9999, rows), 7 + np.arange(rows)             # runs through several blocks, with these between
+    slot[3::5], slot[11], slot[40] = -1, n_slots, 2 ** 62
+    pos[20:23], pos[50] = -1, -(2 ** 31)
+    qkv = torch.tensor(rng.standard_normal((rows, first_k + 2 * c.n_kv_heads * c.head_dim)), dtype=torch.float32).to(c.torch_dtype).to(DEV)
+    nan = qkv.clone()
+    nan[torch.tensor((slot < 0) | (slot >= n_slots), device=DEV), first_k:] = float("nan")
+    nan[torch.tensor(pos < 0, device=DEV)] = float("nan")
+    results = []
+    for x in (qkv, nan):
+        pool, q = random_pool(layer, np.random.default_rng(7)), torch.full((rows, c.n_q_heads, c.head_dim), 7.0, dtype=c.torch_dtype, device=DEV)
+        layer.rope_append(x, i32(pos), torch.tensor(slot, dtype=torch.int64, device=DEV), pool, q)
+        results.append((pool, q))
+    assert all(same_bits(a, b) for a, b in zip(*results)) and not bool(torch.isnan(results[1][1]).any()) and bool((results[1][1][20:23] == 7).all())
+    layer.close()
+
+
 # ---- NaN and infinities in what is read -----------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(Hq=40, Hkv=2), dict(D=64), dict(D=64, bf16=False), dict(bf16=False), dict(bk=32), dict(bk=8), dict(D=36, bk=5),
@@ -169,4 +193,35 @@ def test_append_of_more_rows_than_a_launch_holds(kw, rows):
     for part in parts:
         assert same_bits(layer.rope_append(qkv[part].clone(), pos[part].clone(), slot[part].clone(), pools[1]), q[part])
     assert same_bits(*pools) and int((pools[1] != 0).sum()) >= 280 * 2 * c.head_dim
+    layer.close()
+
+
+# ---- a graph that outlives its lengths --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw", [dict(Hq=8, Hkv=2), dict(Hq=8, Hkv=2, fp8=True, qk_norm=True), dict(Hq=4, Hkv=4, D=64, bf16=False), dict(Hq=6, Hkv=2, D=96)], ids=str)
+@pytest.mark.parametrize("columns", [300, 1500, 40000])
+def test_captured_step_over_a_wide_table(kw, columns):
+    """A table as wide as its sequences may become: scores and choice are launches of their own.  Every replay is the eager step, and the step over a
+    table that is as wide as its sequences are, bit for bit."""
+    print("case:", kw, columns, flush=True)
+    layer = make(num_blocks=400, **kw)
+    loops = [_loop(layer, 5) for _ in range(3)]                              # narrow, wide, wide and captured
+    for b in loops[1:]:
+        b["table"] = torch.cat([b["table"], torch.full((b["table"].shape[0], columns - 40), -1, dtype=torch.int32, device=DEV)], 1).contiguous()
+    _step(layer, _loop(layer, 5))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _step(layer, loops[2])
+    for i in range(18):
+        for b in loops:
+            b["qkv"].mul_(-1)
+        _step(layer, loops[0])
+        _step(layer, loops[1])
+        graph.replay()
+        if i % 4 == 0:
+            torch.cuda.synchronize()
+        narrow, eager, replayed = ([x[:, :40] if n == 2 else x for n, x in enumerate(_state(b))] for b in loops)
+        assert all(same_bits(a, b) and same_bits(a, d) for a, b, d in zip(narrow, eager, replayed)), i
+        (loops[2]["out"].float() * 2).sum().item()
     layer.close()
