@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(256) k_block_attn_generic(BlockAttnArgs a, int
 // Items are short -- a list of 64 blocks is 8 groups to a wave -- and what an item waits for before its first key is a chain of reads: its list entry, the block id of the
 // entry, the block.  So while item i is walked, the ids of item i + 1 and its queries, and the list entries of item i + 2 are on their way, and the first blocks of item i + 1
 // are requested before the waves' states of item i are put together.
-// 64 sequences, 1-8 agents, 64 blocks (268 MB): 57.5 us, 4.7 TB/s, of which about 10 us are the first item's start and the last one's end.  Two workgroups to a CU, a buffer of
+// 64 sequences, 1-8 agents, 64 blocks (268 MB): 57.9 us, 4.7 TB/s, of which about 10 us are the first item's start and the last one's end.  Two workgroups to a CU, a buffer of
 // keys and one of values each: 75 us; one with two buffers, each item from nothing: 70-75 us.  More than three tiles: the queries are dealt to
 // workgroups three tiles at a time (16 sequences over an FP8 cache, 72 queries, 256 blocks 39 us; five tiles to a workgroup and half the list 51 us).
 //
@@ -112,11 +112,27 @@ struct Item {
 // One group of two blocks for N query tiles: scores of all of them, one look whether any softmax reference has to move (rare: see compute_group), and then straight-line code in
 // which the weights of one tile and the products of the tile before can be under way together -- with a branch to a tile, as compute_group has it, a wave
 // that is alone on its SIMD waits out every step of every tile.  there: tokens of this lane's block (masked only).
+//
+// Weights and the values' product.  Weights of one bfloat16 (half a step, 2^-8, each) add as much error, squared, as the output's own rounding: 0.0023 of the output
+// where that alone is 0.0017.  bfloat16 values: what the rounding leaves goes through a second product (2^-16; 64 sequences 57.4 -> 57.9 us, 1 sequence 8.2 -> 8.35).  FP8
+// values, whose codes are float16 numbers too: weights in float16 (2^-11, at the same speed; a second product 39 -> 48 us), kLift powers of two up, to at most 2^14, so
+// that only weights below 2^-20 of the reference lose bits to float16's least exponent.
+constexpr float kLift = 6.f;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)lo, (_Float16)hi}); }
+// 8 FP8 codes (two dwords) -> 8 float16, exactly.
+__device__ __forceinline__ uint4 cvt8_f16(uint32_t lo, uint32_t hi) {
+    return make_uint4(__builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true)),
+                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true)));
+}
 template <int NT, int N, bool KV8, bool masked, typename Frag>
 __device__ __forceinline__ void group_of(State<NT> &st, const Frag &f, const bf16x8 (&qr)[NT][kKS], const bf16x8 *__restrict__ qlds, int there, float scale_log2, int lane) {
     const int t0 = 8 * ((lane >> 4) & 1);
     f32x4 sc[N][2];
-    bf16x8 v[kDT];
+    uint4 v[kDT];
 #pragma unroll
     for (int qt = 0; qt < N; ++qt) sc[qt][0] = sc[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -145,12 +161,9 @@ __device__ __forceinline__ void group_of(State<NT> &st, const Frag &f, const bf1
     }
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt) {
-        if constexpr (KV8) v[dt] = cvt8(f.v[dt].x, f.v[dt].y);
-        else v[dt] = f.v[dt];
-        if (masked) {
-            const uint4 r = __builtin_bit_cast(uint4, v[dt]);
-            v[dt] = __builtin_bit_cast(bf16x8, make_uint4(r.x & keep[0], r.y & keep[1], r.z & keep[2], r.w & keep[3]));
-        }
+        if constexpr (KV8) v[dt] = cvt8_f16(f.v[dt].x, f.v[dt].y);
+        else v[dt] = __builtin_bit_cast(uint4, f.v[dt]);
+        if (masked) v[dt] = make_uint4(v[dt].x & keep[0], v[dt].y & keep[1], v[dt].z & keep[2], v[dt].w & keep[3]);
     }
     float mx[N];
     bool move = false;
@@ -184,15 +197,28 @@ __device__ __forceinline__ void group_of(State<NT> &st, const Frag &f, const bf1
     }
 #pragma unroll
     for (int qt = 0; qt < N; ++qt) {
-        const float m_ref = st.m[qt] == -INFINITY ? 0.f : st.m[qt];  // nothing yet: every weight 0
+        const float m_ref = (st.m[qt] == -INFINITY ? 0.f : st.m[qt]) - (KV8 ? kLift : 0.f);  // nothing yet: every weight 0
         float e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 2][i & 3], scale_log2, -m_ref));
-        // rounded to bfloat16 for the matrix cores (half a step, 2^-8, each); the sum takes them as they are
-        const uint4 p = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
-        st.l[qt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        st.l[qt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));  // as they are
+        if constexpr (KV8) {
+            const f16x8 p = __builtin_bit_cast(f16x8, make_uint4(pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]), pack_f16(e[6], e[7])));
 #pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[dt], __builtin_bit_cast(bf16x8, p), st.o[dt][qt], 0, 0, 0);
+            for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v[dt]), p, st.o[dt][qt], 0, 0, 0);
+        } else {
+            uint32_t p[4], rest[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[i] = pack_bf16(e[2 * i], e[2 * i + 1]);
+                rest[i] = pack_bf16(e[2 * i] - __uint_as_float(p[i] << 16), e[2 * i + 1] - __uint_as_float(p[i] & 0xffff0000u));
+            }
+            const bf16x8 hi = __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3])), lo = __builtin_bit_cast(bf16x8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[dt]), hi, st.o[dt][qt], 0, 0, 0);
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[dt]), lo, st.o[dt][qt], 0, 0, 0);
+        }
     }
 }
 

@@ -1,5 +1,7 @@
 """What include/icarus_blocks.h promises beyond each operator's values: results that do not go by hints, cache entries that do not go by the call that
 wrote them, NaN that is not hidden."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -126,6 +128,60 @@ def test_append_does_not_go_by_what_it_leaves_out(kw):
         layer.rope_append(x, i32(pos), torch.tensor(slot, dtype=torch.int64, device=DEV), pool, q)
         results.append((pool, q))
     assert all(same_bits(a, b) for a, b in zip(*results)) and not bool(torch.isnan(results[1][1]).any()) and bool((results[1][1][20:23] == 7).all())
+    layer.close()
+
+
+# ---- bits -------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True, k_scale=0.5, v_scale=0.3), dict(Hq=40, Hkv=2), dict(Hq=40, Hkv=2, fp8=True), dict(D=64), dict(D=64, fp8=True), dict(mode=1), dict(bk=32)],
+                         ids=str)
+@pytest.mark.parametrize("top,unit", [(1, 0.1), (2, 1.0), (38, 1.0), (38, 4.0)])
+def test_attention_keeps_its_weights(kw, top, unit):
+    """Error beyond the rounding of the result: weights have more bits than the result's type, so that they do not add to it."""
+    print("case:", kw, top, unit, flush=True)
+    layer = make(num_blocks=160, **kw)
+    c, rng = layer.cfg, np.random.default_rng(top)
+    pool = random_pool(layer, rng)
+    S, bk = 4, c.block_size
+    table, kv, start = rng.permutation(156).reshape(S, 39), np.array([39 * bk, 39 * bk - 3, 39 * bk, 37 * bk + 1]), np.array([0, 1, 3, 8, 12])
+    blocks = np.stack([[rng.permutation(39)[:top] for _ in range(c.n_kv_heads)] for _ in range(S)])
+    q = torch.tensor(rng.standard_normal((12, c.n_q_heads, c.head_dim)) * unit, dtype=torch.float32).to(c.torch_dtype).to(DEV)
+    got = host(layer.attn_blocks(q, pool, i32(table), i32(kv), i32(start), i32(blocks), i32([top] * S)))
+    want, weight, size = ref.attend(host(q), pool_values(layer, pool), table, kv, start, blocks, [top] * S, bk, np.zeros(q.shape))
+    # run_attend's bound, with the weights' own rounding (half a step of float16, 2^-11) where it has half a step of bfloat16
+    tol = 2.0 ** -8 * np.abs(want) + weight * (2 * (c.head_dim + 3) * E24 * size + 2.0 ** -17 + top * bk * E24 + 2.0 ** -11)
+    assert (np.abs(got - want) <= tol).all(), ((np.abs(got - want) > tol).sum(), (np.abs(got - want) / tol).max())
+    # Roundings have no common direction, so their squares add: the result's own is what the oracle's values lose in bfloat16; weights of float16 add a 64th of it (1.01 in
+    # all), of bfloat16 as much again (1.4)
+    if unit <= 1:
+        own = host(torch.tensor(want).to(c.torch_dtype)) - want
+        assert ((got - want) ** 2).sum() < 1.1 ** 2 * (own ** 2).sum()
+    layer.close()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_attention_keeps_small_weights(fp8):
+    """In every block one key of weight 1 and value 0, and 15 of weight 2^-13 to 2^-22 which alone make the result: in float16 the smallest are below its least normal."""
+    layer = make(num_blocks=256, Hq=4, Hkv=1, fp8=fp8)
+    rng = np.random.default_rng(0)
+    pool = random_pool(layer, rng)
+    k, v = pool.view(256, 1, 2, 16, 128)[:, 0, 0], pool.view(256, 1, 2, 128, 16)[:, 0, 1]
+    k.zero_()
+    k[:, 0, 0] = torch.tensor(1.0).to(torch.float8_e4m3fn).view(torch.uint8).item() if fp8 else 1.0
+    v[:, :, 0] = 0
+    table, kv, start = np.arange(256).reshape(1, 256), [4096], np.array([0, 10])
+    q, r = torch.zeros(10, 4, 128, dtype=torch.bfloat16, device=DEV), np.arange(10)[:, None, None]
+    q[:, :, 0] = (torch.arange(13, 23, device=DEV) * (math.log(2.0) * math.sqrt(128)))[:, None].to(torch.bfloat16)
+    for blocks in (np.arange(256), np.arange(256)[::-1], np.arange(1)):
+        blocks = np.ascontiguousarray(blocks).reshape(1, 1, -1)
+        n = blocks.size
+        got = host(layer.attn_blocks(q, pool, i32(table), i32(kv), i32(start), i32(blocks), i32([n])))
+        want, weight, size = ref.attend(host(q), pool_values(layer, pool), table, kv, start, blocks, [n], 16, np.zeros(q.shape))
+        # run_attend's bound with the weights' own rounding: 2^-16 in two parts of bfloat16; float16 holds 2^6 times the weight, 2^-(7 + r), to half of 2^-24 or of 2^-10 of
+        # itself (q is rounded, so the exponent is off by up to 23 x 2^-8)
+        own = np.maximum(2.0 ** -11, 2.0 ** (r + 0.1 - 18)) if fp8 else 2.0 ** -16
+        tol = 2.0 ** -8 * np.abs(want) + weight * (2 * 131 * E24 * size + 2.0 ** -17 + 16 * n * E24 + own)
+        assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
     layer.close()
 
 
