@@ -678,7 +678,7 @@ TileGroups tile_groups_for(const Dims &dm, int64_t pairs, int64_t rows) {
 }
 
 // Splits of the lists: the number whose rounds of workgroups cost least.  Unit: what 16 tokens take a workgroup that is alone, 0.15 us on the 128 kernel
-// and 0.25 on the float32 one; an item costs kItemCost besides, a join 4 us.  Next to others HBM is shared: 256 blocks of 192 lists take the 128 kernel 76 us in one
+// and 0.25 on the float32 one; an item costs kItemCost besides, a join 4 us and 1 us for each 2000 rows' heads (64 sequences, 340 rows of 32 heads: 9.6).  Next to others HBM is shared: 256 blocks of 192 lists take the 128 kernel 76 us in one
 // part (twice the unit; in four parts, three rounds, 88), of 96 lists 47 (two parts 42), of 8 lists 39 (eight parts 11); 32 blocks of 96 lists the float32 one 15 us (four
 // parts 12).  The chip holds 1 workgroup to a CU of the 128 kernel and 3 of the float32 one (counted on 4: 33 for 29 us on its 25 sequences above, on 8 35).
 // A sum's order goes by the splits, so they go by the arrays' sizes alone: the rows are taken to be spread evenly over the sequences, whatever seq_rows says.
@@ -689,11 +689,12 @@ int splits_for(const Dims &dm, int S, int R, int max_selected) {
     const int limit = (int)std::min<int64_t>({kMaxSplits, max_selected, ((int64_t)max_selected * parts + 7) / 8});  // 8 times 16 tokens: a group of two or two units to a wave
     const int64_t wgs = mfma ? kWgs : 3 * kWgs;
     const auto round = [&](int64_t running, int64_t blocks) { return 128 * kItemCost + blocks * (128 + (mfma ? std::max<int64_t>(running - 64, 0) : running * 5 / 8)); };
+    const int64_t join = 128 * (mfma ? 24 : 16) + 128 * (int64_t)R * dm.Hq / (mfma ? 300 : 500);
     int best = 0;
     int64_t cost = 0;
     for (int n = std::max(1, least); n <= std::max(least, limit) || !best; ++n) {
         const int64_t items = pairs * n, blocks = (int64_t)((max_selected + n - 1) / n) * parts;
-        const int64_t t = items / wgs * round(wgs, blocks) + (items % wgs ? round(items % wgs, blocks) : 0) + (n > 1 ? 128 * (mfma ? 24 : 16) : 0);
+        const int64_t t = items / wgs * round(wgs, blocks) + (items % wgs ? round(items % wgs, blocks) : 0) + (n > 1 ? join : 0);
         if (!best || t < cost) {
             best = n;
             cost = t;
