@@ -643,15 +643,16 @@ __global__ void __launch_bounds__(256) k_block_attn_join(BlockAttnArgs a, SplitO
                 l = l * old + wave_sum(f * mine.y);
                 x *= old;
                 y *= old;
-                for (int k = 0; k < cnt; k += 8) {  // eight loads in flight; behind the last split: the last again, with weight 0
+                for (int k = 0; k < cnt; k += 8) {  // eight loads in flight; behind the last split: the last again, left out
                     float2 o[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = *(const float2 *)(part.o + (at + (k0 + min(k + e, cnt - 1)) * step) * D + d);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float fk = k + e < cnt ? __shfl(f, (k + e) & 63, 64) : 0.f;
-                        x += fk * o[e].x;
-                        y += fk * o[e].y;
+                        const float fk = __shfl(f, (k + e) & 63, 64);  // 0 behind the last
+                        const uint32_t there = (uint32_t)(k + e - cnt >> 31);  // bits, not a condition: that would hold up the loads
+                        x += fk * __uint_as_float(__float_as_uint(o[e].x) & there);
+                        y += fk * __uint_as_float(__float_as_uint(o[e].y) & there);
                     }
                 }
                 mx = m_new;

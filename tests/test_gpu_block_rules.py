@@ -227,6 +227,31 @@ def test_attention_does_not_hide_nan(kw, top):
     layer.close()
 
 
+@pytest.mark.parametrize("kw", [dict(D=64), dict(D=64, bf16=False), dict(bk=32), dict(bk=8), dict(mode=1)], ids=str)
+@pytest.mark.parametrize("top", [1, 7, 120])
+def test_infinite_values_stay_infinite(kw, top):
+    """Values of plus or minus infinity under positive weights make their channels infinite, and no other."""
+    print("case:", kw, top, flush=True)
+    layer = make(num_blocks=200, **kw)
+    c, rng = layer.cfg, np.random.default_rng(top)
+    bk, D, Hkv = c.block_size, c.head_dim, c.n_kv_heads
+    pool = random_pool(layer, rng)
+    table, kv, start = rng.permutation(195).reshape(5, 39), np.full(5, 39 * bk), np.array([0, 3, 5, 7, 8, 10])
+    blocks = rng.integers(0, 39, (5, Hkv, top))
+    v = pool.view(200, Hkv, 2, D, bk)[:, :, 1]
+    for s in range(4):
+        v[table[s, blocks[s, 0, top // 2]], 0, s, rng.integers(0, bk)] = float("inf")
+        v[table[s, blocks[s, 0, top // 2]], 0, D - 1 - s, :] = -float("inf")
+    q = torch.tensor(rng.standard_normal((10, c.n_q_heads, D)), dtype=torch.float32).to(c.torch_dtype).to(DEV)
+    q[0] = 0                                                             # weights of 1
+    got = host(layer.attn_blocks(q, pool, i32(table), i32(kv), i32(start), i32(blocks), i32([top] * 5)))
+    want, _, _ = ref.attend(host(q), pool_values(layer, pool), table, kv, start, blocks, [top] * 5, bk, np.zeros(q.shape))
+    inf = np.isinf(want)
+    assert inf.sum() == 8 * (c.n_q_heads // Hkv) * 2 and not np.isnan(want).any()
+    assert np.array_equal(np.where(inf, got, 0), np.where(inf, want, 0)) and np.isfinite(got[~inf]).all()
+    layer.close()
+
+
 # ---- sizes ------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("kw,rows", [(dict(Hq=1, Hkv=1, D=64), (1 << 23) + 237), (dict(Hq=1, Hkv=1, D=2, bk=5, bf16=False), (1 << 24) + 37)], ids=str)
