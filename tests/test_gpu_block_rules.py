@@ -227,7 +227,7 @@ def test_attention_does_not_hide_nan(kw, top):
     layer.close()
 
 
-@pytest.mark.parametrize("kw", [dict(D=64), dict(D=64, bf16=False), dict(bk=32), dict(bk=8), dict(mode=1)], ids=str)
+@pytest.mark.parametrize("kw", [dict(), dict(Hq=40, Hkv=2), dict(D=64), dict(D=64, bf16=False), dict(bk=32), dict(bk=8), dict(mode=1)], ids=str)
 @pytest.mark.parametrize("top", [1, 7, 120])
 def test_infinite_values_stay_infinite(kw, top):
     """Values of plus or minus infinity under positive weights make their channels infinite, and no other."""
@@ -243,7 +243,7 @@ def test_infinite_values_stay_infinite(kw, top):
         v[table[s, blocks[s, 0, top // 2]], 0, s, rng.integers(0, bk)] = float("inf")
         v[table[s, blocks[s, 0, top // 2]], 0, D - 1 - s, :] = -float("inf")
     q = torch.tensor(rng.standard_normal((10, c.n_q_heads, D)), dtype=torch.float32).to(c.torch_dtype).to(DEV)
-    q[0] = 0                                                             # weights of 1
+    q[0] = 0                                                             # weights of 1: nothing is left for a second product
     got = host(layer.attn_blocks(q, pool, i32(table), i32(kv), i32(start), i32(blocks), i32([top] * 5)))
     want, _, _ = ref.attend(host(q), pool_values(layer, pool), table, kv, start, blocks, [top] * 5, bk, np.zeros(q.shape))
     inf = np.isinf(want)
