@@ -177,9 +177,9 @@ def test_attention_keeps_small_weights(fp8):
         n = blocks.size
         got = host(layer.attn_blocks(q, pool, i32(table), i32(kv), i32(start), i32(blocks), i32([n])))
         want, weight, size = ref.attend(host(q), pool_values(layer, pool), table, kv, start, blocks, [n], 16, np.zeros(q.shape))
-        # run_attend's bound with the weights' own rounding: 2^-16 in two parts of bfloat16; float16 holds 2^6 times the weight, 2^-(7 + r), to half of 2^-24 or of 2^-10 of
+        # run_attend's bound with the weights' own rounding: bfloat16 cuts off less than 2^-7 and rounds that by at most 2^-8 of it; float16 holds 2^6 times the weight, 2^-(7 + r), to half of 2^-24 or of 2^-10 of
         # itself (q is rounded, so the exponent is off by up to 23 x 2^-8)
-        own = np.maximum(2.0 ** -11, 2.0 ** (r + 0.1 - 18)) if fp8 else 2.0 ** -16
+        own = np.maximum(2.0 ** -11, 2.0 ** (r + 0.1 - 18)) if fp8 else 2.0 ** -15
         tol = 2.0 ** -8 * np.abs(want) + weight * (2 * 131 * E24 * size + 2.0 ** -17 + 16 * n * E24 + own)
         assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
     layer.close()
