@@ -31,6 +31,8 @@ EXPORTS = ("icarus_create", "icarus_destroy", "icarus_last_error", "icarus_works
            "icarus_cache_commit", "icarus_cache_release", "icarus_cache_get_stats", "icarus_set_full_decoders",
            "icarus_validate_block_tables", "icarus_set_attn_piece_limit", "icarus_attn_shared_kv_static", "icarus_bench_read",
            "icarus_gemm_tile_order", "icarus_gemm_choice", "icarus_gemm_group_tile", "icarus_append_in_tiles", "icarus_prefill_plan", "icarus_row_order", "icarus_gemm",
+           "icarus_beam_workspace_bytes", "icarus_beam_select", "icarus_fork_workspace_bytes", "icarus_fork_sequences", "icarus_copy_blocks",
+           "icarus_attn_prefix_workspace_bytes", "icarus_attn_prefix",
            "icarus_extend_sequences", "icarus_rope_append", "icarus_key_bounds", "icarus_select_workspace_bytes", "icarus_select_blocks",
            "icarus_attn_blocks_workspace_bytes", "icarus_attn_blocks")
 
@@ -185,6 +187,20 @@ def _load():
     lib.icarus_attn_blocks_workspace_bytes.argtypes = [vp, i32, i32, i32]
     lib.icarus_attn_blocks.restype = C.c_int
     lib.icarus_attn_blocks.argtypes = [vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp]
+    lib.icarus_beam_workspace_bytes.restype = sz
+    lib.icarus_beam_workspace_bytes.argtypes = [vp, i32, i32, i32]
+    lib.icarus_beam_select.restype = C.c_int
+    lib.icarus_beam_select.argtypes = [vp, vp, i32, i32, i64, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.icarus_fork_workspace_bytes.restype = sz
+    lib.icarus_fork_workspace_bytes.argtypes = [vp, i32, i32, i32]
+    lib.icarus_fork_sequences.restype = C.c_int
+    lib.icarus_fork_sequences.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.icarus_copy_blocks.restype = C.c_int
+    lib.icarus_copy_blocks.argtypes = [vp, vp, vp, i32, vp, vp, i32, vp]
+    lib.icarus_attn_prefix_workspace_bytes.restype = sz
+    lib.icarus_attn_prefix_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+    lib.icarus_attn_prefix.restype = C.c_int
+    lib.icarus_attn_prefix.argtypes = [vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, sz, vp]
     lib.icarus_cache_get_stats.restype = C.c_int
     lib.icarus_cache_get_stats.argtypes = [vp, C.POINTER(_CacheStats)]
     return lib
@@ -399,6 +415,28 @@ class SequenceMap:
         self.row_slot = torch.empty(R, dtype=torch.int64, device=device)
         ints = torch.empty(2 * S + 3 + 2 * R, dtype=torch.int32, device=device)
         self.kv_lens, self.row_start, self.counts, self.row_seq, self.row_pos = ints.split([S, S + 1, 2, R, R])
+
+
+class BeamMap:
+    """Device arrays that IcarusLayer.beam_select fills, kept by the caller: parents, tokens, done (int32) and scores (float32) of groups * width beams."""
+
+    def __init__(self, groups: int, width: int, device):
+        self.groups, self.width = int(groups), int(width)
+        S = self.groups * self.width
+        self.parents, self.tokens, self.done = torch.empty(3 * S, dtype=torch.int32, device=device).split(S) if S else [torch.empty(0, dtype=torch.int32, device=device)] * 3
+        self.scores = torch.empty(S, dtype=torch.float32, device=device)
+
+
+class ForkMap:
+    """Device arrays that IcarusLayer.fork_sequences fills, kept by the caller: kv_lens [S], block_tables [S, max_blocks], copy_src and copy_dst [S] for copy_blocks,
+    counts [3] (free ids taken, children refused, blocks freed); S = groups * width.  A step reads one and fills another, so a loop keeps two."""
+
+    def __init__(self, groups: int, width: int, max_blocks: int, device):
+        self.groups, self.width, self.max_blocks = int(groups), int(width), int(max_blocks)
+        S = self.groups * self.width
+        ints = torch.empty(3 * S + 3, dtype=torch.int32, device=device)
+        self.kv_lens, self.copy_src, self.copy_dst, self.counts = ints.split([S, S, S, 3])
+        self.block_tables = torch.zeros(S, self.max_blocks, dtype=torch.int32, device=device)
 
 
 # The calls with lengths on the device take a few microseconds on the GPU, so their marshalling is kept short: one look at a tensor in the common case,
@@ -775,6 +813,94 @@ class IcarusLayer:
         self._check(_launch(index, _lib.icarus_attn_blocks, self._h, q.data_ptr(), kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S,
                             kv_lens.data_ptr(), R, row_start.data_ptr(), seq_rows, blocks.data_ptr(), counts.data_ptr(), width, out.data_ptr(),
                             workspace.data_ptr(), workspace.nbytes))
+        return out
+
+    # -- sequences that branch (include/icarus_branches.h) ---------------------------
+    @staticmethod
+    def _scratch(workspace, need, index):
+        """The caller's workspace, or one of its own for this call."""
+        if workspace is None:
+            return torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
+        if not isinstance(workspace, torch.Tensor) or workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace: need a contiguous tensor on the device of the others")
+        return workspace
+
+    def beam_select(self, logits, scores, beams, row_start=None, done=None, eos: int = -1, workspace=None):
+        """Best continuations of each group of beams.width beams, into `beams` (a BeamMap).  logits [R, vocab] float32 or bfloat16, rows may be strided; a beam takes its last row of
+        row_start [S + 1], without it beam i has row i.  scores [S] float32, done [S] int32 of the beams now.  Returns beams."""
+        m, S = beams, beams.groups * beams.width
+        dt = logits.dtype if isinstance(logits, torch.Tensor) else None
+        index = _index_of(logits, "logits", dt if dt is torch.bfloat16 else torch.float32)
+        if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]):
+            raise ValueError(f"logits: shape {tuple(logits.shape)} with strides {tuple(logits.stride())}, expected rows of contiguous elements")
+        R, vocab = logits.shape
+        _need(scores, "scores", torch.float32, (S,), index)
+        if row_start is not None:
+            _need(row_start, "row_start", torch.int32, (S + 1,), index)
+        if done is not None:
+            _need(done, "done", torch.int32, (S,), index)
+        _need(m.parents, "beams", torch.int32, (S,), index)
+        workspace = self._scratch(workspace, _lib.icarus_beam_workspace_bytes(self._h, m.groups, m.width, vocab), index)
+        self._check(_launch(index, _lib.icarus_beam_select, self._h, logits.data_ptr(), BF16 if dt is torch.bfloat16 else F32, vocab,
+                            max(logits.stride(0), vocab) if R > 1 else vocab, R, m.groups, m.width, None if row_start is None else row_start.data_ptr(), scores.data_ptr(),
+                            None if done is None else done.data_ptr(), eos, m.parents.data_ptr(), m.tokens.data_ptr(), m.scores.data_ptr(), m.done.data_ptr(),
+                            workspace.data_ptr(), workspace.nbytes))
+        return m
+
+    def fork_sequences(self, parents, kv_lens, block_tables, forked, free_ids, free_used, shared=None, workspace=None):
+        """Lengths and tables of the children that `parents` names, into `forked` (a ForkMap), and the free list.  shared [groups]: leading columns of the tables that belong to the
+        common prefix.  Returns forked."""
+        S, max_blocks, index = self._table(block_tables)
+        m = forked
+        if S != m.groups * m.width or max_blocks != m.max_blocks:
+            raise ValueError(f"forked is for {m.groups} groups of {m.width} sequences of {m.max_blocks} blocks, block_tables has shape {(S, max_blocks)}")
+        n_free = free_ids.shape[0] if isinstance(free_ids, torch.Tensor) and free_ids.dim() else 0
+        _need(parents, "parents", torch.int32, (S,), index)
+        _need(kv_lens, "kv_lens", torch.int32, (S,), index)
+        _need(free_ids, "free_ids", torch.int32, (n_free,), index)
+        _need(free_used, "free_used", torch.int32, (1,), index)
+        if shared is not None:
+            _need(shared, "shared", torch.int32, (m.groups,), index)
+        _need(m.block_tables, "forked", torch.int32, (S, max_blocks), index)
+        workspace = self._scratch(workspace, _lib.icarus_fork_workspace_bytes(self._h, m.groups, m.width, max_blocks), index)
+        self._check(_launch(index, _lib.icarus_fork_sequences, self._h, m.groups, m.width, parents.data_ptr(), kv_lens.data_ptr(), block_tables.data_ptr(), max_blocks,
+                            None if shared is None else shared.data_ptr(), free_ids.data_ptr(), n_free, free_used.data_ptr(), m.kv_lens.data_ptr(), m.block_tables.data_ptr(),
+                            m.copy_src.data_ptr(), m.copy_dst.data_ptr(), m.counts.data_ptr(), workspace.data_ptr(), workspace.nbytes))
+        return m
+
+    def copy_blocks(self, arrays, src, dst):
+        """Block src[i] of each of `arrays` (pools, codes, scales: tensors of at least num_blocks blocks) to block dst[i]; -1: no copy."""
+        index = _index_of(src, "src", torch.int32)
+        n = src.shape[0] if src.dim() else 0
+        _need(src, "src", torch.int32, (n,), index)
+        _need(dst, "dst", torch.int32, (n,), index)
+        for t in arrays:
+            if not isinstance(t, torch.Tensor) or t.dim() < 1 or t.get_device() != index or not t.is_contiguous() or t.shape[0] < self.cfg.num_blocks:
+                raise ValueError(f"arrays: need contiguous tensors of at least {self.cfg.num_blocks} blocks on the device of src")
+        k = len(arrays)
+        at = (C.c_void_p * k)(*[t.data_ptr() for t in arrays])
+        size = (C.c_int64 * k)(*[t.stride(0) * t.element_size() if t.dim() > 1 else t.element_size() for t in arrays])
+        self._check(_launch(index, _lib.icarus_copy_blocks, self._h, at, size, k, src.data_ptr(), dst.data_ptr(), n))
+
+    def attn_prefix(self, q, kv_pool, block_tables, kv_lens, row_start, group_start, prefix_lens, out=None, workspace=None):
+        """Attention of the rows row_start[s] .. row_start[s + 1] - 1 over sequence s; the leading blocks of prefix_lens[g] tokens that the sequences group_start[g] .. group_start[g + 1] - 1
+        share are read once.  Rows of no sequence or group are left as they were."""
+        S, max_blocks, index = self._table(block_tables)
+        R = self._rows(q, "q", index)
+        self._pool(kv_pool, index)
+        G = prefix_lens.shape[0] if isinstance(prefix_lens, torch.Tensor) and prefix_lens.dim() else 0
+        _need(row_start, "row_start", torch.int32, (S + 1,), index)
+        _need(kv_lens, "kv_lens", torch.int32, (S,), index)
+        _need(group_start, "group_start", torch.int32, (G + 1,), index)
+        _need(prefix_lens, "prefix_lens", torch.int32, (G,), index)
+        if out is None:
+            out = torch.zeros_like(q)
+        self._rows(out, "out", index)
+        if out.shape[0] != R:
+            raise ValueError(f"out has {out.shape[0]} rows, q {R}")
+        workspace = self._scratch(workspace, _lib.icarus_attn_prefix_workspace_bytes(self._h, S, G, R, max_blocks), index)
+        self._check(_launch(index, _lib.icarus_attn_prefix, self._h, q.data_ptr(), kv_pool.data_ptr(), block_tables.data_ptr(), max_blocks, S, kv_lens.data_ptr(), R,
+                            row_start.data_ptr(), G, group_start.data_ptr(), prefix_lens.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.nbytes))
         return out
 
 

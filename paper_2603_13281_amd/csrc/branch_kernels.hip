@@ -1,0 +1,688 @@
+// Sequences that branch: choice of a group's best continuations, tables of the children, copies of blocks, and attention for any shape.  Everything a
+// kernel indexes with -- parents, lengths, block ids, rows -- comes from device memory and is checked where it is used.
+#include "block_util.h"
+#include "branch_ops.h"
+
+#include <algorithm>
+
+namespace icarus {
+namespace {
+
+// ---- choice of the continuations ------------------------------------------------------------------------------------------
+// Two launches.  k_beam_part reads a part of a beam's logits once: its largest logit, its sum of exponentials and its `width` largest logits, of which no other of the
+// part's can be among the group's best.  k_beam_merge puts the parts of a group together.
+//
+// Sums and scores are float64: two beams' candidates are told apart by the difference of their normalisers, and with sums in float32 the order of a group would
+// depend on how the row was split.  A logit and a number below it as the order of the logits, equal ones by the lowest token: packed in 64 bits.
+constexpr int kBeamThreads = 256, kBeamList = 1024;
+constexpr uint32_t kKeyNegInf = 0x007fffffu;  // order_key of minus infinity
+
+__device__ __forceinline__ uint32_t order_key(float x) {  // larger numbers have larger keys
+    const uint32_t u = __float_as_uint(x);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+// A logit as it counts: NaN as minus infinity, plus infinity as the largest finite number, -0 as 0 (which it equals).
+__device__ __forceinline__ float clean_logit(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e38f) + 0.f; }
+
+// exp(d) for d <= 0, to 2^-37 of itself: exp(d) = 2^n exp(r), |r| <= ln 2 / 2, its Taylor polynomial of degree 9.
+__device__ __forceinline__ double exp_of(double d) {
+    const double y = fmax(d * 1.4426950408889634074, -1100.0), n = rint(y);
+    const double r = (y - n) * 0.69314718055994530942;
+    double p = 1.0 / 362880;
+    p = __builtin_fma(p, r, 1.0 / 40320);
+    p = __builtin_fma(p, r, 1.0 / 5040);
+    p = __builtin_fma(p, r, 1.0 / 720);
+    p = __builtin_fma(p, r, 1.0 / 120);
+    p = __builtin_fma(p, r, 1.0 / 24);
+    p = __builtin_fma(p, r, 1.0 / 6);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    return __builtin_ldexp(p, (int)n);
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ __forceinline__ double wave_max_f64(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
+    return v;
+}
+
+// A bound that at least W of the wave's 64 keys reach, bit by bit; not always the largest such.
+__device__ __forceinline__ uint32_t reached_by(uint32_t key, int W) {
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t more = bound | 1u << bit;
+        const int n = __popcll(__ballot(key >= more));
+        if (n < W) continue;
+        bound = more;
+        if (n == W) break;
+    }
+    return bound;
+}
+
+// Row of logits that a beam takes, -1: none.
+__device__ __forceinline__ int beam_row(const BeamArgs &a, int s) {
+    int row = s;
+    if (a.row_start) {
+        const int end = a.row_start[s + 1];
+        row = end > a.row_start[s] ? end - 1 : -1;
+    }
+    return row >= 0 && row < a.R ? row : -1;
+}
+
+struct BeamParts {
+    double2 *sums;   // [G * W][parts]: largest logit, sum of exp(x - largest)
+    uint64_t *best;  // [G * W][parts][W]: key << 32 | ~token, descending; 0: none
+    int parts;
+};
+
+template <typename T, int PER>  // logits of a thread
+__global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamParts out) {
+    constexpr int VE = 16 / sizeof(T), NV = PER / VE;
+    __shared__ uint64_t list[kBeamList];
+    __shared__ float wmax[4];
+    __shared__ double wsum[4];
+    __shared__ uint32_t wbound[4];
+    __shared__ int count;
+    const int s = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
+    const int row = beam_row(a, s);
+    if (row < 0 || (a.done && a.done[s])) return;
+    // Which thread takes a logit goes by the token alone: equal rows have equal sums wherever they begin, and their beams tie.
+    const T *x0 = (const T *)a.logits + (size_t)row * a.ld;
+    struct __attribute__((packed, aligned(sizeof(T)))) Vec { uint32_t u[4]; };  // rows begin at any element
+    const int first = part * NV * kBeamThreads;
+    float x[PER];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int e = (first + j * kBeamThreads + t) * VE;
+        if (e + VE <= a.vocab) {
+            const Vec r = *(const Vec *)(x0 + e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (sizeof(T) == 4) {
+                    x[j * VE + k] = __uint_as_float(r.u[k]);
+                } else {
+                    x[j * VE + 2 * k] = __uint_as_float(r.u[k] << 16);
+                    x[j * VE + 2 * k + 1] = __uint_as_float(r.u[k] & 0xffff0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < VE; ++k) x[j * VE + k] = e + k < a.vocab ? Elem<T>::ld(x0 + e + k) : -INFINITY;
+        }
+    }
+    const auto token_of = [&](int i) { return (first + i / VE * kBeamThreads + t) * VE + i % VE; };
+    float mine = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        x[i] = clean_logit(x[i]);
+        mine = fmaxf(mine, x[i]);
+    }
+    if (t == 0) count = 0;
+    const float wave_most = wave_max(mine);
+    const uint32_t bound_w = reached_by(order_key(mine), a.W);
+    if (lane == 0) {
+        wmax[w] = wave_most;
+        wbound[w] = bound_w;
+    }
+    __syncthreads();
+    const float most = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
+    const uint32_t bound = max(max(max(wbound[0], wbound[1]), max(wbound[2], wbound[3])), kKeyNegInf + 1);
+    uint64_t *best = out.best + ((size_t)s * out.parts + part) * a.W;
+    if (most == -INFINITY) {
+        if (t < a.W) best[t] = 0;
+        if (t == 0) out.sums[(size_t)s * out.parts + part] = make_double2(-INFINITY, 0.0);
+        return;
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        sum += exp_of((double)x[i] - (double)most);
+        if (order_key(x[i]) >= bound) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kBeamList) list[at] = (uint64_t)order_key(x[i]) << 32 | ~(uint32_t)token_of(i);
+        }
+    }
+    sum = wave_sum_f64(sum);
+    if (lane == 0) wsum[w] = sum;
+    __syncthreads();
+    if (t == 0) out.sums[(size_t)s * out.parts + part] = make_double2((double)most, (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]));
+    const int n = count;
+    if (n <= kBeamList) {  // the place of each in the order: how many are larger
+        for (int i = t; i < n; i += kBeamThreads) {
+            const uint64_t v = list[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += list[j] > v;
+            if (rank < a.W) best[rank] = v;
+        }
+        if (t >= n && t < a.W) best[t] = 0;
+        return;
+    }
+    // Many equal logits: one after the other.
+    uint64_t last = ~0ull;
+    for (int k = 0; k < a.W; ++k) {
+        uint64_t v = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint64_t c = (uint64_t)order_key(x[i]) << 32 | ~(uint32_t)token_of(i);
+            if (order_key(x[i]) > kKeyNegInf && c < last && c > v) v = c;
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const uint64_t y = __shfl_xor(v, o, 64);
+            v = y > v ? y : v;
+        }
+        __syncthreads();
+        if (lane == 0) list[w] = v;
+        __syncthreads();
+        v = list[0];
+        for (int i = 1; i < 4; ++i) v = list[i] > v ? list[i] : v;
+        last = v;
+        if (t == 0) best[k] = v;
+    }
+}
+
+// A candidate and its place: larger scores first, then the lowest beam, then the larger logit, then the lowest token.
+struct Candidate {
+    double score;
+    uint64_t what;  // as BeamParts::best; done: the end token's
+    int beam;
+    __device__ __forceinline__ bool before(const Candidate &o) const {
+        if (score != o.score) return score > o.score;
+        if (beam != o.beam) return beam < o.beam;
+        return what > o.what;
+    }
+};
+
+__global__ void __launch_bounds__(kBeamThreads) k_beam_merge(BeamArgs a, BeamParts in) {
+    __shared__ double add[kBeamMost], top[kBeamMost];  // a logit x of the beam scores (x - top) + add: large logits cancel before the rest is added
+    __shared__ int kind[kBeamMost];     // 0: no continuations, 1: live, 2: done
+    __shared__ Candidate list[kBeamList];
+    __shared__ uint32_t wbound[4];
+    __shared__ int count;
+    const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, W = a.W;
+    for (int b = w; b < W; b += 4) {
+        const int s = g * W + b;
+        const float score = a.scores[s];
+        int k = beam_row(a, s) >= 0 && score - score == 0.f ? 1 : 0;
+        if (k && a.done && a.done[s]) k = 2;
+        double most = -INFINITY, sum = 0.0;
+        if (k == 1) {
+            for (int p = lane; p < in.parts; p += 64) most = fmax(most, in.sums[(size_t)s * in.parts + p].x);
+            most = wave_max_f64(most);
+            for (int p = lane; p < in.parts; p += 64) {
+                const double2 v = in.sums[(size_t)s * in.parts + p];
+                if (v.y > 0.0) sum += v.y * exp_of(v.x - most);
+            }
+            sum = wave_sum_f64(sum);
+            if (most == -INFINITY) k = 0;
+        }
+        if (lane == 0) {
+            kind[b] = k;
+            add[b] = k == 1 ? (double)score - log(sum) : (double)score;
+            top[b] = most;
+        }
+    }
+    if (t == 0) count = 0;
+    __syncthreads();
+    const int per_beam = in.parts * W, n_all = W * per_beam;
+    const auto get = [&](int i, Candidate &c) {
+        c.beam = i / per_beam;
+        const int j = i - c.beam * per_beam, k = kind[c.beam];
+        if (k == 0 || (k == 2 && j > 0)) return false;
+        if (k == 2) {
+            c.what = (uint64_t)0x80000000u << 32 | ~(uint32_t)a.eos;
+            c.score = add[c.beam];
+            return true;
+        }
+        c.what = in.best[((size_t)g * W + c.beam) * per_beam + j];
+        c.score = ((double)of_key((uint32_t)(c.what >> 32)) - top[c.beam]) + add[c.beam];
+        return c.what != 0;
+    };
+    const auto key_of = [](double v) {  // of a float that is not above v
+        float f = (float)v;
+        if ((double)f > v) f = nextafterf(f, -INFINITY);
+        return order_key(f);
+    };
+    uint32_t mine = 0;
+    Candidate c;
+    for (int i = t; i < n_all; i += kBeamThreads)
+        if (get(i, c)) mine = max(mine, key_of(c.score));
+    const uint32_t bound_w = reached_by(mine, W);
+    if (lane == 0) wbound[w] = bound_w;
+    __syncthreads();
+    const uint32_t bound = max(max(wbound[0], wbound[1]), max(wbound[2], wbound[3]));
+    for (int i = t; i < n_all; i += kBeamThreads)
+        if (get(i, c) && key_of(c.score) >= bound) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kBeamList) list[at] = c;
+        }
+    __syncthreads();
+    const int n = count;
+    const auto put = [&](int place, const Candidate &v) {
+        const int s = g * W + place, token = (int)~(uint32_t)v.what;
+        a.parents[s] = v.beam;
+        a.tokens[s] = token;
+        a.scores_out[s] = (float)v.score;
+        if (a.done_out) a.done_out[s] = kind[v.beam] == 2 || token == a.eos;
+    };
+    const auto none = [&](int place) {
+        const int s = g * W + place;
+        a.parents[s] = -1;
+        a.tokens[s] = -1;
+        a.scores_out[s] = -INFINITY;
+        if (a.done_out) a.done_out[s] = 0;
+    };
+    if (n <= kBeamList) {
+        for (int i = t; i < n; i += kBeamThreads) {
+            const Candidate v = list[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += list[j].before(v);
+            if (rank < W) put(rank, v);
+        }
+        if (t >= n && t < W) none(t);
+        return;
+    }
+    Candidate last{INFINITY, ~0ull, -1};
+    for (int k = 0; k < W; ++k) {
+        Candidate v{-INFINITY, 0, kBeamMost};
+        for (int i = t; i < n_all; i += kBeamThreads)
+            if (get(i, c) && last.before(c) && c.before(v)) v = c;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            Candidate y;
+            y.score = __shfl_xor(v.score, o, 64);
+            y.what = __shfl_xor(v.what, o, 64);
+            y.beam = __shfl_xor(v.beam, o, 64);
+            if (y.before(v)) v = y;
+        }
+        __syncthreads();
+        if (lane == 0) list[w] = v;
+        __syncthreads();
+        for (int i = 0; i < 4; ++i)
+            if (list[i].before(v)) v = list[i];
+        last = v;
+        if (t == 0) {
+            if (v.beam < kBeamMost) put(k, v);
+            else none(k);
+        }
+    }
+}
+
+constexpr int kBeamFew = 8, kBeamMany = 32;
+int beam_parts(int vocab, int per) { return (int)(((int64_t)vocab + kBeamThreads * per - 1) / (kBeamThreads * per)); }
+int beam_per(int G, int W, int vocab) { return (int64_t)G * W * beam_parts(vocab, kBeamMany) >= 512 ? kBeamMany : kBeamFew; }
+
+// ---- children ------------------------------------------------------------------------------------------------------------------
+// Two launches over parts of 128 columns of a group's tables, a thread to a column.  k_fork_count finds the blocks that no child holds: in a column, of the old sequences that nobody
+// continues, the ids that none of the continued ones names.  k_fork_write adds up the parts before its own, enters the freed ids, and writes the children's tables.
+struct ForkParts {
+    int32_t *freed_n;  // [G * parts]
+    int32_t *fresh_n;  // [G]
+    int32_t *freed;    // [G * parts][W * kForkCols]: ids by column and sequence
+    int parts;
+};
+
+struct ForkGroup {  // in LDS: a group's sequences
+    int len[kBeamMost], nb[kBeamMost], parent[kBeamMost], fresh[kBeamMost];  // old length and blocks; of a child: its parent, 1 where it needs a block
+    uint64_t kept;                                                             // parents
+    int shared, n_fresh;
+};
+
+__device__ __forceinline__ void fork_group(const ForkArgs &a, int g, ForkGroup &f) {  // by the first wave
+    const int i = threadIdx.x;
+    if (i < 64) {
+        const bool in = i < a.W;
+        const int64_t room = (int64_t)a.max_blocks * a.Bk;
+        const int n = in ? (int)min((int64_t)max(a.kv_lens[g * a.W + i], 0), room) : 0, p = in ? a.parents[g * a.W + i] : -1;
+        const int parent = p >= 0 && p < a.W ? p : -1, shared = a.shared ? max(a.shared[g], 0) : 0;
+        f.len[i] = n;
+        f.nb[i] = n / a.Bk + (n % a.Bk != 0);
+        f.parent[i] = parent;
+        bool first = parent >= 0;
+        for (int j = 0; j < a.W; ++j) {
+            const int q = __shfl(parent, j, 64);
+            if (j < i && q == parent) first = false;
+        }
+        const int plen = __shfl(n, max(parent, 0), 64);
+        const bool fresh = parent >= 0 && plen % a.Bk != 0 && (!first || plen / a.Bk < shared);
+        f.fresh[i] = fresh;
+        uint64_t kept = 0;
+        for (int j = 0; j < a.W; ++j) {
+            const int q = __shfl(parent, j, 64);
+            if (q >= 0) kept |= 1ull << q;
+        }
+        const int n_fresh = __popcll(__ballot(fresh));
+        if (i == 0) {
+            f.kept = kept;
+            f.shared = shared;
+            f.n_fresh = n_fresh;
+        }
+    }
+    __syncthreads();
+}
+
+// The old ids of this thread's column, in LDS, -1 behind a sequence's last block and outside the pool; which of them are freed.
+__device__ __forceinline__ void fork_tile(const ForkArgs &a, int g, int c, const ForkGroup &f, int32_t *tile) {
+    for (int i = 0; i < a.W; ++i) tile[i * kForkCols + threadIdx.x] = c < f.nb[i] ? a.bt[((size_t)g * a.W + i) * a.max_blocks + c] : -1;
+}
+__device__ __forceinline__ uint64_t fork_freed(const ForkArgs &a, int c, const ForkGroup &f, const int32_t *tile) {
+    uint64_t freed = 0;
+    if (c < f.shared) return 0;
+    const int32_t *mine = tile + threadIdx.x;
+    for (int i = 0; i < a.W; ++i) {
+        if (f.kept >> i & 1 || c >= f.nb[i]) continue;
+        const int id = mine[i * kForkCols];
+        bool held = id < 0 || id >= a.num_blocks;
+        for (int j = 0; j < a.W && !held; ++j) held = (j < i || f.kept >> j & 1) && c < f.nb[j] && mine[j * kForkCols] == id;
+        if (!held) freed |= 1ull << i;
+    }
+    return freed;
+}
+
+__global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts p) {
+    extern __shared__ int32_t tile[];  // [W][kForkCols]
+    __shared__ ForkGroup f;
+    __shared__ int wsum[kForkCols / 64];
+    const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
+    fork_group(a, g, f);
+    fork_tile(a, g, c, f, tile);
+    const uint64_t freed = fork_freed(a, c, f, tile);
+    const int n = __popcll(freed);
+    int x = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+    }
+    if (lane == 63) wsum[w] = x;
+    __syncthreads();
+    int at = x - n, all = 0;
+    for (int i = 0; i < kForkCols / 64; ++i) {
+        if (i < w) at += wsum[i];
+        all += wsum[i];
+    }
+    int32_t *out = p.freed + ((size_t)g * p.parts + part) * a.W * kForkCols;
+    for (int i = 0; i < a.W; ++i)
+        if (freed >> i & 1) out[at++] = tile[i * kForkCols + t];
+    if (t == 0) {
+        p.freed_n[(size_t)g * p.parts + part] = all;
+        if (part == 0) p.fresh_n[g] = f.n_fresh;
+    }
+}
+
+__global__ void __launch_bounds__(kForkCols) k_fork_write(ForkArgs a, ForkParts p) {
+    extern __shared__ int32_t tile[];
+    __shared__ ForkGroup f;
+    __shared__ int fresh_id[kBeamMost], fresh_at[kBeamMost], red[kForkCols / 64];
+    const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
+    const int n_parts = a.G * p.parts, me = g * p.parts + part;
+    fork_group(a, g, f);
+    fork_tile(a, g, c, f, tile);
+    // sums over the parts and groups before this one, and over all
+    int before = 0, all = 0, fresh_before = 0, fresh_all = 0;
+    for (int i = t; i < n_parts; i += kForkCols) {
+        const int n = p.freed_n[i];
+        all += n;
+        if (i < me) before += n;
+    }
+    for (int i = t; i < a.G; i += kForkCols) {
+        const int n = p.fresh_n[i];
+        fresh_all += n;
+        if (i < g) fresh_before += n;
+    }
+    const auto sum_of = [&](int v) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+        __syncthreads();
+        if (lane == 0) red[w] = v;
+        __syncthreads();
+        int sum = 0;
+        for (int k = 0; k < kForkCols / 64; ++k) sum += red[k];
+        return sum;
+    };
+    before = sum_of(before);
+    all = sum_of(all);
+    fresh_before = sum_of(fresh_before);
+    fresh_all = sum_of(fresh_all);
+    const int head = min(max(*a.free_used, 0), a.n_free), low = head - all, start = max(low, 0);  // freed id j stands at low + j
+    const int32_t *mine = p.freed + (size_t)me * a.W * kForkCols;
+    for (int j = t; j < p.freed_n[me]; j += kForkCols)
+        if (low + before + j >= 0) a.free_ids[low + before + j] = mine[j];
+    // Fresh ids of the group's children: entries start + fresh_before .. of the list.  Those before the head are freed ids of this call: from the parts' lists, since another workgroup
+    // may not have entered them yet.
+    if (t < 64) {
+        const bool need = t < a.W && f.fresh[t];
+        const int64_t at = (int64_t)start + fresh_before + __popcll(__ballot(need) & ((1ull << t) - 1));
+        int id = -1;
+        if (need && at < a.n_free && at >= head) id = a.free_ids[at];
+        fresh_at[t] = need ? (at < a.n_free ? (int)at : -1) : -2;
+        fresh_id[t] = id;
+    }
+    __syncthreads();
+    if (f.n_fresh && start + fresh_before < head) {
+        int done = 0;  // freed ids of the parts of the rounds before
+        for (int i0 = 0; i0 < n_parts; i0 += kForkCols) {
+            const int i = i0 + t, n = i < n_parts ? p.freed_n[i] : 0;
+            int x = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(x, o, 64);
+                if (lane >= o) x += y;
+            }
+            __syncthreads();
+            if (lane == 63) red[w] = x;
+            __syncthreads();
+            int from = done + x - n;
+            for (int k = 0; k < w; ++k) from += red[k];
+            for (int k = 0; k < kForkCols / 64; ++k) done += red[k];
+            if (n)
+                for (int j = 0; j < a.W; ++j) {
+                    const int64_t k = (int64_t)fresh_at[j] - low - from;
+                    if (fresh_at[j] >= 0 && fresh_at[j] < head && k >= 0 && k < n) fresh_id[j] = p.freed[(size_t)i * a.W * kForkCols + k];
+                }
+        }
+        __syncthreads();
+    }
+    for (int i = 0; i < a.W; ++i) {
+        const int q = f.parent[i];
+        if (q < 0 || fresh_at[i] == -1 || c >= f.nb[q]) continue;
+        int id = tile[q * kForkCols + t];
+        if (fresh_at[i] >= 0 && c == f.nb[q] - 1) id = fresh_id[i] >= 0 && fresh_id[i] < a.num_blocks ? fresh_id[i] : -1;
+        a.new_bt[((size_t)g * a.W + i) * a.max_blocks + c] = id;
+    }
+    if (part == 0 && t < a.W) {
+        const int q = f.parent[t];
+        a.new_lens[g * a.W + t] = q < 0 || fresh_at[t] == -1 ? 0 : f.len[q];
+        int src = -1, dst = -1;
+        if (fresh_at[t] >= 0) {
+            src = a.bt[((size_t)g * a.W + q) * a.max_blocks + f.nb[q] - 1];
+            dst = fresh_id[t];
+            if (src < 0 || src >= a.num_blocks || dst < 0 || dst >= a.num_blocks) src = dst = -1;
+        }
+        a.copy_src[g * a.W + t] = src;
+        a.copy_dst[g * a.W + t] = dst;
+    }
+    if (me == 0 && t == 0) {
+        const int64_t end = (int64_t)start + fresh_all;
+        a.counts[0] = (int)min(end, (int64_t)a.n_free);
+        a.counts[1] = (int)max(end - a.n_free, (int64_t)0);
+        a.counts[2] = all;
+    }
+}
+
+// ---- copies of blocks --------------------------------------------------------------------------------------------------------
+constexpr int kCopyArrays = 64, kCopyPiece = 16384, kCopyThreads = 256;
+struct CopyArrays {
+    uint32_t *at[kCopyArrays];
+    int64_t bytes[kCopyArrays];
+};
+// A workgroup to a piece of 16 KB of a block in one array, 16 bytes a lane where the array's blocks begin at multiples of them.
+__global__ void __launch_bounds__(kCopyThreads) k_copy_blocks(CopyArrays a, const int32_t *src, const int32_t *dst, int pieces, int num_blocks) {
+    const int i = blockIdx.x / pieces, piece = blockIdx.x % pieces, s = src[i], d = dst[i];
+    const int64_t bytes = a.bytes[blockIdx.y], first = (int64_t)piece * kCopyPiece;
+    if (s < 0 || d < 0 || s >= num_blocks || d >= num_blocks || s == d || first >= bytes) return;
+    char *const p = (char *)a.at[blockIdx.y];
+    const char *from = p + s * bytes + first;
+    char *to = p + d * bytes + first;
+    const int n = (int)min((int64_t)kCopyPiece, bytes - first);
+    if (((uintptr_t)p | bytes) % 16 == 0) {
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if ((k * kCopyThreads + threadIdx.x) * 16 < n) v[k] = *(const uint4 *)(from + (k * kCopyThreads + threadIdx.x) * 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if ((k * kCopyThreads + threadIdx.x) * 16 < n) *(uint4 *)(to + (k * kCopyThreads + threadIdx.x) * 16) = v[k];
+    } else {
+        for (int k = threadIdx.x * 4; k < n; k += kCopyThreads * 4) *(uint32_t *)(to + k) = *(const uint32_t *)(from + k);
+    }
+}
+
+// ---- attention over a shared prefix, any shape -------------------------------------------------------------------------------------
+// A workgroup to a query head of a sequence; a thread to a position for the scores, to a channel for the sum of the values.  Running maximum and sum in float32, rounds
+// of kChunk positions.  Each sequence reads its own table from the first column on: right for every block and head size, and slow.
+constexpr int kChunk = 512;
+template <typename T, typename KT>
+__global__ void __launch_bounds__(256) k_prefix_attn_generic(PrefixAttnArgs a, int Hq, int Hkv, int D, int Bk, float scale, float k_scale, float v_scale) {
+    __shared__ float qs[256], sc[kChunk], red[16];
+    __shared__ int64_t where[kChunk];  // a position's element of channel 0 of the values, -1: masked
+    const int s = blockIdx.y, h = blockIdx.x, c = h / (Hq / Hkv);
+    bool grouped = false;
+    for (int g = threadIdx.x; g < a.G; g += 256) grouped |= a.group_start[g] <= s && s < a.group_start[g + 1];
+    if (!__syncthreads_or(grouped)) return;
+    const int row0 = min(max(a.row_start[s], 0), a.R), row1 = min(max(a.row_start[s + 1], row0), a.R);
+    const int64_t n = min((int64_t)max(a.kv_lens[s], 0), (int64_t)a.max_blocks * Bk);
+    const int32_t *bt = a.bt + (size_t)s * a.max_blocks;
+    const KT *pool = (const KT *)a.pool + (size_t)c * 2 * Bk * D;
+    const size_t blk_stride = (size_t)Hkv * 2 * Bk * D;
+    for (int row = row0; row < row1; ++row) {
+        const T *q = (const T *)a.q + ((size_t)row * Hq + h) * D;
+        __syncthreads();
+        for (int i = threadIdx.x; i < D; i += 256) qs[i] = Elem<T>::ld(q + i);
+        float m = -INFINITY, l = 0.f, acc = 0.f;
+        for (int64_t t0 = 0; t0 < n; t0 += kChunk) {
+            const int cnt = (int)min((int64_t)kChunk, n - t0);
+            __syncthreads();
+            float most = -INFINITY;
+            for (int t = threadIdx.x; t < cnt; t += 256) {
+                const int off = (int)((t0 + t) % Bk), id = bt[(t0 + t) / Bk];
+                float dot = -INFINITY;
+                where[t] = -1;
+                if (id >= 0 && id < a.num_blocks) {
+                    const KT *k = pool + (size_t)id * blk_stride + (size_t)off * D;
+                    dot = 0.f;
+                    for (int i = 0; i < D; ++i) dot += qs[i] * KVElem<KT>::ld(k + i, k_scale);
+                    dot *= scale;
+                    where[t] = (int64_t)((size_t)id * blk_stride + (size_t)Bk * D + off);
+                }
+                sc[t] = dot;
+                most = fmaxf(most, dot);
+            }
+            const float m_new = fmaxf(m, block_max(most, red));
+            const float m_ref = m_new == -INFINITY ? 0.f : m_new;  // nothing yet, or nothing but NaN, which the maximum passes over
+            float sum = 0.f;
+            for (int t = threadIdx.x; t < cnt; t += 256) {
+                const float p = __expf(sc[t] - m_ref);
+                sc[t] = p;
+                sum += p;
+            }
+            sum = block_sum(sum, red);
+            if (m_new == -INFINITY && sum == 0.f) continue;
+            const float alpha = m == -INFINITY ? 1.f : __expf(m - m_new);  // before the first score there is nothing, or only NaN
+            l = l * alpha + sum;
+            acc *= alpha;
+            m = m_new;
+            if (threadIdx.x < D)
+                for (int t = 0; t < cnt; ++t)
+                    if (where[t] >= 0) acc += sc[t] * KVElem<KT>::ld(pool + where[t] + (size_t)threadIdx.x * Bk, v_scale);
+        }
+        if (threadIdx.x < D) Elem<T>::st((T *)a.out + ((size_t)row * Hq + h) * D + threadIdx.x, l == 0.f ? 0.f : acc / l);  // a NaN stays one
+    }
+}
+
+}  // namespace
+
+size_t beam_workspace(int G, int W, int vocab) {
+    if (G == 0) return 256;
+    return (size_t)G * W * beam_parts(vocab, beam_per(G, W, vocab)) * (16 + 8 * (size_t)W) + 256;
+}
+
+hipError_t launch_beam(const BeamArgs &a, void *workspace, hipStream_t st) {
+    const int per = beam_per(a.G, a.W, a.vocab);
+    BeamParts p;
+    p.parts = beam_parts(a.vocab, per);
+    p.sums = (double2 *)workspace;
+    p.best = (uint64_t *)(p.sums + (size_t)a.G * a.W * p.parts);
+    const dim3 grid(p.parts, a.G * a.W);
+#define BEAM_PART(T)                                                                                                  \
+    if (per == kBeamMany) hipLaunchKernelGGL((k_beam_part<T, kBeamMany>), grid, dim3(kBeamThreads), 0, st, a, p);     \
+    else hipLaunchKernelGGL((k_beam_part<T, kBeamFew>), grid, dim3(kBeamThreads), 0, st, a, p)
+    if (a.bf16) { BEAM_PART(bf16_t); }
+    else { BEAM_PART(float); }
+#undef BEAM_PART
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_beam_merge, dim3(a.G), dim3(kBeamThreads), 0, st, a, p);
+    return hipGetLastError();
+}
+
+static int fork_parts(int max_blocks) { return std::max(1, (max_blocks + kForkCols - 1) / kForkCols); }
+size_t fork_workspace(int G, int W, int max_blocks) {
+    const size_t parts = (size_t)G * fork_parts(max_blocks);
+    return (parts * W * kForkCols + parts + G) * 4 + 256;
+}
+
+hipError_t launch_fork(const ForkArgs &a, void *workspace, hipStream_t st) {
+    ForkParts p;
+    p.parts = fork_parts(a.max_blocks);
+    p.freed = (int32_t *)workspace;
+    p.freed_n = p.freed + (size_t)a.G * p.parts * a.W * kForkCols;
+    p.fresh_n = p.freed_n + (size_t)a.G * p.parts;
+    const dim3 grid(p.parts, a.G);
+    const size_t lds = (size_t)a.W * kForkCols * 4;
+    hipLaunchKernelGGL(k_fork_count, grid, dim3(kForkCols), lds, st, a, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_fork_write, grid, dim3(kForkCols), lds, st, a, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_copy_blocks(void *const *arrays, const int64_t *block_bytes, int n_arrays, const int32_t *src, const int32_t *dst, int n, int num_blocks, hipStream_t st) {
+    for (int i0 = 0; i0 < n_arrays; i0 += kCopyArrays) {
+        CopyArrays c{};
+        const int cnt = std::min(kCopyArrays, n_arrays - i0);
+        int64_t most = 4;
+        for (int i = 0; i < cnt; ++i) {
+            c.at[i] = (uint32_t *)arrays[i0 + i];
+            c.bytes[i] = block_bytes[i0 + i];
+            most = std::max(most, c.bytes[i]);
+        }
+        const int pieces = (int)((most + kCopyPiece - 1) / kCopyPiece);
+        const int per_launch = std::max(1, (1 << 22) / pieces);  // a launch has fewer than 2^32 work items
+        for (int e = 0; e < n; e += per_launch) {
+            hipLaunchKernelGGL(k_copy_blocks, dim3((unsigned)std::min(per_launch, n - e) * pieces, cnt), dim3(kCopyThreads), 0, st, c, src + e, dst + e, pieces, num_blocks);
+            const hipError_t err = hipGetLastError();
+            if (err != hipSuccess) return err;
+        }
+    }
+    return hipSuccess;
+}
+
+bool prefix_attn_fast(const Dims &) { return false; }
+size_t prefix_attn_workspace(const Dims &, int, int, int, int) { return 256; }
+hipError_t launch_prefix_attn(const Dims &dm, const PrefixAttnArgs &a, void *, hipStream_t st) { return launch_prefix_attn_generic(dm, a, st); }
+
+hipError_t launch_prefix_attn_generic(const Dims &dm, const PrefixAttnArgs &a, hipStream_t st) {
+    const float scale = 1.f / sqrtf((float)dm.D);
+    DISPATCH_TK(dm.bf16, dm.kv8, hipLaunchKernelGGL((k_prefix_attn_generic<T, KT>), dim3(dm.Hq, a.S), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D, dm.Bk, scale,
+                                                    dm.k_scale, dm.v_scale));
+    return hipGetLastError();
+}
+
+}  // namespace icarus

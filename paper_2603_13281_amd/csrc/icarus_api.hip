@@ -13,8 +13,9 @@
 #include <new>
 #include <vector>
 
-#include "../../include/icarus_blocks.h"
+#include "../../include/icarus_branches.h"
 #include "block_ops.h"
+#include "branch_ops.h"
 
 using namespace icarus;
 
@@ -2150,6 +2151,144 @@ icarus_status icarus_attn_blocks(icarus_ctx *ctx, const void *q, const void *kv_
     const bool fast = ctx->mode == 0 && block_attn_fast(ctx->dm);
     PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ATTN,
           fast ? launch_block_attn(ctx->dm, a, workspace, (hipStream_t)stream) : launch_block_attn_generic(ctx->dm, a, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+// ---- sequences that branch (icarus_branches.h) --------------------------------------------------------------------------
+
+namespace {
+constexpr int kBranchMaxVocab = 1 << 24, kBranchMaxParts = 1 << 17, kBranchMaxCopies = 1 << 20;
+bool beam_supported(int G, int W, int vocab) { return W <= kBeamMost && (int64_t)G * W <= kBlockMaxSeqs && vocab <= kBranchMaxVocab; }
+bool fork_supported(int G, int W, int max_blocks) {
+    return W <= kBeamMost && (int64_t)G * W <= kBlockMaxSeqs && max_blocks <= kBlockMaxTable && (int64_t)G * (max_blocks / kForkCols + 1) <= kBranchMaxParts;
+}
+bool prefix_supported(const icarus_ctx *ctx, int S, int G, int R, int max_blocks) {
+    return S <= kBlockMaxSeqs && G <= kBlockMaxSeqs && R <= kBlockMaxRows && max_blocks <= kBlockMaxTable && !too_many_queries(ctx, R);
+}
+}  // namespace
+
+size_t icarus_beam_workspace_bytes(const icarus_ctx *ctx, int32_t groups, int32_t width, int32_t vocab) {
+    if (!ctx || groups < 0 || width < 1 || vocab < 1 || !beam_supported(groups, width, vocab)) return 0;
+    return beam_workspace(groups, width, vocab);
+}
+
+icarus_status icarus_beam_select(icarus_ctx *ctx, const void *logits, int32_t logits_dtype, int32_t vocab, int64_t ld, int32_t R, int32_t groups, int32_t width,
+                                 const int32_t *row_start, const float *scores, const int32_t *done, int32_t eos, int32_t *parents, int32_t *tokens,
+                                 float *scores_out, int32_t *done_out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (logits_dtype != ICARUS_F32 && logits_dtype != ICARUS_BF16) return fail(ctx, ICARUS_ERR_INVALID_ARG, "logits_dtype %d: ICARUS_F32 or ICARUS_BF16", logits_dtype);
+    if (R < 0 || groups < 0 || width < 1 || vocab < 1) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size, or a width or vocabulary below 1");
+    if (!beam_supported(groups, width, vocab) || R > kBlockMaxRows)
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d groups of %d beams over %d tokens, %d rows: at most %d beams in a group, %d in all, %d tokens and %d rows", groups, width, vocab, R,
+                    kBeamMost, kBlockMaxSeqs, kBranchMaxVocab, kBlockMaxRows);
+    if (ld < vocab) return fail(ctx, ICARUS_ERR_SHAPE, "rows of logits are %lld elements apart, a row has %d", (long long)ld, vocab);
+    if (eos < -1 || eos >= vocab || (eos < 0 && done)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "eos %d: a token, or -1 where no beam can be done", eos);
+    if (groups == 0) return ICARUS_OK;
+    if (any_null({scores, parents, tokens, scores_out, workspace}) || (R && !logits)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({logits, workspace}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "logits and workspace must be 16-byte aligned");
+    if (!all_aligned({row_start, scores, done, parents, tokens, scores_out, done_out}, 4)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "arrays must be aligned to their element");
+    const size_t beams = (size_t)groups * width * 4, es = logits_dtype == ICARUS_BF16 ? 2 : 4, n_logits = R ? ((size_t)(R - 1) * ld + vocab) * es : 0;
+    const void *outs[] = {parents, tokens, scores_out, done_out};
+    for (int i = 0; i < 4; ++i) {
+        if (!outs[i]) continue;
+        bool shared = overlap(outs[i], beams, scores, beams) || (done && overlap(outs[i], beams, done, beams)) || (row_start && overlap(outs[i], beams, row_start, beams + 4)) ||
+                      overlap(outs[i], beams, logits, n_logits);
+        for (int j = 0; j < i; ++j) shared = shared || (outs[j] && overlap(outs[i], beams, outs[j], beams));
+        if (shared) return fail(ctx, ICARUS_ERR_INVALID_ARG, "the outputs must not share memory with what the call reads, nor with each other");
+    }
+    const size_t need = beam_workspace(groups, width, vocab);
+    if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
+    BeamArgs a{logits, logits_dtype == ICARUS_BF16, vocab, ld, R, groups, width, row_start, scores, done, eos, parents, tokens, scores_out, done_out};
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_beam(a, workspace, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+size_t icarus_fork_workspace_bytes(const icarus_ctx *ctx, int32_t groups, int32_t width, int32_t max_blocks) {
+    if (!ctx || groups < 0 || width < 1 || max_blocks < 0 || !fork_supported(groups, width, max_blocks)) return 0;
+    return fork_workspace(groups, width, max_blocks);
+}
+
+icarus_status icarus_fork_sequences(icarus_ctx *ctx, int32_t groups, int32_t width, const int32_t *parents, const int32_t *kv_lens, const int32_t *block_tables,
+                                    int32_t max_blocks, const int32_t *shared, int32_t *free_ids, int32_t n_free, const int32_t *free_used,
+                                    int32_t *new_lens, int32_t *new_tables, int32_t *copy_src, int32_t *copy_dst, int32_t *counts, void *workspace,
+                                    size_t workspace_bytes, void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (groups < 0 || width < 1 || max_blocks < 0 || n_free < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size, or a width below 1");
+    if (!fork_supported(groups, width, max_blocks) || n_free > kBlockMaxRows)
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d groups of %d sequences of %d blocks, %d free ids: at most %d sequences in a group, %d in all, %d parts of %d columns and %d free ids", groups,
+                    width, max_blocks, n_free, kBeamMost, kBlockMaxSeqs, kBranchMaxParts, kForkCols, kBlockMaxRows);
+    if (groups == 0) return ICARUS_OK;
+    if (any_null({parents, kv_lens, free_used, new_lens, copy_src, copy_dst, counts, workspace}) || (max_blocks && any_null({block_tables, new_tables})) || (n_free && !free_ids))
+        return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({parents, kv_lens, block_tables, shared, free_ids, free_used, new_lens, new_tables, copy_src, copy_dst, counts}, 4))
+        return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays must be aligned to their element");
+    if (!aligned16(workspace)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "workspace must be 16-byte aligned");
+    const size_t seqs = (size_t)groups * width * 4, table = seqs * max_blocks;
+    const struct { const void *p; size_t n; } in[] = {{parents, seqs}, {kv_lens, seqs}, {block_tables, table}, {shared, shared ? (size_t)groups * 4 : 0}, {free_used, 4}},
+        out[] = {{new_lens, seqs}, {new_tables, table}, {copy_src, seqs}, {copy_dst, seqs}, {counts, 12}, {free_ids, (size_t)n_free * 4}};
+    for (const auto &o : out) {
+        if (!o.n) continue;
+        for (const auto &i : in)
+            if (i.n && overlap(o.p, o.n, i.p, i.n)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "the outputs must not share memory with what the call reads");
+        for (const auto &q : out)
+            if (&q != &o && q.n && overlap(o.p, o.n, q.p, q.n)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "the outputs must not share memory with each other");
+    }
+    const size_t need = fork_workspace(groups, width, max_blocks);
+    if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
+    ForkArgs a{parents, kv_lens, block_tables, max_blocks, ctx->cfg.block_size, ctx->cfg.num_blocks, groups, width, shared, free_ids, n_free, free_used,
+               new_lens, new_tables, copy_src, copy_dst, counts};
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_fork(a, workspace, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+icarus_status icarus_copy_blocks(icarus_ctx *ctx, void *const *arrays, const int64_t *block_bytes, int32_t n_arrays, const int32_t *src, const int32_t *dst, int32_t n,
+                                 void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (n_arrays < 0 || n < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
+    if (n > kBranchMaxCopies) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d copies: at most %d per call", n, kBranchMaxCopies);
+    if (n_arrays == 0 || n == 0) return ICARUS_OK;
+    if (any_null({arrays, block_bytes, src, dst})) return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({src, dst}, 4)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "src and dst must be aligned to their element");
+    for (int i = 0; i < n_arrays; ++i) {
+        if (!arrays[i]) return fail(ctx, ICARUS_ERR_INVALID_ARG, "array %d is null", i);
+        if (block_bytes[i] < 4 || block_bytes[i] % 4) return fail(ctx, ICARUS_ERR_SHAPE, "array %d: blocks of %lld bytes, a positive multiple of 4 is wanted", i, (long long)block_bytes[i]);
+        if (block_bytes[i] > 1 << 30) return fail(ctx, ICARUS_ERR_UNSUPPORTED, "array %d: blocks of %lld bytes, at most 2^30", i, (long long)block_bytes[i]);
+        if (!aligned(arrays[i], 4)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "array %d must be 4-byte aligned", i);
+    }
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ELEMWISE, launch_copy_blocks(arrays, block_bytes, n_arrays, src, dst, n, ctx->cfg.num_blocks, (hipStream_t)stream));
+    return ICARUS_OK;
+}
+
+size_t icarus_attn_prefix_workspace_bytes(const icarus_ctx *ctx, int32_t S, int32_t G, int32_t R, int32_t max_blocks) {
+    if (!ctx || S < 0 || G < 0 || R < 0 || max_blocks < 0 || !prefix_supported(ctx, S, G, R, max_blocks)) return 0;
+    return prefix_attn_workspace(ctx->dm, S, G, R, max_blocks);
+}
+
+icarus_status icarus_attn_prefix(icarus_ctx *ctx, const void *q, const void *kv_pool, const int32_t *block_tables, int32_t max_blocks, int32_t S,
+                                 const int32_t *kv_lens, int32_t R, const int32_t *row_start, int32_t G, const int32_t *group_start,
+                                 const int32_t *prefix_lens, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!ctx) return ICARUS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(ctx->mu);
+    if (max_blocks < 0 || S < 0 || R < 0 || G < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
+    const icarus_layer_config &c = ctx->cfg;
+    if (!prefix_supported(ctx, S, G, R, max_blocks))
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d sequences, %d groups, %d rows, %d blocks of a sequence: at most %d sequences and groups, %d rows, 2^30 queries of a kv-head and %d blocks per call",
+                    S, G, R, max_blocks, kBlockMaxSeqs, kBlockMaxRows, kBlockMaxTable);
+    if (S == 0 || G == 0 || R == 0) return ICARUS_OK;
+    if (any_null({q, kv_pool, kv_lens, row_start, group_start, prefix_lens, out, workspace}) || (max_blocks && !block_tables)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");
+    if (!all_aligned({q, kv_pool, out, workspace}, 16)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "q, kv_pool, out and workspace must be 16-byte aligned");
+    if (!all_aligned({block_tables, kv_lens, row_start, group_start, prefix_lens}, 4)) return fail(ctx, ICARUS_ERR_ALIGNMENT, "integer arrays must be aligned to their element");
+    const size_t q_bytes = (size_t)R * c.n_q_heads * c.head_dim * (c.dtype == ICARUS_BF16 ? 2 : 4);
+    if (overlap(out, q_bytes, q, q_bytes)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "out must not share memory with q");
+    const size_t need = prefix_attn_workspace(ctx->dm, S, G, R, max_blocks);
+    if (workspace_bytes < need) return fail(ctx, ICARUS_ERR_CAPACITY, "workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
+    PrefixAttnArgs a{q, kv_pool, block_tables, max_blocks, c.num_blocks, S, kv_lens, R, row_start, G, group_start, prefix_lens, out};
+    const bool fast = ctx->mode == 0 && prefix_attn_fast(ctx->dm);
+    PHASE(ctx, (hipStream_t)stream, ICARUS_PH_ATTN,
+          fast ? launch_prefix_attn(ctx->dm, a, workspace, (hipStream_t)stream) : launch_prefix_attn_generic(ctx->dm, a, (hipStream_t)stream));
     return ICARUS_OK;
 }
 

@@ -1,0 +1,657 @@
+"""The operators of include/icarus_branches.h on the GPU against plain float64 (branch_reference.py), at the sizes and contents where they can go
+wrong.  Whole numbers and copied bytes are equal; floats are within bounds that are derived beside them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import branch_reference as ref
+from block_reference import blocks_of
+from paper_2603_13281_amd import binding
+from test_gpu_block_ops import DEV, E24, host, i32, make, pool_values, random_pool
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- choice of the continuations ----------------------------------------------------------------------------------------
+
+def run_choose(layer, logits, groups, width, scores, row_start=None, done=None, eos=-1):
+    beams = binding.BeamMap(groups, width, DEV)
+    for t in (beams.parents, beams.tokens, beams.done):
+        t.fill_(-77)
+    beams.scores.fill_(7.0)
+    layer.beam_select(logits, torch.tensor(scores, dtype=torch.float32, device=DEV), beams, None if row_start is None else i32(row_start), None if done is None else i32(done), eos)
+    torch.cuda.synchronize()
+    p, t, v, d, gaps = ref.choose(host(logits), row_start, np.asarray(scores, dtype=np.float32), done, eos, groups, width)
+    # A sum of exponentials, each to 2^-37, and its logarithm are off by less than 2^-36 and 2^-50 of the numbers added: where no two candidates of different beams are nearer than
+    # 2^-30 the order is the reference's.
+    assert all(x == 0.0 or x > 2.0 ** -30 for x in gaps)
+    got = [x.cpu().numpy() for x in (beams.parents, beams.tokens, beams.done)]
+    for a, b, name in zip(got, (p, t, d), ("parents", "tokens", "done")):
+        assert np.array_equal(a, b), (name, np.argwhere(a != b)[:5].ravel(), a[:20], b[:20])
+    s = host(beams.scores)
+    there = p >= 0
+    assert (s[~there] == -math.inf).all()
+    assert (np.abs(s[there] - v[there]) <= E24 * np.abs(v[there]) + 2.0 ** -34).all()
+    return beams
+
+
+def words(rng, rows, vocab, dt):
+    x = rng.standard_normal((rows, vocab)) * 2
+    top = rng.integers(0, vocab, (rows, 20))
+    np.put_along_axis(x, top, np.take_along_axis(x, top, 1) + 9 * rng.random(top.shape), 1)
+    return torch.tensor(x, dtype=torch.float32).to(dt).to(DEV)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("groups,width,vocab", [(1, 1, 1), (2, 3, 2), (1, 64, 5), (3, 5, 301), (1, 4, 2048), (2, 64, 4099), (5, 2, 8193), (20, 3, 50021), (2, 16, 128256)])
+def test_choose(groups, width, vocab, dt):
+    print("case:", groups, width, vocab, dt, flush=True)
+    layer, rng = make(), np.random.default_rng(vocab + width)
+    S = groups * width
+    logits = words(rng, S, vocab, dt)
+    scores = -20 * rng.random(S)
+    run_choose(layer, logits, groups, width, scores)
+    eos = vocab // 2
+    run_choose(layer, logits, groups, width, scores, done=(rng.random(S) < 0.3).astype(int), eos=eos)
+    start = np.concatenate([[0], np.cumsum(rng.integers(0, 4, S))])       # some beams have no row, the others take their last
+    run_choose(layer, words(rng, int(start[-1]) + 1, vocab, dt), groups, width, scores, row_start=start, eos=eos)
+    layer.close()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("vocab,gap", [(5000, 3), (5000, 1), (4096, 64), (333, 0)])
+def test_choose_strided_rows(vocab, gap, dt):
+    """Rows at any distance, what lies between them is not read as logits."""
+    layer, rng = make(), np.random.default_rng(gap)
+    whole = torch.full((9, vocab + gap), 1e30, dtype=dt, device=DEV)
+    logits = whole[:, :vocab]
+    logits.copy_(words(rng, 9, vocab, dt))
+    run_choose(layer, logits, 3, 3, -5 * rng.random(9))
+    layer.close()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("vocab", [7, 1000, 20000])
+def test_choose_equal_logits(vocab, dt):
+    """Beams and tokens that tie: the lowest beam, then the lowest token; more of them than a workgroup lists."""
+    layer, rng = make(), np.random.default_rng(vocab)
+    same = torch.zeros(8, vocab, dtype=dt, device=DEV)
+    run_choose(layer, same, 2, 4, [-1.0] * 8)
+    same[:, ::2] = -0.0                                                   # equal to 0
+    run_choose(layer, same, 2, 4, [-1.0, -1.0, -2.0, -1.0] * 2)
+    few = torch.tensor(rng.integers(0, 3, (1, vocab)), dtype=dt, device=DEV).expand(8, vocab).contiguous()
+    run_choose(layer, few, 2, 4, [-1.0, -3.0, -1.0, -1.0] * 2)
+    run_choose(layer, few[:1], 1, 1, [0.0])
+    run_choose(layer, few.repeat(8, 1), 1, 64, [-1.0] * 64)
+    layer.close()
+
+
+def test_choose_masked_logits():
+    """Minus infinity, NaN and plus infinity among the logits; beams that are not live; fewer continuations than beams."""
+    layer, rng = make(), np.random.default_rng(0)
+    inf, nan = float("inf"), float("nan")
+    x = words(rng, 12, 3000, torch.float32)
+    x[0] = -inf
+    x[1, 5:] = -inf
+    x[2] = nan
+    x[3, 100] = nan
+    x[4, 17], x[4, 2900] = inf, inf
+    x[5, 1:] = -inf
+    x[6] = -inf
+    x[7] = -inf
+    x[8] = -3e38
+    x[9] *= 1e30
+    x[10] = -inf
+    x[10, 2999] = -1e20
+    x[11] = inf
+    run_choose(layer, x, 3, 4, -rng.random(12))
+    scores = -rng.random(12)
+    scores[[0, 4, 5, 9]] = -inf, inf, nan, -inf
+    run_choose(layer, x, 3, 4, scores)
+    run_choose(layer, x, 1, 12, scores, done=np.arange(12) % 3, eos=2999)
+    run_choose(layer, x, 12, 1, scores, done=np.ones(12, dtype=int), eos=0)
+    only = torch.full((4, 3000), -inf, device=DEV)
+    only[:, 0::1024] = 0.5                                               # a few tokens that fall to one thread
+    run_choose(layer, only, 1, 4, [-1.0, -2.0, -1.5, -1.0])
+    run_choose(layer, torch.full((4, 3000), -inf, device=DEV), 1, 4, [-1.0] * 4)
+    run_choose(layer, x[:0], 1, 4, [-1.0] * 4)
+    run_choose(layer, x, 2, 4, [-1.0] * 8, row_start=np.array([0, 1, 1, -3, 2, 40, 41, 3, 12]))  # rows outside are none
+    layer.close()
+
+
+# ---- children -------------------------------------------------------------------------------------------------------------
+
+def run_fork(layer, parents, kv, table, shared, free, used, width):
+    c, (S, max_blocks) = layer.cfg, table.shape
+    want = ref.fork(parents, kv, table, shared, free, used, c.block_size, c.num_blocks, width, np.full(table.shape, -77))
+    m = binding.ForkMap(S // width, width, max_blocks, DEV)
+    for t in (m.kv_lens, m.copy_src, m.copy_dst, m.counts, m.block_tables):
+        t.fill_(-77)
+    f = i32(free)
+    layer.fork_sequences(i32(parents), i32(kv), i32(table).reshape(table.shape), m, f, i32([used]), None if shared is None else i32(shared))
+    torch.cuda.synchronize()
+    for name in ("kv_lens", "counts", "copy_src", "copy_dst", "block_tables"):
+        got = getattr(m, name).cpu().numpy()
+        assert np.array_equal(got, want[name]), (name, np.argwhere(got != want[name])[:5], got.ravel()[:30], want[name].ravel()[:30])
+    assert np.array_equal(f.cpu().numpy(), want["free"]), (f.cpu().numpy()[:40], want["free"][:40])
+    return want
+
+
+def family(rng, groups, width, max_blocks, bk, shared):
+    """Tables of sequences that came apart somewhere, the number of blocks in use, and their lengths."""
+    S, at = groups * width, 0
+    table, kv = np.full((S, max_blocks), -1), np.zeros(S, dtype=int)
+    for g in range(groups):
+        trunk = np.arange(at, at + max_blocks)
+        at += max_blocks
+        for i in range(width):
+            n = int(rng.integers(0, max_blocks * bk + 1))
+            nb, apart = blocks_of(n, bk), int(rng.integers(0, max_blocks + 1))
+            s = g * width + i
+            kv[s] = n
+            table[s, :nb] = trunk[:nb]
+            apart = max(apart, shared)
+            if apart < nb:
+                table[s, apart:nb] = np.arange(at, at + nb - apart)
+                at += nb - apart
+    ids = rng.permutation(at)
+    return np.where(table >= 0, ids[table], -1), kv, at
+
+
+@pytest.mark.parametrize("bk", [1, 16, 7])
+@pytest.mark.parametrize("groups,width,max_blocks,shared", [(1, 1, 1, 0), (3, 4, 5, 2), (1, 64, 130, 60), (7, 8, 129, 0), (40, 3, 20, 19), (2, 5, 600, 300), (300, 2, 3, 1)])
+def test_fork(groups, width, max_blocks, shared, bk):
+    print("case:", groups, width, max_blocks, shared, bk, flush=True)
+    rng = np.random.default_rng(groups + bk)
+    table, kv, used = family(rng, groups, width, max_blocks, bk, shared)
+    S = groups * width
+    layer = make(bk=bk, num_blocks=used + S + 3)
+    free = rng.permutation(used + S)
+    for parents in (rng.integers(0, width, S), rng.integers(-1, width + 1, S), np.zeros(S, dtype=int), np.full(S, -1), np.arange(S) % width):
+        run_fork(layer, parents, kv, table, np.full(groups, shared), free, used, width)
+        run_fork(layer, parents, kv, table, None, free, used, width)
+    layer.close()
+
+
+def test_fork_where_blocks_run_out():
+    """Children that find no block are refused, in the order of the sequences; freed ids are there for them; ids that the list has no room for are left out."""
+    rng = np.random.default_rng(1)
+    table, kv, used = family(rng, 9, 6, 30, 16, 4)
+    layer = make(num_blocks=used + 5)
+    parents = rng.integers(0, 3, 54)
+    for n_free, head in ((used, used), (used + 4, used), (used + 4, used + 4), (10, 3), (10, 10), (0, 0), (used, -7), (used, used + 1000), (40, 40), (400, 0)):
+        print("case:", n_free, head, flush=True)
+        run_fork(layer, parents, kv, table, rng.integers(-2, 8, 9), rng.integers(0, used + 5, n_free), head, 6)
+        run_fork(layer, np.zeros(54, dtype=int), kv, table, None, rng.integers(0, used + 5, n_free), head, 6)
+    layer.close()
+
+
+def test_fork_of_what_is_out_of_range():
+    """Lengths below 0 and beyond the table, parents and ids outside, shared columns beyond the table."""
+    rng = np.random.default_rng(2)
+    table, kv, used = family(rng, 6, 5, 40, 16, 0)
+    kv[[0, 7, 12]] = -5, 10 ** 9, 40 * 16 + 1
+    table[7] = rng.integers(0, used, 40)
+    table[rng.random(table.shape) < 0.1] = -3
+    table[rng.random(table.shape) < 0.1] = used + 99
+    layer = make(num_blocks=used)
+    free = rng.integers(-2, used + 4, used + 50)
+    for seed in range(4):
+        parents = rng.integers(-2, 7, 30)
+        parents[seed] = 2 ** 31 - 1
+        run_fork(layer, parents, kv, table, rng.integers(-1, 45, 6), free, used, 5)
+    run_fork(layer, rng.integers(0, 5, 30), kv, np.zeros((30, 0), dtype=int), None, free, 20, 5)
+    layer.close()
+
+
+# ---- copies ----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(D=64, Hq=4, Hkv=4, bf16=False), dict(D=20, Hkv=1, bk=3)], ids=str)
+@pytest.mark.parametrize("n", [1, 9, 700])
+def test_copy(kw, n):
+    print("case:", kw, n, flush=True)
+    layer, rng = make(num_blocks=2 * n + 5, **kw), np.random.default_rng(n)
+    c = layer.cfg
+    perm = rng.permutation(2 * n + 5)
+    src, dst = perm[:n].copy(), perm[n:2 * n].copy()
+    if n > 5:
+        src[1], dst[2], src[3], dst[4] = -1, -1, 2 * n + 5, 2 ** 31 - 1
+        dst[5] = src[5]
+    spare = torch.randint(0, 256, (4 * (2 * n + 5) * 12 + 4,), dtype=torch.uint8, device=DEV)
+    arrays = [random_pool(layer, rng) for _ in range(3)] + [torch.randint(-127, 127, (2 * n + 5, 2, 2, c.head_dim), dtype=torch.int8, device=DEV), torch.rand(2 * n + 5, 2, device=DEV),
+                                                            torch.rand(2 * n + 5, device=DEV), spare[4:].view(2 * n + 5, 48), torch.rand(2 * n + 9, 4099, device=DEV)]
+    want = [t.clone() for t in arrays]
+    for t in want:
+        for s, d in zip(src, dst):
+            if 0 <= s < 2 * n + 5 and 0 <= d < 2 * n + 5:
+                t[d] = t[s].clone()
+    layer.copy_blocks(arrays, i32(src), i32(dst))
+    torch.cuda.synchronize()
+    for a, b in zip(arrays, want):
+        assert torch.equal(a.reshape(-1).view(torch.uint8), b.reshape(-1).view(torch.uint8))
+    layer.copy_blocks([], i32(src), i32(dst))
+    layer.copy_blocks(arrays, i32([]), i32([]))
+    layer.close()
+
+
+def test_copy_many_arrays_and_large_blocks():
+    layer = make(num_blocks=4)
+    arrays = [torch.rand(4, 5, device=DEV) for _ in range(130)] + [torch.randint(0, 100, (4, 1 << 22), dtype=torch.int32, device=DEV)]
+    want = [t.clone() for t in arrays]
+    for t in want:
+        t[3] = t[0]
+    layer.copy_blocks(arrays, i32([0, -1]), i32([3, 1]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(arrays, want))
+    layer.close()
+
+
+# ---- attention over a shared prefix -------------------------------------------------------------------------------------------
+
+def bound(layer, want, weight, size, count):
+    """A score is a sum of D products in float32 (D half steps of the sum of sizes, and 3 for the scale and the code's scale): off by ds, so each p by 2 ds of itself (its own and the
+    sum's); exp, its argument (below 2^7 where p counts) and the sums over up to n tokens: 2^-17 + n 2^-24, all of sum p |v|.  On the matrix cores a weight is two numbers of
+    bfloat16 (2^-15 of sum p |v| more), over an FP8 cache one of float16 (2^-11)."""
+    c = layer.cfg
+    ds = (c.head_dim + 3) * E24 * size
+    return (2.0 ** -8 if c.bf16 else E24) * np.abs(want) + weight * (2 * ds + 2.0 ** -17 + count * E24 + (0.0 if not c.bf16 else 2.0 ** -11 if c.kv_fp8 else 2.0 ** -15)) + 1e-30
+
+
+def run_attend(layer, q, pool, table, kv, row_start, group_start, prefix, out=None):
+    c = layer.cfg
+    out = torch.full(q.shape, 7.0, dtype=c.torch_dtype, device=DEV)
+    layer.attn_prefix(q, pool, i32(table).reshape(table.shape), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
+    torch.cuda.synchronize()
+    want, weight, size, count = ref.attend(host(q), pool_values(layer, pool), table, kv, row_start, group_start, c.block_size, np.full(q.shape, 7.0))
+    got = host(out)
+    ok = np.abs(got - want) <= bound(layer, want, weight, size, count)
+    assert ok.all(), (np.argwhere(~ok)[:5], np.argwhere(~ok).shape, np.nanmax(np.abs(got - want)))
+    return out
+
+
+def blocks_that_may_be_read(layer, pool, table, kv):
+    """Everything else becomes NaN."""
+    c = layer.cfg
+    seen = np.zeros((c.num_blocks, c.block_size), dtype=bool)
+    for row, n in zip(table, kv):
+        n = min(max(int(n), 0), len(row) * c.block_size)
+        for i in range(blocks_of(n, c.block_size)):
+            if 0 <= row[i] < c.num_blocks:
+                seen[row[i], :n - i * c.block_size] = True
+    gone = torch.tensor(~seen, device=DEV)
+    nan = torch.tensor(float("nan")).to(torch.float8_e4m3fn).view(torch.uint8).item() if c.kv_fp8 else float("nan")
+    pool.view(c.num_blocks, c.n_kv_heads, 2, c.block_size, c.head_dim)[:, :, 0].masked_fill_(gone[:, None, :, None], nan)
+    pool.view(c.num_blocks, c.n_kv_heads, 2, c.head_dim, c.block_size)[:, :, 1].masked_fill_(gone[:, None, None, :], nan)
+
+
+def crowd(layer, rng, groups, max_blocks):
+    """groups: (rows of each sequence, tokens of the prefix, tails).  Tables that share the prefix's whole blocks, lengths, row_start, group_start, prefix lengths."""
+    bk, at, table, kv, rows, start = layer.cfg.block_size, 0, [], [], [], [0]
+    ids = rng.permutation(layer.cfg.num_blocks)
+    for n_rows, pre, tails in groups:
+        whole = ids[at:at + pre // bk]
+        at += pre // bk
+        for r, t in zip(n_rows, tails):
+            nb = blocks_of(pre + t, bk) - pre // bk if t >= 0 else 0
+            row = np.full(max_blocks, -1)
+            row[:pre // bk] = whole
+            row[pre // bk:pre // bk + nb] = ids[at:at + nb]
+            at += nb
+            table.append(row)
+            kv.append(pre + t if t >= 0 else 0)
+            rows.append(r)
+        start.append(len(table))
+    assert at <= layer.cfg.num_blocks
+    return np.array(table), np.array(kv), np.concatenate([[0], np.cumsum(rows)]), np.array(start), np.array([g[1] for g in groups])
+
+
+def queries(layer, rng, rows, size=1.0):
+    c = layer.cfg
+    return torch.tensor(rng.standard_normal((rows, c.n_q_heads, c.head_dim)) * size, dtype=torch.float32).to(c.torch_dtype).to(DEV)
+
+
+SHAPES = [dict(), dict(Hq=4, Hkv=4), dict(Hq=32, Hkv=8), dict(fp8=True, k_scale=0.5, v_scale=0.25), dict(Hq=16, Hkv=2, fp8=True, k_scale=0.05, v_scale=0.03), dict(Hq=40, Hkv=2), dict(Hq=3, Hkv=1),
+          dict(D=64), dict(Hq=4, Hkv=4, D=64, bf16=False), dict(bf16=False), dict(D=80), dict(D=256), dict(D=112, bf16=False), dict(D=64, fp8=True, k_scale=2.0), dict(bf16=False, fp8=True, v_scale=0.5),
+          dict(D=256, bf16=False, fp8=True), dict(bk=32), dict(bk=48, fp8=True, k_scale=0.3), dict(bk=64, bf16=False), dict(bk=128, D=64), dict(mode=1), dict(bk=5, D=30), dict(bk=8)]
+
+
+@pytest.mark.parametrize("kw", SHAPES, ids=str)
+def test_attend(kw):
+    """Groups of one and of many, prefixes that end inside a block, at its end and at zero, tails of nothing and of many blocks, sequences that are empty or have no rows;
+    everything that must not be read holds NaN."""
+    print("case:", kw, flush=True)
+    layer = make(num_blocks=400, **kw)
+    bk, rng = layer.cfg.block_size, np.random.default_rng(3)
+    pool = random_pool(layer, rng)
+    groups = [([1], 0, [1]), ([2, 1, 3], 5 * bk, [0, 1, bk]), ([1] * 17, 9 * bk + bk // 2, list(range(17))), ([4, 0, 2], 3 * bk - 1, [2 * bk, 5, 7 * bk + 1]), ([2, 2], 0, [-1, -1]),
+              ([1, 5, 1, 1], 12 * bk, [3, -1, 0, 20 * bk]), ([9, 9, 9], 70 * bk + 1, [1, 9 * bk, 33]), ([0, 0], 2 * bk, [1, 1]), ([30], 6 * bk, [17])]
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, groups, 90)
+    blocks_that_may_be_read(layer, pool, table, kv)
+    q = queries(layer, rng, int(row_start[-1]) + 2, 2.0)
+    run_attend(layer, q, pool, table, kv, row_start, group_start, prefix)
+    run_attend(layer, q, pool, table, kv, row_start, group_start, np.zeros_like(prefix))                 # nothing is shared
+    run_attend(layer, q, pool, table, kv, row_start, group_start, np.maximum(prefix - bk, -3))
+    run_attend(layer, q, pool, table, kv, row_start, group_start[2:5], prefix[2:4])                      # the other sequences are in no group
+    run_attend(layer, q, pool, table, kv, row_start, np.arange(len(kv) + 1), kv)                         # every sequence for itself, all of it shared
+    layer.close()
+
+
+@pytest.mark.parametrize("kw", [dict(Hq=32, Hkv=8), dict(Hq=8, Hkv=1, fp8=True), dict(Hq=8, Hkv=4, bf16=False), dict(Hq=8, Hkv=1, D=64)], ids=str)
+@pytest.mark.parametrize("n,rows", [(1, 1), (2, 8), (5, 3), (33, 1), (40, 4), (70, 5)])
+def test_attend_crowds(kw, n, rows):
+    """Numbers of queries around those of a tile, a wave and a workgroup, over one long prefix."""
+    print("case:", kw, n, rows, flush=True)
+    layer = make(num_blocks=700, **kw)
+    rng = np.random.default_rng(n)
+    pool = random_pool(layer, rng)
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, [([rows] * n, 4000 + n, [int(t) for t in rng.integers(0, 60, n)])], 260)
+    blocks_that_may_be_read(layer, pool, table, kv)
+    run_attend(layer, queries(layer, rng, n * rows, 2.0), pool, table, kv, row_start, group_start, prefix)
+    layer.close()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(D=64, bf16=False), dict(mode=1)], ids=str)
+def test_attend_many_groups(kw):
+    layer = make(num_blocks=3000, **kw)
+    rng = np.random.default_rng(5)
+    pool = random_pool(layer, rng)
+    groups = [([int(r) for r in rng.integers(0, 4, n)], int(rng.integers(0, 200)), [int(t) for t in rng.integers(-1, 40, n)]) for n in rng.integers(0, 5, 180)]
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, groups, 20)
+    run_attend(layer, queries(layer, rng, int(row_start[-1])), pool, table, kv, row_start, group_start, prefix)
+    layer.close()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True, k_scale=0.5), dict(bf16=False)], ids=str)
+def test_attend_large_scores(kw):
+    """Scores in the hundreds: the running maximum moves, and one part's sums are nothing beside another's."""
+    layer = make(num_blocks=200, Hq=8, Hkv=2, **kw)
+    rng = np.random.default_rng(0)
+    pool = random_pool(layer, rng)
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, [([3, 3, 3], 1500, [40, 200, 0])], 120)
+    run_attend(layer, queries(layer, rng, 9, 30.0), pool, table, kv, row_start, group_start, prefix)
+    layer.close()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(bf16=False), dict(D=64), dict(mode=1)], ids=str)
+def test_attend_scores_of_minus_infinity(kw):
+    """Keys whose scores are minus infinity weigh nothing; a row with no others becomes zeros; NaN and plus infinity make NaN, for the rows that see them."""
+    layer = make(num_blocks=100, Hq=8, Hkv=2, **kw)
+    c, rng = layer.cfg, np.random.default_rng(2)
+    pool = random_pool(layer, rng)
+    q = queries(layer, rng, 6)
+    q[:, :, 0] = 1.0
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, [([2, 2, 2], 320, [0, 100, 40])], 30)
+    keys = pool.view(100, 2, 2, 16, c.head_dim)[:, :, 0]
+    keys[torch.tensor(table[0, :20].copy(), device=DEV), :, :, 0] = -float("inf")   # the whole prefix
+    run_attend(layer, q, pool, table, kv, row_start, group_start, prefix)
+    keys[int(table[1, 22]), :, :, 0] = -float("inf")
+    run_attend(layer, q, pool, table, kv, row_start, group_start, prefix)
+    keys[int(table[2, 21]), 1, 3, 5] = float("nan")
+    out = torch.zeros_like(q)
+    layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
+    bad = torch.isnan(out.float()).any(-1).cpu().numpy()
+    assert bad[4:, 4:].all() and not bad[:4].any() and not bad[4:, :4].any()
+    keys[int(table[2, 21]), 1, 3, 5] = 0.0
+    keys[int(table[0, 3]), 0, 3, 0] = float("inf")
+    layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
+    bad = torch.isnan(out.float()).any(-1).cpu().numpy()
+    assert bad[:, :4].all() and not bad[:, 4:].any()
+    layer.close()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(D=64, bf16=False), dict(mode=1)], ids=str)
+def test_attend_ids_outside_the_pool(kw):
+    layer = make(num_blocks=300, **kw)
+    rng = np.random.default_rng(7)
+    pool = random_pool(layer, rng)
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, [([2, 3], 700, [100, 50]), ([1] * 9, 200, [30] * 9)], 60)
+    table[0:2, 7], table[0:2, 20], table[1, 45], table[5] = -1, 300, 2 ** 31 - 1, np.where(np.arange(60) < 12, table[5], -5)
+    table[3:, 11:] = np.where(rng.random(table[3:, 11:].shape) < 0.5, table[3:, 11:], -1)
+    kv[10] = 10 ** 9                                                      # beyond the table
+    run_attend(layer, queries(layer, rng, 14), pool, table, kv, row_start, group_start, prefix)
+    run_attend(layer, queries(layer, rng, 14), pool, np.full_like(table, -1), kv, row_start, group_start, prefix)
+    run_attend(layer, queries(layer, rng, 14), pool, table[:, :0], kv, row_start, group_start, prefix)
+    layer.close()
+
+
+def test_prefix_beyond_32_bits():
+    """A pool of more than 2^32 elements, read at its end."""
+    layer = make(Hq=32, Hkv=8, num_blocks=140000)
+    c = layer.cfg
+    pool = torch.zeros(c.pool_shape(), dtype=torch.bfloat16, device=DEV)
+    rng = np.random.default_rng(0)
+    ids = np.arange(139960, 140000)
+    small = make(Hq=32, Hkv=8, num_blocks=40)
+    some = random_pool(small, rng)
+    pool[139960:] = some
+    table = np.stack([np.concatenate([ids[:20], ids[20:30]]), np.concatenate([ids[:20], ids[30:]])])
+    q = queries(layer, rng, 4)
+    args = ([470, 480], np.array([0, 2, 4]), np.array([0, 2]), [320])
+    want = run_attend(small, q, some, table - 139960, *args)
+    out = torch.zeros_like(q)
+    layer.attn_prefix(q, pool, i32(table), i32(args[0]), i32(args[1]), i32(args[2]), i32(args[3]), out)
+    assert torch.equal(out, want)
+    layer.copy_blocks([pool], i32([139990, 3]), i32([1, 139999]))
+    assert torch.equal(pool[1], some[30]) and not pool[139999].any()
+    layer.close()
+    small.close()
+
+
+def test_integer_arrays_need_only_their_own_alignment():
+    layer, rng = make(num_blocks=200), np.random.default_rng(0)
+
+    def off(a):
+        t = torch.empty(int(np.size(a)) + 1, dtype=torch.int32, device=DEV)
+        t[1:] = i32(a).reshape(-1)
+        return t[1:].view(np.shape(a))
+    pool = random_pool(layer, rng)
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, [([2, 1], 333, [20, 31])], 30)
+    q = queries(layer, rng, 3)
+    a = layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32(group_start), i32(prefix))
+    b = layer.attn_prefix(q, pool, off(table), off(kv), off(row_start), off(group_start), off(prefix))
+    assert torch.equal(a, b)
+    got = []
+    for put in (i32, off):
+        m = binding.ForkMap(1, 2, 30, DEV)
+        m.block_tables.fill_(-1)
+        free = put(np.arange(200))
+        layer.fork_sequences(put([1, 1]), put(kv), put(table), m, free, put([60]), put([20]))
+        got.append([m.kv_lens, m.block_tables, m.copy_src, m.copy_dst, m.counts, free])
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+    layer.close()
+
+
+def test_workspaces_elsewhere_are_refused():
+    layer = make(num_blocks=20)
+    small, away = torch.zeros(16, dtype=torch.uint8, device=DEV), torch.zeros(1 << 20, dtype=torch.uint8)
+    table, q = i32([[1, 2]]), torch.zeros(1, 8, 128, dtype=torch.bfloat16, device=DEV)
+    pool, beams, forked = torch.zeros(layer.cfg.pool_shape(), dtype=torch.bfloat16, device=DEV), binding.BeamMap(1, 1, DEV), binding.ForkMap(1, 1, 2, DEV)
+    calls = (lambda ws: layer.attn_prefix(q, pool, table, i32([20]), i32([0, 1]), i32([0, 1]), i32([16]), workspace=ws),
+             lambda ws: layer.beam_select(torch.zeros(1, 50, device=DEV), torch.zeros(1, device=DEV), beams, workspace=ws),
+             lambda ws: layer.fork_sequences(i32([0]), i32([20]), table, forked, i32([3, 4]), i32([0]), workspace=ws))
+    for call in calls:
+        with pytest.raises(ValueError):
+            call(away)
+        with pytest.raises(binding.IcarusError, match="CAPACITY"):
+            call(small)
+    layer.close()
+
+
+# ---- together ------------------------------------------------------------------------------------------------------------------
+
+def _search(layer, seed, groups=3, width=4, max_blocks=40, vocab=5003):
+    """A beam search's buffers: two sets of tables that a step reads and fills, prompts of different lengths whose whole blocks are shared, two layers' pools."""
+    c, rng = layer.cfg, np.random.default_rng(seed)
+    S = groups * width
+    kv = np.repeat(rng.integers(40, 300, groups), width)
+    ids = rng.permutation(c.num_blocks)
+    table, at = np.full((S, max_blocks), -1), 0
+    for g in range(groups):
+        nb = blocks_of(kv[g * width], 16)
+        table[g * width:(g + 1) * width, :nb] = ids[at:at + nb]             # the partly filled one too: the first fork copies it
+        at += nb
+    b = dict(S=S, groups=groups, rng=rng, shared=i32(kv[::width] // 16), prefix=i32(kv[::width]), group_start=i32(np.arange(0, S + 1, width)), used=i32([at]), free=i32(ids),
+             new=i32([1] * S), act=i32([1] * S), rows=binding.SequenceMap(S, 2 * S, DEV), vocab=vocab, step=0)
+    b["tables"] = [binding.ForkMap(groups, width, max_blocks, DEV) for _ in range(2)]
+    b["beams"] = [binding.BeamMap(groups, width, DEV) for _ in range(2)]
+    for t in b["tables"]:
+        t.block_tables.fill_(-1)
+    b["tables"][0].kv_lens.copy_(i32(kv))
+    b["tables"][0].block_tables.copy_(i32(table))
+    first = b["beams"][0]
+    first.scores.fill_(-math.inf)
+    first.scores[::width] = 0.0                                            # one beam is live at first
+    first.done.zero_()
+    b["pools"] = [random_pool(layer, rng) for _ in range(2)]
+    b["codes"], b["scales"] = layer.new_key_bounds(DEV)
+    b["logits"] = torch.empty(2 * S, vocab, device=DEV)
+    b["row_start"] = i32(2 * np.arange(S + 1))
+    b["qkv"] = torch.empty(2 * S, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, dtype=c.torch_dtype, device=DEV)
+    b["q"] = torch.zeros(2 * S, c.n_q_heads, c.head_dim, dtype=c.torch_dtype, device=DEV)
+    b["out"] = [torch.zeros_like(b["q"]) for _ in range(2)]
+    return b
+
+
+def _feed(b, i):
+    """What a model would give the step: logits and projections, from the seed and the step alone."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1000 + i)
+    b["logits"].normal_(generator=gen).mul_(3)
+    b["logits"][:, 7] += 4.0 * (i > 4)                                      # the end token, likely later on
+    b["qkv"].copy_(torch.randn(b["qkv"].shape, generator=gen, device=DEV))
+
+
+def _half(layer, b, k):
+    """One step from tables and beams k into the others."""
+    now, nxt, old, new = b["tables"][k], b["tables"][1 - k], b["beams"][k], b["beams"][1 - k]
+    layer.beam_select(b["logits"], old.scores, new, row_start=b["row_start"], done=old.done, eos=7)
+    layer.fork_sequences(new.parents, now.kv_lens, now.block_tables, nxt, b["free"], b["used"], shared=b["shared"])
+    b["used"].copy_(nxt.counts[:1])
+    layer.copy_blocks(b["pools"] + [b["codes"], b["scales"]], nxt.copy_src, nxt.copy_dst)
+    m = layer.extend_sequences(b["rows"], nxt.kv_lens, b["new"], nxt.block_tables, b["free"], b["used"], streams=b["act"])
+    b["used"].copy_(m.counts[:1])
+    for pool, out in zip(b["pools"], b["out"]):
+        layer.rope_append(b["qkv"], m.row_pos, m.row_slot, pool, b["q"])
+        layer.attn_prefix(b["q"], pool, nxt.block_tables, m.kv_lens, m.row_start, b["group_start"], b["prefix"], out)
+    nxt.kv_lens.copy_(m.kv_lens)
+
+
+def _state(b):
+    every = [b["used"], b["q"], *b["out"], *b["pools"], b["rows"].row_slot]
+    for m in b["beams"]:
+        every += [m.parents, m.tokens, m.scores, m.done]
+    for m in b["tables"]:
+        every += [m.kv_lens, m.block_tables, m.copy_src, m.copy_dst, m.counts]
+    return [t.clone() for t in every]
+
+
+def _same(a, b):
+    return all(torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8)) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(Hq=4, Hkv=4, D=64, bf16=False)], ids=str)
+def test_a_search_keeps_its_histories(kw):
+    """Twenty steps: every beam's attention is the one over its own history, gathered from its ancestors token by token, and no block is lost or in two hands."""
+    layer = make(num_blocks=260, **kw)
+    c, b = layer.cfg, _search(layer, 3)
+    S, W = b["S"], 4
+    first = b["tables"][0]
+    pool0 = pool_values(layer, b["pools"][0]).reshape(c.num_blocks, c.n_kv_heads, 2, -1)
+
+    def tokens(table, n, values):
+        k = np.stack([values[int(table[p // 16]), :, 0].reshape(c.n_kv_heads, 16, -1)[:, p % 16] for p in range(n)])
+        v = np.stack([values[int(table[p // 16]), :, 1].reshape(c.n_kv_heads, -1, 16)[:, :, p % 16] for p in range(n)])
+        return np.stack([k, v], 1)
+    table0, kv0 = first.block_tables.cpu().numpy(), first.kv_lens.cpu().numpy()
+    history = [tokens(table0[s], int(kv0[s]), pool0) for s in range(S)]
+    prefix_blocks = {int(x) for s in range(0, S, W) for x in table0[s, :kv0[s] // 16]}
+    total = int(b["used"].item())
+    for i in range(20):
+        _feed(b, i)
+        _half(layer, b, i & 1)
+        torch.cuda.synchronize()
+        nxt = b["tables"][1 - (i & 1)]
+        parents = b["beams"][1 - (i & 1)].parents.cpu().numpy()
+        table, kv = nxt.block_tables.cpu().numpy(), nxt.kv_lens.cpu().numpy()
+        values = pool_values(layer, b["pools"][0]).reshape(c.num_blocks, c.n_kv_heads, 2, -1)
+        grown = []
+        for s in range(S):
+            n = int(kv[s])
+            if parents[s] < 0:
+                assert n == 1                                              # a child of nobody starts anew
+                grown.append(tokens(table[s], 1, values))
+                continue
+            mine = tokens(table[s], n, values)
+            assert np.array_equal(mine[:-1], history[s // W * W + parents[s]]), (i, s)
+            grown.append(mine)
+        history = grown
+        held = {int(x) for s in range(S) for x in table[s, :blocks_of(kv[s], 16)]}
+        left = set(b["free"].cpu().numpy()[int(b["used"].item()):].tolist())
+        assert not held & left and left | held | prefix_blocks | set(table0[:, :].ravel().tolist()) >= set(range(c.num_blocks)) - {-1}
+        assert len(left) == c.num_blocks - int(b["used"].item())
+        rows = b["rows"].row_start.cpu().numpy()
+        want, weight, size, count = ref.attend(host(b["q"]), values, table, kv, rows, np.arange(0, S + 1, W), 16, host(b["out"][0]))
+        assert (np.abs(host(b["out"][0]) - want) <= bound(layer, want, weight, size, count)).all(), i
+    assert total > 0
+    layer.close()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(Hq=4, Hkv=4, D=64, bf16=False)], ids=str)
+def test_captured_search_replays(kw):
+    """Two searches, each captured once (two steps, one from each set of tables) and replayed in turn with the program's own work between; every replay is the eager
+    pair of steps, bit for bit."""
+    layer = make(num_blocks=400, **kw)
+    eager, captured, graphs = [], [], []
+    for seed in (1, 2):
+        warm = _search(layer, seed)
+        _feed(warm, 0)
+        _half(layer, warm, 0)
+        b, want = _search(layer, seed), []
+        for i in range(10):
+            _feed(b, i)
+            _half(layer, b, 0)
+            _half(layer, b, 1)
+            want.append(_state(b))
+        eager.append(want)
+        captured.append(_search(layer, seed))
+    torch.cuda.synchronize()
+    for b in captured:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            _half(layer, b, 0)
+            _half(layer, b, 1)
+        graphs.append(g)
+    for i in range(10):
+        for want, b, g in zip(eager, captured, graphs):
+            _feed(b, i)
+            g.replay()
+            if i % 3 == 0:
+                torch.cuda.synchronize()
+            assert _same(_state(b), want[i]), i
+            (b["out"][0].float() * 2).sum().item()
+    layer.close()
+
+
+def test_two_searches_on_two_streams():
+    layer = make(num_blocks=400)
+    want, loops = [], []
+    for seed in (3, 4):
+        b = _search(layer, seed)
+        _feed(b, seed)
+        for i in range(6):
+            _half(layer, b, i & 1)
+        want.append(_state(b))
+        loops.append(_search(layer, seed))
+        _feed(loops[-1], seed)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in loops]
+    for i in range(6):
+        for b, st in zip(loops, streams):
+            with torch.cuda.stream(st):
+                _half(layer, b, i & 1)
+    torch.cuda.synchronize()
+    for b, w in zip(loops, want):
+        assert _same(_state(b), w)
+    layer.close()
