@@ -232,6 +232,17 @@ __device__ __forceinline__ bf16x8 cvt8(uint32_t lo, uint32_t hi) {
     return __builtin_bit_cast(bf16x8, r);
 }
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)lo, (_Float16)hi}); }
+// 8 FP8 codes (two dwords) -> 8 float16, exactly.
+__device__ __forceinline__ uint4 cvt8_f16(uint32_t lo, uint32_t hi) {
+    return make_uint4(__builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true)),
+                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true)));
+}
+
 // compute_group for raw FP8 fragments: the scores of all N tiles first (K codes are converted one
 // k-step at a time and die at once), then the softmax of every tile, then PV with V^T codes converted
 // one d tile at a time.  scale_log2 includes the K scale; the V scale is applied when the piece ends.

@@ -119,16 +119,6 @@ struct Item {
 // values, whose codes are float16 numbers too: weights in float16 (2^-11, at the same speed; a second product 39 -> 48 us), kLift powers of two up, to at most 2^14, so
 // that only weights below 2^-20 of the reference lose bits to float16's least exponent.
 constexpr float kLift = 6.f;
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)lo, (_Float16)hi}); }
-// 8 FP8 codes (two dwords) -> 8 float16, exactly.
-__device__ __forceinline__ uint4 cvt8_f16(uint32_t lo, uint32_t hi) {
-    return make_uint4(__builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false)),
-                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true)),
-                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false)),
-                      __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true)));
-}
 template <int NT, int N, bool KV8, bool masked, typename Frag>
 __device__ __forceinline__ void group_of(State<NT> &st, const Frag &f, const bf16x8 (&qr)[NT][kKS], const bf16x8 *__restrict__ qlds, int there, float scale_log2, int lane) {
     const int t0 = 8 * ((lane >> 4) & 1);

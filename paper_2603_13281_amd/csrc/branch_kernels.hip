@@ -674,10 +674,6 @@ hipError_t launch_copy_blocks(void *const *arrays, const int64_t *block_bytes, i
     return hipSuccess;
 }
 
-bool prefix_attn_fast(const Dims &) { return false; }
-size_t prefix_attn_workspace(const Dims &, int, int, int, int) { return 256; }
-hipError_t launch_prefix_attn(const Dims &dm, const PrefixAttnArgs &a, void *, hipStream_t st) { return launch_prefix_attn_generic(dm, a, st); }
-
 hipError_t launch_prefix_attn_generic(const Dims &dm, const PrefixAttnArgs &a, hipStream_t st) {
     const float scale = 1.f / sqrtf((float)dm.D);
     DISPATCH_TK(dm.bf16, dm.kv8, hipLaunchKernelGGL((k_prefix_attn_generic<T, KT>), dim3(dm.Hq, a.S), dim3(256), 0, st, a, dm.Hq, dm.Hkv, dm.D, dm.Bk, scale,

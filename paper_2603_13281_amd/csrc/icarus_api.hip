@@ -2163,7 +2163,8 @@ bool fork_supported(int G, int W, int max_blocks) {
     return W <= kBeamMost && (int64_t)G * W <= kBlockMaxSeqs && max_blocks <= kBlockMaxTable && (int64_t)G * (max_blocks / kForkCols + 1) <= kBranchMaxParts;
 }
 bool prefix_supported(const icarus_ctx *ctx, int S, int G, int R, int max_blocks) {
-    return S <= kBlockMaxSeqs && G <= kBlockMaxSeqs && R <= kBlockMaxRows && max_blocks <= kBlockMaxTable && !too_many_queries(ctx, R);
+    return S <= kBlockMaxSeqs && G <= kBlockMaxSeqs && R <= kBlockMaxRows && max_blocks <= kBlockMaxTable && !too_many_queries(ctx, R) &&
+           prefix_attn_workspace(ctx->dm, S, G, R, max_blocks) > 0;
 }
 }  // namespace
 
@@ -2275,7 +2276,7 @@ icarus_status icarus_attn_prefix(icarus_ctx *ctx, const void *q, const void *kv_
     if (max_blocks < 0 || S < 0 || R < 0 || G < 0) return fail(ctx, ICARUS_ERR_INVALID_ARG, "negative size");
     const icarus_layer_config &c = ctx->cfg;
     if (!prefix_supported(ctx, S, G, R, max_blocks))
-        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d sequences, %d groups, %d rows, %d blocks of a sequence: at most %d sequences and groups, %d rows, 2^30 queries of a kv-head and %d blocks per call",
+        return fail(ctx, ICARUS_ERR_UNSUPPORTED, "%d sequences, %d groups, %d rows, %d blocks of a sequence: at most %d sequences and groups, %d rows, 2^30 queries of a kv-head, %d blocks and 2^24 workgroups per call",
                     S, G, R, max_blocks, kBlockMaxSeqs, kBlockMaxRows, kBlockMaxTable);
     if (S == 0 || G == 0 || R == 0) return ICARUS_OK;
     if (any_null({q, kv_pool, kv_lens, row_start, group_start, prefix_lens, out, workspace}) || (max_blocks && !block_tables)) return fail(ctx, ICARUS_ERR_INVALID_ARG, "null array");

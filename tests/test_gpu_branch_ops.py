@@ -408,7 +408,7 @@ def test_attend_ids_outside_the_pool(kw):
     pool = random_pool(layer, rng)
     table, kv, row_start, group_start, prefix = crowd(layer, rng, [([2, 3], 700, [100, 50]), ([1] * 9, 200, [30] * 9)], 60)
     table[0:2, 7], table[0:2, 20], table[1, 45], table[5] = -1, 300, 2 ** 31 - 1, np.where(np.arange(60) < 12, table[5], -5)
-    table[3:, 11:] = np.where(rng.random(table[3:, 11:].shape) < 0.5, table[3:, 11:], -1)
+    table[3:, 12:] = np.where(rng.random(table[3:, 12:].shape) < 0.5, table[3:, 12:], -1)  # behind the 200 // 16 columns that the group shares
     kv[10] = 10 ** 9                                                      # beyond the table
     run_attend(layer, queries(layer, rng, 14), pool, table, kv, row_start, group_start, prefix)
     run_attend(layer, queries(layer, rng, 14), pool, np.full_like(table, -1), kv, row_start, group_start, prefix)
