@@ -16,6 +16,7 @@ namespace {
 
 struct PrefixUnit { int row0, rows, seq, b0, nb, len, chunks, slot; };  // its rows; the sequence whose table has the blocks b0 .. b0 + nb - 1; positions end; parts and the first one's place
 struct PrefixItem { int row0, rows, j0, seq, b0, nb, len, slot; };      // j0: the first of its queries among the unit's
+struct PrefixJoin { int row0, rows, n_shared, shared, shared_rows, n_own, own, pad; };  // a sequence's rows; place of part k of row r: shared + k * shared_rows + r, then own + k * rows + r - row0
 constexpr int kPlanThreads = 1024, kMostBlocks = 1024;                   // blocks of an item, at most
 
 struct PrefixPlan {
@@ -23,6 +24,7 @@ struct PrefixPlan {
     int *seq_group;     // [S], -1: none
     PrefixItem *items;
     int *n_items;
+    PrefixJoin *join;   // [S]
     float *o;           // parts [slot][Hq][D], slot: unit's first + part * rows + row
     float2 *ml;         // [slot][Hq]: maximum in log2 units, sum
     int cap_items;
@@ -161,6 +163,149 @@ __global__ void __launch_bounds__(kPlanThreads) k_prefix_plan(PrefixAttnArgs a, 
         slots += all_slots;
     }
     if (t == 0) *p.n_items = (int)min(items, (int64_t)p.cap_items);
+    for (int s = t; s < a.S; s += kPlanThreads) {
+        PrefixJoin j{};
+        const int group = p.seq_group[s];
+        if (group >= 0) {
+            const PrefixUnit u = p.units[a.G + s], v = p.units[group];
+            j = PrefixJoin{u.row0, u.rows, v.chunks, v.slot - v.row0, v.rows, u.chunks, u.slot, 0};
+            if (u.len == 0) j.n_shared = j.n_own = 0;  // an empty sequence among others: the shared parts are not its own
+        }
+        p.join[s] = j;
+    }
+}
+
+// The same for up to THREADS sequences and groups: one of each to a thread, everything in registers and LDS after one round of reads.
+__device__ __forceinline__ int sat(int64_t v) { return (int)min(v, (int64_t)1 << 30); }
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a, PrefixPlan p, int g, int Bk) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ int begin[THREADS], end[THREADS], least[THREADS], first[THREADS], live[THREADS], row_at[THREADS + 1], at_item[2 * THREADS], red[4][WAVES];
+    __shared__ int64_t red_work[WAVES];
+    __shared__ PrefixUnit units[2 * THREADS];
+    __shared__ int size_of[2 * THREADS];  // blocks of an item of the unit
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    const bool is_seq = t < a.S, is_group = t < a.G;
+    const int len = is_seq ? (int)min((int64_t)max(a.kv_lens[t], 0), (int64_t)a.max_blocks * Bk) : 0;
+    const int row_here = is_seq ? min(max(a.row_start[t], 0), a.R) : 0, row_last = t == 0 ? min(max(a.row_start[a.S], 0), a.R) : 0;
+    const int group_begin = is_group ? min(max(a.group_start[t], 0), a.S) : a.S;
+    const int group_end = is_group ? min(max(a.group_start[t + 1], group_begin), a.S) : a.S;
+    const int prefix = is_group ? max(a.prefix_lens[t], 0) : 0;
+    begin[t] = group_begin;
+    end[t] = group_end;
+    least[t] = first[t] = INT32_MAX;
+    live[t] = 0;
+    if (is_seq) row_at[t] = row_here;
+    if (t == 0) row_at[a.S] = row_last;
+    __syncthreads();
+    int group = -1;
+    if (is_seq) {  // the last group that begins at or before this sequence
+        int lo = 0, hi = a.G - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (begin[mid] <= t) lo = mid;
+            else hi = mid - 1;
+        }
+        if (begin[lo] <= t && t < end[lo]) group = lo;
+        if (group >= 0 && len > 0) {
+            atomicMin(&least[group], len);
+            atomicMin(&first[group], t);
+            atomicAdd(&live[group], 1);
+        }
+    }
+    __syncthreads();
+    PrefixUnit u{}, v{};  // of the group, of the sequence
+    if (is_group) {
+        const int shared = live[t] > 1 ? min(prefix, least[t]) / Bk : 0;  // one sequence reads all of its blocks by itself
+        u.row0 = row_at[group_begin];
+        u.rows = max(row_at[group_end] - u.row0, 0);
+        u.seq = first[t];
+        u.nb = u.rows ? shared : 0;
+        u.len = shared * Bk;
+        least[t] = shared;
+    }
+    __syncthreads();
+    if (group >= 0) {
+        v.row0 = row_here;
+        v.rows = max(row_at[t + 1] - row_here, 0);
+        v.seq = t;
+        v.b0 = least[group];
+        v.len = len;
+        v.nb = v.rows ? max(len / Bk + (len % Bk != 0) - v.b0, 0) : 0;
+    }
+    const auto groups_of = [&](const PrefixUnit &y) { return ((int)(((int64_t)y.rows * g + 15) / 16) + p.tiles - 1) / p.tiles; };
+    const int tg_u = groups_of(u), tg_v = groups_of(v);
+    int64_t work = (int64_t)u.nb * tg_u + (int64_t)v.nb * tg_v;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) work += __shfl_xor(work, o, 64);
+    if (lane == 0) red_work[w] = work;
+    __syncthreads();
+    int64_t total = 0;
+    for (int i = 0; i < WAVES; ++i) total += red_work[i];
+    int per = (int)min((total + p.target - 1) / p.target, (int64_t)kMostBlocks);
+    per = max((per + p.step - 1) / p.step, 1) * p.step;
+    const auto cut = [&](PrefixUnit &y) {  // even parts
+        if (y.nb == 0) return per;
+        const int chunks = (y.nb + per - 1) / per, mine = ((y.nb + chunks - 1) / chunks + p.step - 1) / p.step * p.step;
+        y.chunks = (y.nb + mine - 1) / mine;
+        return mine;
+    };
+    size_of[t] = cut(u);
+    size_of[THREADS + t] = cut(v);
+    const int n[4] = {sat((int64_t)u.chunks * tg_u), sat((int64_t)v.chunks * tg_v), sat((int64_t)u.chunks * u.rows), sat((int64_t)v.chunks * v.rows)};
+    int x[4] = {n[0], n[1], n[2], n[3]}, all[4];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int y = __shfl_up(x[k], o, 64);
+            if (lane >= o) x[k] = min(x[k] + y, 1 << 30);
+        }
+    if (lane == 63)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) red[k][w] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        int before = 0, sum = 0;
+        for (int i = 0; i < WAVES; ++i) {
+            if (i < w) before = min(before + red[k][i], 1 << 30);
+            sum = min(sum + red[k][i], 1 << 30);
+        }
+        x[k] = min(before + x[k], 1 << 30);  // with this thread's own
+        all[k] = sum;
+    }
+    const int64_t item_u = (int64_t)x[0] - n[0], item_v = (int64_t)all[0] + x[1] - n[1], slot_u = (int64_t)x[2] - n[2], slot_v = (int64_t)all[2] + x[3] - n[3];
+    if (item_u + n[0] > p.cap_items || slot_u + n[2] > p.cap_slots) u.chunks = 0;  // only where rows or groups overlap
+    if (item_v + n[1] > p.cap_items || slot_v + n[3] > p.cap_slots) v.chunks = 0;
+    u.slot = (int)slot_u;
+    v.slot = (int)slot_v;
+    at_item[t] = (int)min(item_u, (int64_t)p.cap_items);
+    at_item[THREADS + t] = (int)min(item_v, (int64_t)p.cap_items);
+    units[t] = u;
+    units[THREADS + t] = v;
+    __syncthreads();
+    const int n_items = (int)min((int64_t)all[0] + all[1], (int64_t)p.cap_items);
+    for (int k = t; k < n_items; k += THREADS) {
+        int lo = 0, hi = 2 * THREADS - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (at_item[mid] <= k) lo = mid;
+            else hi = mid - 1;
+        }
+        const PrefixUnit y = units[lo];
+        const int groups = max(groups_of(y), 1), chunk = (k - at_item[lo]) / groups, size = size_of[lo], b = chunk * size;
+        p.items[k] = PrefixItem{y.row0, y.rows, (k - at_item[lo]) % groups * p.tiles * 16, y.seq, y.b0 + b, chunk < y.chunks ? min(size, y.nb - b) : 0, y.len, y.slot + chunk * y.rows};
+    }
+    if (t == 0) *p.n_items = n_items;
+    if (is_seq) {
+        PrefixJoin j{};
+        if (group >= 0) {
+            const PrefixUnit &y = units[group];
+            j = PrefixJoin{v.row0, v.rows, len ? y.chunks : 0, y.slot - y.row0, y.rows, len ? v.chunks : 0, v.slot, 0};
+        }
+        p.join[t] = j;
+    }
 }
 
 // 16-byte LDS-direct load: lane i copies 16 bytes from its own global address to LDS byte lds_base + 16 i (lds_base wave-uniform, passed in m0); the load counts in vmcnt until the
@@ -183,6 +328,16 @@ template <bool KV8> constexpr int kStageGroups = KV8 ? 4 : 2;  // 32 tokens each
 // product (2^-15).  The rest is greater than 0 (by 2^-20 of the weight) wherever the weight is, so that an infinite value stays what it is.  FP8 values, whose codes are float16
 // numbers too: weights in float16 (2^-11), kLift powers of two up, to at most 2^14, so that only weights below 2^-20 of the reference lose bits to float16's least exponent.
 constexpr float kLift = 6.f;
+// By hand: for fmaxf the compiler first turns every score into itself, in case it were a signalling NaN.  Only for operands that no matrix instruction has just written: the compiler does
+// not keep the distance that such a result needs before it is read in front of assembly (settled()).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// Sixteen wait states behind the products: a result of a 16 x 16 x 32 product may be read after fewer.
+__device__ __forceinline__ void settled(f32x4 (&s)[1][2]) { asm volatile("s_nop 15" : "+v"(s[0][0]), "+v"(s[0][1])); }
+__device__ __forceinline__ void settled(f32x4 (&s)[2][2]) { asm volatile("s_nop 15" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1])); }
 template <int N, bool KV8, bool masked>
 __device__ __forceinline__ void prefix_group(State<kNT> &st, const char *__restrict__ src, const bf16x8 (&qr)[kNT][kKS], int there, float scale_log2, int lane) {
     const int m = lane & 15, q = lane >> 4, t0 = 8 * (q & 1);
@@ -217,6 +372,7 @@ __device__ __forceinline__ void prefix_group(State<kNT> &st, const char *__restr
     }
     float mx[N];
     bool move = false;
+    settled(sc);
 #pragma unroll
     for (int qt = 0; qt < N; ++qt) {
         if (masked)
@@ -224,7 +380,7 @@ __device__ __forceinline__ void prefix_group(State<kNT> &st, const char *__restr
             for (int i = 0; i < 8; ++i)
                 if (t0 + i >= there) sc[qt][i >> 2][i & 3] = -INFINITY;
         const f32x4 a = sc[qt][0], b = sc[qt][1];
-        mx[qt] = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]))) * scale_log2;
+        mx[qt] = max3(max3(a[0], a[1], a[2]), max3(a[3], b[0], b[1]), max3(b[2], b[3], b[3])) * scale_log2;
         move |= mx[qt] > st.m[qt] + kSlack;
     }
     if (__any(move)) {
@@ -294,29 +450,16 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
     constexpr int SG = kStageGroups<KV8>, SB = 2 * SG, kGroupBytes = KV8 ? 8192 : 16384, kStageBytes = SG * kGroupBytes;
     static_assert(2 * Image<kNT>::kBytes <= 2 * kStageBytes, "the states of two waves fit the ring");
     __shared__ __attribute__((aligned(1024))) char ring[2 * kStageBytes];
-    __shared__ int ids[kMostBlocks + SB];
-    __shared__ __attribute__((aligned(8))) uint8_t fill[kMostBlocks + SB];  // tokens of a block, 0: not in the pool
+    __shared__ int ids[kMostBlocks + SB], found[4], part_id;
     const int i = blockIdx.x / Hkv, c = blockIdx.x % Hkv;
     if (i >= *p.n_items) return;
     const PrefixItem x = p.items[i];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, q = lane >> 4, g = Hq / Hkv;
-    const int G = x.rows * g, tiles = min((G - x.j0 + 15) >> 4, kItemTiles), stages = (x.nb + SB - 1) / SB;
+    const int G = x.rows * g, tiles = min((G - x.j0 + 15) >> 4, kItemTiles);
     if (x.nb <= 0) return;
-    // this wave's tiles and groups of a stage
+    // this wave's tiles
     const bool apart = tiles > 4, single = tiles <= 2;
     const int tile0 = apart ? 2 * w : single ? (w & 1) : 2 * (w & 1), n_mine = max(min(single ? 1 : 2, tiles - tile0), 0);
-    const int first_group = apart ? 0 : w >> 1, group_step = apart ? 1 : 2;
-
-    for (int b = threadIdx.x; b < stages * SB; b += 256) {
-        int id = 0, n = 0;
-        if (b < x.nb) {
-            id = a.bt[(size_t)x.seq * a.max_blocks + x.b0 + b];
-            n = min(kBk, x.len - (x.b0 + b) * kBk);
-            if (id < 0 || id >= a.num_blocks) id = n = 0;
-        }
-        ids[b] = id;
-        fill[b] = (uint8_t)n;
-    }
     bf16x8 qr[kNT][kKS];
 #pragma unroll
     for (int qt = 0; qt < kNT; ++qt) {
@@ -325,6 +468,29 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
 #pragma unroll
         for (int ks = 0; ks < kKS; ++ks) qr[qt][ks] = qt < n_mine && j < G ? *(const bf16x8 *)(qp + (KV8 ? 64 * (ks >> 1) + 16 * q + 8 * (ks & 1) : 32 * ks + 8 * q)) : zero8();
     }
+    // The blocks, without those outside the pool: full ones, then the one that ends early, if there is one (the last).  Their order does not matter to the sums.
+    const int part_n = min(kBk, x.len - (x.b0 + x.nb - 1) * kBk);
+    int n_full = 0;
+    if (threadIdx.x == 0) part_id = -1;
+    for (int b0 = 0; b0 < x.nb; b0 += 256) {
+        const int b = b0 + threadIdx.x, id = b < x.nb ? a.bt[(size_t)x.seq * a.max_blocks + x.b0 + b] : -1;
+        const bool there = id >= 0 && id < a.num_blocks, full = there && (b < x.nb - 1 || part_n == kBk);
+        const unsigned long long mask = __ballot(full);
+        __syncthreads();
+        if (lane == 0) found[w] = __popcll(mask);
+        if (there && !full) part_id = id;
+        __syncthreads();
+        int at = n_full + __popcll(mask & ((1ull << lane) - 1));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k < w) at += found[k];
+            n_full += found[k];
+        }
+        if (full) ids[at] = id;
+    }
+    n_full = __builtin_amdgcn_readfirstlane(n_full);
+    const int last = __builtin_amdgcn_readfirstlane(part_id), n_blk = n_full + (last >= 0);
+    if (threadIdx.x < SB) ids[n_full + threadIdx.x] = threadIdx.x == 0 && last >= 0 ? last : 0;  // behind the last block: something to load
     State<kNT> st;
 #pragma unroll
     for (int qt = 0; qt < kNT; ++qt) {
@@ -361,29 +527,40 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
         __syncthreads();
     };
+    const int stages = (n_blk + SB - 1) / SB, plain = n_full / SB;  // stages, and those without masks
     __syncthreads();  // ids
-    request(0);
+    if (stages) request(0);
     meet();
-    const auto walk = [&](auto n_tiles) {
+    const auto walk = [&](auto n_tiles, auto all) {
         constexpr int N = decltype(n_tiles)::value;
+        constexpr bool ALL = decltype(all)::value;  // this wave takes all groups of a stage, else every other one
+        const auto group = [&](auto masked, int s, int gi) {
+            constexpr bool M = decltype(masked)::value;
+            const int b = s * SB + 2 * gi + (q >> 1);  // this lane's block
+            const int there = !M ? kBk : b < n_full ? kBk : b < n_blk ? part_n : 0;
+            if constexpr (N > 0) prefix_group<N, KV8, M>(st, ring + (s & 1) * kStageBytes + gi * kGroupBytes, qr, there, scale_log2, lane);
+        };
+        int s = 0;
 #pragma nounroll
-        for (int s = 0; s < stages; ++s) {
+        for (; s < plain; ++s) {
             if (s + 1 < stages) request(s + 1);
-            if constexpr (N > 0) {
+#pragma unroll
+            for (int gi = 0; gi < (ALL ? SG : SG / 2); ++gi) group(std::false_type(), s, ALL ? gi : 2 * gi + (w >> 1));
+            meet();
+        }
 #pragma nounroll
-                for (int gi = first_group; gi < SG; gi += group_step) {
-                    const char *src = ring + (s & 1) * kStageBytes + gi * kGroupBytes;
-                    const int both = __builtin_amdgcn_readfirstlane(*(const uint16_t *)(fill + s * SB + 2 * gi));
-                    if (both == (kBk << 8 | kBk)) prefix_group<N, KV8, false>(st, src, qr, kBk, scale_log2, lane);
-                    else if (both) prefix_group<N, KV8, true>(st, src, qr, both >> (q >> 1) * 8 & 0xff, scale_log2, lane);
-                }
-            }
+        for (; s < stages; ++s) {  // at most one
+#pragma nounroll
+            for (int gi = ALL ? 0 : w >> 1; gi < SG; gi += ALL ? 1 : 2)
+                if (s * SB + 2 * gi < n_blk) group(std::true_type(), s, gi);
             meet();
         }
     };
-    if (n_mine == 0) walk(std::integral_constant<int, 0>());
-    else if (n_mine == 1) walk(std::integral_constant<int, 1>());
-    else walk(std::integral_constant<int, 2>());
+    if (n_mine == 0) walk(std::integral_constant<int, 0>(), std::true_type());
+    else if (apart && n_mine == 1) walk(std::integral_constant<int, 1>(), std::true_type());
+    else if (apart) walk(std::integral_constant<int, 2>(), std::true_type());
+    else if (n_mine == 1) walk(std::integral_constant<int, 1>(), std::false_type());
+    else walk(std::integral_constant<int, 2>(), std::false_type());
     if (!apart) {  // the states of waves w and w + 2
         char *img = ring + (w & 1) * Image<kNT>::kBytes;
         if (w >= 2) image_store<kNT>(st, img, lane);
@@ -549,51 +726,53 @@ __global__ void __launch_bounds__(256) k_prefix_attn_f32(PrefixAttnArgs a, Prefi
     if (p4 == 0) p.ml[at] = make_float2(mx, sum);
 }
 
-// A row's parts put together: a wave to a head, two channels at a time to a lane; first the parts of the group's shared blocks, then those of its own.
+// A row's parts put together, first the parts of the group's shared blocks, then those of its own: a wave to a head, four channels to a lane, so that D / 4 lanes take a part and the wave
+// 256 / D of them at once (up to 256 channels).  Bound by its chain of two reads, so the first values are on their way before the maxima are known.
 template <typename T>
 __global__ void __launch_bounds__(256) k_prefix_join(PrefixAttnArgs a, PrefixPlan p, int Hq, int D) {
-    const int s = blockIdx.x, h = blockIdx.z * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int group = p.seq_group[s];
-    if (h >= Hq || group < 0) return;
-    const PrefixUnit own = p.units[a.G + s], shared = p.units[group];
-    const bool empty = own.len == 0;  // an empty sequence among others: the shared parts are not its own
-    const int n_shared = empty ? 0 : shared.chunks, n = empty ? 0 : n_shared + own.chunks;
-    for (int r = blockIdx.y; r < own.rows; r += gridDim.y) {
-        const int row = own.row0 + r;
-        const size_t out = (size_t)row * Hq + h;
-        const auto part = [&](int k) {
-            return ((size_t)(k < n_shared ? shared.slot + k * shared.rows + row - shared.row0 : own.slot + (k - n_shared) * own.rows + r) * Hq) + h;
-        };
-        for (int d0 = 0; d0 < D; d0 += 128) {
-            const int d = min(d0 + 2 * lane, D - 2);
-            float mx = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
-            for (int k0 = 0; k0 < n; k0 += 64) {
-                const int cnt = min(64, n - k0);
-                const float2 mine = lane < cnt ? p.ml[part(k0 + lane)] : make_float2(-INFINITY, 0.f);
-                const float m_new = fmaxf(mx, wave_max(mine.x));
-                const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine.x - m_new), old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m_new);
-                l = l * old + wave_sum(f * mine.y);
-                x *= old;
-                y *= old;
-                for (int k = 0; k < cnt; k += 8) {  // eight loads in flight; behind the last part: the last again, left out
-                    float2 o[8];
+    const int h = blockIdx.z * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (h >= Hq) return;
+    const PrefixJoin j = p.join[blockIdx.x];
+    const int n = j.n_shared + j.n_own, lanes = D <= 64 ? 16 : D <= 128 ? 32 : 64, side = lane / lanes, sides = 64 / lanes, d = min((lane & (lanes - 1)) * 4, D - 4);
+    for (int r = blockIdx.y; r < j.rows; r += gridDim.y) {
+        const int row = j.row0 + r;
+        const auto part = [&](int k) { return (size_t)(k < j.n_shared ? j.shared + k * j.shared_rows + row : j.own + (k - j.n_shared) * j.rows + r) * Hq + h; };
+        float mx = -INFINITY, l = 0.f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int k0 = 0; k0 < n; k0 += 64) {
+            const int cnt = min(64, n - k0);
+            constexpr int AHEAD = 8;
+            f32x4 o[AHEAD];
+            const auto load = [&](int e0) {  // behind the last part: the last again, left out
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = *(const float2 *)(p.o + part(k0 + min(k + e, cnt - 1)) * D + d);
+                for (int e = 0; e < AHEAD; ++e) o[e] = *(const f32x4 *)(p.o + part(k0 + min((e0 + e) * sides + side, cnt - 1)) * D + d);
+            };
+            load(0);
+            const float2 mine = lane < cnt ? p.ml[part(k0 + lane)] : make_float2(-INFINITY, 0.f);
+            const float m_new = fmaxf(mx, wave_max(mine.x));
+            const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine.x - m_new), old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m_new);
+            l = l * old + wave_sum(f * mine.y);
+            x *= old;
+            mx = m_new;
+            for (int e0 = 0; e0 * sides < cnt; e0 += AHEAD) {
+                if (e0) load(e0);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float fk = __shfl(f, (k + e) & 63, 64);  // 0 behind the last
-                        const uint32_t there = (uint32_t)(k + e - cnt >> 31);  // bits, not a condition: that would hold up the loads
-                        x += fk * __uint_as_float(__float_as_uint(o[e].x) & there);
-                        y += fk * __uint_as_float(__float_as_uint(o[e].y) & there);
-                    }
+                for (int e = 0; e < AHEAD; ++e) {
+                    const int k = (e0 + e) * sides + side;
+                    const float fk = __shfl(f, k & 63, 64);  // 0 behind the last
+                    if (k < cnt) x += fk * o[e];
                 }
-                mx = m_new;
             }
-            const float inv = l > 0.f ? 1.f / l : 0.f;  // a NaN stays one: the sums of values are NaN then too
-            if (d0 + 2 * lane < D) {
-                if constexpr (sizeof(T) == 2) *(uint32_t *)((T *)a.out + out * D + d) = pack_bf16(x * inv, y * inv);
-                else *(float2 *)((T *)a.out + out * D + d) = make_float2(x * inv, y * inv);
-            }
+        }
+        for (int q = lanes; q < 64; q <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], q, 64);
+        const float inv = l > 0.f ? 1.f / l : 0.f;  // a NaN stays one: the sums of values are NaN then too
+        x *= inv;
+        if (side == 0 && (lane & (lanes - 1)) * 4 < D) {
+            T *out = (T *)a.out + ((size_t)row * Hq + h) * D + d;
+            if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+            else *(f32x4 *)out = x;
         }
     }
 }
@@ -631,6 +810,7 @@ static size_t place(const Dims &dm, int S, int G, PrefixPlan &p, char *ws) {
     p.units = (PrefixUnit *)take((size_t)(G + S) * sizeof(PrefixUnit));
     p.seq_group = (int *)take((size_t)S * 4);
     p.items = (PrefixItem *)take((size_t)p.cap_items * sizeof(PrefixItem));
+    p.join = (PrefixJoin *)take((size_t)S * sizeof(PrefixJoin));
     p.ml = (float2 *)take((size_t)p.cap_slots * dm.Hq * 8);
     p.o = (float *)take((size_t)p.cap_slots * dm.Hq * dm.D * 4);
     return at;
@@ -659,7 +839,10 @@ hipError_t launch_prefix_attn(const Dims &dm, const PrefixAttnArgs &a, void *wor
     PrefixPlan p;
     if (!plan_for(dm, a.S, a.G, a.R, a.max_blocks, p)) return hipErrorInvalidValue;  // its workspace has size 0, so no call gets here
     place(dm, a.S, a.G, p, (char *)workspace);
-    hipLaunchKernelGGL(k_prefix_plan, dim3(1), dim3(kPlanThreads), 0, st, a, p, dm.Hq / dm.Hkv, dm.Bk);
+    const int g = dm.Hq / dm.Hkv, most = std::max(a.S, a.G);
+    if (most <= 256) hipLaunchKernelGGL(k_prefix_plan_small<256>, dim3(1), dim3(256), 0, st, a, p, g, dm.Bk);
+    else if (most <= 512) hipLaunchKernelGGL(k_prefix_plan_small<512>, dim3(1), dim3(512), 0, st, a, p, g, dm.Bk);
+    else hipLaunchKernelGGL(k_prefix_plan, dim3(1), dim3(kPlanThreads), 0, st, a, p, g, dm.Bk);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (on_matrix_cores(dm)) {
