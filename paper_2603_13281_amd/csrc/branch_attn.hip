@@ -308,26 +308,75 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
     }
 }
 
-// 16-byte LDS-direct load: lane i copies 16 bytes from its own global address to LDS byte lds_base + 16 i (lds_base wave-uniform, passed in m0); the load counts in vmcnt until the
+// 16-byte LDS-direct load: lane i copies 16 bytes from byte `at` (its own) behind g (the wave's) to LDS byte lds_base + 16 i (the wave's, passed in m0); the load counts in vmcnt until the
 // data is in LDS.
-__device__ __forceinline__ void to_lds16(const void *g, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(g) : "memory");
+__device__ __forceinline__ void to_lds16(const char *g, uint32_t at, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(at), "s"(g) : "memory");
 }
 
 // ---- matrix cores: bf16 storage, head_dim 128, blocks of 16 -------------------------------------------------------------
-// Keys and values of a stage go straight to LDS as the fragments that the matrix cores take, the next stage's while this one is multiplied; two workgroups to a CU.  The waves
-// share the item's tiles: of more than four, each wave has two and multiplies every group of the stage; of up to four, a pair of waves has each tile and each wave of it half of the groups,
-// and the two states are put together at the end.
-constexpr int kItemTiles = 8, kNT = 2;
-template <bool KV8> constexpr int kStageGroups = KV8 ? 4 : 2;  // 32 tokens each: a stage is 32 KB
-
-// One group of 32 tokens for N query tiles, its fragments read from LDS as they are needed: scores of all tiles, one look whether any softmax reference has to move (rare: see
-// compute_group), the weights, and the values' product.  there: tokens of this lane's block (masked only).
+// Products of 32 x 32 x 16 (operand layout of lane l, h = l / 32: A[row l % 32][k 8h .. 8h + 7], B[k 8h .. 8h + 7][col l % 32], C[row 8 (i / 4) + 4h + i % 4][col l % 32], i = 0 .. 15): beside one
+// of them, 32 cycles, a SIMD issues six vector instructions, beside two of 16 x 16 x 32 four.  Scores are keys [token][channel] times queries [channel][query]; row r of a group of two blocks is
+// token 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4 of block r / 16, so that a lane's scores 8 s + e are tokens 8h + e of block s: at once the right operand of the values' product, whose
+// left operand is a row piece of the transposed block.
 //
-// A weight of one bfloat16 (half a step, 2^-8) would add as much error, squared, as the output's own rounding; the weight is cut to 8 bits and the rest goes through a second
-// product (2^-15).  The rest is greater than 0 (by 2^-20 of the weight) wherever the weight is, so that an infinite value stays what it is.  FP8 values, whose codes are float16
-// numbers too: weights in float16 (2^-11), kLift powers of two up, to at most 2^14, so that only weights below 2^-20 of the reference lose bits to float16's least exponent.
-constexpr float kLift = 6.f;
+// Keys and values go straight to LDS; two workgroups to a CU.  An item's queries are up to four tiles of 32, and a wave has one of them.
+//   Three or four tiles: a group is a slot of a ring, requested some groups ahead by a quarter by each wave, and every wave multiplies every group.  While a group's weights are formed on the vector
+//   units, the scores of the next one are multiplied.
+//   One or two tiles, where each product is used less often than its operands are read from HBM: every wave (or two waves, one for each tile) takes groups of its own, into a part of LDS of its own,
+//   without barriers -- a group's keys are in registers before its scores are formed, and their places are taken by the next group's at once --, and the states are put together at the end.
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+constexpr int kItemTiles = 8;  // of 16 queries
+template <bool KV8> constexpr int kSlots = KV8 ? 8 : 4;
+template <bool KV8> constexpr int kGroupBytes = KV8 ? 8192 : 16384;
+
+struct PrefixState {
+    f32x16 o[4];  // sums of values of four tiles of 32 channels
+    float m, l;   // reference in log2 units, the same in both halves of the wave; sum of this half's weights
+};
+
+// A group in LDS.  Keys: rows of 8 chunks of 16 bytes (bf16: two such rows to a token, 4096 bytes apart), chunk c of row r in place c ^ (r / 2 % 8), so that lanes that read one chunk of
+// 16 rows, 256 bytes in all, meet all banks.  Then values: of each block, bf16 [tile of 32 channels][lane] as the products take them, FP8 [channel][token].
+struct PrefixPlaces { int key[4], value; };  // of this lane's chunks of keys 2 j + h; of its values
+template <bool KV8>
+__device__ __forceinline__ PrefixPlaces prefix_places(int lane) {
+    const int r = lane & 31, h = lane >> 5;
+    PrefixPlaces x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.key[j] = r * 128 + ((2 * j + h) ^ (r >> 1 & 7)) * 16;
+    x.value = KV8 ? 4096 + r * 16 + 8 * h : 8192 + lane * 16;
+    return x;
+}
+
+// The fragments are read well ahead of the products that take them: a wave issues in order, and one that waits for LDS at each product has nothing under way meanwhile.
+template <bool KV8> struct PrefixKeys { uint4 f[KV8 ? 4 : 8]; };
+template <bool KV8>
+__device__ __forceinline__ void prefix_keys(PrefixKeys<KV8> &k, const char *__restrict__ src, const PrefixPlaces &at) {
+#pragma unroll
+    for (int j = 0; j < (KV8 ? 4 : 8); ++j) k.f[j] = *(const uint4 *)(src + at.key[j & 3] + (j >> 2) * 4096);
+}
+template <bool KV8> struct PrefixValues { typename std::conditional<KV8, uint2, uint4>::type f[4]; };  // of one block
+template <bool KV8>
+__device__ __forceinline__ void prefix_block(PrefixValues<KV8> &v, const char *__restrict__ src, const PrefixPlaces &at, int s) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v.f[x] = *(const typename std::conditional<KV8, uint2, uint4>::type *)(src + at.value + s * (KV8 ? 2048 : 4096) + x * (KV8 ? 512 : 1024));
+}
+// Scores of a group, raw.
+template <bool KV8>
+__device__ __forceinline__ void prefix_scores(f32x16 &sc, const PrefixKeys<KV8> &k, const bf16x8 (&qr)[8]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < (KV8 ? 4 : 8); ++j) {
+        if constexpr (KV8) {
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cvt8(k.f[j].x, k.f[j].y), qr[2 * j], sc, 0, 0, 0);
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cvt8(k.f[j].z, k.f[j].w), qr[2 * j + 1], sc, 0, 0, 0);
+        } else {
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k.f[j]), qr[j], sc, 0, 0, 0);
+        }
+    }
+}
+
 // By hand: for fmaxf the compiler first turns every score into itself, in case it were a signalling NaN.  Only for operands that no matrix instruction has just written: the compiler does
 // not keep the distance that such a result needs before it is read in front of assembly (settled()).
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -335,111 +384,77 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
-// Sixteen wait states behind the products: a result of a 16 x 16 x 32 product may be read after fewer.
-__device__ __forceinline__ void settled(f32x4 (&s)[1][2]) { asm volatile("s_nop 15" : "+v"(s[0][0]), "+v"(s[0][1])); }
-__device__ __forceinline__ void settled(f32x4 (&s)[2][2]) { asm volatile("s_nop 15" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1])); }
-template <int N, bool KV8, bool masked>
-__device__ __forceinline__ void prefix_group(State<kNT> &st, const char *__restrict__ src, const bf16x8 (&qr)[kNT][kKS], int there, float scale_log2, int lane) {
-    const int m = lane & 15, q = lane >> 4, t0 = 8 * (q & 1);
-    f32x4 sc[N][2];
-#pragma unroll
-    for (int qt = 0; qt < N; ++qt)
-        sc[qt][0] = sc[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if constexpr (KV8) {
-#pragma unroll
-        for (int sl = 0; sl < 2; ++sl) {
-            const uint4 r0 = *(const uint4 *)(src + sl * 1024 + lane * 16), r1 = *(const uint4 *)(src + (2 + sl) * 1024 + lane * 16);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bf16x8 k0 = h ? cvt8(r0.z, r0.w) : cvt8(r0.x, r0.y), k1 = h ? cvt8(r1.z, r1.w) : cvt8(r1.x, r1.y);
-#pragma unroll
-                for (int qt = 0; qt < N; ++qt) {
-                    sc[qt][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qr[qt][2 * sl + h], sc[qt][0], 0, 0, 0);
-                    sc[qt][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qr[qt][2 * sl + h], sc[qt][1], 0, 0, 0);
-                }
-            }
-        }
-    } else {
-#pragma unroll
-        for (int ks = 0; ks < kKS; ++ks) {
-            const bf16x8 k0 = *(const bf16x8 *)(src + ks * 1024 + lane * 16), k1 = *(const bf16x8 *)(src + (kKS + ks) * 1024 + lane * 16);
-#pragma unroll
-            for (int qt = 0; qt < N; ++qt) {
-                sc[qt][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qr[qt][ks], sc[qt][0], 0, 0, 0);
-                sc[qt][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qr[qt][ks], sc[qt][1], 0, 0, 0);
-            }
-        }
-    }
-    float mx[N];
-    bool move = false;
+// Twenty wait states behind the products: any result may be read after fewer.
+__device__ __forceinline__ void settled(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
+
+// One look whether the softmax reference has to move (rare: see compute_group).  there: tokens of the two blocks (masked only).
+template <bool masked>
+__device__ __forceinline__ void prefix_reference(PrefixState &st, f32x16 &sc, int there0, int there1, float scale_log2, int lane) {
+    const int t0 = 8 * (lane >> 5);
     settled(sc);
+    if (masked)
 #pragma unroll
-    for (int qt = 0; qt < N; ++qt) {
-        if (masked)
+        for (int i = 0; i < 16; ++i)
+            if (t0 + i % 8 >= (i < 8 ? there0 : there1)) sc[i] = -INFINITY;
+    const float a = max3(sc[0], sc[1], sc[2]), b = max3(sc[3], sc[4], sc[5]), c = max3(sc[6], sc[7], sc[8]), d = max3(sc[9], sc[10], sc[11]), e = max3(sc[12], sc[13], sc[14]);
+    float mx = max3(max3(a, b, c), max3(d, e, sc[15]), sc[15]) * scale_log2;
+    if (__builtin_expect(__any(mx > st.m + kSlack), 0)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(st.m, mx), f = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
+        st.m = m_new;
+        st.l *= f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (t0 + i >= there) sc[qt][i >> 2][i & 3] = -INFINITY;
-        const f32x4 a = sc[qt][0], b = sc[qt][1];
-        mx[qt] = max3(max3(a[0], a[1], a[2]), max3(a[3], b[0], b[1]), max3(b[2], b[3], b[3])) * scale_log2;
-        move |= mx[qt] > st.m[qt] + kSlack;
+        for (int x = 0; x < 4; ++x) st.o[x] *= f;
     }
-    if (__any(move)) {
+}
+
+// Weights of a group and the values' product.
+//
+// A weight of one bfloat16 (half a step, 2^-8) would add as much error, squared, as the output's own rounding; the weight is cut to 8 bits and the rest goes through a second
+// product (2^-15).  The rest is greater than 0 (by 2^-20 of the weight) wherever the weight is, so that an infinite value stays what it is.  FP8 values, whose codes are float16
+// numbers too: weights in float16 (2^-11), kLift powers of two up, to at most 2^14, so that only weights below 2^-20 of the reference lose bits to float16's least exponent.
+constexpr float kLift = 6.f;
+template <bool KV8, bool masked>
+__device__ __forceinline__ void prefix_values(PrefixState &st, const f32x16 &sc, const PrefixValues<KV8> (&vf)[2], int there0, int there1, float scale_log2, int lane) {
+    const int t0 = 8 * (lane >> 5);
+    const float m_ref = (st.m == -INFINITY ? 0.f : st.m) - (KV8 ? kLift : 0.f);  // nothing yet: every weight 0
 #pragma unroll
-        for (int qt = 0; qt < N; ++qt) {
-            float m_new = fmaxf(mx[qt], __shfl_xor(mx[qt], 16, 64));
-            m_new = fmaxf(st.m[qt], fmaxf(m_new, __shfl_xor(m_new, 32, 64)));
-            if (!__any(mx[qt] > st.m[qt] + kSlack)) m_new = st.m[qt];  // a tile's results must not depend on the tiles beside it
-            const float c = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[qt] - m_new);
-            st.m[qt] = m_new;
-            st.l[qt] *= c;
-#pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] *= c;
-        }
-    }
-    uint4 hi[N], lo[N];
-#pragma unroll
-    for (int qt = 0; qt < N; ++qt) {
-        const float m_ref = (st.m[qt] == -INFINITY ? 0.f : st.m[qt]) - (KV8 ? kLift : 0.f);  // nothing yet: every weight 0
+    for (int s = 0; s < 2; ++s) {
         float e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 2][i & 3], scale_log2, -m_ref));
-        st.l[qt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));  // as they are
+        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * s + i], scale_log2, -m_ref));
+        st.l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));  // as they are
+        uint4 hi, lo;
         if constexpr (KV8) {
-            hi[qt] = make_uint4(pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]), pack_f16(e[6], e[7]));
+            hi = make_uint4(pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]), pack_f16(e[6], e[7]));
         } else {
             uint32_t p[4], rest[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t x = __float_as_uint(e[2 * i]) & 0xffff0000u, y = __float_as_uint(e[2 * i + 1]) & 0xffff0000u;
-                p[i] = x >> 16 | y;
+                p[i] = __builtin_amdgcn_perm(__float_as_uint(e[2 * i + 1]), __float_as_uint(e[2 * i]), 0x07060302u);
                 rest[i] = pack_bf16(__builtin_fmaf(e[2 * i], 1.f + 0x1p-20f, -__uint_as_float(x)), __builtin_fmaf(e[2 * i + 1], 1.f + 0x1p-20f, -__uint_as_float(y)));
             }
-            hi[qt] = make_uint4(p[0], p[1], p[2], p[3]);
-            lo[qt] = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+            hi = make_uint4(p[0], p[1], p[2], p[3]);
+            lo = make_uint4(rest[0], rest[1], rest[2], rest[3]);
         }
-    }
-    uint32_t keep[4];  // places behind the last token may hold anything
-    if (masked) {
+        const int there = s ? there1 : there0;
+        uint32_t keep[4];  // places behind the last token may hold anything
+        if (masked) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) keep[i] = (t0 + 2 * i < there ? 0xffffu : 0u) | (t0 + 2 * i + 1 < there ? 0xffff0000u : 0u);
-    }
-#pragma unroll
-    for (int dt = 0; dt < kDT; ++dt) {
-        uint4 v;
-        if constexpr (KV8) {
-            const uint2 r = *(const uint2 *)(src + 4096 + (q >> 1) * 2048 + (16 * dt + m) * 16 + t0);
-            v = cvt8_f16(r.x, r.y);
-        } else {
-            v = *(const uint4 *)(src + (2 * kKS + dt) * 1024 + lane * 16);
+            for (int i = 0; i < 4; ++i) keep[i] = (t0 + 2 * i < there ? 0xffffu : 0u) | (t0 + 2 * i + 1 < there ? 0xffff0000u : 0u);
         }
-        if (masked) v = make_uint4(v.x & keep[0], v.y & keep[1], v.z & keep[2], v.w & keep[3]);
 #pragma unroll
-        for (int qt = 0; qt < N; ++qt) {
+        for (int x = 0; x < 4; ++x) {
+            uint4 v;
+            if constexpr (KV8) v = cvt8_f16(vf[s].f[x].x, vf[s].f[x].y);
+            else v = vf[s].f[x];
+            if (masked) v = make_uint4(v.x & keep[0], v.y & keep[1], v.z & keep[2], v.w & keep[3]);
             if constexpr (KV8) {
-                st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, hi[qt]), st.o[dt][qt], 0, 0, 0);
+                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, hi), st.o[x], 0, 0, 0);
             } else {
-                st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, hi[qt]), st.o[dt][qt], 0, 0, 0);
-                st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, lo[qt]), st.o[dt][qt], 0, 0, 0);
+                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, hi), st.o[x], 0, 0, 0);
+                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, lo), st.o[x], 0, 0, 0);
             }
         }
     }
@@ -447,26 +462,24 @@ __device__ __forceinline__ void prefix_group(State<kNT> &st, const char *__restr
 
 template <bool KV8>
 __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, PrefixPlan p, int Hq, int Hkv, float scale_log2, float v_scale) {
-    constexpr int SG = kStageGroups<KV8>, SB = 2 * SG, kGroupBytes = KV8 ? 8192 : 16384, kStageBytes = SG * kGroupBytes;
-    static_assert(2 * Image<kNT>::kBytes <= 2 * kStageBytes, "the states of two waves fit the ring");
-    __shared__ __attribute__((aligned(1024))) char ring[2 * kStageBytes];
-    __shared__ int ids[kMostBlocks + SB], found[4], part_id;
-    const int i = blockIdx.x / Hkv, c = blockIdx.x % Hkv;
-    if (i >= *p.n_items) return;
+    constexpr int SLOTS = kSlots<KV8>, BYTES = kGroupBytes<KV8>, ES = KV8 ? 1 : 2;
+    __shared__ __attribute__((aligned(1024))) char ring[SLOTS * BYTES];
+    static_assert(SLOTS * BYTES == 4 * 16384, "a state to a wave");
+    __shared__ __attribute__((aligned(8))) int ids[kMostBlocks + 2];
+    __shared__ int found[4], part_id;
+    __shared__ float2 state_ml[4][64];
+    const int i = blockIdx.x / Hkv, c = blockIdx.x % Hkv, n_items = *p.n_items;
     const PrefixItem x = p.items[i];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, q = lane >> 4, g = Hq / Hkv;
-    const int G = x.rows * g, tiles = min((G - x.j0 + 15) >> 4, kItemTiles);
-    if (x.nb <= 0) return;
-    // this wave's tiles
-    const bool apart = tiles > 4, single = tiles <= 2;
-    const int tile0 = apart ? 2 * w : single ? (w & 1) : 2 * (w & 1), n_mine = max(min(single ? 1 : 2, tiles - tile0), 0);
-    bf16x8 qr[kNT][kKS];
-#pragma unroll
-    for (int qt = 0; qt < kNT; ++qt) {
-        const int j = x.j0 + 16 * (tile0 + qt) + m;
+    if (i >= n_items || x.nb <= 0) return;
+    const int lane = threadIdx.x & 63, h = lane >> 5, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = Hq / Hkv;
+    const int G = x.rows * g, tiles = min((G - x.j0 + 31) >> 5, kItemTiles / 2);
+    const bool narrow = tiles <= 2;
+    const int tile = narrow ? w & (tiles - 1) : w, j = x.j0 + 32 * tile + (lane & 31);
+    bf16x8 qr[8];
+    {
         const bf16_t *qp = (const bf16_t *)a.q + ((size_t)(x.row0 + j / g) * Hq + c * g + j % g) * kD;
 #pragma unroll
-        for (int ks = 0; ks < kKS; ++ks) qr[qt][ks] = qt < n_mine && j < G ? *(const bf16x8 *)(qp + (KV8 ? 64 * (ks >> 1) + 16 * q + 8 * (ks & 1) : 32 * ks + 8 * q)) : zero8();
+        for (int k = 0; k < 8; ++k) qr[k] = tile < tiles && j < G ? *(const bf16x8 *)(qp + (KV8 ? 32 * (k >> 1) + 16 * h + 8 * (k & 1) : 16 * k + 8 * h)) : zero8();
     }
     // The blocks, without those outside the pool: full ones, then the one that ends early, if there is one (the last).  Their order does not matter to the sums.
     const int part_n = min(kBk, x.len - (x.b0 + x.nb - 1) * kBk);
@@ -489,107 +502,202 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
         if (full) ids[at] = id;
     }
     n_full = __builtin_amdgcn_readfirstlane(n_full);
-    const int last = __builtin_amdgcn_readfirstlane(part_id), n_blk = n_full + (last >= 0);
-    if (threadIdx.x < SB) ids[n_full + threadIdx.x] = threadIdx.x == 0 && last >= 0 ? last : 0;  // behind the last block: something to load
-    State<kNT> st;
+    const int last = __builtin_amdgcn_readfirstlane(part_id), n_blk = n_full + (last >= 0), n_grp = (n_blk + 1) / 2;
+    if (threadIdx.x < 2) ids[n_full + threadIdx.x] = threadIdx.x == 0 && last >= 0 ? last : 0;  // behind the last block: something to load
+    PrefixState st;
+    st.m = -INFINITY;
+    st.l = 0.f;
 #pragma unroll
-    for (int qt = 0; qt < kNT; ++qt) {
-        st.m[qt] = -INFINITY;
-        st.l[qt] = 0.f;
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+        for (int k = 0; k < 16; ++k) st.o[t][k] = 0.f;
+    const PrefixPlaces at = prefix_places<KV8>(lane);
+    // Where this lane's 16 bytes of a load stand in a block.  Keys: eight rows of 128 bytes to a load; the next eight rows are 4 tokens on.  Values: a KB to a load.
+    const int r8 = lane >> 3, chunk = (lane & 7) ^ (r8 >> 1), token = 8 * (r8 >> 2) + (r8 & 3);
+    const int key = token * kD * ES + chunk * 16, on = 4 * kD * ES + ((chunk ^ 4) - chunk) * 16;
+    const int value = kBk * kD * ES + (KV8 ? 16 * lane : 32 * (lane & 31) + 16 * h);
+    const char *const pool = (const char *)a.pool + (size_t)c * (2 * kBk * kD * ES);
+    const size_t stride = (size_t)Hkv * 2 * kBk * kD * ES;
     const uint32_t ring0 = (uint32_t)(size_t)(__attribute__((address_space(3))) char *)ring;
-    // This wave's quarter of a group: w = 0, 1 the key rows of tile w; w = 2, 3 value rows (bf16: four d tiles of both blocks; FP8: one block).
-    const auto request = [&](int stage) {
-        const uint32_t to = ring0 + (stage & 1) * kStageBytes;
-#pragma unroll
-        for (int gi = 0; gi < SG; ++gi) {
-            const int *id2 = ids + stage * SB + 2 * gi;
-            if constexpr (KV8) {
-                const size_t head = (size_t)2 * kBk * kD;
-                const int sel = w < 2 ? m >> 3 : w - 2;
-                const uint8_t *blk = (const uint8_t *)a.pool + ((size_t)id2[sel] * Hkv + c) * head;
-                const uint8_t *from = w < 2 ? blk + (8 * ((m >> 2) & 1) + (m & 3) + 4 * w) * kD + 16 * q : blk + kBk * kD + 16 * lane;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) to_lds16(from + k * (w < 2 ? 64 : 1024), to + gi * kGroupBytes + (2 * w + k) * 1024);
-            } else {
-                const size_t head = (size_t)2 * kBk * kD;
-                const int sel = w < 2 ? m >> 3 : q >> 1;
-                const bf16_t *blk = (const bf16_t *)a.pool + ((size_t)id2[sel] * Hkv + c) * head;
-                const bf16_t *from = w < 2 ? blk + (8 * ((m >> 2) & 1) + (m & 3) + 4 * w) * kD + 8 * q : blk + kBk * kD + (64 * (w - 2) + m) * kBk + 8 * (q & 1);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) to_lds16(from + k * (w < 2 ? 32 : 16 * kBk), to + gi * kGroupBytes + (4 * w + k) * 1024);
-            }
-        }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the queries are here, so the waits below count the requests alone
+    __syncthreads();                     // ids
+    const auto blocks_of_group = [&](int grp) {  // wave-uniform
+        const int2 v = *(const int2 *)(ids + 2 * grp);
+        return make_int2(__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y));
     };
-    const auto meet = [&] {  // what this wave brought has landed in LDS, and so has what the others brought
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-        __syncthreads();
+    const auto tokens_of = [&](int b) { return b < n_full ? kBk : b < n_blk ? part_n : 0; };
+    const auto put = [&](const f32x16 &o, int t) {  // sums of channel tile t
+        const size_t to = (size_t)(x.slot + j / g) * Hq + c * g + j % g;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *(f32x4 *)(p.o + to * kD + 32 * t + 8 * k + 4 * h) = f32x4{o[4 * k] * v_scale, o[4 * k + 1] * v_scale, o[4 * k + 2] * v_scale, o[4 * k + 3] * v_scale};
     };
-    const int stages = (n_blk + SB - 1) / SB, plain = n_full / SB;  // stages, and those without masks
-    __syncthreads();  // ids
-    if (stages) request(0);
-    meet();
-    const auto walk = [&](auto n_tiles, auto all) {
-        constexpr int N = decltype(n_tiles)::value;
-        constexpr bool ALL = decltype(all)::value;  // this wave takes all groups of a stage, else every other one
-        const auto group = [&](auto masked, int s, int gi) {
-            constexpr bool M = decltype(masked)::value;
-            const int b = s * SB + 2 * gi + (q >> 1);  // this lane's block
-            const int there = !M ? kBk : b < n_full ? kBk : b < n_blk ? part_n : 0;
-            if constexpr (N > 0) prefix_group<N, KV8, M>(st, ring + (s & 1) * kStageBytes + gi * kGroupBytes, qr, there, scale_log2, lane);
+    const auto put_ml = [&](float m, float l) { p.ml[(size_t)(x.slot + j / g) * Hq + c * g + j % g] = make_float2(m, l); };
+
+    if (narrow) {
+        constexpr int LOADS = KV8 ? 4 : 8;  // of a group's keys, and of its values
+        const int step = 4 / tiles, first = w / tiles;  // one tile: groups w, w + 4, ..; two: w / 2, w / 2 + 2, ..
+        const uint32_t to = ring0 + w * 16384;
+        const char *const src = ring + w * 16384;
+        const auto request_keys = [&](int2 b) {
+            const char *const from0 = pool + b.x * stride, *const from1 = pool + b.y * stride;
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) to_lds16((k & 3) < 2 ? from0 : from1, key + (k & 1) * on + (k >> 2) * 128, to + k * 1024);
         };
-        int s = 0;
-#pragma nounroll
-        for (; s < plain; ++s) {
-            if (s + 1 < stages) request(s + 1);
+        const auto request_values = [&](int2 b) {
+            const char *const from0 = pool + b.x * stride, *const from1 = pool + b.y * stride;
 #pragma unroll
-            for (int gi = 0; gi < (ALL ? SG : SG / 2); ++gi) group(std::false_type(), s, ALL ? gi : 2 * gi + (w >> 1));
-            meet();
+            for (int k = 0; k < LOADS; ++k) to_lds16(k < LOADS / 2 ? from0 : from1, value + (k & (LOADS / 2 - 1)) * 1024, to + (LOADS + k) * 1024);
+        };
+        if (first < n_grp) {
+            const int2 b = blocks_of_group(first);
+            request_keys(b);
+            request_values(b);
         }
 #pragma nounroll
-        for (; s < stages; ++s) {  // at most one
-#pragma nounroll
-            for (int gi = ALL ? 0 : w >> 1; gi < SG; gi += ALL ? 1 : 2)
-                if (s * SB + 2 * gi < n_blk) group(std::true_type(), s, gi);
-            meet();
+        for (int k = first; k < n_grp; k += step) {
+            const bool more = k + step < n_grp;
+            const int2 b = blocks_of_group(more ? k + step : k);
+            const int there0 = tokens_of(2 * k), there1 = tokens_of(2 * k + 1);
+            PrefixKeys<KV8> kf;
+            PrefixValues<KV8> vf[2];
+            f32x16 sc;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");  // the keys have landed, the values may be under way
+            prefix_keys<KV8>(kf, src, at);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // and are in registers
+            if (more) request_keys(b);
+            prefix_scores<KV8>(sc, kf, qr);
+            prefix_reference<true>(st, sc, there0, there1, scale_log2, lane);
+            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            prefix_block<KV8>(vf[0], src, at, 0);
+            prefix_block<KV8>(vf[1], src, at, 1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (more) request_values(b);
+            prefix_values<KV8, true>(st, sc, vf, there0, there1, scale_log2, lane);
+        }
+        // The states of the waves that have the same tile: each leaves its own in LDS, in its own part, and takes 4 / step of the channels.
+        f32x4 *const mine = (f32x4 *)(ring + w * 16384);
+        state_ml[w][lane] = make_float2(st.m, st.l);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mine[(4 * t + k) * 64 + lane] = f32x4{st.o[t][4 * k], st.o[t][4 * k + 1], st.o[t][4 * k + 2], st.o[t][4 * k + 3]};
+        __syncthreads();
+        float m = -INFINITY, l = 0.f, f[4];
+        for (int k = 0; k < step; ++k) m = fmaxf(m, state_ml[tile + k * tiles][lane].x);
+        for (int k = 0; k < step; ++k) {
+            const float2 v = state_ml[tile + k * tiles][lane];
+            f[k] = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v.x - m);
+            l += f[k] * v.y;
+        }
+        l += __shfl_xor(l, 32, 64);
+        if (j >= G) return;
+        for (int t = first; t < 4; t += step) {
+            f32x16 o;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k] = 0.f;
+            for (int y = 0; y < step; ++y)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const f32x4 v = ((const f32x4 *)(ring + (tile + y * tiles) * 16384))[(4 * t + k) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[4 * k + e] += f[y] * v[e];
+                }
+            put(o, t);
+        }
+        if (first == 0 && h == 0) put_ml(m, l);
+        return;
+    }
+
+    constexpr int LOADS = KV8 ? 2 : 4;
+    int2 pair = make_int2(0, 0);  // the blocks of the group that is requested next, read ahead: what an address waits for, every product behind it waits for
+    // This wave's quarter of a group.  w = 0, 1: keys, bf16 half w of all 32 rows, FP8 the rows of block w; w = 2, 3: the values of block w - 2.
+    const auto request = [&](int grp) {
+        const uint32_t to = ring0 + (grp & (SLOTS - 1)) * BYTES + LOADS * 1024 * w;
+        const char *const from0 = pool + pair.x * stride, *const from1 = pool + pair.y * stride;
+        if (w < 2 && !KV8) {  // rows 0 .. 15 are the first block's
+            to_lds16(from0, key + 128 * w, to);
+            to_lds16(from0, key + 128 * w + on, to + 1024);
+            to_lds16(from1, key + 128 * w, to + 2048);
+            to_lds16(from1, key + 128 * w + on, to + 3072);
+        } else {
+            const char *const from = w & 1 ? from1 : from0;
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) to_lds16(from, w < 2 ? key + k * on : value + k * 1024, to + k * 1024);
         }
     };
-    if (n_mine == 0) walk(std::integral_constant<int, 0>(), std::true_type());
-    else if (apart && n_mine == 1) walk(std::integral_constant<int, 1>(), std::true_type());
-    else if (apart) walk(std::integral_constant<int, 2>(), std::true_type());
-    else if (n_mine == 1) walk(std::integral_constant<int, 1>(), std::false_type());
-    else walk(std::integral_constant<int, 2>(), std::false_type());
-    if (!apart) {  // the states of waves w and w + 2
-        char *img = ring + (w & 1) * Image<kNT>::kBytes;
-        if (w >= 2) image_store<kNT>(st, img, lane);
+    // Before group k is multiplied, all that this wave requested of it has landed (younger requests may be under way), and behind the barrier what the other waves requested too.
+    const auto landed = [&](int k) {
+        constexpr int younger = (SLOTS - 3) * LOADS;  // of groups k + 1 .. k + SLOTS - 3
+        static_assert(younger < 16, "one field of the wait's count");
+        if (k + SLOTS - 3 < n_grp) __builtin_amdgcn_s_waitcnt(0x0f70 | younger);
+        else __builtin_amdgcn_s_waitcnt(0x0f70);
         __syncthreads();
-        if (w >= 2) return;
-        const float2 *ml = (const float2 *)(img + Image<kNT>::kO * 16);
-#pragma unroll
-        for (int qt = 0; qt < kNT; ++qt) {
-            const float2 other = ml[qt * 64 + lane];
-            const float mx = fmaxf(st.m[qt], other.x);
-            const float f = st.m[qt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[qt] - mx), fo = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x - mx);
-            st.m[qt] = mx;
-            st.l[qt] = f * st.l[qt] + fo * other.y;
-#pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) st.o[dt][qt] = f * st.o[dt][qt] + fo * ((const f32x4 *)img)[(dt * kNT + qt) * 64 + lane];
+    };
+    const auto slot = [&](int k) { return ring + (k & (SLOTS - 1)) * BYTES; };
+    if (n_grp > 0) {
+        for (int k = 0; k < min(SLOTS - 2, n_grp); ++k) {
+            pair = blocks_of_group(k);
+            request(k);
+        }
+        pair = blocks_of_group(min(SLOTS - 2, n_grp - 1));
+        landed(0);
+        if (SLOTS - 2 < n_grp) request(SLOTS - 2);
+        pair = blocks_of_group(min(SLOTS - 1, n_grp - 1));
+    }
+    if (tile >= tiles) {
+        for (int k = 0; k + 1 < n_grp; ++k) {
+            landed(k + 1);
+            if (k + SLOTS - 1 < n_grp) request(k + SLOTS - 1);
+            pair = blocks_of_group(min(k + SLOTS, n_grp - 1));
+        }
+        return;
+    }
+    if (n_grp > 0) {
+        f32x16 now, next;
+        PrefixKeys<KV8> kf;
+        PrefixValues<KV8> vf[2];
+        prefix_keys<KV8>(kf, slot(0), at);
+        prefix_scores<KV8>(now, kf, qr);
+        const auto step = [&](int k, f32x16 &x0, f32x16 &x1) {
+            landed(k + 1);  // and every wave is done with group k - 1, whose slot is taken now
+            if (k + SLOTS - 1 < n_grp) request(k + SLOTS - 1);
+            const int2 ahead = *(const int2 *)(ids + 2 * min(k + SLOTS, n_grp - 1));
+            prefix_keys<KV8>(kf, slot(k + 1), at);
+            prefix_block<KV8>(vf[0], slot(k), at, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            prefix_reference<false>(st, x0, kBk, kBk, scale_log2, lane);
+            prefix_block<KV8>(vf[1], slot(k), at, 1);
+            prefix_scores<KV8>(x1, kf, qr);
+            prefix_values<KV8, false>(st, x0, vf, kBk, kBk, scale_log2, lane);
+            pair = make_int2(__builtin_amdgcn_readfirstlane(ahead.x), __builtin_amdgcn_readfirstlane(ahead.y));
+        };
+        int k = 0;
+#pragma nounroll
+        for (; k + 2 < n_grp; k += 2) {
+            step(k, now, next);
+            step(k + 1, next, now);
+        }
+        const auto end = [&](f32x16 &y) {  // the last group, of which a block may end early or be missing
+            const int there0 = tokens_of(2 * (n_grp - 1)), there1 = tokens_of(2 * n_grp - 1);
+            prefix_block<KV8>(vf[0], slot(n_grp - 1), at, 0);
+            prefix_block<KV8>(vf[1], slot(n_grp - 1), at, 1);
+            prefix_reference<true>(st, y, there0, there1, scale_log2, lane);
+            prefix_values<KV8, true>(st, y, vf, there0, there1, scale_log2, lane);
+        };
+        if (k + 1 < n_grp) {
+            step(k, now, next);
+            end(next);
+        } else {
+            end(now);
         }
     }
+    const float l = st.l + __shfl_xor(st.l, 32, 64);
+    if (j >= G) return;
 #pragma unroll
-    for (int qt = 0; qt < kNT; ++qt) {
-        float l = st.l[qt];
-        l += __shfl_xor(l, 16, 64);
-        l += __shfl_xor(l, 32, 64);
-        const int j = x.j0 + 16 * (tile0 + qt) + m;
-        if (qt >= n_mine || j >= G) continue;
-        const size_t at = (size_t)(x.slot + j / g) * Hq + c * g + j % g;
-#pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) *(f32x4 *)(p.o + at * kD + 16 * dt + 4 * q) = st.o[dt][qt] * v_scale;
-        if (q == 0) p.ml[at] = make_float2(st.m[qt], l);
-    }
+    for (int t = 0; t < 4; ++t) put(st.o[t], t);
+    if (h == 0) put_ml(st.m, l);
 }
 
 bool on_matrix_cores(const Dims &dm) { return dm.bf16 && dm.D == kD && dm.Bk == kBk; }
@@ -784,7 +892,7 @@ bool plan_for(const Dims &dm, int S, int G, int R, int max_blocks, PrefixPlan &p
     const int g = dm.Hq / dm.Hkv;
     p = PrefixPlan{};
     p.tiles = mfma ? kItemTiles : 1;
-    p.step = mfma ? (dm.kv8 ? 2 * kStageGroups<true> : 2 * kStageGroups<false>) : std::max(1, 8 * 16 / dm.Bk);
+    p.step = mfma ? 4 : std::max(1, 8 * 16 / dm.Bk);
     p.target = std::max(1, (mfma ? 512 : 1024) / dm.Hkv);
     const int64_t groups = 2 * (((int64_t)R * g + 15) / 16 / p.tiles + 1) + G + S;  // tile groups of all units, at most
     const int64_t items = std::max<int64_t>(p.target, groups * ((int64_t)max_blocks / kMostBlocks + 1)) + 2 * groups;
