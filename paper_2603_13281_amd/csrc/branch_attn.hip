@@ -414,48 +414,50 @@ __device__ __forceinline__ void prefix_reference(PrefixState &st, f32x16 &sc, in
 // product (2^-15).  The rest is greater than 0 (by 2^-20 of the weight) wherever the weight is, so that an infinite value stays what it is.  FP8 values, whose codes are float16
 // numbers too: weights in float16 (2^-11), kLift powers of two up, to at most 2^14, so that only weights below 2^-20 of the reference lose bits to float16's least exponent.
 constexpr float kLift = 6.f;
-template <bool KV8, bool masked>
-__device__ __forceinline__ void prefix_values(PrefixState &st, const f32x16 &sc, const PrefixValues<KV8> (&vf)[2], int there0, int there1, float scale_log2, int lane) {
-    const int t0 = 8 * (lane >> 5);
+struct PrefixWeights { uint4 hi, lo; };  // of one block's 8 tokens of this lane
+template <bool KV8>
+__device__ __forceinline__ PrefixWeights prefix_weights(PrefixState &st, const f32x16 &sc, int s, float scale_log2) {
     const float m_ref = (st.m == -INFINITY ? 0.f : st.m) - (KV8 ? kLift : 0.f);  // nothing yet: every weight 0
+    float e[8];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        float e[8];
+    for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * s + i], scale_log2, -m_ref));
+    st.l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));  // as they are
+    PrefixWeights p;
+    if constexpr (KV8) {
+        p.hi = p.lo = make_uint4(pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]), pack_f16(e[6], e[7]));
+    } else {
+        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * s + i], scale_log2, -m_ref));
-        st.l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));  // as they are
-        uint4 hi, lo;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = __float_as_uint(e[2 * i]) & 0xffff0000u, y = __float_as_uint(e[2 * i + 1]) & 0xffff0000u;
+            hi[i] = __builtin_amdgcn_perm(__float_as_uint(e[2 * i + 1]), __float_as_uint(e[2 * i]), 0x07060302u);
+            lo[i] = pack_bf16(__builtin_fmaf(e[2 * i], 1.f + 0x1p-20f, -__uint_as_float(x)), __builtin_fmaf(e[2 * i + 1], 1.f + 0x1p-20f, -__uint_as_float(y)));
+        }
+        p.hi = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        p.lo = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    return p;
+}
+// there: tokens of the block (masked only: places behind the last one may hold anything).
+template <bool KV8, bool masked>
+__device__ __forceinline__ void prefix_product(PrefixState &st, const PrefixWeights &p, const PrefixValues<KV8> &vf, int there, int lane) {
+    const int t0 = 8 * (lane >> 5);
+    uint32_t keep[4];
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keep[i] = (t0 + 2 * i < there ? 0xffffu : 0u) | (t0 + 2 * i + 1 < there ? 0xffff0000u : 0u);
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        uint4 v;
+        if constexpr (KV8) v = cvt8_f16(vf.f[x].x, vf.f[x].y);
+        else v = vf.f[x];
+        if (masked) v = make_uint4(v.x & keep[0], v.y & keep[1], v.z & keep[2], v.w & keep[3]);
         if constexpr (KV8) {
-            hi = make_uint4(pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]), pack_f16(e[6], e[7]));
+            st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, p.hi), st.o[x], 0, 0, 0);
         } else {
-            uint32_t p[4], rest[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t x = __float_as_uint(e[2 * i]) & 0xffff0000u, y = __float_as_uint(e[2 * i + 1]) & 0xffff0000u;
-                p[i] = __builtin_amdgcn_perm(__float_as_uint(e[2 * i + 1]), __float_as_uint(e[2 * i]), 0x07060302u);
-                rest[i] = pack_bf16(__builtin_fmaf(e[2 * i], 1.f + 0x1p-20f, -__uint_as_float(x)), __builtin_fmaf(e[2 * i + 1], 1.f + 0x1p-20f, -__uint_as_float(y)));
-            }
-            hi = make_uint4(p[0], p[1], p[2], p[3]);
-            lo = make_uint4(rest[0], rest[1], rest[2], rest[3]);
-        }
-        const int there = s ? there1 : there0;
-        uint32_t keep[4];  // places behind the last token may hold anything
-        if (masked) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) keep[i] = (t0 + 2 * i < there ? 0xffffu : 0u) | (t0 + 2 * i + 1 < there ? 0xffff0000u : 0u);
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            uint4 v;
-            if constexpr (KV8) v = cvt8_f16(vf[s].f[x].x, vf[s].f[x].y);
-            else v = vf[s].f[x];
-            if (masked) v = make_uint4(v.x & keep[0], v.y & keep[1], v.z & keep[2], v.w & keep[3]);
-            if constexpr (KV8) {
-                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, hi), st.o[x], 0, 0, 0);
-            } else {
-                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, hi), st.o[x], 0, 0, 0);
-                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, lo), st.o[x], 0, 0, 0);
-            }
+            st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p.hi), st.o[x], 0, 0, 0);
+            st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p.lo), st.o[x], 0, 0, 0);
         }
     }
 }
@@ -574,7 +576,8 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
             prefix_block<KV8>(vf[1], src, at, 1);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (more) request_values(b);
-            prefix_values<KV8, true>(st, sc, vf, there0, there1, scale_log2, lane);
+            prefix_product<KV8, true>(st, prefix_weights<KV8>(st, sc, 0, scale_log2), vf[0], there0, lane);
+            prefix_product<KV8, true>(st, prefix_weights<KV8>(st, sc, 1, scale_log2), vf[1], there1, lane);
         }
         // The states of the waves that have the same tile: each leaves its own in LDS, in its own part, and takes 4 / step of the channels.
         f32x4 *const mine = (f32x4 *)(ring + w * 16384);
@@ -627,67 +630,88 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
             for (int k = 0; k < LOADS; ++k) to_lds16(from, w < 2 ? key + k * on : value + k * 1024, to + k * 1024);
         }
     };
-    // Before group k is multiplied, all that this wave requested of it has landed (younger requests may be under way), and behind the barrier what the other waves requested too.
-    const auto landed = [&](int k) {
-        constexpr int younger = (SLOTS - 3) * LOADS;  // of groups k + 1 .. k + SLOTS - 3
-        static_assert(younger < 16, "one field of the wait's count");
-        if (k + SLOTS - 3 < n_grp) __builtin_amdgcn_s_waitcnt(0x0f70 | younger);
+    // All that this wave requested of group k has landed (of `ahead` younger groups it may be under way), and behind the barrier what the other waves requested too.
+    const auto landed = [&](int k, auto younger) {
+        constexpr int ahead = decltype(younger)::value;
+        static_assert(ahead * LOADS < 16, "one field of the wait's count");
+        if (k + ahead < n_grp) __builtin_amdgcn_s_waitcnt(0x0f70 | ahead * LOADS);
         else __builtin_amdgcn_s_waitcnt(0x0f70);
         __syncthreads();
     };
     const auto slot = [&](int k) { return ring + (k & (SLOTS - 1)) * BYTES; };
+    const auto next_slot = [&](int k, auto all) {  // group k - SLOTS is in every wave's registers; all: k < n_grp
+        if constexpr (decltype(all)::value) {
+            __builtin_amdgcn_s_waitcnt(0x0f70 | (SLOTS - 3) * LOADS);
+            __syncthreads();
+            request(k);
+        } else {
+            landed(k - SLOTS + 2, std::integral_constant<int, SLOTS - 3>());
+            if (k < n_grp) request(k);
+        }
+    };
     if (n_grp > 0) {
-        for (int k = 0; k < min(SLOTS - 2, n_grp); ++k) {
+        for (int k = 0; k < min(SLOTS, n_grp); ++k) {
             pair = blocks_of_group(k);
             request(k);
         }
-        pair = blocks_of_group(min(SLOTS - 2, n_grp - 1));
-        landed(0);
-        if (SLOTS - 2 < n_grp) request(SLOTS - 2);
-        pair = blocks_of_group(min(SLOTS - 1, n_grp - 1));
+        pair = blocks_of_group(min(SLOTS, n_grp - 1));
+        landed(1, std::integral_constant<int, SLOTS - 2>());
     }
     if (tile >= tiles) {
         for (int k = 0; k + 1 < n_grp; ++k) {
-            landed(k + 1);
-            if (k + SLOTS - 1 < n_grp) request(k + SLOTS - 1);
-            pair = blocks_of_group(min(k + SLOTS, n_grp - 1));
+            next_slot(k + SLOTS, std::false_type());
+            pair = blocks_of_group(min(k + SLOTS + 1, n_grp - 1));
         }
         return;
     }
     if (n_grp > 0) {
         f32x16 now, next;
         PrefixKeys<KV8> kf;
-        PrefixValues<KV8> vf[2];
+        PrefixValues<KV8> v0, v1;
         prefix_keys<KV8>(kf, slot(0), at);
         prefix_scores<KV8>(now, kf, qr);
-        const auto step = [&](int k, f32x16 &x0, f32x16 &x1) {
-            landed(k + 1);  // and every wave is done with group k - 1, whose slot is taken now
-            if (k + SLOTS - 1 < n_grp) request(k + SLOTS - 1);
-            const int2 ahead = *(const int2 *)(ids + 2 * min(k + SLOTS, n_grp - 1));
-            prefix_keys<KV8>(kf, slot(k + 1), at);
-            prefix_block<KV8>(vf[0], slot(k), at, 0);
+        prefix_keys<KV8>(kf, slot(1), at);  // of no use where there is one group
+        prefix_block<KV8>(v0, slot(0), at, 0);
+        // A group's weights are formed beside products that do not wait for them: those of its first block beside the next group's scores, those of the second beside the first one's values.
+        // Fragments are read a part ahead, and the barrier stands where the last of a group have been.
+        const auto step = [&](int k, f32x16 &x0, f32x16 &x1, auto all) {
+            prefix_block<KV8>(v1, slot(k), at, 1);
+            const int2 ahead = *(const int2 *)(ids + 2 * min(k + SLOTS + 1, n_grp - 1));
             __builtin_amdgcn_sched_barrier(0);
             prefix_reference<false>(st, x0, kBk, kBk, scale_log2, lane);
-            prefix_block<KV8>(vf[1], slot(k), at, 1);
             prefix_scores<KV8>(x1, kf, qr);
-            prefix_values<KV8, false>(st, x0, vf, kBk, kBk, scale_log2, lane);
+            const PrefixWeights p0 = prefix_weights<KV8>(st, x0, 0, scale_log2);
+            prefix_product<KV8, false>(st, p0, v0, kBk, lane);
+            PrefixWeights p1 = prefix_weights<KV8>(st, x0, 1, scale_log2);
+            asm volatile("" : "+v"(p1.hi.x), "+v"(p1.hi.y), "+v"(p1.hi.z), "+v"(p1.hi.w), "+v"(p1.lo.x), "+v"(p1.lo.y), "+v"(p1.lo.z), "+v"(p1.lo.w));  // here, not where they are needed
+            __builtin_amdgcn_sched_barrier(0);
+            next_slot(k + SLOTS, all);
+            prefix_keys<KV8>(kf, slot(k + 2), at);
+            prefix_block<KV8>(v0, slot(k + 1), at, 0);
             pair = make_int2(__builtin_amdgcn_readfirstlane(ahead.x), __builtin_amdgcn_readfirstlane(ahead.y));
+            __builtin_amdgcn_sched_barrier(0);
+            prefix_product<KV8, false>(st, p1, v1, kBk, lane);
         };
         int k = 0;
 #pragma nounroll
+        for (; k + 1 + SLOTS < n_grp; k += 2) {
+            step(k, now, next, std::true_type());
+            step(k + 1, next, now, std::true_type());
+        }
+#pragma nounroll
         for (; k + 2 < n_grp; k += 2) {
-            step(k, now, next);
-            step(k + 1, next, now);
+            step(k, now, next, std::false_type());
+            step(k + 1, next, now, std::false_type());
         }
         const auto end = [&](f32x16 &y) {  // the last group, of which a block may end early or be missing
             const int there0 = tokens_of(2 * (n_grp - 1)), there1 = tokens_of(2 * n_grp - 1);
-            prefix_block<KV8>(vf[0], slot(n_grp - 1), at, 0);
-            prefix_block<KV8>(vf[1], slot(n_grp - 1), at, 1);
+            prefix_block<KV8>(v1, slot(n_grp - 1), at, 1);
             prefix_reference<true>(st, y, there0, there1, scale_log2, lane);
-            prefix_values<KV8, true>(st, y, vf, there0, there1, scale_log2, lane);
+            prefix_product<KV8, true>(st, prefix_weights<KV8>(st, y, 0, scale_log2), v0, there0, lane);
+            prefix_product<KV8, true>(st, prefix_weights<KV8>(st, y, 1, scale_log2), v1, there1, lane);
         };
         if (k + 1 < n_grp) {
-            step(k, now, next);
+            step(k, now, next, std::false_type());
             end(next);
         } else {
             end(now);
