@@ -22,22 +22,26 @@ __device__ __forceinline__ uint32_t order_key(float x) {  // larger numbers have
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-// A logit as it counts: NaN as minus infinity, plus infinity as the largest finite number, -0 as 0 (which it equals).
-__device__ __forceinline__ float clean_logit(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e38f) + 0.f; }
+// A logit as it counts: NaN as minus infinity, plus infinity as the largest finite number.  The median of three, which is their minimum where one is NaN; by hand, since the compiler takes
+// it for a minimum of the outer two.
+__device__ __forceinline__ float clean_logit(float x) {
+    float r;
+    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(__builtin_canonicalizef(x)), "v"(-INFINITY), "v"(3.402823466e38f));
+    return r;
+}
 
-// exp(d) for d <= 0, to 2^-37 of itself: exp(d) = 2^n exp(r), |r| <= ln 2 / 2, its Taylor polynomial of degree 9.
+// exp(d) for d <= 0, to 2^-39 of itself (and 0 where it is below 2^-1000): exp(d) = 2^n exp(r), |r| <= ln 2 / 2, the polynomial that meets exp at the nine Chebyshev nodes of that interval.
 __device__ __forceinline__ double exp_of(double d) {
-    const double y = fmax(d * 1.4426950408889634074, -1100.0), n = rint(y);
-    const double r = (y - n) * 0.69314718055994530942;
-    double p = 1.0 / 362880;
-    p = __builtin_fma(p, r, 1.0 / 40320);
-    p = __builtin_fma(p, r, 1.0 / 5040);
-    p = __builtin_fma(p, r, 1.0 / 720);
-    p = __builtin_fma(p, r, 1.0 / 120);
-    p = __builtin_fma(p, r, 1.0 / 24);
-    p = __builtin_fma(p, r, 1.0 / 6);
-    p = __builtin_fma(p, r, 0.5);
-    p = __builtin_fma(p, r, 1.0);
+    d = fmax(d, -700.0);
+    const double n = rint(d * 1.4426950408889634074), r = __builtin_fma(n, -0.69314718055994530942, d);
+    double p = 2.4876164180131435e-05;
+    p = __builtin_fma(p, r, 0.00019915867076303128);
+    p = __builtin_fma(p, r, 0.0013888821677344278);
+    p = __builtin_fma(p, r, 0.008333266097680215);
+    p = __builtin_fma(p, r, 0.04166666689095846);
+    p = __builtin_fma(p, r, 0.16666666891047124);
+    p = __builtin_fma(p, r, 0.49999999999797934);
+    p = __builtin_fma(p, r, 0.9999999999797851);
     p = __builtin_fma(p, r, 1.0);
     return __builtin_ldexp(p, (int)n);
 }
@@ -119,13 +123,12 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamPart
     const auto token_of = [&](int i) { return (first + i / VE * kBeamThreads + t) * VE + i % VE; };
     float mine = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        x[i] = clean_logit(x[i]);
-        mine = fmaxf(mine, x[i]);
-    }
+    for (int i = 0; i < PER; ++i) x[i] = clean_logit(x[i]);
+#pragma unroll
+    for (int i = 0; i < PER; i += 2) mine = fmaxf(mine, fmaxf(x[i], x[i + 1]));
     if (t == 0) count = 0;
     const float wave_most = wave_max(mine);
-    const uint32_t bound_w = reached_by(order_key(mine), a.W);
+    const uint32_t bound_w = reached_by(order_key(mine + 0.f), a.W);
     if (lane == 0) {
         wmax[w] = wave_most;
         wbound[w] = bound_w;
@@ -140,14 +143,16 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamPart
         return;
     }
     double sum = 0.0;
+    const double most_d = most;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        sum += exp_of((double)x[i] - (double)most);
-        if (order_key(x[i]) >= bound) {
+    for (int i = 0; i < PER; ++i) sum += exp_of((double)x[i] - most_d);
+    const float least = of_key(bound);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (x[i] >= least) {  // rare: a comparison and a branch to a logit
             const int at = atomicAdd(&count, 1);
-            if (at < kBeamList) list[at] = (uint64_t)order_key(x[i]) << 32 | ~(uint32_t)token_of(i);
+            if (at < kBeamList) list[at] = (uint64_t)order_key(x[i] + 0.f) << 32 | ~(uint32_t)token_of(i);  // -0 equals 0
         }
-    }
     sum = wave_sum_f64(sum);
     if (lane == 0) wsum[w] = sum;
     __syncthreads();
@@ -169,8 +174,8 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamPart
         uint64_t v = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const uint64_t c = (uint64_t)order_key(x[i]) << 32 | ~(uint32_t)token_of(i);
-            if (order_key(x[i]) > kKeyNegInf && c < last && c > v) v = c;
+            const uint64_t c = (uint64_t)order_key(x[i] + 0.f) << 32 | ~(uint32_t)token_of(i);
+            if (x[i] > -INFINITY && c < last && c > v) v = c;
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
@@ -199,23 +204,35 @@ struct Candidate {
     }
 };
 
-__global__ void __launch_bounds__(kBeamThreads) k_beam_merge(BeamArgs a, BeamParts in) {
+// A workgroup to a group; the candidates that fit stay in registers, on their way before the normalisers are summed: what the kernel waits for is its chain of reads and sums.
+constexpr int kMergeThreads = 512, kMergeWaves = kMergeThreads / 64, kMergeHeld = 4;
+__global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a, BeamParts in) {
     __shared__ double add[kBeamMost], top[kBeamMost];  // a logit x of the beam scores (x - top) + add: large logits cancel before the rest is added
-    __shared__ int kind[kBeamMost];     // 0: no continuations, 1: live, 2: done
+    __shared__ int kind[kBeamMost];                    // 0: no continuations, 1: live, 2: done
     __shared__ Candidate list[kBeamList];
-    __shared__ uint32_t wbound[4];
+    __shared__ int rank[kBeamList];
+    __shared__ uint32_t wbound[kMergeWaves];
     __shared__ int count;
     const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, W = a.W;
-    for (int b = w; b < W; b += 4) {
+    const int per_beam = in.parts * W, n_all = W * per_beam;
+    const uint64_t *best = in.best + (size_t)g * n_all;
+    uint64_t held[kMergeHeld];
+#pragma unroll
+    for (int k = 0; k < kMergeHeld; ++k) held[k] = best[min(t + k * kMergeThreads, n_all - 1)];
+    for (int b = w; b < W; b += kMergeWaves) {
         const int s = g * W + b;
         const float score = a.scores[s];
+        const int done = a.done ? a.done[s] : 0;
+        const double2 first = in.sums[(size_t)s * in.parts + min(lane, in.parts - 1)];  // of a beam that is not live: anything
         int k = beam_row(a, s) >= 0 && score - score == 0.f ? 1 : 0;
-        if (k && a.done && a.done[s]) k = 2;
+        if (k && done) k = 2;
         double most = -INFINITY, sum = 0.0;
         if (k == 1) {
-            for (int p = lane; p < in.parts; p += 64) most = fmax(most, in.sums[(size_t)s * in.parts + p].x);
+            most = lane < in.parts ? first.x : -INFINITY;
+            for (int p = lane + 64; p < in.parts; p += 64) most = fmax(most, in.sums[(size_t)s * in.parts + p].x);
             most = wave_max_f64(most);
-            for (int p = lane; p < in.parts; p += 64) {
+            if (lane < in.parts && first.y > 0.0) sum = first.y * exp_of(first.x - most);
+            for (int p = lane + 64; p < in.parts; p += 64) {
                 const double2 v = in.sums[(size_t)s * in.parts + p];
                 if (v.y > 0.0) sum += v.y * exp_of(v.x - most);
             }
@@ -229,39 +246,47 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_merge(BeamArgs a, BeamPar
         }
     }
     if (t == 0) count = 0;
+    for (int i = t; i < kBeamList; i += kMergeThreads) rank[i] = 0;
     __syncthreads();
-    const int per_beam = in.parts * W, n_all = W * per_beam;
-    const auto get = [&](int i, Candidate &c) {
+    const auto make = [&](int i, uint64_t what, Candidate &c) {
         c.beam = i / per_beam;
-        const int j = i - c.beam * per_beam, k = kind[c.beam];
-        if (k == 0 || (k == 2 && j > 0)) return false;
+        const int k = kind[c.beam];
+        if (k == 0 || (k == 2 && i != c.beam * per_beam)) return false;
         if (k == 2) {
             c.what = (uint64_t)0x80000000u << 32 | ~(uint32_t)a.eos;
             c.score = add[c.beam];
             return true;
         }
-        c.what = in.best[((size_t)g * W + c.beam) * per_beam + j];
-        c.score = ((double)of_key((uint32_t)(c.what >> 32)) - top[c.beam]) + add[c.beam];
-        return c.what != 0;
+        c.what = what;
+        c.score = ((double)of_key((uint32_t)(what >> 32)) - top[c.beam]) + add[c.beam];
+        return what != 0;
     };
     const auto key_of = [](double v) {  // of a float that is not above v
         float f = (float)v;
         if ((double)f > v) f = nextafterf(f, -INFINITY);
         return order_key(f);
     };
+    const auto each = [&](auto &&f) {  // all candidates of this thread
+        Candidate c;
+#pragma unroll
+        for (int k = 0; k < kMergeHeld; ++k)
+            if (t + k * kMergeThreads < n_all && make(t + k * kMergeThreads, held[k], c)) f(c);
+        for (int i = t + kMergeHeld * kMergeThreads; i < n_all; i += kMergeThreads)
+            if (make(i, best[i], c)) f(c);
+    };
     uint32_t mine = 0;
-    Candidate c;
-    for (int i = t; i < n_all; i += kBeamThreads)
-        if (get(i, c)) mine = max(mine, key_of(c.score));
+    each([&](const Candidate &c) { mine = max(mine, key_of(c.score)); });
     const uint32_t bound_w = reached_by(mine, W);
     if (lane == 0) wbound[w] = bound_w;
     __syncthreads();
-    const uint32_t bound = max(max(wbound[0], wbound[1]), max(wbound[2], wbound[3]));
-    for (int i = t; i < n_all; i += kBeamThreads)
-        if (get(i, c) && key_of(c.score) >= bound) {
-            const int at = atomicAdd(&count, 1);
-            if (at < kBeamList) list[at] = c;
-        }
+    uint32_t bound = wbound[0];
+#pragma unroll
+    for (int k = 1; k < kMergeWaves; ++k) bound = max(bound, wbound[k]);
+    each([&](const Candidate &c) {
+        if (key_of(c.score) < bound) return;
+        const int at = atomicAdd(&count, 1);
+        if (at < kBeamList) list[at] = c;
+    });
     __syncthreads();
     const int n = count;
     const auto put = [&](int place, const Candidate &v) {
@@ -278,21 +303,25 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_merge(BeamArgs a, BeamPar
         a.scores_out[s] = -INFINITY;
         if (a.done_out) a.done_out[s] = 0;
     };
-    if (n <= kBeamList) {
-        for (int i = t; i < n; i += kBeamThreads) {
+    if (n <= kBeamList) {  // the place of each: how many are better; each wave counts among its share
+        for (int i = lane; i < n; i += 64) {
             const Candidate v = list[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += list[j].before(v);
-            if (rank < W) put(rank, v);
+            int better = 0;
+            for (int j = w; j < n; j += kMergeWaves) better += list[j].before(v);
+            if (better) atomicAdd(&rank[i], better);
         }
+        __syncthreads();
+        for (int i = t; i < n; i += kMergeThreads)
+            if (rank[i] < W) put(rank[i], list[i]);
         if (t >= n && t < W) none(t);
         return;
     }
     Candidate last{INFINITY, ~0ull, -1};
     for (int k = 0; k < W; ++k) {
         Candidate v{-INFINITY, 0, kBeamMost};
-        for (int i = t; i < n_all; i += kBeamThreads)
-            if (get(i, c) && last.before(c) && c.before(v)) v = c;
+        each([&](const Candidate &c) {
+            if (last.before(c) && c.before(v)) v = c;
+        });
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
             Candidate y;
@@ -304,7 +333,7 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_merge(BeamArgs a, BeamPar
         __syncthreads();
         if (lane == 0) list[w] = v;
         __syncthreads();
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kMergeWaves; ++i)
             if (list[i].before(v)) v = list[i];
         last = v;
         if (t == 0) {
@@ -334,43 +363,50 @@ struct ForkGroup {  // in LDS: a group's sequences
     int shared, n_fresh;
 };
 
-__device__ __forceinline__ void fork_group(const ForkArgs &a, int g, ForkGroup &f) {  // by the first wave
-    const int i = threadIdx.x;
-    if (i < 64) {
-        const bool in = i < a.W;
-        const int64_t room = (int64_t)a.max_blocks * a.Bk;
-        const int n = in ? (int)min((int64_t)max(a.kv_lens[g * a.W + i], 0), room) : 0, p = in ? a.parents[g * a.W + i] : -1;
-        const int parent = p >= 0 && p < a.W ? p : -1, shared = a.shared ? max(a.shared[g], 0) : 0;
-        f.len[i] = n;
-        f.nb[i] = n / a.Bk + (n % a.Bk != 0);
-        f.parent[i] = parent;
-        bool first = parent >= 0;
-        for (int j = 0; j < a.W; ++j) {
-            const int q = __shfl(parent, j, 64);
-            if (j < i && q == parent) first = false;
-        }
-        const int plen = __shfl(n, max(parent, 0), 64);
-        const bool fresh = parent >= 0 && plen % a.Bk != 0 && (!first || plen / a.Bk < shared);
-        f.fresh[i] = fresh;
-        uint64_t kept = 0;
-        for (int j = 0; j < a.W; ++j) {
-            const int q = __shfl(parent, j, 64);
-            if (q >= 0) kept |= 1ull << q;
-        }
-        const int n_fresh = __popcll(__ballot(fresh));
-        if (i == 0) {
-            f.kept = kept;
-            f.shared = shared;
-            f.n_fresh = n_fresh;
-        }
+// The old ids of this thread's column, of all sequences as they stand, in LDS: read whether they are in use or not, so that they are on their way beside the lengths.
+__device__ __forceinline__ void fork_tile(const ForkArgs &a, int g, int c, int32_t *tile) {
+    if (c >= a.max_blocks) return;
+    const int32_t *from = a.bt + (size_t)g * a.W * a.max_blocks + c;
+    int i = 0;
+    for (; i + 8 <= a.W; i += 8) {
+        int32_t v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = from[(size_t)(i + k) * a.max_blocks];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) tile[(i + k) * kForkCols + threadIdx.x] = v[k];
     }
-    __syncthreads();
+    for (; i < a.W; ++i) tile[i * kForkCols + threadIdx.x] = from[(size_t)i * a.max_blocks];
 }
 
-// The old ids of this thread's column, in LDS, -1 behind a sequence's last block and outside the pool; which of them are freed.
-__device__ __forceinline__ void fork_tile(const ForkArgs &a, int g, int c, const ForkGroup &f, int32_t *tile) {
-    for (int i = 0; i < a.W; ++i) tile[i * kForkCols + threadIdx.x] = c < f.nb[i] ? a.bt[((size_t)g * a.W + i) * a.max_blocks + c] : -1;
+__device__ __forceinline__ void fork_group(const ForkArgs &a, int g, ForkGroup &f) {  // by the first wave; a barrier follows
+    const int i = threadIdx.x;
+    if (i >= 64) return;
+    const bool in = i < a.W;
+    const int64_t room = (int64_t)a.max_blocks * a.Bk;
+    const int n = in ? (int)min((int64_t)max(a.kv_lens[g * a.W + i], 0), room) : 0, p = in ? a.parents[g * a.W + i] : -1;
+    const int parent = p >= 0 && p < a.W ? p : -1, shared = a.shared ? max(a.shared[g], 0) : 0;
+    f.len[i] = n;
+    f.nb[i] = n / a.Bk + (n % a.Bk != 0);
+    f.parent[i] = parent;
+    bool first = parent >= 0;
+    uint64_t kept = 0;
+    for (int j = 0; j < a.W; ++j) {
+        const int q = __builtin_amdgcn_readlane(parent, j);
+        if (j < i && q == parent) first = false;
+        if (q >= 0) kept |= 1ull << q;
+    }
+    const int plen = __shfl(n, max(parent, 0), 64);
+    const bool fresh = parent >= 0 && plen % a.Bk != 0 && (!first || plen / a.Bk < shared);
+    f.fresh[i] = fresh;
+    const int n_fresh = __popcll(__ballot(fresh));
+    if (i == 0) {
+        f.kept = kept;
+        f.shared = shared;
+        f.n_fresh = n_fresh;
+    }
 }
+
+// Which of this thread's column are freed.
 __device__ __forceinline__ uint64_t fork_freed(const ForkArgs &a, int c, const ForkGroup &f, const int32_t *tile) {
     uint64_t freed = 0;
     if (c < f.shared) return 0;
@@ -385,31 +421,36 @@ __device__ __forceinline__ uint64_t fork_freed(const ForkArgs &a, int c, const F
     return freed;
 }
 
-__global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts p) {
-    extern __shared__ int32_t tile[];  // [W][kForkCols]
-    __shared__ ForkGroup f;
-    __shared__ int wsum[kForkCols / 64];
-    const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
-    fork_group(a, g, f);
-    fork_tile(a, g, c, f, tile);
-    const uint64_t freed = fork_freed(a, c, f, tile);
-    const int n = __popcll(freed);
-    int x = n;
+// Inclusive sum over the wave.
+__device__ __forceinline__ int wave_scan(int x) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int y = __shfl_up(x, o, 64);
-        if (lane >= o) x += y;
+        if ((int)(threadIdx.x & 63) >= o) x += y;
     }
+    return x;
+}
+constexpr int kForkWaves = kForkCols / 64;
+
+__global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts p) {
+    extern __shared__ int32_t tile[];  // [W][kForkCols]
+    __shared__ ForkGroup f;
+    __shared__ int wsum[kForkWaves];
+    const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
+    fork_group(a, g, f);
+    fork_tile(a, g, c, tile);
+    __syncthreads();
+    const uint64_t freed = fork_freed(a, c, f, tile);
+    const int n = __popcll(freed), x = wave_scan(n);
     if (lane == 63) wsum[w] = x;
     __syncthreads();
     int at = x - n, all = 0;
-    for (int i = 0; i < kForkCols / 64; ++i) {
+    for (int i = 0; i < kForkWaves; ++i) {
         if (i < w) at += wsum[i];
         all += wsum[i];
     }
     int32_t *out = p.freed + ((size_t)g * p.parts + part) * a.W * kForkCols;
-    for (int i = 0; i < a.W; ++i)
-        if (freed >> i & 1) out[at++] = tile[i * kForkCols + t];
+    for (uint64_t left = freed; left; left &= left - 1) out[at++] = tile[(__ffsll((unsigned long long)left) - 1) * kForkCols + t];
     if (t == 0) {
         p.freed_n[(size_t)g * p.parts + part] = all;
         if (part == 0) p.fresh_n[g] = f.n_fresh;
@@ -419,40 +460,40 @@ __global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts 
 __global__ void __launch_bounds__(kForkCols) k_fork_write(ForkArgs a, ForkParts p) {
     extern __shared__ int32_t tile[];
     __shared__ ForkGroup f;
-    __shared__ int fresh_id[kBeamMost], fresh_at[kBeamMost], red[kForkCols / 64];
+    __shared__ int fresh_id[kBeamMost], fresh_at[kBeamMost], red[4][kForkWaves];
     const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
     const int n_parts = a.G * p.parts, me = g * p.parts + part;
-    fork_group(a, g, f);
-    fork_tile(a, g, c, f, tile);
+    const int used = *a.free_used, n_mine = p.freed_n[me];
     // sums over the parts and groups before this one, and over all
-    int before = 0, all = 0, fresh_before = 0, fresh_all = 0;
+    int sum[4] = {0, 0, 0, 0};
     for (int i = t; i < n_parts; i += kForkCols) {
         const int n = p.freed_n[i];
-        all += n;
-        if (i < me) before += n;
+        sum[1] += n;
+        if (i < me) sum[0] += n;
     }
     for (int i = t; i < a.G; i += kForkCols) {
         const int n = p.fresh_n[i];
-        fresh_all += n;
-        if (i < g) fresh_before += n;
+        sum[3] += n;
+        if (i < g) sum[2] += n;
     }
-    const auto sum_of = [&](int v) {
+    fork_group(a, g, f);
+    fork_tile(a, g, c, tile);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-        __syncthreads();
-        if (lane == 0) red[w] = v;
-        __syncthreads();
-        int sum = 0;
-        for (int k = 0; k < kForkCols / 64; ++k) sum += red[k];
-        return sum;
-    };
-    before = sum_of(before);
-    all = sum_of(all);
-    fresh_before = sum_of(fresh_before);
-    fresh_all = sum_of(fresh_all);
-    const int head = min(max(*a.free_used, 0), a.n_free), low = head - all, start = max(low, 0);  // freed id j stands at low + j
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum[k] += __shfl_xor(sum[k], o, 64);
+        if (lane == 0) red[k][w] = sum[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        sum[k] = red[k][0];
+        for (int i = 1; i < kForkWaves; ++i) sum[k] += red[k][i];
+    }
+    const int before = sum[0], all = sum[1], fresh_before = sum[2], fresh_all = sum[3];
+    const int head = min(max(used, 0), a.n_free), low = head - all, start = max(low, 0);  // freed id j stands at low + j
     const int32_t *mine = p.freed + (size_t)me * a.W * kForkCols;
-    for (int j = t; j < p.freed_n[me]; j += kForkCols)
+    for (int j = t; j < n_mine; j += kForkCols)
         if (low + before + j >= 0) a.free_ids[low + before + j] = mine[j];
     // Fresh ids of the group's children: entries start + fresh_before .. of the list.  Those before the head are freed ids of this call: from the parts' lists, since another workgroup
     // may not have entered them yet.
@@ -466,22 +507,17 @@ __global__ void __launch_bounds__(kForkCols) k_fork_write(ForkArgs a, ForkParts 
     }
     __syncthreads();
     if (f.n_fresh && start + fresh_before < head) {
+        // the parts whose freed ids those are: at most as many as there are children, in a run that begins where the sum passes start + fresh_before - low
         int done = 0;  // freed ids of the parts of the rounds before
         for (int i0 = 0; i0 < n_parts; i0 += kForkCols) {
-            const int i = i0 + t, n = i < n_parts ? p.freed_n[i] : 0;
-            int x = n;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int y = __shfl_up(x, o, 64);
-                if (lane >= o) x += y;
-            }
+            const int i = i0 + t, n = i < n_parts ? p.freed_n[i] : 0, x = wave_scan(n);
             __syncthreads();
-            if (lane == 63) red[w] = x;
+            if (lane == 63) red[0][w] = x;
             __syncthreads();
             int from = done + x - n;
-            for (int k = 0; k < w; ++k) from += red[k];
-            for (int k = 0; k < kForkCols / 64; ++k) done += red[k];
-            if (n)
+            for (int k = 0; k < w; ++k) from += red[0][k];
+            for (int k = 0; k < kForkWaves; ++k) done += red[0][k];
+            if (n && from < start + fresh_before + f.n_fresh - low && from + n > start + fresh_before - low)
                 for (int j = 0; j < a.W; ++j) {
                     const int64_t k = (int64_t)fresh_at[j] - low - from;
                     if (fresh_at[j] >= 0 && fresh_at[j] < head && k >= 0 && k < n) fresh_id[j] = p.freed[(size_t)i * a.W * kForkCols + k];
@@ -522,25 +558,28 @@ struct CopyArrays {
     uint32_t *at[kCopyArrays];
     int64_t bytes[kCopyArrays];
 };
-// A workgroup to a piece of 16 KB of a block in one array, 16 bytes a lane where the array's blocks begin at multiples of them.
-__global__ void __launch_bounds__(kCopyThreads) k_copy_blocks(CopyArrays a, const int32_t *src, const int32_t *dst, int pieces, int num_blocks) {
-    const int i = blockIdx.x / pieces, piece = blockIdx.x % pieces, s = src[i], d = dst[i];
-    const int64_t bytes = a.bytes[blockIdx.y], first = (int64_t)piece * kCopyPiece;
+// A workgroup to a piece of 16 KB of a block in one array, 16 bytes a lane where the array's blocks begin at multiples of them.  grid: pieces, copies, arrays.
+__global__ void __launch_bounds__(kCopyThreads) k_copy_blocks(CopyArrays a, const int32_t *src, const int32_t *dst, int num_blocks) {
+    char *const p = (char *)a.at[blockIdx.z];
+    const int64_t bytes = a.bytes[blockIdx.z], first = (int64_t)blockIdx.x * kCopyPiece;
+    const int s = src[blockIdx.y], d = dst[blockIdx.y];
     if (s < 0 || d < 0 || s >= num_blocks || d >= num_blocks || s == d || first >= bytes) return;
-    char *const p = (char *)a.at[blockIdx.y];
-    const char *from = p + s * bytes + first;
-    char *to = p + d * bytes + first;
+    const char *from = p + s * bytes + first + threadIdx.x * 16;
+    char *to = p + d * bytes + first + threadIdx.x * 16;
     const int n = (int)min((int64_t)kCopyPiece, bytes - first);
-    if (((uintptr_t)p | bytes) % 16 == 0) {
-        uint4 v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if ((k * kCopyThreads + threadIdx.x) * 16 < n) v[k] = *(const uint4 *)(from + (k * kCopyThreads + threadIdx.x) * 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if ((k * kCopyThreads + threadIdx.x) * 16 < n) *(uint4 *)(to + (k * kCopyThreads + threadIdx.x) * 16) = v[k];
+    const bool wide = ((uintptr_t)p | bytes) % 16 == 0;
+    if (wide && n == kCopyPiece) {
+        const uint4 v0 = *(const uint4 *)from, v1 = *(const uint4 *)(from + 4096), v2 = *(const uint4 *)(from + 8192), v3 = *(const uint4 *)(from + 12288);
+        *(uint4 *)to = v0;
+        *(uint4 *)(to + 4096) = v1;
+        *(uint4 *)(to + 8192) = v2;
+        *(uint4 *)(to + 12288) = v3;
+    } else if (wide) {
+        for (int k = threadIdx.x * 16; k < n; k += kCopyThreads * 16, from += kCopyThreads * 16, to += kCopyThreads * 16) *(uint4 *)to = *(const uint4 *)from;
     } else {
-        for (int k = threadIdx.x * 4; k < n; k += kCopyThreads * 4) *(uint32_t *)(to + k) = *(const uint32_t *)(from + k);
+        from -= threadIdx.x * 12;
+        to -= threadIdx.x * 12;
+        for (int k = threadIdx.x * 4; k < n; k += kCopyThreads * 4, from += kCopyThreads * 4, to += kCopyThreads * 4) *(uint32_t *)to = *(const uint32_t *)from;
     }
 }
 
@@ -628,7 +667,7 @@ hipError_t launch_beam(const BeamArgs &a, void *workspace, hipStream_t st) {
 #undef BEAM_PART
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_beam_merge, dim3(a.G), dim3(kBeamThreads), 0, st, a, p);
+    hipLaunchKernelGGL(k_beam_merge, dim3(a.G), dim3(kMergeThreads), 0, st, a, p);
     return hipGetLastError();
 }
 
@@ -663,10 +702,9 @@ hipError_t launch_copy_blocks(void *const *arrays, const int64_t *block_bytes, i
             c.bytes[i] = block_bytes[i0 + i];
             most = std::max(most, c.bytes[i]);
         }
-        const int pieces = (int)((most + kCopyPiece - 1) / kCopyPiece);
-        const int per_launch = std::max(1, (1 << 22) / pieces);  // a launch has fewer than 2^32 work items
-        for (int e = 0; e < n; e += per_launch) {
-            hipLaunchKernelGGL(k_copy_blocks, dim3((unsigned)std::min(per_launch, n - e) * pieces, cnt), dim3(kCopyThreads), 0, st, c, src + e, dst + e, pieces, num_blocks);
+        const unsigned pieces = (unsigned)((most + kCopyPiece - 1) / kCopyPiece);  // at most 2^16
+        for (int e = 0; e < n; e += 65535) {
+            hipLaunchKernelGGL(k_copy_blocks, dim3(pieces, std::min(65535, n - e), cnt), dim3(kCopyThreads), 0, st, c, src + e, dst + e, num_blocks);
             const hipError_t err = hipGetLastError();
             if (err != hipSuccess) return err;
         }
