@@ -15,7 +15,6 @@ namespace {
 // Sums and scores are float64: two beams' candidates are told apart by the difference of their normalisers, and with sums in float32 the order of a group would
 // depend on how the row was split.  A logit and a number below it as the order of the logits, equal ones by the lowest token: packed in 64 bits.
 constexpr int kBeamThreads = 256, kBeamList = 1024;
-constexpr uint32_t kKeyNegInf = 0x007fffffu;  // order_key of minus infinity
 
 __device__ __forceinline__ uint32_t order_key(float x) {  // larger numbers have larger keys
     const uint32_t u = __float_as_uint(x);
@@ -26,7 +25,12 @@ __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k &
 // it for a minimum of the outer two.
 __device__ __forceinline__ float clean_logit(float x) {
     float r;
-    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(__builtin_canonicalizef(x)), "v"(-INFINITY), "v"(3.402823466e38f));
+    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(-INFINITY), "v"(3.402823466e38f));
+    return r;
+}
+__device__ __forceinline__ float max_of_3(float a, float b, float c) {  // by hand: for fmaxf the compiler first turns what clean_logit gives into itself
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 
@@ -56,17 +60,32 @@ __device__ __forceinline__ double wave_max_f64(double v) {
     return v;
 }
 
-// A bound that at least W of the wave's 64 keys reach, bit by bit; not always the largest such.
-__device__ __forceinline__ uint32_t reached_by(uint32_t key, int W) {
-    uint32_t bound = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t more = bound | 1u << bit;
-        const int n = __popcll(__ballot(key >= more));
-        if (n < W) continue;
-        bound = more;
-        if (n == W) break;
+// A number that at least W of the wave's 64 reach, and not many more.  Up to 16: of sixteen runs of four lanes the largest each, and of those the least that fewer than W exceed; else of W runs
+// (the next power of two) the least.  A part of 8192 logits lists 27 of them for 8 beams, by runs alone 53, and ranking the list is what the choice spends its time on.
+template <int CTRL>
+__device__ __forceinline__ float lane_of(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float reached_by(float x, int W) {
+    int run = W > 1 && W <= 16 ? 4 : 64;
+    while (W > 16 && run > 1 && 64 / run < W) run >>= 1;
+    const auto join = [&](float y, int size) { x = size <= run ? fmaxf(x, y) : fminf(x, y); };
+    join(lane_of<0xb1>(x), 2);  // lane ^ 1
+    join(lane_of<0x4e>(x), 4);  // lane ^ 2
+    if (W > 1 && W <= 16) {
+        int above = 0;
+        const auto row = [&](float y) {  // the four runs of a row of 16 lanes, each turned past this one
+            above += (y > x) + (lane_of<0x124>(y) > x) + (lane_of<0x128>(y) > x) + (lane_of<0x12c>(y) > x);
+        };
+        row(x);
+        row(__shfl_xor(x, 16, 64));
+        row(__shfl_xor(x, 32, 64));
+        row(__shfl_xor(x, 48, 64));
+        if (above >= W) x = INFINITY;
     }
-    return bound;
+    join(lane_of<0x141>(x), 8);   // of the other four of eight, all alike
+    join(lane_of<0x140>(x), 16);  // of the other eight of sixteen
+    join(__shfl_xor(x, 16, 64), 32);
+    join(__shfl_xor(x, 32, 64), 64);
+    return x;
 }
 
 // Row of logits that a beam takes, -1: none.
@@ -88,11 +107,11 @@ struct BeamParts {
 template <typename T, int PER>  // logits of a thread
 __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamParts out) {
     constexpr int VE = 16 / sizeof(T), NV = PER / VE;
+    constexpr int SEG = kBeamList / 4;  // a list to a wave
     __shared__ uint64_t list[kBeamList];
-    __shared__ float wmax[4];
+    __shared__ float wmax[4], wbound[4];
     __shared__ double wsum[4];
-    __shared__ uint32_t wbound[4];
-    __shared__ int count;
+    __shared__ int listed[4];
     const int s = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
     const int row = beam_row(a, s);
     if (row < 0 || (a.done && a.done[s])) return;
@@ -125,49 +144,58 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamPart
 #pragma unroll
     for (int i = 0; i < PER; ++i) x[i] = clean_logit(x[i]);
 #pragma unroll
-    for (int i = 0; i < PER; i += 2) mine = fmaxf(mine, fmaxf(x[i], x[i + 1]));
-    if (t == 0) count = 0;
-    const float wave_most = wave_max(mine);
-    const uint32_t bound_w = reached_by(order_key(mine + 0.f), a.W);
+    for (int i = 0; i < PER; i += 2) mine = max_of_3(mine, x[i], x[i + 1]);
+    const float wave_most = reached_by(mine, 1), bound_w = reached_by(mine, a.W);
     if (lane == 0) {
         wmax[w] = wave_most;
         wbound[w] = bound_w;
     }
     __syncthreads();
     const float most = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
-    const uint32_t bound = max(max(max(wbound[0], wbound[1]), max(wbound[2], wbound[3])), kKeyNegInf + 1);
+    const float least = fmaxf(fmaxf(fmaxf(wbound[0], wbound[1]), fmaxf(wbound[2], wbound[3])), -3.402823466e38f);  // at least W logits reach it, or all that count
     uint64_t *best = out.best + ((size_t)s * out.parts + part) * a.W;
     if (most == -INFINITY) {
         if (t < a.W) best[t] = 0;
         if (t == 0) out.sums[(size_t)s * out.parts + part] = make_double2(-INFINITY, 0.0);
         return;
     }
-    double sum = 0.0;
+    double sum = 0.0, sum1 = 0.0;
     const double most_d = most;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += exp_of((double)x[i] - most_d);
-    const float least = of_key(bound);
+    for (int i = 0; i < PER; i += 2) {
+        sum += exp_of((double)x[i] - most_d);
+        sum1 += exp_of((double)x[i + 1] - most_d);
+    }
+    sum = wave_sum_f64(sum + sum1);
+    int n = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (x[i] >= least) {  // rare: a comparison and a branch to a logit
-            const int at = atomicAdd(&count, 1);
-            if (at < kBeamList) list[at] = (uint64_t)order_key(x[i] + 0.f) << 32 | ~(uint32_t)token_of(i);  // -0 equals 0
+    for (int i = 0; i < PER; ++i) {
+        const unsigned long long mask = __ballot(x[i] >= least);
+        if (mask) {  // few
+            const int at = n + __popcll(mask & ((1ull << lane) - 1));
+            if ((mask >> lane & 1) && at < SEG) list[w * SEG + at] = (uint64_t)order_key(x[i] + 0.f) << 32 | ~(uint32_t)token_of(i);  // -0 equals 0
+            n += __popcll(mask);
         }
-    sum = wave_sum_f64(sum);
-    if (lane == 0) wsum[w] = sum;
+    }
+    if (lane == 0) {
+        wsum[w] = sum;
+        listed[w] = n;
+    }
     __syncthreads();
     if (t == 0) out.sums[(size_t)s * out.parts + part] = make_double2((double)most, (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]));
-    const int n = count;
-    if (n <= kBeamList) {  // the place of each in the order: how many are larger
-        for (int i = t; i < n; i += kBeamThreads) {
-            const uint64_t v = list[i];
+    const int n0 = listed[0], n1 = listed[1], n2 = listed[2], n3 = listed[3], all = n0 + n1 + n2 + n3;
+    if (max(max(n0, n1), max(n2, n3)) <= SEG) {  // the place of each in the order: how many are larger
+        for (int i = lane; i < n; i += 64) {
+            const uint64_t v = list[w * SEG + i];
             int rank = 0;
-            for (int j = 0; j < n; ++j) rank += list[j] > v;
+            for (int k = 0; k < 4; ++k)
+                for (int j = 0; j < listed[k]; ++j) rank += list[k * SEG + j] > v;
             if (rank < a.W) best[rank] = v;
         }
-        if (t >= n && t < a.W) best[t] = 0;
+        if (t >= all && t < a.W) best[t] = 0;
         return;
     }
+    __syncthreads();
     // Many equal logits: one after the other.
     uint64_t last = ~0ull;
     for (int k = 0; k < a.W; ++k) {
@@ -211,7 +239,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a, BeamPa
     __shared__ int kind[kBeamMost];                    // 0: no continuations, 1: live, 2: done
     __shared__ Candidate list[kBeamList];
     __shared__ int rank[kBeamList];
-    __shared__ uint32_t wbound[kMergeWaves];
+    __shared__ float wbound[kMergeWaves];
     __shared__ int count;
     const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, W = a.W;
     const int per_beam = in.parts * W, n_all = W * per_beam;
@@ -261,10 +289,9 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a, BeamPa
         c.score = ((double)of_key((uint32_t)(what >> 32)) - top[c.beam]) + add[c.beam];
         return what != 0;
     };
-    const auto key_of = [](double v) {  // of a float that is not above v
-        float f = (float)v;
-        if ((double)f > v) f = nextafterf(f, -INFINITY);
-        return order_key(f);
+    const auto below = [](double v) {  // a float that is not above v
+        const float f = (float)v;
+        return (double)f > v ? nextafterf(f, -INFINITY) : f;
     };
     const auto each = [&](auto &&f) {  // all candidates of this thread
         Candidate c;
@@ -274,16 +301,16 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a, BeamPa
         for (int i = t + kMergeHeld * kMergeThreads; i < n_all; i += kMergeThreads)
             if (make(i, best[i], c)) f(c);
     };
-    uint32_t mine = 0;
-    each([&](const Candidate &c) { mine = max(mine, key_of(c.score)); });
-    const uint32_t bound_w = reached_by(mine, W);
+    float mine = -INFINITY;
+    each([&](const Candidate &c) { mine = fmaxf(mine, below(c.score)); });
+    const float bound_w = reached_by(mine, W);
     if (lane == 0) wbound[w] = bound_w;
     __syncthreads();
-    uint32_t bound = wbound[0];
+    float bound = wbound[0];
 #pragma unroll
-    for (int k = 1; k < kMergeWaves; ++k) bound = max(bound, wbound[k]);
+    for (int k = 1; k < kMergeWaves; ++k) bound = fmaxf(bound, wbound[k]);
     each([&](const Candidate &c) {
-        if (key_of(c.score) < bound) return;
+        if (below(c.score) < bound) return;
         const int at = atomicAdd(&count, 1);
         if (at < kBeamList) list[at] = c;
     });
