@@ -18,6 +18,7 @@ struct PrefixUnit { int row0, rows, seq, b0, nb, len, chunks, slot; };  // its r
 struct PrefixItem { int row0, rows, j0, seq, b0, nb, len, slot; };      // j0: the first of its queries among the unit's
 struct PrefixJoin { int row0, rows, n_shared, shared, shared_rows, n_own, own, pad; };  // a sequence's rows; place of part k of row r: shared + k * shared_rows + r, then own + k * rows + r - row0
 constexpr int kPlanThreads = 1024, kMostBlocks = 1024;                   // blocks of an item, at most
+constexpr float kItemCost = 14.f, kAlone = 0.65f;                        // what an item costs beside its blocks, in blocks; time of one that has a CU to itself by that of two that share one
 
 struct PrefixPlan {
     PrefixUnit *units;  // [G] shared blocks of a group, [S] the rest of a sequence
@@ -184,6 +185,7 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
     __shared__ int64_t red_work[WAVES];
     __shared__ PrefixUnit units[2 * THREADS];
     __shared__ int size_of[2 * THREADS];  // blocks of an item of the unit
+    __shared__ float4 red_size[WAVES][16];
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     const bool is_seq = t < a.S, is_group = t < a.G;
     const int len = is_seq ? (int)min((int64_t)max(a.kv_lens[t], 0), (int64_t)a.max_blocks * Bk) : 0;
@@ -242,8 +244,48 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
     __syncthreads();
     int64_t total = 0;
     for (int i = 0; i < WAVES; ++i) total += red_work[i];
-    int per = (int)min((total + p.target - 1) / p.target, (int64_t)kMostBlocks);
-    per = max((per + p.step - 1) / p.step, 1) * p.step;
+    const int even = (int)min((total + p.target - 1) / p.target, (int64_t)kMostBlocks);
+    int per = max((even + p.step - 1) / p.step, 1) * p.step;
+    if (even > 2 * p.step && even < kMostBlocks) {
+        // The largest size of an item.  Even shares would be `even` blocks, but a unit is cut into whole items, and a few more than run at once cost a round.  Of sixteen sizes the one is taken
+        // whose sum is least, in blocks: all work over the workgroups that run at once, and the rounds of the large items, a last round of at most one to a CU counting kAlone.  Over seven sets of
+        // sequences (9 to 140 units, 2000 to 25600 blocks) and 13 sizes each, this choice was 0.7 % behind the best one timed, 2.6 % at most; even shares 5 and 12 %.
+        if (is_group) size_of[t] = u.nb, at_item[t] = tg_u;
+        if (is_seq) size_of[a.G + t] = v.nb, at_item[a.G + t] = tg_v;
+        __syncthreads();
+        const int k = t & 15;
+        const int most = min((int)ceilf(even * __builtin_amdgcn_exp2f(0.12f * (k - 6)) / p.step) * p.step, kMostBlocks);
+        const float inv = __builtin_amdgcn_rcpf(most);
+        float all_work = 0.f, large = 0.f, longest = 0.f;
+        for (int i = t >> 4; i < a.G + a.S; i += THREADS / 16) {
+            const float nb = size_of[i], tg = at_item[i];
+            const float chunks = fmaxf(ceilf(nb * inv - 1e-4f), 1.f), size = nb * __builtin_amdgcn_rcpf(chunks), items = nb > 0.f ? tg * chunks : 0.f;
+            all_work += items * (size + kItemCost);
+            large += size > 0.4f * most ? items : 0.f;
+            longest = fmaxf(longest, size);
+        }
+        const auto over = [&](auto op, float x) {  // the lanes of the same size
+            x = op(x, __shfl_xor(x, 16, 64));
+            return op(x, __shfl_xor(x, 32, 64));
+        };
+        const auto sum = [](float x, float y) { return x + y; };
+        const auto max_of = [](float x, float y) { return fmaxf(x, y); };
+        all_work = over(sum, all_work), large = over(sum, large), longest = over(max_of, longest);
+        if (lane < 16) red_size[w][lane] = make_float4(all_work, large, longest, 0.f);
+        __syncthreads();
+        all_work = large = longest = 0.f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const float4 r = red_size[i][k];
+            all_work += r.x, large += r.y, longest = fmaxf(longest, r.z);
+        }
+        const float rounds = large / p.target, full = floorf(rounds), rest = rounds - full;
+        const float time = all_work / p.target + (full + (rest <= 0.f ? 0.f : rest <= 0.5f ? kAlone : 1.f)) * (longest + kItemCost);
+        float least = time;
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) least = fminf(least, __shfl_xor(least, o, 64));
+        per = __shfl(most, __ffsll(__ballot(time == least)) - 1, 64);
+    }
     const auto cut = [&](PrefixUnit &y) {  // even parts
         if (y.nb == 0) return per;
         const int chunks = (y.nb + per - 1) / per, mine = ((y.nb + chunks - 1) / chunks + p.step - 1) / p.step * p.step;
@@ -312,6 +354,18 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
 // data is in LDS.
 __device__ __forceinline__ void to_lds16(const char *g, uint32_t at, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(at), "s"(g) : "memory");
+}
+
+// Sequence s with all of its blocks and rows as one item, for tables of at most kMostBlocks blocks; false: it is in no group, or has no rows.
+__device__ __forceinline__ bool whole_sequence(const PrefixAttnArgs &a, int s, int Bk, PrefixItem &x) {
+    x.row0 = min(max(a.row_start[s], 0), a.R);
+    x.rows = min(max(a.row_start[s + 1], x.row0), a.R) - x.row0;
+    x.seq = s;
+    x.b0 = 0;
+    x.len = (int)min((int64_t)max(a.kv_lens[s], 0), (int64_t)a.max_blocks * Bk);
+    x.nb = x.len / Bk + (x.len % Bk != 0);
+    x.slot = 0;
+    return a.group_start[0] <= s && s < a.group_start[a.G] && x.rows > 0;
 }
 
 // ---- matrix cores: bf16 storage, head_dim 128, blocks of 16 -------------------------------------------------------------
@@ -462,7 +516,7 @@ __device__ __forceinline__ void prefix_product(PrefixState &st, const PrefixWeig
     }
 }
 
-template <bool KV8>
+template <bool KV8, bool DIRECT>
 __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, PrefixPlan p, int Hq, int Hkv, float scale_log2, float v_scale) {
     constexpr int SLOTS = kSlots<KV8>, BYTES = kGroupBytes<KV8>, ES = KV8 ? 1 : 2;
     __shared__ __attribute__((aligned(1024))) char ring[SLOTS * BYTES];
@@ -470,10 +524,18 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
     __shared__ __attribute__((aligned(8))) int ids[kMostBlocks + 2];
     __shared__ int found[4], part_id;
     __shared__ float2 state_ml[4][64];
-    const int i = blockIdx.x / Hkv, c = blockIdx.x % Hkv, n_items = *p.n_items;
-    const PrefixItem x = p.items[i];
-    if (i >= n_items || x.nb <= 0) return;
-    const int lane = threadIdx.x & 63, h = lane >> 5, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = Hq / Hkv;
+    const int i = blockIdx.x / Hkv, c = blockIdx.x % Hkv, g = Hq / Hkv;
+    PrefixItem x;
+    if constexpr (DIRECT) {
+        if (!whole_sequence(a, i, kBk, x)) return;
+        x.j0 = blockIdx.y * kItemTiles * 16;
+        if (x.j0 >= x.rows * g) return;
+    } else {
+        const int n_items = *p.n_items;
+        x = p.items[i];
+        if (i >= n_items || x.nb <= 0) return;
+    }
+    const int lane = threadIdx.x & 63, h = lane >> 5, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int G = x.rows * g, tiles = min((G - x.j0 + 31) >> 5, kItemTiles / 2);
     const bool narrow = tiles <= 2;
     const int tile = narrow ? w & (tiles - 1) : w, j = x.j0 + 32 * tile + (lane & 31);
@@ -487,6 +549,7 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
     const int part_n = min(kBk, x.len - (x.b0 + x.nb - 1) * kBk);
     int n_full = 0;
     if (threadIdx.x == 0) part_id = -1;
+    if (DIRECT && x.nb <= 0) __syncthreads();
     for (int b0 = 0; b0 < x.nb; b0 += 256) {
         const int b = b0 + threadIdx.x, id = b < x.nb ? a.bt[(size_t)x.seq * a.max_blocks + x.b0 + b] : -1;
         const bool there = id >= 0 && id < a.num_blocks, full = there && (b < x.nb - 1 || part_n == kBk);
@@ -528,13 +591,21 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
         return make_int2(__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y));
     };
     const auto tokens_of = [&](int b) { return b < n_full ? kBk : b < n_blk ? part_n : 0; };
-    const auto put = [&](const f32x16 &o, int t) {  // sums of channel tile t
+    const auto put = [&](const f32x16 &o, int t, float l) {  // sums of channel tile t; l: sum of the weights
+        if constexpr (DIRECT) {
+            const float inv = l > 0.f ? v_scale / l : 0.f;  // a NaN stays one: the sums of values are NaN then too
+            bf16_t *const to = (bf16_t *)a.out + ((size_t)(x.row0 + j / g) * Hq + c * g + j % g) * kD + 32 * t + 4 * h;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *(uint2 *)(to + 8 * k) = make_uint2(pack_bf16(o[4 * k] * inv, o[4 * k + 1] * inv), pack_bf16(o[4 * k + 2] * inv, o[4 * k + 3] * inv));
+            return;
+        }
         const size_t to = (size_t)(x.slot + j / g) * Hq + c * g + j % g;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             *(f32x4 *)(p.o + to * kD + 32 * t + 8 * k + 4 * h) = f32x4{o[4 * k] * v_scale, o[4 * k + 1] * v_scale, o[4 * k + 2] * v_scale, o[4 * k + 3] * v_scale};
     };
-    const auto put_ml = [&](float m, float l) { p.ml[(size_t)(x.slot + j / g) * Hq + c * g + j % g] = make_float2(m, l); };
+    const auto put_ml = [&](float m, float l) { if constexpr (!DIRECT) p.ml[(size_t)(x.slot + j / g) * Hq + c * g + j % g] = make_float2(m, l); };
 
     if (narrow) {
         constexpr int LOADS = KV8 ? 4 : 8;  // of a group's keys, and of its values
@@ -607,7 +678,7 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[4 * k + e] += f[y] * v[e];
                 }
-            put(o, t);
+            put(o, t, l);
         }
         if (first == 0 && h == 0) put_ml(m, l);
         return;
@@ -720,7 +791,7 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
     const float l = st.l + __shfl_xor(st.l, 32, 64);
     if (j >= G) return;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) put(st.o[t], t);
+    for (int t = 0; t < 4; ++t) put(st.o[t], t, l);
     if (h == 0) put_ml(st.m, l);
 }
 
@@ -730,18 +801,25 @@ bool on_matrix_cores(const Dims &dm) { return dm.bf16 && dm.D == kD && dm.Bk == 
 // For float32, head sizes other than 128 and blocks of more than 16 tokens.  An item has a tile of 16 queries; a wave takes sixteen tokens of a block in turn.  Products of 16 x 16 x 4 with the
 // transposed operands, see k_block_attn_f32: scores of keys [token][channel] times queries [channel][query] leave lane t + 16 p query t's scores of tokens 4 p .. 4 p + 3, which are
 // at once the right operand of the values' product, so nothing passes through LDS until the waves join.
-template <typename T, typename KT, int DT, bool EXACT>  // tiles of 16 channels: at most DT, or DT exactly
+template <typename T, typename KT, int DT, bool EXACT, bool DIRECT>  // tiles of 16 channels: at most DT, or DT exactly
 __global__ void __launch_bounds__(256) k_prefix_attn_f32(PrefixAttnArgs a, PrefixPlan p, int Hq, int Hkv, int D_, int Bk, float scale_log2, float v_scale) {
     typedef typename Quad<KT>::raw Raw;
     __shared__ f32x4 image[2][DT][64];
     __shared__ int2 ids[kMostBlocks];  // block of the pool, and its tokens
     __shared__ float image_m[4][16], image_l[4][16];
-    const int item = blockIdx.x / Hkv, c = blockIdx.x % Hkv;
-    if (item >= *p.n_items) return;
-    const PrefixItem x = p.items[item];
-    if (x.nb <= 0) return;
+    const int item = blockIdx.x / Hkv, c = blockIdx.x % Hkv, g = Hq / Hkv;
+    PrefixItem x;
+    if constexpr (DIRECT) {
+        if (!whole_sequence(a, item, Bk, x)) return;
+        x.j0 = blockIdx.y * 16;
+        if (x.j0 >= x.rows * g) return;
+    } else {
+        const int n_items = *p.n_items;
+        x = p.items[item];
+        if (item >= n_items || x.nb <= 0) return;
+    }
     const int D = EXACT ? 16 * DT : D_, d16 = D / 16;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, p4 = 4 * (lane >> 4), g = Hq / Hkv;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, p4 = 4 * (lane >> 4);
     const int G = x.rows * g, parts = Bk / 16, units = x.nb * parts, step = 4 / parts, step_parts = 4 % parts;  // sixteen tokens of a block are a unit
     for (int b = threadIdx.x; b < x.nb; b += 256) {
         int2 v = make_int2(0, 0);
@@ -851,6 +929,17 @@ __global__ void __launch_bounds__(256) k_prefix_attn_f32(PrefixAttnArgs a, Prefi
     if (w != 0) return;
     take(1);
     if (x.j0 + t >= G) return;
+    if constexpr (DIRECT) {
+        const float inv = sum > 0.f ? v_scale / sum : 0.f;  // a NaN stays one: the sums of values are NaN then too
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            if (!EXACT && d >= d16) continue;
+            T *out = (T *)a.out + row * D + 16 * d + p4;
+            if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(pack_bf16(o[d][0] * inv, o[d][1] * inv), pack_bf16(o[d][2] * inv, o[d][3] * inv));
+            else *(f32x4 *)out = o[d] * inv;
+        }
+        return;
+    }
     const size_t at = (size_t)(x.slot + j / g) * Hq + c * g + j % g;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -909,7 +998,7 @@ __global__ void __launch_bounds__(256) k_prefix_join(PrefixAttnArgs a, PrefixPla
     }
 }
 
-// Sizes that hold whatever the lengths are.  Items of a kv-head: a unit of n blocks and t tile groups has t * ceil(n / per) of them, and per is at least the sum of
+// Sizes that hold whatever the lengths are.  Items of a kv-head: a unit of n blocks and t tile groups has t * ceil(n / per) of them, and per is at least half the sum of
 // n * t over all units by `target`, or kMostBlocks.  Rows of a tile group: at most tiles * 16 / g and one more.
 bool plan_for(const Dims &dm, int S, int G, int R, int max_blocks, PrefixPlan &p) {  // false: more than a launch counts
     const bool mfma = on_matrix_cores(dm);
@@ -919,10 +1008,10 @@ bool plan_for(const Dims &dm, int S, int G, int R, int max_blocks, PrefixPlan &p
     p.step = mfma ? 4 : std::max(1, 8 * 16 / dm.Bk);
     p.target = std::max(1, (mfma ? 512 : 1024) / dm.Hkv);
     const int64_t groups = 2 * (((int64_t)R * g + 15) / 16 / p.tiles + 1) + G + S;  // tile groups of all units, at most
-    const int64_t items = std::max<int64_t>(p.target, groups * ((int64_t)max_blocks / kMostBlocks + 1)) + 2 * groups;
+    const int64_t items = std::max<int64_t>(p.target * 5 / 3, groups * ((int64_t)max_blocks / kMostBlocks + 1)) + 2 * groups;
     if (items * dm.Hkv >= 1 << 24) return false;
     p.cap_items = (int)items;
-    const int64_t most_parts = std::max<int64_t>(p.target, (int64_t)max_blocks / kMostBlocks + 1) + 2;
+    const int64_t most_parts = std::max<int64_t>(p.target * 5 / 3, (int64_t)max_blocks / kMostBlocks + 1) + 2;
     p.cap_slots = std::min<int64_t>(2 * (int64_t)R * most_parts, (int64_t)p.cap_items * (p.tiles * 16 / g + 1));
     return p.cap_slots <= INT32_MAX;
 }
@@ -954,11 +1043,24 @@ size_t prefix_attn_workspace(const Dims &dm, int S, int G, int R, int max_blocks
     return plan_for(dm, S, G, R, max_blocks, p) ? place(dm, S, G, p, nullptr) + 256 : 0;
 }
 
+// Tables so short that one launch in which every sequence reads all of its own costs less than three that read the shared blocks once.  1 to 128 sequences that share all but 30 tokens, 8 kv-heads,
+// us for three and for one launch, one sequence and 128 of them: 512 tokens 19 and 37 to 12 and 26, 1024 tokens 19 and 39 to 14 and 37, 2048 tokens 18 and 42 to 22 and 61 (FP8 cache the same way).
+// Without matrix cores: 256 tokens 16 and 17 to 12 and 12, 512 tokens 16 and 17 to 12 and 18, 1024 tokens 16 and 20 to 20 and 30.  Not timed beyond 1024 sequences x kv-heads.
+static int direct_tiles(const Dims &dm, const PrefixAttnArgs &a) {  // tile groups of the launch, 0: not this way
+    const int64_t tiles = ((int64_t)a.R * (dm.Hq / dm.Hkv) + 15) / 16, groups = on_matrix_cores(dm) ? (tiles + kItemTiles - 1) / kItemTiles : tiles;
+    const int64_t tokens = (int64_t)a.max_blocks * dm.Bk, items = (int64_t)a.S * dm.Hkv;
+    return tokens <= (on_matrix_cores(dm) ? 1024 : 512) && items <= 1024 && items * groups <= 8192 ? (int)groups : 0;
+}
+
 template <typename T, typename KT>
-static hipError_t launch_f32(const Dims &dm, const PrefixAttnArgs &a, const PrefixPlan &p, hipStream_t st) {
-    const dim3 grid((unsigned)p.cap_items * dm.Hkv);
+static hipError_t launch_f32(const Dims &dm, const PrefixAttnArgs &a, const PrefixPlan &p, int direct, hipStream_t st) {
+    const dim3 grid(direct ? (unsigned)a.S * dm.Hkv : (unsigned)p.cap_items * dm.Hkv, direct ? direct : 1);
     const float scale_log2 = kLog2e / sqrtf((float)dm.D) * (sizeof(KT) == 1 ? dm.k_scale : 1.f), v_scale = sizeof(KT) == 1 ? dm.v_scale : 1.f;
-#define PREFIX_ATTN_F32(DT, EXACT) hipLaunchKernelGGL((k_prefix_attn_f32<T, KT, DT, EXACT>), grid, dim3(256), 0, st, a, p, dm.Hq, dm.Hkv, dm.D, dm.Bk, scale_log2, v_scale)
+#define PREFIX_ATTN_F32(DT, EXACT)                                                                                                                                                    \
+    do {                                                                                                                                                                               \
+        if (direct) hipLaunchKernelGGL((k_prefix_attn_f32<T, KT, DT, EXACT, true>), grid, dim3(256), 0, st, a, p, dm.Hq, dm.Hkv, dm.D, dm.Bk, scale_log2, v_scale);                    \
+        else hipLaunchKernelGGL((k_prefix_attn_f32<T, KT, DT, EXACT, false>), grid, dim3(256), 0, st, a, p, dm.Hq, dm.Hkv, dm.D, dm.Bk, scale_log2, v_scale);                          \
+    } while (0)
     if (dm.D == 64) PREFIX_ATTN_F32(4, true);
     else if (dm.D == 128) PREFIX_ATTN_F32(8, true);
     else if (dm.D < 128) PREFIX_ATTN_F32(8, false);
@@ -967,25 +1069,33 @@ static hipError_t launch_f32(const Dims &dm, const PrefixAttnArgs &a, const Pref
     return hipGetLastError();
 }
 
+template <bool DIRECT>
+static hipError_t launch_mfma(const Dims &dm, const PrefixAttnArgs &a, const PrefixPlan &p, dim3 grid, hipStream_t st) {
+    const float scale_log2 = kLog2e / sqrtf((float)kD) * (dm.kv8 ? dm.k_scale : 1.f);
+    if (dm.kv8) hipLaunchKernelGGL((k_prefix_attn<true, DIRECT>), grid, dim3(256), 0, st, a, p, dm.Hq, dm.Hkv, scale_log2, dm.v_scale);
+    else hipLaunchKernelGGL((k_prefix_attn<false, DIRECT>), grid, dim3(256), 0, st, a, p, dm.Hq, dm.Hkv, scale_log2, 1.f);
+    return hipGetLastError();
+}
+
 hipError_t launch_prefix_attn(const Dims &dm, const PrefixAttnArgs &a, void *workspace, hipStream_t st) {
     PrefixPlan p;
+    hipError_t e = hipSuccess;
+    if (const int direct = direct_tiles(dm, a)) {
+        p = PrefixPlan{};
+        if (on_matrix_cores(dm)) return launch_mfma<true>(dm, a, p, dim3((unsigned)a.S * dm.Hkv, direct), st);
+        DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_f32<T, KT>(dm, a, p, direct, st)));
+        return e;
+    }
     if (!plan_for(dm, a.S, a.G, a.R, a.max_blocks, p)) return hipErrorInvalidValue;  // its workspace has size 0, so no call gets here
     place(dm, a.S, a.G, p, (char *)workspace);
     const int g = dm.Hq / dm.Hkv, most = std::max(a.S, a.G);
     if (most <= 256) hipLaunchKernelGGL(k_prefix_plan_small<256>, dim3(1), dim3(256), 0, st, a, p, g, dm.Bk);
     else if (most <= 512) hipLaunchKernelGGL(k_prefix_plan_small<512>, dim3(1), dim3(512), 0, st, a, p, g, dm.Bk);
     else hipLaunchKernelGGL(k_prefix_plan, dim3(1), dim3(kPlanThreads), 0, st, a, p, g, dm.Bk);
-    hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (on_matrix_cores(dm)) {
-        const dim3 grid((unsigned)p.cap_items * dm.Hkv);
-        const float scale_log2 = kLog2e / sqrtf((float)kD) * (dm.kv8 ? dm.k_scale : 1.f);
-        if (dm.kv8) hipLaunchKernelGGL(k_prefix_attn<true>, grid, dim3(256), 0, st, a, p, dm.Hq, dm.Hkv, scale_log2, dm.v_scale);
-        else hipLaunchKernelGGL(k_prefix_attn<false>, grid, dim3(256), 0, st, a, p, dm.Hq, dm.Hkv, scale_log2, 1.f);
-        e = hipGetLastError();
-    } else {
-        DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_f32<T, KT>(dm, a, p, st)));
-    }
+    if (on_matrix_cores(dm)) e = launch_mfma<false>(dm, a, p, dim3((unsigned)p.cap_items * dm.Hkv), st);
+    else DISPATCH_TK(dm.bf16, dm.kv8, e = (launch_f32<T, KT>(dm, a, p, 0, st)));
     if (e != hipSuccess) return e;
     const int rows = std::min(64, std::max(1, 2 * ((a.R + a.S - 1) / a.S)));
     DISPATCH_T(dm.bf16, hipLaunchKernelGGL(k_prefix_join<T>, dim3(a.S, rows, (dm.Hq + 3) / 4), dim3(256), 0, st, a, p, dm.Hq, dm.D));

@@ -259,16 +259,23 @@ def bound(layer, want, weight, size, count):
     return (2.0 ** -8 if c.bf16 else E24) * np.abs(want) + weight * (2 * ds + 2.0 ** -17 + count * E24 + (0.0 if not c.bf16 else 2.0 ** -11 if c.kv_fp8 else 2.0 ** -15)) + 1e-30
 
 
-def run_attend(layer, q, pool, table, kv, row_start, group_start, prefix, out=None):
+def both_widths(table, bk):
+    """The table, and the same one with columns of no block behind it: one of at most 1024 tokens may be read in one launch, wider ones are cut into items."""
+    return [table, np.concatenate([table, np.full((len(table), 1024 // bk + 1), -1)], axis=1)]
+
+
+def run_attend(layer, q, pool, table, kv, row_start, group_start, prefix):
     c = layer.cfg
-    out = torch.full(q.shape, 7.0, dtype=c.torch_dtype, device=DEV)
-    layer.attn_prefix(q, pool, i32(table).reshape(table.shape), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
-    torch.cuda.synchronize()
     want, weight, size, count = ref.attend(host(q), pool_values(layer, pool), table, kv, row_start, group_start, c.block_size, np.full(q.shape, 7.0))
-    got = host(out)
-    ok = np.abs(got - want) <= bound(layer, want, weight, size, count)
-    assert ok.all(), (np.argwhere(~ok)[:5], np.argwhere(~ok).shape, np.nanmax(np.abs(got - want)))
-    return out
+    outs = []
+    for t in both_widths(table, c.block_size):
+        outs.append(torch.full(q.shape, 7.0, dtype=c.torch_dtype, device=DEV))
+        layer.attn_prefix(q, pool, i32(t).reshape(t.shape), i32(kv), i32(row_start), i32(group_start), i32(prefix), outs[-1])
+        torch.cuda.synchronize()
+        got = host(outs[-1])
+        ok = np.abs(got - want) <= bound(layer, want, weight, size, count)
+        assert ok.all(), (t.shape, np.argwhere(~ok)[:5], np.argwhere(~ok).shape, np.nanmax(np.abs(got - want)))
+    return outs
 
 
 def blocks_that_may_be_read(layer, pool, table, kv):
@@ -363,6 +370,38 @@ def test_attend_many_groups(kw):
     layer.close()
 
 
+@pytest.mark.parametrize("kw,tokens", [(dict(), 1024), (dict(fp8=True), 1024), (dict(bf16=False), 512), (dict(D=64), 512)], ids=str)
+@pytest.mark.parametrize("beyond", [0, 1])
+@pytest.mark.parametrize("n,rows", [(3, 1), (1, 70), (130, 1)])
+def test_attend_tables_as_wide_as_one_launch_takes(kw, tokens, beyond, n, rows):
+    """And one column wider; many rows of a sequence, many sequences, tables that are full."""
+    layer = make(num_blocks=1000, Hq=32, Hkv=8, **kw)
+    rng = np.random.default_rng(n)
+    pool = random_pool(layer, rng)
+    cols, apart = tokens // 16 + beyond, min(5, 900 // n)
+    tails = [int(t) for t in rng.integers(0, apart * 16 + 1, n)]
+    tails[-1] = apart * 16
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, [([rows] * n, (cols - apart) * 16, tails)], cols)
+    run_attend(layer, queries(layer, rng, n * rows, 2.0), pool, table, kv, row_start, group_start, prefix)
+    layer.close()
+
+
+@pytest.mark.parametrize("kw", [dict(Hq=4, Hkv=1), dict(Hq=4, Hkv=1, fp8=True), dict(Hq=2, Hkv=1, D=64)], ids=str)
+@pytest.mark.parametrize("n,groups", [(256, 1), (257, 3), (512, 200), (513, 40), (1100, 1), (1500, 700)])
+def test_attend_many_sequences(kw, n, groups):
+    """Counts of sequences around those that a plan holds to a thread."""
+    print("case:", kw, n, groups, flush=True)
+    layer = make(num_blocks=6000, **kw)
+    rng = np.random.default_rng(n)
+    pool = random_pool(layer, rng)
+    parts = np.diff(np.concatenate([[0], np.sort(rng.integers(0, n + 1, groups - 1)), [n]]))
+    spec = [([int(r) for r in rng.integers(0, 3, m)], int(rng.integers(0, 40)), [int(t) for t in rng.integers(-1, 33, m)]) for m in parts]
+    spec[0] = (spec[0][0], 16 * 60 + 3, spec[0][2])
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, spec, 66)
+    run_attend(layer, queries(layer, rng, int(row_start[-1])), pool, table, kv, row_start, group_start, prefix)
+    layer.close()
+
+
 @pytest.mark.parametrize("kw", [dict(), dict(fp8=True, k_scale=0.5), dict(bf16=False)], ids=str)
 def test_attend_large_scores(kw):
     """Scores in the hundreds: the running maximum moves, and one part's sums are nothing beside another's."""
@@ -388,16 +427,19 @@ def test_attend_scores_of_minus_infinity(kw):
     run_attend(layer, q, pool, table, kv, row_start, group_start, prefix)
     keys[int(table[1, 22]), :, :, 0] = -float("inf")
     run_attend(layer, q, pool, table, kv, row_start, group_start, prefix)
-    keys[int(table[2, 21]), 1, 3, 5] = float("nan")
-    out = torch.zeros_like(q)
-    layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
-    bad = torch.isnan(out.float()).any(-1).cpu().numpy()
-    assert bad[4:, 4:].all() and not bad[:4].any() and not bad[4:, :4].any()
-    keys[int(table[2, 21]), 1, 3, 5] = 0.0
-    keys[int(table[0, 3]), 0, 3, 0] = float("inf")
-    layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
-    bad = torch.isnan(out.float()).any(-1).cpu().numpy()
-    assert bad[:, :4].all() and not bad[:, 4:].any()
+    for t in both_widths(table, 16):
+        out = torch.zeros_like(q)
+        keys[int(table[2, 21]), 1, 3, 5] = float("nan")
+        layer.attn_prefix(q, pool, i32(t), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
+        bad = torch.isnan(out.float()).any(-1).cpu().numpy()
+        assert bad[4:, 4:].all() and not bad[:4].any() and not bad[4:, :4].any()
+        keys[int(table[2, 21]), 1, 3, 5] = 0.0
+        was = keys[int(table[0, 3]), 0, 3, 0].clone()
+        keys[int(table[0, 3]), 0, 3, 0] = float("inf")
+        layer.attn_prefix(q, pool, i32(t), i32(kv), i32(row_start), i32(group_start), i32(prefix), out)
+        bad = torch.isnan(out.float()).any(-1).cpu().numpy()
+        assert bad[:, :4].all() and not bad[:, 4:].any()
+        keys[int(table[0, 3]), 0, 3, 0] = was
     layer.close()
 
 
@@ -430,9 +472,10 @@ def test_prefix_beyond_32_bits():
     q = queries(layer, rng, 4)
     args = ([470, 480], np.array([0, 2, 4]), np.array([0, 2]), [320])
     want = run_attend(small, q, some, table - 139960, *args)
-    out = torch.zeros_like(q)
-    layer.attn_prefix(q, pool, i32(table), i32(args[0]), i32(args[1]), i32(args[2]), i32(args[3]), out)
-    assert torch.equal(out, want)
+    for t, w in zip(both_widths(table, 16), want):
+        out = torch.zeros_like(q)
+        layer.attn_prefix(q, pool, i32(t), i32(args[0]), i32(args[1]), i32(args[2]), i32(args[3]), out)
+        assert torch.equal(out, w)
     layer.copy_blocks([pool], i32([139990, 3]), i32([1, 139999]))
     assert torch.equal(pool[1], some[30]) and not pool[139999].any()
     layer.close()
@@ -449,9 +492,10 @@ def test_integer_arrays_need_only_their_own_alignment():
     pool = random_pool(layer, rng)
     table, kv, row_start, group_start, prefix = crowd(layer, rng, [([2, 1], 333, [20, 31])], 30)
     q = queries(layer, rng, 3)
-    a = layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32(group_start), i32(prefix))
-    b = layer.attn_prefix(q, pool, off(table), off(kv), off(row_start), off(group_start), off(prefix))
-    assert torch.equal(a, b)
+    for t in both_widths(table, 16):
+        a = layer.attn_prefix(q, pool, i32(t), i32(kv), i32(row_start), i32(group_start), i32(prefix))
+        b = layer.attn_prefix(q, pool, off(t), off(kv), off(row_start), off(group_start), off(prefix))
+        assert torch.equal(a, b)
     got = []
     for put in (i32, off):
         m = binding.ForkMap(1, 2, 30, DEV)
