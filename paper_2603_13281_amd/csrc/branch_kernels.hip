@@ -390,28 +390,83 @@ struct ForkGroup {  // in LDS: a group's sequences
     int shared, n_fresh;
 };
 
-// The old ids of this thread's column, of all sequences as they stand, in LDS: read whether they are in use or not, so that they are on their way beside the lengths.
-__device__ __forceinline__ void fork_tile(const ForkArgs &a, int g, int c, int32_t *tile) {
-    if (c >= a.max_blocks) return;
-    const int32_t *from = a.bt + (size_t)g * a.W * a.max_blocks + c;
-    int i = 0;
-    for (; i + 8 <= a.W; i += 8) {
-        int32_t v[8];
+// The old ids of this thread's column, of all sequences as they stand: read whether they are in use or not, so that they are on their way beside the lengths.  M sequences at most are held
+// in registers (64 groups of 8 sequences, 1000 columns: the count takes 4.9 us, 9.8 from LDS), any number in LDS (M = 0).
+template <int M>
+struct ForkColumn {
+    int32_t v[M ? M : 1];
+    __device__ __forceinline__ void load(const ForkArgs &a, int g, int c, int32_t *tile) {
+        const int32_t *from = a.bt + (size_t)g * a.W * a.max_blocks + c;
+        if constexpr (M > 0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = from[(size_t)(i + k) * a.max_blocks];
+            for (int i = 0; i < M; ++i) v[i] = -1;
+            if (c >= a.max_blocks) return;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) tile[(i + k) * kForkCols + threadIdx.x] = v[k];
+            for (int i = 0; i < M; ++i)
+                if (i < a.W) v[i] = from[(size_t)i * a.max_blocks];
+            return;
+        }
+        if (c >= a.max_blocks) return;
+        int i = 0;
+        for (; i + 8 <= a.W; i += 8) {
+            int32_t x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = from[(size_t)(i + k) * a.max_blocks];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) tile[(i + k) * kForkCols + threadIdx.x] = x[k];
+        }
+        for (; i < a.W; ++i) tile[i * kForkCols + threadIdx.x] = from[(size_t)i * a.max_blocks];
     }
-    for (; i < a.W; ++i) tile[i * kForkCols + threadIdx.x] = from[(size_t)i * a.max_blocks];
+    __device__ __forceinline__ void to_tile(const ForkArgs &a, int32_t *tile) const {
+        if constexpr (M > 0) {
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                if (i < a.W) tile[i * kForkCols + threadIdx.x] = v[i];
+        }
+    }
+    // Which are freed: no sequence with children has the block in this column, and no earlier one of those without.
+    __device__ __forceinline__ uint64_t freed(const ForkArgs &a, int c, const ForkGroup &f, const int32_t *tile) const {
+        uint64_t out = 0;
+        if constexpr (M > 0) {
+            const uint32_t kept = __builtin_amdgcn_readfirstlane((uint32_t)f.kept);
+            int32_t u[M];  // -1: no block
+#pragma unroll
+            for (int i = 0; i < M; ++i) u[i] = i < a.W && c < f.nb[i] && v[i] >= 0 && v[i] < a.num_blocks ? v[i] : -1;
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                if (i >= a.W || kept >> i & 1) continue;
+                bool held = u[i] < 0;
+#pragma unroll
+                for (int j = 0; j < M; ++j)
+                    if (j < i || (j > i && kept >> j & 1)) held |= u[j] == u[i];
+                if (!held) out |= 1ull << i;
+            }
+            return c < f.shared ? 0 : out;
+        }
+        if (c < f.shared) return 0;
+        const int32_t *mine = tile + threadIdx.x;
+        for (int i = 0; i < a.W; ++i) {
+            if (f.kept >> i & 1 || c >= f.nb[i]) continue;
+            const int id = mine[i * kForkCols];
+            bool held = id < 0 || id >= a.num_blocks;
+            for (int j = 0; j < a.W && !held; ++j) held = (j < i || f.kept >> j & 1) && c < f.nb[j] && mine[j * kForkCols] == id;
+            if (!held) out |= 1ull << i;
+        }
+        return out;
+    }
+};
+
+struct ForkSequence { int len, parent, shared; };  // what the arrays hold for this thread's
+__device__ __forceinline__ ForkSequence fork_sequence(const ForkArgs &a, int g) {
+    const int i = threadIdx.x;
+    return i < a.W ? ForkSequence{a.kv_lens[g * a.W + i], a.parents[g * a.W + i], a.shared ? a.shared[g] : 0} : ForkSequence{0, -1, 0};
 }
 
-__device__ __forceinline__ void fork_group(const ForkArgs &a, int g, ForkGroup &f) {  // by the first wave; a barrier follows
+__device__ __forceinline__ void fork_group(const ForkArgs &a, const ForkSequence &mine, ForkGroup &f) {  // by the first wave; a barrier follows
     const int i = threadIdx.x;
     if (i >= 64) return;
-    const bool in = i < a.W;
     const int64_t room = (int64_t)a.max_blocks * a.Bk;
-    const int n = in ? (int)min((int64_t)max(a.kv_lens[g * a.W + i], 0), room) : 0, p = in ? a.parents[g * a.W + i] : -1;
-    const int parent = p >= 0 && p < a.W ? p : -1, shared = a.shared ? max(a.shared[g], 0) : 0;
+    const int n = (int)min((int64_t)max(mine.len, 0), room), parent = mine.parent >= 0 && mine.parent < a.W ? mine.parent : -1, shared = __builtin_amdgcn_readfirstlane(max(mine.shared, 0));
     f.len[i] = n;
     f.nb[i] = n / a.Bk + (n % a.Bk != 0);
     f.parent[i] = parent;
@@ -433,21 +488,6 @@ __device__ __forceinline__ void fork_group(const ForkArgs &a, int g, ForkGroup &
     }
 }
 
-// Which of this thread's column are freed.
-__device__ __forceinline__ uint64_t fork_freed(const ForkArgs &a, int c, const ForkGroup &f, const int32_t *tile) {
-    uint64_t freed = 0;
-    if (c < f.shared) return 0;
-    const int32_t *mine = tile + threadIdx.x;
-    for (int i = 0; i < a.W; ++i) {
-        if (f.kept >> i & 1 || c >= f.nb[i]) continue;
-        const int id = mine[i * kForkCols];
-        bool held = id < 0 || id >= a.num_blocks;
-        for (int j = 0; j < a.W && !held; ++j) held = (j < i || f.kept >> j & 1) && c < f.nb[j] && mine[j * kForkCols] == id;
-        if (!held) freed |= 1ull << i;
-    }
-    return freed;
-}
-
 // Inclusive sum over the wave.
 __device__ __forceinline__ int wave_scan(int x) {
 #pragma unroll
@@ -459,15 +499,18 @@ __device__ __forceinline__ int wave_scan(int x) {
 }
 constexpr int kForkWaves = kForkCols / 64;
 
+template <int M>
 __global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts p) {
-    extern __shared__ int32_t tile[];  // [W][kForkCols]
+    extern __shared__ int32_t tile[];  // [W][kForkCols], M = 0
     __shared__ ForkGroup f;
     __shared__ int wsum[kForkWaves];
     const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
-    fork_group(a, g, f);
-    fork_tile(a, g, c, tile);
+    ForkColumn<M> col;
+    const ForkSequence seq = fork_sequence(a, g);
+    col.load(a, g, c, tile);
+    fork_group(a, seq, f);
     __syncthreads();
-    const uint64_t freed = fork_freed(a, c, f, tile);
+    const uint64_t freed = col.freed(a, c, f, tile);
     const int n = __popcll(freed), x = wave_scan(n);
     if (lane == 63) wsum[w] = x;
     __syncthreads();
@@ -477,34 +520,57 @@ __global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts 
         all += wsum[i];
     }
     int32_t *out = p.freed + ((size_t)g * p.parts + part) * a.W * kForkCols;
-    for (uint64_t left = freed; left; left &= left - 1) out[at++] = tile[(__ffsll((unsigned long long)left) - 1) * kForkCols + t];
+    if constexpr (M > 0) {
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+            if (freed >> i & 1) out[at++] = col.v[i];
+    } else {
+        for (uint64_t left = freed; left; left &= left - 1) out[at++] = tile[(__ffsll((unsigned long long)left) - 1) * kForkCols + t];
+    }
     if (t == 0) {
         p.freed_n[(size_t)g * p.parts + part] = all;
         if (part == 0) p.fresh_n[g] = f.n_fresh;
     }
 }
 
+template <int M>
 __global__ void __launch_bounds__(kForkCols) k_fork_write(ForkArgs a, ForkParts p) {
-    extern __shared__ int32_t tile[];
+    extern __shared__ int32_t tile[];  // [W][kForkCols]
     __shared__ ForkGroup f;
     __shared__ int fresh_id[kBeamMost], fresh_at[kBeamMost], red[4][kForkWaves];
+    __shared__ int64_t fresh_from[kBeamMost];  // where a child's id stands in the parts' lists
     const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
     const int n_parts = a.G * p.parts, me = g * p.parts + part;
+    // Every read that waits for no other comes first: the parts' lists and counts are another launch's, and each round of reads is a microsecond.
+    const ForkSequence seq = fork_sequence(a, g);
     const int used = *a.free_used, n_mine = p.freed_n[me];
-    // sums over the parts and groups before this one, and over all
-    int sum[4] = {0, 0, 0, 0};
-    for (int i = t; i < n_parts; i += kForkCols) {
-        const int n = p.freed_n[i];
-        sum[1] += n;
-        if (i < me) sum[0] += n;
+    const int32_t *mine = p.freed + (size_t)me * a.W * kForkCols;
+    const int first_mine = mine[t];  // of no use from n_mine on
+    int n_fresh = t < a.G ? p.fresh_n[t] : 0;
+    ForkColumn<M> col;
+    col.load(a, g, c, tile);
+    // sums over the parts and groups before this one, and over all; a thread takes a run of parts
+    constexpr int RUN = 8;
+    int sum[4] = {0, 0, 0, 0}, n[RUN];
+    const int run = (n_parts + kForkCols - 1) / kForkCols, run0 = min(t * run, n_parts), run1 = min(run0 + run, n_parts);
+    for (int i0 = run0; i0 < run1; i0 += RUN) {
+#pragma unroll
+        for (int k = 0; k < RUN; ++k) n[k] = i0 + k < run1 ? p.freed_n[i0 + k] : 0;
+#pragma unroll
+        for (int k = 0; k < RUN; ++k) {
+            sum[1] += n[k];
+            if (i0 + k < me) sum[0] += n[k];
+        }
     }
     for (int i = t; i < a.G; i += kForkCols) {
-        const int n = p.fresh_n[i];
-        sum[3] += n;
-        if (i < g) sum[2] += n;
+        if (i != t) n_fresh = p.fresh_n[i];
+        sum[3] += n_fresh;
+        if (i < g) sum[2] += n_fresh;
     }
-    fork_group(a, g, f);
-    fork_tile(a, g, c, tile);
+    fork_group(a, seq, f);
+    col.to_tile(a, tile);
+    const int run_n = sum[1];
+    int run_at = wave_scan(run_n) - run_n;  // freed ids before this thread's parts; the waves before are added below
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
 #pragma unroll
@@ -517,59 +583,73 @@ __global__ void __launch_bounds__(kForkCols) k_fork_write(ForkArgs a, ForkParts 
         sum[k] = red[k][0];
         for (int i = 1; i < kForkWaves; ++i) sum[k] += red[k][i];
     }
+    for (int i = 0; i < w; ++i) run_at += red[1][i];
     const int before = sum[0], all = sum[1], fresh_before = sum[2], fresh_all = sum[3];
     const int head = min(max(used, 0), a.n_free), low = head - all, start = max(low, 0);  // freed id j stands at low + j
-    const int32_t *mine = p.freed + (size_t)me * a.W * kForkCols;
     for (int j = t; j < n_mine; j += kForkCols)
-        if (low + before + j >= 0) a.free_ids[low + before + j] = mine[j];
+        if (low + before + j >= 0) a.free_ids[low + before + j] = j == t ? first_mine : mine[j];
     // Fresh ids of the group's children: entries start + fresh_before .. of the list.  Those before the head are freed ids of this call: from the parts' lists, since another workgroup
     // may not have entered them yet.
     if (t < 64) {
         const bool need = t < a.W && f.fresh[t];
         const int64_t at = (int64_t)start + fresh_before + __popcll(__ballot(need) & ((1ull << t) - 1));
-        int id = -1;
-        if (need && at < a.n_free && at >= head) id = a.free_ids[at];
         fresh_at[t] = need ? (at < a.n_free ? (int)at : -1) : -2;
-        fresh_id[t] = id;
+        fresh_id[t] = -1;
+        fresh_from[t] = -1;
     }
     __syncthreads();
-    if (f.n_fresh && start + fresh_before < head) {
-        // the parts whose freed ids those are: at most as many as there are children, in a run that begins where the sum passes start + fresh_before - low
-        int done = 0;  // freed ids of the parts of the rounds before
-        for (int i0 = 0; i0 < n_parts; i0 += kForkCols) {
-            const int i = i0 + t, n = i < n_parts ? p.freed_n[i] : 0, x = wave_scan(n);
-            __syncthreads();
-            if (lane == 63) red[0][w] = x;
-            __syncthreads();
-            int from = done + x - n;
-            for (int k = 0; k < w; ++k) from += red[0][k];
-            for (int k = 0; k < kForkWaves; ++k) done += red[0][k];
-            if (n && from < start + fresh_before + f.n_fresh - low && from + n > start + fresh_before - low)
-                for (int j = 0; j < a.W; ++j) {
-                    const int64_t k = (int64_t)fresh_at[j] - low - from;
-                    if (fresh_at[j] >= 0 && fresh_at[j] < head && k >= 0 && k < n) fresh_id[j] = p.freed[(size_t)i * a.W * kForkCols + k];
+    if (f.n_fresh) {
+        const int want = start + fresh_before - low;  // the first of them among all freed ids
+        if (run_at < want + f.n_fresh && run_at + run_n > want) {
+            const auto find = [&](int i, int count) {
+                for (int j = 0; j < a.W && run_at < want + f.n_fresh && run_at + count > want; ++j) {
+                    const int k = fresh_at[j] - low - run_at;
+                    if (fresh_at[j] >= 0 && fresh_at[j] < head && k >= 0 && k < count) fresh_from[j] = (int64_t)i * a.W * kForkCols + k;
                 }
+                run_at += count;
+            };
+            if (run <= RUN) {
+#pragma unroll
+                for (int k = 0; k < RUN; ++k)
+                    if (n[k]) find(run0 + k, n[k]);
+            } else {
+                for (int i = run0; i < run1; ++i) find(i, p.freed_n[i]);
+            }
         }
         __syncthreads();
+        if (t < a.W && fresh_at[t] >= head) fresh_id[t] = a.free_ids[fresh_at[t]];
+        else if (t < a.W && fresh_from[t] >= 0) fresh_id[t] = p.freed[fresh_from[t]];
+        __syncthreads();
     }
-    for (int i = 0; i < a.W; ++i) {
-        const int q = f.parent[i];
-        if (q < 0 || fresh_at[i] == -1 || c >= f.nb[q]) continue;
-        int id = tile[q * kForkCols + t];
-        if (fresh_at[i] >= 0 && c == f.nb[q] - 1) id = fresh_id[i] >= 0 && fresh_id[i] < a.num_blocks ? fresh_id[i] : -1;
-        a.new_bt[((size_t)g * a.W + i) * a.max_blocks + c] = id;
+    for (int i0 = 0; i0 < a.W; i0 += 8) {  // eight children at a time, for the chains of reads from LDS
+        int q[8], at[8], id[8], nb[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = min(i0 + k, a.W - 1);
+            q[k] = f.parent[i], at[k] = fresh_at[i], id[k] = fresh_id[i];
+            if (i0 + k >= a.W || at[k] == -1) q[k] = -1;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int last = f.nb[max(q[k], 0)] - 1, old = tile[max(q[k], 0) * kForkCols + t];
+            nb[k] = q[k] < 0 ? 0 : last + 1;
+            if (at[k] < 0 || c != last) {
+                id[k] = old;
+            } else if (q[k] >= 0) {  // the block that is not full
+                if (id[k] < 0 || id[k] >= a.num_blocks) id[k] = -1;
+                const bool copy = id[k] >= 0 && old >= 0 && old < a.num_blocks;
+                a.copy_src[g * a.W + i0 + k] = copy ? old : -1;
+                a.copy_dst[g * a.W + i0 + k] = copy ? id[k] : -1;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (c < nb[k]) a.new_bt[((size_t)g * a.W + i0 + k) * a.max_blocks + c] = id[k];
     }
     if (part == 0 && t < a.W) {
         const int q = f.parent[t];
         a.new_lens[g * a.W + t] = q < 0 || fresh_at[t] == -1 ? 0 : f.len[q];
-        int src = -1, dst = -1;
-        if (fresh_at[t] >= 0) {
-            src = a.bt[((size_t)g * a.W + q) * a.max_blocks + f.nb[q] - 1];
-            dst = fresh_id[t];
-            if (src < 0 || src >= a.num_blocks || dst < 0 || dst >= a.num_blocks) src = dst = -1;
-        }
-        a.copy_src[g * a.W + t] = src;
-        a.copy_dst[g * a.W + t] = dst;
+        if (fresh_at[t] < 0) a.copy_src[g * a.W + t] = a.copy_dst[g * a.W + t] = -1;
     }
     if (me == 0 && t == 0) {
         const int64_t end = (int64_t)start + fresh_all;
@@ -712,10 +792,14 @@ hipError_t launch_fork(const ForkArgs &a, void *workspace, hipStream_t st) {
     p.fresh_n = p.freed_n + (size_t)a.G * p.parts;
     const dim3 grid(p.parts, a.G);
     const size_t lds = (size_t)a.W * kForkCols * 4;
-    hipLaunchKernelGGL(k_fork_count, grid, dim3(kForkCols), lds, st, a, p);
+    if (a.W <= 8) hipLaunchKernelGGL(k_fork_count<8>, grid, dim3(kForkCols), 0, st, a, p);
+    else if (a.W <= 16) hipLaunchKernelGGL(k_fork_count<16>, grid, dim3(kForkCols), 0, st, a, p);
+    else hipLaunchKernelGGL(k_fork_count<0>, grid, dim3(kForkCols), lds, st, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_fork_write, grid, dim3(kForkCols), lds, st, a, p);
+    if (a.W <= 8) hipLaunchKernelGGL(k_fork_write<8>, grid, dim3(kForkCols), lds, st, a, p);
+    else if (a.W <= 16) hipLaunchKernelGGL(k_fork_write<16>, grid, dim3(kForkCols), lds, st, a, p);
+    else hipLaunchKernelGGL(k_fork_write<0>, grid, dim3(kForkCols), lds, st, a, p);
     return hipGetLastError();
 }
 
