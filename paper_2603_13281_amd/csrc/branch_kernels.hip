@@ -61,7 +61,7 @@ __device__ __forceinline__ double wave_max_f64(double v) {
 }
 
 // A number that at least W of the wave's 64 reach, and not many more.  Up to 16: of sixteen runs of four lanes the largest each, and of those the least that fewer than W exceed; else of W runs
-// (the next power of two) the least.  A part of 8192 logits lists 27 of them for 8 beams, by runs alone 53, and ranking the list is what the choice spends its time on.
+// (the next power of two) the least.  A part of 8192 logits lists 27 of them for 8 beams, by runs alone 53.
 template <int CTRL>
 __device__ __forceinline__ float lane_of(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true)); }
 __device__ __forceinline__ float reached_by(float x, int W) {
@@ -184,13 +184,17 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamPart
     __syncthreads();
     if (t == 0) out.sums[(size_t)s * out.parts + part] = make_double2((double)most, (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]));
     const int n0 = listed[0], n1 = listed[1], n2 = listed[2], n3 = listed[3], all = n0 + n1 + n2 + n3;
-    if (max(max(n0, n1), max(n2, n3)) <= SEG) {  // the place of each in the order: how many are larger
-        for (int i = lane; i < n; i += 64) {
+    if (max(max(n0, n1), max(n2, n3)) <= SEG) {  // the place of each in the order: how many are larger; several lanes to one, each of which looks at a share of the lists
+        int lanes = 64;
+        while (lanes > 1 && lanes * n > 64) lanes >>= 1;
+        const int share = lane & (lanes - 1);
+        for (int i = lane / lanes; i < n; i += 64 / lanes) {
             const uint64_t v = list[w * SEG + i];
             int rank = 0;
             for (int k = 0; k < 4; ++k)
-                for (int j = 0; j < listed[k]; ++j) rank += list[k * SEG + j] > v;
-            if (rank < a.W) best[rank] = v;
+                for (int j = share; j < listed[k]; j += lanes) rank += list[k * SEG + j] > v;
+            for (int o = 1; o < lanes; o <<= 1) rank += __shfl_xor(rank, o, 64);
+            if (share == 0 && rank < a.W) best[rank] = v;
         }
         if (t >= all && t < a.W) best[t] = 0;
         return;

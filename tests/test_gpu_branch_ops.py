@@ -88,6 +88,19 @@ def test_choose_equal_logits(vocab, dt):
     layer.close()
 
 
+def test_choose_logits_far_from_zero():
+    """Rows around the size where a part needs more care, lowest numbers beside ordinary ones."""
+    layer, rng = make(), np.random.default_rng(9)
+    for offset in (0.0, 4000.0, 8180.0, 8200.0, -8180.0, -8300.0, 1e6, -1e6):
+        x = words(rng, 6, 20011, torch.float32) + offset
+        x[1, ::3] = -1e6
+        x[2, 5:9000] = -3.4028234e38
+        x[3, 17] = -float("inf")
+        x[4, 8000] = float("nan")
+        run_choose(layer, x, 2, 3, -rng.random(6))
+    layer.close()
+
+
 def test_choose_masked_logits():
     """Minus infinity, NaN and plus infinity among the logits; beams that are not live; fewer continuations than beams."""
     layer, rng = make(), np.random.default_rng(0)
