@@ -104,7 +104,7 @@ struct BeamParts {
     int parts;
 };
 
-// Bound by arithmetic, not by its one pass over the logits: 512 rows of 128256 float32 logits (263 MB) take 63 us, without the exponentials 40 (6.6 TB/s), without the candidates 53.  A logit
+// Bound by arithmetic, not by its one pass over the logits: 460 rows of 128256 float32 logits (236 MB) take 63 us, without the exponentials 40 (5.9 TB/s), without the candidates 53.  A logit
 // costs 17 instructions of float64 and six others.  (Skipping the cleaning and the limit of ordinary logits, three of the 17, changed nothing; more waves to a SIMD spill or wait: 66 -> 76.)
 template <typename T, int PER>  // logits of a thread
 __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamParts out) {
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a, BeamPa
 }
 
 // Parts of 8192 logits, of 2048 where those would be fewer than 128 workgroups.  Rows of 128256, us of both kernels with small and large parts: 4 rows 10.5, 11.1; 16 rows 20.1, 14.0; 32 rows
-// 25.5, 16.2 -- the merge reads what the parts leave.  Parts of 4096: 512 rows 76.8 + 10.9 for 66.3 + 7.7.
+// 25.5, 16.2 -- the merge reads what the parts leave.  Parts of 4096: 460 rows 76.8 + 10.9 for 66.3 + 7.7.
 constexpr int kBeamFew = 8, kBeamMany = 32;
 int beam_parts(int vocab, int per) { return (int)(((int64_t)vocab + kBeamThreads * per - 1) / (kBeamThreads * per)); }
 int beam_per(int G, int W, int vocab) { return (int64_t)G * W * beam_parts(vocab, kBeamMany) >= 128 ? kBeamMany : kBeamFew; }
