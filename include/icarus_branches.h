@@ -82,7 +82,7 @@ icarus_status icarus_copy_blocks(icarus_ctx *ctx, void *const *arrays /*host*/, 
 
 /* out[r, h] = softmax(q[r, h] K^T / sqrt(D)) V over positions 0 .. kv_lens[s] - 1 of sequence s, for the rows row_start[s] .. row_start[s + 1] - 1 of each sequence, one token per row, as
  * icarus_attn_shared_kv.  Sequences group_start[g] .. group_start[g + 1] - 1 form group g; the first prefix_lens[g] / block_size columns (rounded down) of
- * their tables name the same blocks, which are read once for all rows of the group.  Results go by the tables alone where that holds; what is shared, the lengths and the sizes of the arrays say
+ * their tables name the same blocks, which are read once for all rows of the group (short tables may be read by every sequence).  Results go by the tables alone where that holds; what is shared, the lengths and the sizes of the arrays say
  * how sums are split, so calls that differ in them agree up to rounding.
  * Positions whose block lies outside the pool and positions beyond the table are left out.  A row with nothing to attend to, or only scores of minus infinity, becomes zeros; a NaN or a score of
  * plus infinity makes NaN.  Rows of no sequence, and of sequences in no group, keep what out holds.  Shared columns count up to the shortest sequence of the group that is not empty.

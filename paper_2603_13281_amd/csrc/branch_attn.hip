@@ -18,7 +18,7 @@ struct PrefixUnit { int row0, rows, seq, b0, nb, len, chunks, slot; };  // its r
 struct PrefixItem { int row0, rows, j0, seq, b0, nb, len, slot; };      // j0: the first of its queries among the unit's
 struct PrefixJoin { int row0, rows, n_shared, shared, shared_rows, n_own, own, pad; };  // a sequence's rows; place of part k of row r: shared + k * shared_rows + r, then own + k * rows + r - row0
 constexpr int kPlanThreads = 1024, kMostBlocks = 1024;                   // blocks of an item, at most
-constexpr float kItemCost = 14.f, kAlone = 0.65f;                        // what an item costs beside its blocks, in blocks; time of one that has a CU to itself by that of two that share one
+constexpr float kItemCost = 4.f, kAlone = 0.6f, kRounds = 0.7f;          // of the choice of an item's size: an item's cost beside its blocks, in blocks; a last round of at most one to a CU; weight of the rounds
 
 struct PrefixPlan {
     PrefixUnit *units;  // [G] shared blocks of a group, [S] the rest of a sequence
@@ -249,8 +249,8 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
     int per = max((even + p.step - 1) / p.step, 1) * p.step;
     if (even > 2 * p.step && even < kMostBlocks) {
         // The largest size of an item.  Even shares would be `even` blocks, but a unit is cut into whole items, and a few more than run at once cost a round.  Of sixteen sizes the one is taken
-        // whose sum is least, in blocks: all work over the workgroups that run at once, and the rounds of the large items, a last round of at most one to a CU counting kAlone.  Over seven sets of
-        // sequences (9 to 140 units, 2000 to 25600 blocks) and 13 sizes each, this choice was 0.7 % behind the best one timed, 2.6 % at most; even shares 5 and 12 %.
+        // whose sum is least, in blocks: all work over the workgroups that run at once, and kRounds times the rounds of the large items, a last round of at most one to a CU counting kAlone.  Over 16
+        // sets of sequences (9 to 140 units, 600 to 25600 blocks) and eleven sizes each, this choice was 1.8 % behind the best one timed, 11 % at most; even shares 5 and 13 %.
         if (is_group) size_of[t] = u.nb, at_item[t] = tg_u;
         if (is_seq) size_of[a.G + t] = v.nb, at_item[a.G + t] = tg_v;
         __syncthreads();
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
             all_work += r.x, large += r.y, longest = fmaxf(longest, r.z);
         }
         const float rounds = large / p.target, full = floorf(rounds), rest = rounds - full;
-        const float time = all_work / p.target + (full + (rest <= 0.f ? 0.f : rest <= 0.5f ? kAlone : 1.f)) * (longest + kItemCost);
+        const float time = all_work / p.target + kRounds * (full + (rest <= 0.f ? 0.f : rest <= 0.5f ? kAlone : 1.f)) * (longest + kItemCost);
         float least = time;
 #pragma unroll
         for (int o = 1; o < 16; o <<= 1) least = fminf(least, __shfl_xor(least, o, 64));
@@ -956,7 +956,7 @@ __global__ void __launch_bounds__(256) k_prefix_attn_f32(PrefixAttnArgs a, Prefi
 
 // A row's parts put together, first the parts of the group's shared blocks, then those of its own: a wave to a head, four channels to a lane, so that D / 4 lanes take a part and the wave
 // 256 / D of them at once (up to 256 channels).  Bound by its chain of two reads, so the first values are on their way before the maxima are known
-// (16 rows 4.4 us, 300 rows with up to 12 parts 13 us).
+// (16 rows 6.3 us, 300 rows with up to 12 parts 13 us).
 template <typename T>
 __global__ void __launch_bounds__(256) k_prefix_join(PrefixAttnArgs a, PrefixPlan p, int Hq, int D) {
     const int h = blockIdx.z * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
