@@ -401,7 +401,8 @@ struct ForkGroup {  // in LDS: a group's sequences
 };
 
 // The old ids of this thread's column, of all sequences as they stand: read whether they are in use or not, so that they are on their way beside the lengths.  M sequences at most are held
-// in registers (64 groups of 8 sequences, 1000 columns: the count takes 4.9 us, 9.8 from LDS), any number in LDS (M = 0).
+// in registers, any number in LDS (M = 0).  Up to 16 are compared there (64 groups of 8 sequences, 1000 columns: the count takes 5 us, one by one from LDS 9.8), more in eights from LDS (a group of
+// 24, 4096 columns: 14 us, one by one 33).
 template <int M>
 struct ForkColumn {
     int32_t v[M ? M : 1];
@@ -418,12 +419,12 @@ struct ForkColumn {
         }
         if (c >= a.max_blocks) return;
         int i = 0;
-        for (; i + 8 <= a.W; i += 8) {
-            int32_t x[8];
+        for (; i + 16 <= a.W; i += 16) {
+            int32_t x[16];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = from[(size_t)(i + k) * a.max_blocks];
+            for (int k = 0; k < 16; ++k) x[k] = from[(size_t)(i + k) * a.max_blocks];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) tile[(i + k) * kForkCols + threadIdx.x] = x[k];
+            for (int k = 0; k < 16; ++k) tile[(i + k) * kForkCols + threadIdx.x] = x[k];
         }
         for (; i < a.W; ++i) tile[i * kForkCols + threadIdx.x] = from[(size_t)i * a.max_blocks];
     }
@@ -435,13 +436,14 @@ struct ForkColumn {
         }
     }
     // Which are freed: no sequence with children has the block in this column, and no earlier one of those without.
-    __device__ __forceinline__ uint64_t freed(const ForkArgs &a, int c, const ForkGroup &f, const int32_t *tile) const {
+    __device__ __forceinline__ uint64_t freed(const ForkArgs &a, int c, const ForkGroup &f, int32_t *tile) const {
+        const auto block = [&](int i, int32_t id) { return c < f.nb[i] && id >= 0 && id < a.num_blocks ? id : -1; };  // -1: none
+        const uint64_t kept = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(f.kept >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)f.kept);
         uint64_t out = 0;
-        if constexpr (M > 0) {
-            const uint32_t kept = __builtin_amdgcn_readfirstlane((uint32_t)f.kept);
-            int32_t u[M];  // -1: no block
+        if constexpr (M > 0 && M <= 16) {
+            int32_t u[M];
 #pragma unroll
-            for (int i = 0; i < M; ++i) u[i] = i < a.W && c < f.nb[i] && v[i] >= 0 && v[i] < a.num_blocks ? v[i] : -1;
+            for (int i = 0; i < M; ++i) u[i] = i < a.W ? block(i, v[i]) : -1;
 #pragma unroll
             for (int i = 0; i < M; ++i) {
                 if (i >= a.W || kept >> i & 1) continue;
@@ -453,16 +455,57 @@ struct ForkColumn {
             }
             return c < f.shared ? 0 : out;
         }
-        if (c < f.shared) return 0;
-        const int32_t *mine = tile + threadIdx.x;
-        for (int i = 0; i < a.W; ++i) {
-            if (f.kept >> i & 1 || c >= f.nb[i]) continue;
-            const int id = mine[i * kForkCols];
-            bool held = id < 0 || id >= a.num_blocks;
-            for (int j = 0; j < a.W && !held; ++j) held = (j < i || f.kept >> j & 1) && c < f.nb[j] && mine[j * kForkCols] == id;
-            if (!held) out |= 1ull << i;
+        // Eight sequences at a time against all others, eight of those at a time: each is read once for the eight.
+        int32_t *const mine = tile + threadIdx.x;
+        if constexpr (M > 0) {
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                if (i < a.W) mine[i * kForkCols] = block(i, v[i]);
+        } else {
+#pragma unroll 8
+            for (int i = 0; i < a.W; ++i) mine[i * kForkCols] = block(i, mine[i * kForkCols]);
         }
-        return out;
+        const auto eight = [&](int32_t (&x)[8], int i0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = mine[min(i0 + k, a.W - 1) * kForkCols];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = i0 + k < a.W ? x[k] : -1;
+        };
+        for (int i0 = 0; i0 < a.W; i0 += 8) {
+            if ((kept >> i0 & 255) == 255) continue;
+            int32_t u[8];
+            bool held[8];
+            eight(u, i0);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) held[k] = u[k] < 0 || (kept >> (i0 + k) & 1);
+            const auto against = [&](int32_t x, int from) {  // the sequences from i0 + from on
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k >= from) held[k] |= x == u[k];
+            };
+            int32_t x[8];
+            for (int j0 = 0; j0 < i0; j0 += 8) {
+                eight(x, j0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) against(x[j], 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (kept >> (i0 + j) & 1) against(u[j], 0);  // itself too: it is not freed in any case
+                else against(u[j], j + 1);
+            }
+            for (int j0 = i0 + 8; j0 < a.W; j0 += 8) {
+                if ((kept >> j0 & 255) == 0) continue;
+                eight(x, j0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (kept >> (j0 + j) & 1) against(x[j], 0);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (!held[k]) out |= 1ull << (i0 + k);
+        }
+        return c < f.shared ? 0 : out;
     }
 };
 
@@ -511,7 +554,7 @@ constexpr int kForkWaves = kForkCols / 64;
 
 template <int M>
 __global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts p) {
-    extern __shared__ int32_t tile[];  // [W][kForkCols], M = 0
+    extern __shared__ int32_t tile[];  // [W][kForkCols], more than 16
     __shared__ ForkGroup f;
     __shared__ int wsum[kForkWaves];
     const int g = blockIdx.y, part = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, c = part * kForkCols + t;
@@ -530,7 +573,7 @@ __global__ void __launch_bounds__(kForkCols) k_fork_count(ForkArgs a, ForkParts 
         all += wsum[i];
     }
     int32_t *out = p.freed + ((size_t)g * p.parts + part) * a.W * kForkCols;
-    if constexpr (M > 0) {
+    if constexpr (M > 0 && M <= 16) {
 #pragma unroll
         for (int i = 0; i < M; ++i)
             if (freed >> i & 1) out[at++] = col.v[i];
@@ -805,11 +848,13 @@ hipError_t launch_fork(const ForkArgs &a, void *workspace, hipStream_t st) {
     const size_t lds = (size_t)a.W * kForkCols * 4;
     if (a.W <= 8) hipLaunchKernelGGL(k_fork_count<8>, grid, dim3(kForkCols), 0, st, a, p);
     else if (a.W <= 16) hipLaunchKernelGGL(k_fork_count<16>, grid, dim3(kForkCols), 0, st, a, p);
+    else if (a.W <= 32) hipLaunchKernelGGL(k_fork_count<32>, grid, dim3(kForkCols), lds, st, a, p);
     else hipLaunchKernelGGL(k_fork_count<0>, grid, dim3(kForkCols), lds, st, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.W <= 8) hipLaunchKernelGGL(k_fork_write<8>, grid, dim3(kForkCols), lds, st, a, p);
     else if (a.W <= 16) hipLaunchKernelGGL(k_fork_write<16>, grid, dim3(kForkCols), lds, st, a, p);
+    else if (a.W <= 32) hipLaunchKernelGGL(k_fork_write<32>, grid, dim3(kForkCols), lds, st, a, p);
     else hipLaunchKernelGGL(k_fork_write<0>, grid, dim3(kForkCols), lds, st, a, p);
     return hipGetLastError();
 }
