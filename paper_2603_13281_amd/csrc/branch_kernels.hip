@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(kForkCols) k_fork_write(ForkArgs a, ForkParts 
     __syncthreads();
     if (f.n_fresh) {
         const int want = start + fresh_before - low;  // the first of them among all freed ids
-        if (run_at < want + f.n_fresh && run_at + run_n > want) {
+        if (run_n > 0 && run_at < want + f.n_fresh && run_at + run_n > want) {  // 0: the thread may have no parts, and n nothing
             const auto find = [&](int i, int count) {
                 for (int j = 0; j < a.W && run_at < want + f.n_fresh && run_at + count > want; ++j) {
                     const int k = fresh_at[j] - low - run_at;
