@@ -174,7 +174,7 @@ def family(rng, groups, width, max_blocks, bk, shared):
 
 
 @pytest.mark.parametrize("bk", [1, 16, 7])
-@pytest.mark.parametrize("groups,width,max_blocks,shared", [(1, 1, 1, 0), (3, 4, 5, 2), (1, 64, 130, 60), (7, 8, 129, 0), (40, 3, 20, 19), (2, 5, 600, 300), (300, 2, 3, 1), (5, 9, 140, 30), (3, 16, 260, 100), (2, 17, 129, 64), (64, 8, 140, 100), (3, 24, 300, 50), (2, 32, 140, 0), (2, 33, 200, 0), (4, 64, 150, 10)])
+@pytest.mark.parametrize("groups,width,max_blocks,shared", [(1, 1, 1, 0), (3, 4, 5, 2), (1, 64, 130, 60), (7, 8, 129, 0), (40, 3, 20, 19), (2, 5, 600, 300), (300, 2, 3, 1), (5, 9, 140, 30), (3, 16, 260, 100), (2, 17, 129, 64), (64, 8, 140, 100), (3, 24, 300, 50), (2, 32, 140, 0), (2, 33, 200, 0), (4, 64, 150, 10), (1100, 2, 3, 0)])
 def test_fork(groups, width, max_blocks, shared, bk):
     print("case:", groups, width, max_blocks, shared, bk, flush=True)
     rng = np.random.default_rng(groups + bk)
