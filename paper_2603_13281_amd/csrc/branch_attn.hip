@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, Prefix
             to_lds16(from0, key + 128 * w, to);
             to_lds16(from0, key + 128 * w + on, to + 1024);
             to_lds16(from1, key + 128 * w, to + 2048);
-            to_lds16(from1, key + 128 * w + on, to + 3072);
+            to_lds16(from1, key + 128 * w + on, to + 3 * 1024);
         } else {
             const char *const from = w & 1 ? from1 : from0;
 #pragma unroll
