@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from dataclasses import dataclass
 
 import numpy as np
@@ -874,13 +875,13 @@ class IcarusLayer:
         n = src.shape[0] if src.dim() else 0
         _need(src, "src", torch.int32, (n,), index)
         _need(dst, "dst", torch.int32, (n,), index)
+        blocks, at, size = self.cfg.num_blocks, array("q"), array("q")
         for t in arrays:
-            if not isinstance(t, torch.Tensor) or t.dim() < 1 or t.get_device() != index or not t.is_contiguous() or t.shape[0] < self.cfg.num_blocks:
-                raise ValueError(f"arrays: need contiguous tensors of at least {self.cfg.num_blocks} blocks on the device of src")
-        k = len(arrays)
-        at = (C.c_void_p * k)(*[t.data_ptr() for t in arrays])
-        size = (C.c_int64 * k)(*[t.stride(0) * t.element_size() if t.dim() > 1 else t.element_size() for t in arrays])
-        self._check(_launch(index, _lib.icarus_copy_blocks, self._h, at, size, k, src.data_ptr(), dst.data_ptr(), n))
+            if not isinstance(t, torch.Tensor) or not t.dim() or t.get_device() != index or t.size(0) < blocks or not t.is_contiguous():
+                raise ValueError(f"arrays: need contiguous tensors of at least {blocks} blocks on the device of src")
+            at.append(t.data_ptr())
+            size.append(t.stride(0) * t.element_size())
+        self._check(_launch(index, _lib.icarus_copy_blocks, self._h, at.buffer_info()[0], size.buffer_info()[0], len(at), src.data_ptr(), dst.data_ptr(), n))
 
     def attn_prefix(self, q, kv_pool, block_tables, kv_lens, row_start, group_start, prefix_lens, out=None, workspace=None):
         """Attention of the rows row_start[s] .. row_start[s + 1] - 1 over sequence s; the leading blocks of prefix_lens[g] tokens that the sequences group_start[g] .. group_start[g + 1] - 1

@@ -714,13 +714,15 @@ __global__ void __launch_bounds__(kForkCols) k_fork_write(ForkArgs a, ForkParts 
 
 // ---- copies of blocks --------------------------------------------------------------------------------------------------------
 constexpr int kCopyArrays = 64, kCopyPiece = 16384, kCopyThreads = 256;
+template <int N>  // in the kernel's arguments: 8 for a few, which the host writes half a microsecond faster, or 64
 struct CopyArrays {
-    uint32_t *at[kCopyArrays];
-    int64_t bytes[kCopyArrays];
+    uint32_t *at[N];
+    int64_t bytes[N];
 };
 // A workgroup to a piece of 16 KB of a block in one array, 16 bytes a lane where the array's blocks begin at multiples of them.  grid: pieces, copies, arrays.  Bound by HBM where there is
 // much to copy: 307 blocks of 64 KB in 8 pools, 322 MB, 55 us, 5.9 TB/s read and written.
-__global__ void __launch_bounds__(kCopyThreads) k_copy_blocks(CopyArrays a, const int32_t *src, const int32_t *dst, int num_blocks) {
+template <int N>
+__global__ void __launch_bounds__(kCopyThreads) k_copy_blocks(CopyArrays<N> a, const int32_t *src, const int32_t *dst, int num_blocks) {
     char *const p = (char *)a.at[blockIdx.z];
     const int64_t bytes = a.bytes[blockIdx.z], first = (int64_t)blockIdx.x * kCopyPiece;
     const int s = src[blockIdx.y], d = dst[blockIdx.y];
@@ -859,22 +861,30 @@ hipError_t launch_fork(const ForkArgs &a, void *workspace, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <int N>
+static hipError_t copy_launches(void *const *arrays, const int64_t *block_bytes, int cnt, const int32_t *src, const int32_t *dst, int n, int num_blocks, hipStream_t st) {
+    CopyArrays<N> c{};
+    int64_t most = 4;
+    for (int i = 0; i < cnt; ++i) {
+        c.at[i] = (uint32_t *)arrays[i];
+        c.bytes[i] = block_bytes[i];
+        most = std::max(most, c.bytes[i]);
+    }
+    const unsigned pieces = (unsigned)((most + kCopyPiece - 1) / kCopyPiece);  // at most 2^16
+    for (int e = 0; e < n; e += 65535) {
+        hipLaunchKernelGGL(k_copy_blocks<N>, dim3(pieces, std::min(65535, n - e), cnt), dim3(kCopyThreads), 0, st, c, src + e, dst + e, num_blocks);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
+}
+
 hipError_t launch_copy_blocks(void *const *arrays, const int64_t *block_bytes, int n_arrays, const int32_t *src, const int32_t *dst, int n, int num_blocks, hipStream_t st) {
-    for (int i0 = 0; i0 < n_arrays; i0 += kCopyArrays) {
-        CopyArrays c{};
-        const int cnt = std::min(kCopyArrays, n_arrays - i0);
-        int64_t most = 4;
-        for (int i = 0; i < cnt; ++i) {
-            c.at[i] = (uint32_t *)arrays[i0 + i];
-            c.bytes[i] = block_bytes[i0 + i];
-            most = std::max(most, c.bytes[i]);
-        }
-        const unsigned pieces = (unsigned)((most + kCopyPiece - 1) / kCopyPiece);  // at most 2^16
-        for (int e = 0; e < n; e += 65535) {
-            hipLaunchKernelGGL(k_copy_blocks, dim3(pieces, std::min(65535, n - e), cnt), dim3(kCopyThreads), 0, st, c, src + e, dst + e, num_blocks);
-            const hipError_t err = hipGetLastError();
-            if (err != hipSuccess) return err;
-        }
+    for (int i = 0; i < n_arrays; i += kCopyArrays) {
+        const int cnt = std::min(kCopyArrays, n_arrays - i);
+        const hipError_t e = cnt <= 8 ? copy_launches<8>(arrays + i, block_bytes + i, cnt, src, dst, n, num_blocks, st)
+                                      : copy_launches<kCopyArrays>(arrays + i, block_bytes + i, cnt, src, dst, n, num_blocks, st);
+        if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
