@@ -18,7 +18,7 @@ struct PrefixUnit { int row0, rows, seq, b0, nb, len, chunks, slot; };  // its r
 struct PrefixItem { int row0, rows, j0, seq, b0, nb, len, slot; };      // j0: the first of its queries among the unit's
 struct PrefixJoin { int row0, rows, n_shared, shared, shared_rows, n_own, own, pad; };  // a sequence's rows; place of part k of row r: shared + k * shared_rows + r, then own + k * rows + r - row0
 constexpr int kPlanThreads = 1024, kMostBlocks = 1024;                   // blocks of an item, at most
-constexpr float kItemCost = 4.f, kAlone = 0.6f, kRounds = 0.7f;          // of the choice of an item's size: an item's cost beside its blocks, in blocks; a last round of at most one to a CU; weight of the rounds
+constexpr float kItemCost = 5.f, kAlone = 0.55f, kRounds = 0.6f;         // of the choice of an item's size: an item's cost beside its blocks, in blocks; a last round of at most one to a CU; weight of the rounds
 
 struct PrefixPlan {
     PrefixUnit *units;  // [G] shared blocks of a group, [S] the rest of a sequence
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
     if (even > 2 * p.step && even < kMostBlocks) {
         // The largest size of an item.  Even shares would be `even` blocks, but a unit is cut into whole items, and a few more than run at once cost a round.  Of sixteen sizes the one is taken
         // whose sum is least, in blocks: all work over the workgroups that run at once, and kRounds times the rounds of the large items, a last round of at most one to a CU counting kAlone.  Over 16
-        // sets of sequences (9 to 140 units, 600 to 25600 blocks) and eleven sizes each, this choice was 1.8 % behind the best one timed, 11 % at most; even shares 5 and 13 %.
+        // sets of sequences (9 to 140 units, 600 to 25600 blocks) and eleven sizes each, called on one state after the other, this choice was 1.8 % behind the best one timed, 7.5 % at most; even shares 3.6 and 11 %.
         if (is_group) size_of[t] = u.nb, at_item[t] = tg_u;
         if (is_seq) size_of[a.G + t] = v.nb, at_item[a.G + t] = tg_v;
         __syncthreads();
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
             const float nb = size_of[i], tg = at_item[i];
             const float chunks = fmaxf(ceilf(nb * inv - 1e-4f), 1.f), size = nb * __builtin_amdgcn_rcpf(chunks), items = nb > 0.f ? tg * chunks : 0.f;
             all_work += items * (size + kItemCost);
-            large += size > 0.4f * most ? items : 0.f;
+            large += size > 0.3f * most ? items : 0.f;
             longest = fmaxf(longest, size);
         }
         const auto over = [&](auto op, float x) {  // the lanes of the same size
@@ -956,7 +956,7 @@ __global__ void __launch_bounds__(256) k_prefix_attn_f32(PrefixAttnArgs a, Prefi
 
 // A row's parts put together, first the parts of the group's shared blocks, then those of its own: a wave to a head, four channels to a lane, so that D / 4 lanes take a part and the wave
 // 256 / D of them at once (up to 256 channels).  Bound by its chain of two reads, so the first values are on their way before the maxima are known
-// (16 rows 6.3 us, 300 rows with up to 12 parts 13 us).
+// (16 rows 4.7 us, 300 rows with up to 12 parts 13 us).
 template <typename T>
 __global__ void __launch_bounds__(256) k_prefix_join(PrefixAttnArgs a, PrefixPlan p, int Hq, int D) {
     const int h = blockIdx.z * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
