@@ -22,10 +22,10 @@ __device__ __forceinline__ uint32_t order_key(float x) {  // larger numbers have
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 // A logit as it counts: NaN as minus infinity, plus infinity as the largest finite number.  The median of three, which is their minimum where one is NaN; by hand, since the compiler takes
-// it for a minimum of the outer two.
+// it for a minimum of the outer two.  A signalling NaN is made a quiet one first: the minimum of it and minus infinity would be a quiet NaN, and the next minimum the largest number.
 __device__ __forceinline__ float clean_logit(float x) {
     float r;
-    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(-INFINITY), "v"(3.402823466e38f));
+    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(__builtin_canonicalizef(x)), "v"(-INFINITY), "v"(3.402823466e38f));
     return r;
 }
 __device__ __forceinline__ float max_of_3(float a, float b, float c) {  // by hand: for fmaxf the compiler first turns what clean_logit gives into itself

@@ -134,6 +134,21 @@ def test_choose_masked_logits():
     layer.close()
 
 
+@pytest.mark.parametrize("dt,patterns", [(torch.float32, (0x7f800001, 0x7fbfffff, 0x7fc00000, -0x7fffff, -0x400001)), (torch.bfloat16, (0x7f81, 0x7fbf, 0x7fc0, -0x7f, -0x41))], ids=str)
+def test_choose_every_kind_of_nan(dt, patterns):
+    """Signalling and quiet ones of either sign count as minus infinity, in the middle of a row and at its end, and where they are all that there is."""
+    layer, rng = make(), np.random.default_rng(4)
+    x = words(rng, 2 * len(patterns), 4099, dt)
+    bits = x.view(torch.int32 if dt is torch.float32 else torch.int16)
+    for i, p in enumerate(patterns):
+        bits[i, [0, 77, 2048, 4096, 4098]] = p
+        bits[len(patterns) + i, :] = p
+    assert torch.isnan(x[:5, 77]).all() and torch.isnan(x[5:]).all()
+    run_choose(layer, x, 2, len(patterns), -rng.random(len(x)))
+    run_choose(layer, x, len(x), 1, -rng.random(len(x)))
+    layer.close()
+
+
 # ---- children -------------------------------------------------------------------------------------------------------------
 
 def run_fork(layer, parents, kv, table, shared, free, used, width):
