@@ -832,7 +832,7 @@ class IcarusLayer:
         m, S = beams, beams.groups * beams.width
         dt = logits.dtype if isinstance(logits, torch.Tensor) else None
         index = _index_of(logits, "logits", dt if dt is torch.bfloat16 else torch.float32)
-        if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]):
+        if logits.dim() != 2 or (logits.shape[0] and logits.shape[1] > 1 and logits.stride(1) != 1) or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]):
             raise ValueError(f"logits: shape {tuple(logits.shape)} with strides {tuple(logits.stride())}, expected rows of contiguous elements")
         R, vocab = logits.shape
         _need(scores, "scores", torch.float32, (S,), index)

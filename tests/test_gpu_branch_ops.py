@@ -149,6 +149,15 @@ def test_choose_every_kind_of_nan(dt, patterns):
     layer.close()
 
 
+def test_choose_without_a_row():
+    """An array of no rows, whatever its strides are."""
+    layer = make()
+    for logits in (torch.zeros(0, 9, device=DEV), torch.zeros(9, 0, device=DEV).t(), torch.tensor(np.zeros((0, 9)), dtype=torch.bfloat16).to(DEV)):
+        run_choose(layer, logits, 2, 2, [-1.0] * 4)
+        run_choose(layer, logits, 2, 2, [-1.0] * 4, row_start=np.zeros(5, dtype=int))
+    layer.close()
+
+
 # ---- children -------------------------------------------------------------------------------------------------------------
 
 def run_fork(layer, parents, kv, table, shared, free, used, width):
