@@ -34,8 +34,8 @@ extern "C" {
  *     scores[beam] + x[t] - log(sum over u of exp(x[u])),   x its row of logits,
  * and the group's best `width` continuations, best first, are its next beams: equal scores go to the lowest beam, then the larger logit, then the lowest token.  A beam that is done has one
  * continuation: itself, with token eos and its score as it is.  The sums are formed in float64, and the scores compared in it.
- * A beam takes the logits of its last row, row_start[beam + 1] - 1, as icarus_stack_decode's seq_next does.  No continuations: a beam without rows, with a row outside 0 .. R - 1 or a
- * score that is not finite; tokens with logits of minus infinity, which NaN counts as.  Plus infinity counts as the largest finite float.
+ * A beam takes the logits of its last row, row_start[beam + 1] - 1, as icarus_stack_decode's seq_next does; one that is done takes none and needs no row.  No continuations: a beam with a score
+ * that is not finite, one that is not done and has no rows or a row outside 0 .. R - 1; tokens with logits of minus infinity, which NaN counts as.  Plus infinity counts as the largest finite float.
  *   logits        device [R, ld], elements of logits_dtype (ICARUS_F32 as icarus_stack_decode gives them, or ICARUS_BF16); ld >= vocab elements between rows
  *   row_start     device int32 [groups * width + 1], or null: beam i has row i
  *   scores        device float [groups * width]

@@ -828,7 +828,7 @@ class IcarusLayer:
 
     def beam_select(self, logits, scores, beams, row_start=None, done=None, eos: int = -1, workspace=None):
         """Best continuations of each group of beams.width beams, into `beams` (a BeamMap).  logits [R, vocab] float32 or bfloat16, rows may be strided; a beam takes its last row of
-        row_start [S + 1], without it beam i has row i.  scores [S] float32, done [S] int32 of the beams now.  Returns beams."""
+        row_start [S + 1], without it beam i has row i; a finished one needs none.  scores [S] float32, done [S] int32 of the beams now.  Returns beams."""
         m, S = beams, beams.groups * beams.width
         dt = logits.dtype if isinstance(logits, torch.Tensor) else None
         index = _index_of(logits, "logits", dt if dt is torch.bfloat16 else torch.float32)

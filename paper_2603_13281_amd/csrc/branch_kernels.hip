@@ -259,8 +259,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a, BeamPa
         const float score = a.scores[s];
         const int done = a.done ? a.done[s] : 0;
         const double2 first = in.sums[(size_t)s * in.parts + min(lane, in.parts - 1)];  // of a beam that is not live: anything
-        int k = beam_row(a, s) >= 0 && score - score == 0.f ? 1 : 0;
-        if (k && done) k = 2;
+        int k = score - score != 0.f ? 0 : done ? 2 : beam_row(a, s) >= 0 ? 1 : 0;  // a finished beam needs no row
         double most = -INFINITY, sum = 0.0;
         if (k == 1) {
             most = lane < in.parts ? first.x : -INFINITY;

@@ -158,6 +158,37 @@ def test_choose_without_a_row():
     layer.close()
 
 
+def last_rows(logits, row_start, scores, done):
+    """What a choice among beams of which some have no row is, as one among beams that all have one: a finished beam needs none, another one without is not live."""
+    rows = [ref.beam_row(row_start, s, len(logits)) for s in range(len(scores))]
+    x = np.stack([logits[r] if r >= 0 else np.zeros(logits.shape[1]) for r in rows])
+    return x, np.array([v if r >= 0 or d else -math.inf for v, r, d in zip(scores, rows, done)], dtype=np.float32)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("groups,width,vocab", [(1, 1, 9), (3, 4, 3001), (2, 20, 20011)])
+def test_choose_finished_beams_without_rows(groups, width, vocab, dt):
+    """A finished beam is its own continuation whether it has a row of logits or not, and where its row lies outside; a live one without a row has none."""
+    print("case:", groups, width, vocab, dt, flush=True)
+    layer, rng = make(), np.random.default_rng(width)
+    S = groups * width
+    done = (np.arange(S) % 3 == 0).astype(int)
+    for start in (np.concatenate([[0], np.cumsum(np.where(done, 0, rng.integers(0, 3, S)))]), np.zeros(S + 1, dtype=int), np.concatenate([[0], np.where(done, 10 ** 6, np.arange(S)) + 1])):
+        scores = (-20 * rng.random(S)).astype(np.float32)
+        if S > 6:
+            scores[6] = -math.inf                                          # finished, and not live all the same
+        logits = words(rng, int(start[start < 10 ** 6].max()), vocab, dt)
+        x, live = last_rows(host(logits), start, scores, done)
+        p, t, v, d, gaps = ref.choose(x, None, live, done, 2, groups, width)
+        assert all(g == 0.0 or g > 2.0 ** -30 for g in gaps)
+        beams = binding.BeamMap(groups, width, DEV)
+        layer.beam_select(logits, torch.tensor(scores, device=DEV), beams, row_start=i32(start), done=i32(done), eos=2)
+        for got, want in zip((beams.parents, beams.tokens, beams.done), (p, t, d)):
+            assert np.array_equal(got.cpu().numpy(), want), (got, want)
+        assert (p >= 0).sum() >= (S > 1) and np.allclose(host(beams.scores)[p >= 0], v[p >= 0], rtol=2.0 ** -23, atol=2.0 ** -34)
+    layer.close()
+
+
 # ---- children -------------------------------------------------------------------------------------------------------------
 
 def run_fork(layer, parents, kv, table, shared, free, used, width):
@@ -735,4 +766,46 @@ def test_two_searches_on_two_streams():
     torch.cuda.synchronize()
     for b, w in zip(loops, want):
         assert _same(_state(b), w)
+    layer.close()
+
+
+def test_finished_beams_that_are_fed_no_more():
+    """A search that gives finished beams no new token, so no row, keeps them, their lengths and their scores until better ones push them out."""
+    layer, rng = make(num_blocks=300), np.random.default_rng(8)
+    groups, width, vocab, eos, cols = 3, 4, 601, 7, 12
+    S = groups * width
+    kv = np.repeat(rng.integers(20, 90, groups), width)
+    table = np.full((S, cols), -1)
+    for s in range(S):
+        table[s, :blocks_of(kv[s], 16)] = s // width * cols + np.arange(blocks_of(kv[s], 16))
+    used, free = i32([groups * cols]), i32(np.arange(300))
+    maps, beams = [binding.ForkMap(groups, width, cols, DEV) for _ in range(2)], [binding.BeamMap(groups, width, DEV) for _ in range(2)]
+    maps[0].kv_lens.copy_(i32(kv))
+    maps[0].block_tables.copy_(i32(table))
+    beams[0].scores.fill_(-math.inf)
+    beams[0].scores[::width] = 0.0
+    beams[0].done.zero_()
+    rows, start, shared = binding.SequenceMap(S, S, DEV), i32(np.arange(S + 1)), i32(kv[::width] // 16)
+    kept = 0
+    for i in range(12):
+        now, nxt, old, new = maps[i & 1], maps[1 - (i & 1)], beams[i & 1], beams[1 - (i & 1)]
+        logits = words(rng, S, vocab, torch.float32)
+        logits[:, eos] += 9.0 * (i in (2, 5))
+        x, live = last_rows(host(logits), start.cpu().numpy(), old.scores.cpu().numpy(), old.done.cpu().numpy())
+        p, t, v, d, _ = ref.choose(x, None, live, old.done.cpu().numpy(), eos, groups, width)
+        layer.beam_select(logits, old.scores, new, row_start=start, done=old.done, eos=eos)
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip((new.parents, new.tokens, new.done), (p, t, d))), i
+        layer.fork_sequences(new.parents, now.kv_lens, now.block_tables, nxt, free, used, shared=shared)
+        used.copy_(nxt.counts[:1])
+        m = layer.extend_sequences(rows, nxt.kv_lens, ((new.parents >= 0) & (new.done == 0)).int(), nxt.block_tables, free, used)
+        used.copy_(m.counts[:1])
+        start = m.row_start.clone()
+        for s in range(S):
+            q = s // width * width + p[s]
+            was = p[s] >= 0 and old.done[q].item()
+            kept += bool(was)
+            assert m.kv_lens[s] == (0 if p[s] < 0 else now.kv_lens[q] + (0 if d[s] else 1))
+            assert not was or (new.scores[s] == old.scores[q] and t[s] == eos and start[s] == start[s + 1])
+        nxt.kv_lens.copy_(m.kv_lens)
+    assert kept > 5
     layer.close()
