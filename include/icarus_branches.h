@@ -8,7 +8,8 @@
  *   icarus_beam_select        logits and scores of a group's beams -> its best continuations: parent, token, score
  *   icarus_fork_sequences     parents -> tables and lengths of the children, blocks that nobody holds any more back to the free list
  *   icarus_copy_blocks        the blocks that two children may not share, in the pools of all layers
- *   icarus_extend_sequences, the layers' projections, icarus_rope_append   (icarus_blocks.h)
+ *   icarus_extend_sequences, the layers' projections, icarus_rope_append   (icarus_blocks.h); new_lens is 0 for children that are empty: they would begin a sequence of their own, with
+ *                             blocks in shared columns, which no fork frees; and it may be 0 for beams that are done
  *   icarus_attn_prefix        attention of single-token rows; the blocks that a group shares are read once for all of its rows
  *
  * As in those headers an icarus_status is returned and icarus_last_error() explains it, the caller owns all device memory and all work goes to the
@@ -52,7 +53,10 @@ icarus_status icarus_beam_select(icarus_ctx *ctx, const void *logits, int32_t lo
 
 /* Sequence i of a group becomes a child of the group's sequence parents[i]: it takes that one's length and table.  A parent outside 0 .. width - 1 leaves it empty (length 0).
  * Whole blocks are shared.  A block that is partly filled goes to its parent's first child; every further child gets a block from the free list and an entry in the list of
- * copies.  (Among the group's shared columns every child gets its own.)
+ * copies.  (Among the group's shared columns every child gets its own.)  So outside the shared columns two sequences that have children may not name the same partly filled block: each would hand
+ * it to its first child, and both children would write to it.  Beams that begin from one context in one live sequence do not, nor do children of earlier forks.  Samples of a prompt that
+ * ends inside a block, tables alike and each its own parent, do: for their first fork shared counts that block's column too, so that every child gets a copy and the block stays the prompt's; from the
+ * second one on it counts the prompt's whole blocks alone, since in a shared column every fork copies again and frees nothing.
  * A block that the old tables name in a column from shared[g] on and below the old length, and that no child's table names in that column, goes back to the free list.
  * Blocks of the columns before shared[g], the common prefix, belong to others and stay theirs.  Sequences may share blocks only within their group and in the same column.
  * The free list is that of icarus_extend_sequences: entries free_ids[*free_used ..] are free.  Freed ids are entered before them, in the order of group, column, sequence (those for which the list has

@@ -850,7 +850,8 @@ class IcarusLayer:
 
     def fork_sequences(self, parents, kv_lens, block_tables, forked, free_ids, free_used, shared=None, workspace=None):
         """Lengths and tables of the children that `parents` names, into `forked` (a ForkMap), and the free list.  shared [groups]: leading columns of the tables that belong to the
-        common prefix.  Returns forked."""
+        common prefix.  Behind them two sequences with children may not name the same partly filled block: for the first fork of samples of one prompt, shared counts the prompt's last block too.
+        Returns forked."""
         S, max_blocks, index = self._table(block_tables)
         m = forked
         if S != m.groups * m.width or max_blocks != m.max_blocks:

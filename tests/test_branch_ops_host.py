@@ -242,3 +242,32 @@ def test_reference_of_the_fork(seed):
     left = set(got["free"][got["counts"][0]:].tolist())
     assert len(left) == num - got["counts"][0] and not left & live
     assert left | live | {b for pre in prefix for b in pre} == set(range(num))
+
+
+@pytest.mark.parametrize("seed", range(4))
+@pytest.mark.parametrize("samples", [False, True])
+def test_reference_of_forks_from_one_prompt(samples, seed):
+    """Beams (children of one live sequence) and samples (each its own parent, the prompt's last block a shared column for the first fork) of a prompt that ends inside a block: no block
+    that a child fills is in two tables or the prompt's, and every block is the prompt's, in a table, or free."""
+    rng = np.random.default_rng(seed)
+    W, bk, cols, num = 5, 4, 12, 90
+    n = 4 * bk + int(rng.integers(1, bk))
+    ids = rng.permutation(num)
+    table = np.full((W, cols), -1)
+    table[:, :5] = ids[:5]
+    prompt = set(ids[:5 if samples else 4].tolist())
+    kv, free, used, parents, shared = np.full(W, n), ids, 5, np.arange(W) if samples else np.zeros(W, dtype=int), 5 if samples else 4
+    for step in range(8):
+        got = ref.fork(parents, kv, table, np.array([shared]), free, used, bk, num, W, np.full((W, cols), -1))
+        kv, table, free, used = got["kv_lens"].copy(), got["block_tables"].copy(), got["free"], int(got["counts"][0])
+        filled = [int(table[s, kv[s] // bk]) for s in range(W) if kv[s] % bk]
+        assert len(filled) == len(set(filled)) and not prompt & set(filled), step
+        for s in np.flatnonzero((kv > 0) & (kv < cols * bk)):
+            if kv[s] % bk == 0:
+                table[s, kv[s] // bk] = free[used]
+                used += 1
+            kv[s] += 1
+        held = {int(b) for s in range(W) for b in table[s, :ref.blocks_of(kv[s], bk)]}
+        left = free[used:].tolist()
+        assert len(left) == len(set(left)) and not (held | prompt) & set(left) and held | prompt | set(left) == set(range(num)), step
+        parents, shared = rng.integers(-1, W, W), 4

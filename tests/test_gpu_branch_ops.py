@@ -710,6 +710,53 @@ def test_a_search_keeps_its_histories(kw):
     layer.close()
 
 
+@pytest.mark.parametrize("samples", [False, True])
+@pytest.mark.parametrize("groups,width,ends", [(1, 3, 1), (5, 8, 0), (4, 20, 15)])
+def test_branches_of_one_prompt(groups, width, ends, samples):
+    """Beams (children of one live sequence) and samples (each its own parent, the prompt's last block a shared column for the first fork) that grow for forty steps, some of them dropped:
+    every sequence holds its own tokens, and every block is a prompt's, in a table, or free, once."""
+    print("case:", groups, width, ends, samples, flush=True)
+    rng, cols = np.random.default_rng(width), 8
+    S = groups * width
+    num = groups * cols + S * cols
+    layer, kv = make(num_blocks=num), np.repeat(16 * rng.integers(1, 4, groups) + ends, width)
+    ids, table, at, prompts, shared = rng.permutation(num), np.full((S, cols), -1), 0, set(), [kv[::width] // 16, -(-kv[::width] // 16) if samples else kv[::width] // 16]
+    for g in range(groups):
+        nb = blocks_of(kv[g * width], 16)
+        table[g * width:(g + 1) * width, :nb] = ids[at:at + nb]
+        prompts |= set(ids[at:at + shared[1][g]].tolist())
+        at += nb
+    text = torch.tensor(rng.integers(0, 10 ** 6, (num, 16)), dtype=torch.int32, device=DEV)
+    words_of = lambda row, n, t: [int(t[row[p // 16], p % 16]) for p in range(n)]
+    history = [words_of(table[s], kv[s], text.cpu().numpy()) for s in range(S)]
+    maps, rows = [binding.ForkMap(groups, width, cols, DEV) for _ in range(2)], binding.SequenceMap(S, S, DEV)
+    maps[0].kv_lens.copy_(i32(kv))
+    maps[0].block_tables.copy_(i32(table))
+    free, used = i32(ids), i32([at])
+    parents = np.arange(S) % width if samples else np.zeros(S, dtype=int)
+    for i in range(40):
+        now, nxt = maps[i & 1], maps[1 - (i & 1)]
+        layer.fork_sequences(i32(parents), now.kv_lens, now.block_tables, nxt, free, used, shared=i32(shared[i == 0]))
+        used.copy_(nxt.counts[:1])
+        layer.copy_blocks([text], nxt.copy_src, nxt.copy_dst)
+        m = layer.extend_sequences(rows, nxt.kv_lens, (nxt.kv_lens > 0).int(), nxt.block_tables, free, used)
+        used.copy_(m.counts[:1])
+        slots = m.row_slot[:int(m.row_start[S])].long()
+        text.view(-1)[slots] = i32(rng.integers(0, 10 ** 6, len(slots)))
+        nxt.kv_lens.copy_(m.kv_lens)
+        n, row, t = m.kv_lens.cpu().numpy(), nxt.block_tables.cpu().numpy(), text.cpu().numpy()
+        grown = [words_of(row[s], n[s], t) for s in range(S)]
+        for s, p in enumerate(parents):
+            assert grown[s][:-1] == (history[s // width * width + p] if p >= 0 else []) and len(grown[s]) != 1, (i, s)
+        history = grown
+        held = {int(b) for s in range(S) for b in row[s, :blocks_of(n[s], 16)]}
+        left = free.cpu().numpy()[int(used.item()):].tolist()
+        assert len(left) == len(set(left)) and not (held | prompts) & set(left) and held | prompts | set(left) == set(range(num)), i
+        parents = np.where(rng.random(S) < 0.9, np.arange(S) % width, rng.integers(-1, width, S))
+        parents[:: width] = [next(iter(np.flatnonzero(n[g * width:(g + 1) * width])), 0) for g in range(groups)]
+    layer.close()
+
+
 @pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(Hq=4, Hkv=4, D=64, bf16=False)], ids=str)
 def test_captured_search_replays(kw):
     """Two searches, each captured once (two steps, one from each set of tables) and replayed in turn with the program's own work between; every replay is the eager
