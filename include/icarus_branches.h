@@ -92,7 +92,7 @@ icarus_status icarus_copy_blocks(icarus_ctx *ctx, void *const *arrays /*host*/, 
  * plus infinity makes NaN.  Rows of no sequence, and of sequences in no group, keep what out holds.  Shared columns count up to the shortest sequence of the group that is not empty.
  *   q             device [R, Hq, D], normed and rotated
  *   kv_lens       device int32 [S], the current token included (negative: 0)
- *   row_start     device int32 [S + 1], not decreasing, within 0 .. R
+ *   row_start     device int32 [S + 1], not decreasing, within 0 .. R (rows that lie outside their group's have no part in what it shares)
  *   group_start   device int32 [G + 1], not decreasing, within 0 .. S
  *   prefix_lens   device int32 [G] (negative: 0)
  *   out           device [R, Hq, D], no memory of q

@@ -54,6 +54,9 @@ __device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t *red, int64_t *t
     return before + x - v;
 }
 
+// The rows of sequence u are among those of its group v.  They are not where row_start decreases: the group's parts have no places for them then.
+__device__ __forceinline__ bool within(const PrefixUnit &u, const PrefixUnit &v) { return u.row0 >= v.row0 && u.row0 + u.rows <= v.row0 + v.rows; }
+
 __global__ void __launch_bounds__(kPlanThreads) k_prefix_plan(PrefixAttnArgs a, PrefixPlan p, int g, int Bk) {
     __shared__ int begin[kPlanThreads], end[kPlanThreads], least[kPlanThreads], first[kPlanThreads], live[kPlanThreads];
     __shared__ int64_t red[kPlanThreads / 64];
@@ -170,7 +173,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_prefix_plan(PrefixAttnArgs a, 
         if (group >= 0) {
             const PrefixUnit u = p.units[a.G + s], v = p.units[group];
             j = PrefixJoin{u.row0, u.rows, v.chunks, v.slot - v.row0, v.rows, u.chunks, u.slot, 0};
-            if (u.len == 0) j.n_shared = j.n_own = 0;  // an empty sequence among others: the shared parts are not its own
+            if (u.len == 0) j.n_shared = j.n_own = 0;      // an empty sequence among others: the shared parts are not its own
+            if (!within(u, v)) j.n_shared = 0;
         }
         p.join[s] = j;
     }
@@ -345,7 +349,7 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
         PrefixJoin j{};
         if (group >= 0) {
             const PrefixUnit &y = units[group];
-            j = PrefixJoin{v.row0, v.rows, len ? y.chunks : 0, y.slot - y.row0, y.rows, len ? v.chunks : 0, v.slot, 0};
+            j = PrefixJoin{v.row0, v.rows, len && within(v, y) ? y.chunks : 0, y.slot - y.row0, y.rows, len ? v.chunks : 0, v.slot, 0};
         }
         p.join[t] = j;
     }

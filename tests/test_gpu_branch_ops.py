@@ -526,6 +526,30 @@ def test_attend_ids_outside_the_pool(kw):
     layer.close()
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(fp8=True), dict(D=64, bf16=False)], ids=str)
+@pytest.mark.parametrize("others", [0, 300, 600])
+def test_attend_row_start_that_decreases(kw, others):
+    """Rows that are not among those of their group have no part in its shared blocks: they attend to their sequence's own, and nothing is read where no part of theirs is.  Workspace and
+    what lies around it hold NaN."""
+    print("case:", kw, others, flush=True)
+    layer = make(num_blocks=200, **kw)
+    c, rng = layer.cfg, np.random.default_rng(6)
+    pool = random_pool(layer, rng)
+    table, kv, row_start, group_start, prefix = crowd(layer, rng, [([10, 60, 3], 640, [5, 130, 40])] + [([0] * others, 16, [0] * others)] * (others > 0), 100)
+    row_start = np.concatenate([[50, 0, 60, 63], np.full(others, 63)])     # the group's rows are 50 .. 62, those of its second sequence 0 .. 59
+    q, (S, cols) = queries(layer, rng, 63, 2.0), table.shape
+    own = np.concatenate([table[:, 40:], np.full((S, 40), -1)], axis=1)
+    want = [ref.attend(host(q), pool_values(layer, pool), t, n, row_start, group_start, 16, np.full(q.shape, 7.0)) for t, n in ((own, kv - 640), (table, kv))]
+    need = binding._lib.icarus_attn_prefix_workspace_bytes(layer._h, S, len(prefix), 63, cols)
+    around = torch.full((need + (2 << 20),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full_like(q, 7.0)
+    layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32(group_start), i32(prefix), out, workspace=around[1 << 20:(1 << 20) + need])
+    torch.cuda.synchronize()
+    for rows, (w, weight, size, count) in ((slice(0, 60), want[0]), (slice(60, 63), want[1])):
+        assert (np.abs(host(out) - w) <= bound(layer, w, weight, size, count))[rows].all(), rows
+    layer.close()
+
+
 def test_prefix_beyond_32_bits():
     """A pool of more than 2^32 elements, read at its end."""
     layer = make(Hq=32, Hkv=8, num_blocks=140000)
