@@ -19,8 +19,8 @@
  *
  * A call takes up to 65535 sequences and groups, 64 sequences in a group that is chosen from or forked, 2^29 rows, 2^30 queries of a kv-head, tables of
  * 2^22 blocks (to fork: 2^17 parts of 128 columns over all groups), vocabularies of 2^24 tokens, 2^29 free ids and 2^20 copies; icarus_attn_prefix about
- * (rows * query heads / 8 + sequences and groups times kv-heads) * (max_blocks / 1024 + 3) < 2^24.  More is ICARUS_ERR_UNSUPPORTED, and a workspace for
- * more has size 0.
+ * (rows * query heads / 8 + sequences and groups times kv-heads) * (max_blocks / 1024 + 3) < 2^24, and fewer than 2^30 parts of rows in its workspace (500 GB).  More is
+ * ICARUS_ERR_UNSUPPORTED, and a workspace for more has size 0.
  */
 #ifndef ICARUS_BRANCHES_H
 #define ICARUS_BRANCHES_H

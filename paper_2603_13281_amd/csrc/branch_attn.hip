@@ -18,6 +18,7 @@ struct PrefixUnit { int row0, rows, seq, b0, nb, len, chunks, slot; };  // its r
 struct PrefixItem { int row0, rows, j0, seq, b0, nb, len, slot; };      // j0: the first of its queries among the unit's
 struct PrefixJoin { int row0, rows, n_shared, shared, shared_rows, n_own, own, pad; };  // a sequence's rows; place of part k of row r: shared + k * shared_rows + r, then own + k * rows + r - row0
 constexpr int kPlanThreads = 1024, kMostBlocks = 1024;                   // blocks of an item, at most
+constexpr int kMostParts = (1 << 30) - 1;                                // where sums of items and parts stop: two of them fit an int, and no workspace holds so many
 constexpr float kItemCost = 5.f, kAlone = 0.55f, kRounds = 0.6f;         // of the choice of an item's size: an item's cost beside its blocks, in blocks; a last round of at most one to a CU; weight of the rounds
 
 struct PrefixPlan {
@@ -182,7 +183,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_prefix_plan(PrefixAttnArgs a, 
 
 // The same for up to THREADS sequences and groups: one of each to a thread, everything in registers and LDS after one round of reads.  Bound by its chain: 8 sequences 5.9 us, 64 sequences of 8
 // groups 8.3 us.
-__device__ __forceinline__ int sat(int64_t v) { return (int)min(v, (int64_t)1 << 30); }
+__device__ __forceinline__ int sat(int64_t v) { return (int)min(v, (int64_t)kMostParts); }
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a, PrefixPlan p, int g, int Bk) {
     constexpr int WAVES = THREADS / 64;
@@ -306,7 +307,7 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int y = __shfl_up(x[k], o, 64);
-            if (lane >= o) x[k] = min(x[k] + y, 1 << 30);
+            if (lane >= o) x[k] = min(x[k] + y, kMostParts);
         }
     if (lane == 63)
 #pragma unroll
@@ -316,10 +317,10 @@ __global__ void __launch_bounds__(THREADS) k_prefix_plan_small(PrefixAttnArgs a,
     for (int k = 0; k < 4; ++k) {
         int before = 0, sum = 0;
         for (int i = 0; i < WAVES; ++i) {
-            if (i < w) before = min(before + red[k][i], 1 << 30);
-            sum = min(sum + red[k][i], 1 << 30);
+            if (i < w) before = min(before + red[k][i], kMostParts);
+            sum = min(sum + red[k][i], kMostParts);
         }
-        x[k] = min(before + x[k], 1 << 30);  // with this thread's own
+        x[k] = min(before + x[k], kMostParts);  // with this thread's own
         all[k] = sum;
     }
     const int64_t item_u = (int64_t)x[0] - n[0], item_v = (int64_t)all[0] + x[1] - n[1], slot_u = (int64_t)x[2] - n[2], slot_v = (int64_t)all[2] + x[3] - n[3];
@@ -1025,7 +1026,7 @@ bool plan_for(const Dims &dm, int S, int G, int R, int max_blocks, PrefixPlan &p
     p.cap_items = (int)items;
     const int64_t most_parts = std::max<int64_t>(p.target * 5 / 3, (int64_t)max_blocks / kMostBlocks + 1) + 2;
     p.cap_slots = std::min<int64_t>(2 * (int64_t)R * most_parts, (int64_t)p.cap_items * (p.tiles * 16 / g + 1));
-    return p.cap_slots <= INT32_MAX;
+    return p.cap_slots < kMostParts;  // heads of 128 alone come near it: 500 GB
 }
 
 }  // namespace

@@ -149,6 +149,15 @@ def test_prefix_attention_refusals():
     layer.close()
 
 
+def test_prefix_attention_workspace_of_most_parts():
+    """A plan counts parts of rows in sums that stop below 2^30; sizes that could reach that are refused, and the largest below it are not."""
+    layer, need = _layer(n_q_heads=1, n_kv_heads=1, head_dim=128), binding._lib.icarus_attn_prefix_workspace_bytes
+    assert need(layer._h, 2, 1, 1 << 28, 10) == 0
+    some = [need(layer._h, 2, 1, r << 20, 10) for r in (1, 16, 64, 128, 168)]  # 6 (R / 128) 129 parts, at most: 2^30 at R = 169.3 * 2^20
+    assert all(0 < a < b for a, b in zip(some, some[1:])) and some[-1] < (1 << 30) * (128 * 4 + 8) * 1.01
+    layer.close()
+
+
 def test_binding_refuses_tensors_of_the_host():
     layer = _layer()
     beams, forked = binding.BeamMap(2, 3, "cpu"), binding.ForkMap(2, 3, 4, "cpu")
