@@ -550,6 +550,81 @@ def test_attend_row_start_that_decreases(kw, others):
     layer.close()
 
 
+def attend_repeated(q, pool, table, kv, row_start, bk, num_blocks):
+    """ref.attend of sequences whose tables name few blocks many times: a block counts as often as it is named."""
+    out, weight, size, count = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape[:2] + (1,)), np.zeros(q.shape[:2] + (1,))
+    hkv, D = pool.shape[1], q.shape[2]
+    g = q.shape[1] // hkv
+    for s, n in enumerate(kv):
+        rows, full = slice(row_start[s], row_start[s + 1]), table[s, :n // bk]
+        ids, times = np.unique(full[(full >= 0) & (full < num_blocks)], return_counts=True)
+        parts = [(b, bk, t) for b, t in zip(ids, times)] + ([(table[s, n // bk], n % bk, 1)] if n % bk and 0 <= table[s, n // bk] < num_blocks else [])
+        times = np.concatenate([np.full(m, t) for _, m, t in parts])
+        for c in range(hkv):
+            k = np.concatenate([pool[b, c, 0].reshape(bk, D)[:m] for b, m, _ in parts])
+            v = np.concatenate([pool[b, c, 1].reshape(D, bk).T[:m] for b, m, _ in parts])
+            qq = q[rows, c * g:(c + 1) * g]
+            sc = qq @ k.T / math.sqrt(D)
+            p = times * np.exp(sc - sc.max(-1, keepdims=True))
+            p /= p.sum(-1, keepdims=True)
+            out[rows, c * g:(c + 1) * g], weight[rows, c * g:(c + 1) * g] = p @ v, p @ np.abs(v)
+            size[rows, c * g:(c + 1) * g] = (np.abs(qq) @ np.abs(k).T).max(-1, keepdims=True) / math.sqrt(D)
+            count[rows, c * g:(c + 1) * g] = times.sum()
+    return out, weight, size, count
+
+
+@pytest.mark.parametrize("kw", [dict(Hq=64, Hkv=64), dict(Hq=64, Hkv=64, fp8=True, k_scale=0.5), dict(Hq=64, Hkv=64, D=64, bf16=False), dict(Hq=64, Hkv=64, bk=32)], ids=str)
+@pytest.mark.parametrize("columns,rows", [(4000, [3]), (4000, [50, 0, 60]), (9001, [40, 1, 30, 29]), (9216, [128])], ids=str)
+def test_attend_items_of_many_blocks(kw, columns, rows):
+    """Items of more than 256 blocks, whose ids are gathered in rounds, and of as many as an item may have; ids outside the pool all over, a last block that is not full.  Few blocks, named
+    many times."""
+    print("case:", kw, columns, rows, flush=True)
+    layer, rng, S = make(num_blocks=50, **kw), np.random.default_rng(columns + len(rows)), len(rows)
+    bk, pool = layer.cfg.block_size, random_pool(layer, rng)
+    table = np.repeat(rng.integers(0, 50, (1, columns)), S, axis=0)
+    if columns % 1024:
+        table[:, rng.random(columns) < 0.1] = -1
+        table[:, 7], table[:, columns - 90] = 50, 2 ** 31 - 1
+    table[:, columns - 8:] = rng.integers(0, 50, (S, 8))                 # behind the shared columns
+    table[-1, columns - 5] = -7 if columns % 1024 else 3
+    kv = columns * bk - 8 * bk + rng.integers(1, 8 * bk, S)
+    kv[0] = columns * bk - 3
+    row_start, q = np.concatenate([[0], np.cumsum(rows)]), queries(layer, rng, sum(rows), 2.0)
+    want = attend_repeated(host(q), pool_values(layer, pool), table, kv, row_start, bk, 50)
+    for prefix in ((columns - 8) * bk + 5, 0):
+        out = layer.attn_prefix(q, pool, i32(table), i32(kv), i32(row_start), i32([0, S]), i32([prefix]))
+        assert (np.abs(host(out) - want[0]) <= bound(layer, *want)).all(), prefix
+    layer.close()
+
+
+@pytest.mark.parametrize("kw,first", [(kw, first) for kw in (dict(Hq=4, Hkv=1), dict(Hq=4, Hkv=1, fp8=True), dict(Hq=4, Hkv=1, D=64, bf16=False), dict(Hq=2, Hkv=1, D=256))
+                                      for first in ("growing", "minus infinity", "shrinking") if not ("fp8" in kw and first == "minus infinity")], ids=str)  # no infinity among the codes
+@pytest.mark.parametrize("prefix", [0, 330 * 16])
+def test_attend_rows_of_many_parts(kw, first, prefix):
+    """More than 64 parts to a row, which are joined in rounds: scores that grow along the sequence, so that each round outweighs the ones before, that are minus infinity in the first round, and
+    that shrink."""
+    print("case:", kw, first, prefix, flush=True)
+    layer, rng = make(num_blocks=1300, **kw), np.random.default_rng(1)
+    c, pool = layer.cfg, random_pool(layer, rng)
+    ids = rng.permutation(1300)
+    table = np.stack([ids[:640], np.concatenate([ids[:330], ids[640:950]])])
+    if not prefix:
+        table, kv, row_start, group_start = table[:1], [640 * 16 - 5], [0, 3], [0, 1]
+    else:
+        kv, row_start, group_start = [640 * 16 - 5, 600 * 16 + 1], [0, 3, 5], [0, 2]
+    q = queries(layer, rng, row_start[-1])
+    q[:, :, 0] = 4.0
+    for row in table:                                                       # channel 0 of the keys: scores rise to 4 * 40 / sqrt(D) and more
+        x = np.arange(640)[:, None] / 640 * 40.0
+        x = {"growing": x, "shrinking": 40.0 - x, "minus infinity": np.where(np.arange(640)[:, None] < 300, -math.inf, x)}[first]
+        keys = pool.view(1300, 1, 2, 16, c.head_dim)[:, :, 0]
+        there = torch.tensor(row.copy(), device=DEV)
+        values = torch.tensor(x, dtype=torch.float32, device=DEV).expand(640, 16)
+        keys[there, 0, :, 0] = values.to(torch.float8_e4m3fn).view(torch.uint8) if c.kv_fp8 else values.to(c.torch_dtype)
+    run_attend(layer, q, pool, table, np.array(kv), np.array(row_start), np.array(group_start), np.array([prefix]))
+    layer.close()
+
+
 def test_prefix_beyond_32_bits():
     """A pool of more than 2^32 elements, read at its end."""
     layer = make(Hq=32, Hkv=8, num_blocks=140000)
