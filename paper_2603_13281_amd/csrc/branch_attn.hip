@@ -9,7 +9,6 @@
 #include "branch_ops.h"
 
 #include <algorithm>
-#include <atomic>
 
 namespace icarus {
 namespace {
@@ -58,6 +57,8 @@ __device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t *red, int64_t *t
 // The rows of sequence u are among those of its group v.  They are not where row_start decreases: the group's parts have no places for them then.
 __device__ __forceinline__ bool within(const PrefixUnit &u, const PrefixUnit &v) { return u.row0 >= v.row0 && u.row0 + u.rows <= v.row0 + v.rows; }
 
+// For more than 512 sequences or groups.  Items have even shares, their sizes are not weighed as k_prefix_plan_small does: sequences of two rows and up to 500 tokens of their own behind one prefix of
+// 8192, us of plan and items: 520 of them here 15 + 298, 500 there 14 + 307; eight groups behind 1024 to 8192 tokens, up to nine rows, 520 16 + 474, 496 13 + 423 for a seventh less of the products.
 __global__ void __launch_bounds__(kPlanThreads) k_prefix_plan(PrefixAttnArgs a, PrefixPlan p, int g, int Bk) {
     __shared__ int begin[kPlanThreads], end[kPlanThreads], least[kPlanThreads], first[kPlanThreads], live[kPlanThreads];
     __shared__ int64_t red[kPlanThreads / 64];
@@ -526,7 +527,7 @@ __device__ __forceinline__ void prefix_product(PrefixState &st, const PrefixWeig
 // groups, 135 MB in 31 us, 4.4 TB/s (23 %).  8 groups with tails of up to 2000 tokens: both in turn, 451 MB and 29 GFLOP in 113 us, 4.0 TB/s (30 %).  1000 queries over 8192 tokens: 35 GFLOP, half
 // as many again for the weights' second part, in 68 us (44 %).  1150 queries over two FP8 prefixes of 32768 tokens: 157 GFLOP in 184 us, 0.85 PFLOP/s (45 %), where a large product of bf16 in
 // the library reaches 1.23; products alone between the barriers keep the pipe 72 to 80 % busy, the rest goes to the codes' conversion, to LDS and to the older of a CU's two workgroups, which is
-// served first and leaves the younger one alone for the last third.
+// served first and leaves the younger one alone for the last third.  With bf16 values 38 registers spill (34 where DIRECT): none within the loops of whole groups, but the walk's end reads some back.
 template <bool KV8, bool DIRECT>  // DIRECT: an item is a whole sequence, and the sums go to out
 __global__ void __launch_bounds__(256, 2) k_prefix_attn(PrefixAttnArgs a, PrefixPlan p, int Hq, int Hkv, float scale_log2, float v_scale) {
     constexpr int SLOTS = kSlots<KV8>, BYTES = kGroupBytes<KV8>, ES = KV8 ? 1 : 2;
@@ -812,7 +813,8 @@ bool on_matrix_cores(const Dims &dm) { return dm.bf16 && dm.D == kD && dm.Bk == 
 // For float32, head sizes other than 128 and blocks of more than 16 tokens.  An item has a tile of 16 queries; a wave takes sixteen tokens of a block in turn.  Products of 16 x 16 x 4 with the
 // transposed operands, see k_block_attn_f32: scores of keys [token][channel] times queries [channel][query] leave lane t + 16 p query t's scores of tokens 4 p .. 4 p + 3, which are
 // at once the right operand of the values' product, so nothing passes through LDS until the waves join.  Bound by the float32 products, a sixteenth of the 16-bit rate, where there are many
-// queries; in a short call by its chain (3 sequences of up to 130 tokens, 4 heads of 64: 6 us).
+// queries; in a short call by its chain (3 sequences of up to 130 tokens, 4 heads of 64: 6 us).  32 query and 8 kv-heads, 128 sequences over 8192 tokens, 256 rows: float32 heads of 128, 35 GFLOP, 463 us;
+// bf16 heads of 64 230 us, of 256 1606, blocks of 32 tokens 420, where the 16-bit products take 68 for blocks of 16.
 template <typename T, typename KT, int DT, bool EXACT, bool DIRECT>  // tiles of 16 channels: at most DT, or DT exactly
 __global__ void __launch_bounds__(256) k_prefix_attn_f32(PrefixAttnArgs a, PrefixPlan p, int Hq, int Hkv, int D_, int Bk, float scale_log2, float v_scale) {
     typedef typename Quad<KT>::raw Raw;

@@ -34,7 +34,7 @@ __device__ __forceinline__ float max_of_3(float a, float b, float c) {  // by ha
     return r;
 }
 
-// exp(d) for d <= 0, to 2^-39 of itself (and 0 where it is below 2^-1000): exp(d) = 2^n exp(r), |r| <= ln 2 / 2, the polynomial that meets exp at the nine Chebyshev nodes of that interval.
+// exp(d) for d <= 0, to 2^-39 of itself; below -700, minus infinity included, 2^-1010, which no sum of ours notices: exp(d) = 2^n exp(r), |r| <= ln 2 / 2, the polynomial that meets exp at the nine Chebyshev nodes of that interval.
 __device__ __forceinline__ double exp_of(double d) {
     d = fmax(d, -700.0);
     const double n = rint(d * 1.4426950408889634074), r = __builtin_fma(n, -0.69314718055994530942, d);
@@ -104,8 +104,10 @@ struct BeamParts {
     int parts;
 };
 
-// Bound by arithmetic, not by its one pass over the logits: 460 rows of 128256 float32 logits (236 MB) take 63 us, without the exponentials 40 (5.9 TB/s), without the candidates 53.  A logit
-// costs 17 instructions of float64 and six others.  (Skipping the cleaning and the limit of ordinary logits, three of the 17, changed nothing; more waves to a SIMD spill or wait: 66 -> 76.)
+// A workgroup loads its part, then adds up exponentials, then ranks, and with few rounds of workgroups these phases do not hide one another: 460 rows of 128256 float32 logits (236 MB) take 66 us,
+// nearer the sum than the larger one of the read (without the exponentials 40 us, 5.9 TB/s) and the arithmetic (17 instructions of float64 to a logit, 26 us at the full rate, and seven others);
+// without the candidates 53.  Instructions alone are not what bounds it: three of the 17 less changed nothing.  More waves to a SIMD spill or wait (66 -> 76).  120 rows of 50021 bfloat16 logits (12 MB)
+// take 13.6 us in one round of 840 workgroups: the chain of one of them.
 template <typename T, int PER>  // logits of a thread
 __global__ void __launch_bounds__(kBeamThreads) k_beam_part(BeamArgs a, BeamParts out) {
     constexpr int VE = 16 / sizeof(T), NV = PER / VE;
@@ -377,14 +379,15 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a, BeamPa
 }
 
 // Parts of 8192 logits, of 2048 where those would be fewer than 128 workgroups.  Rows of 128256, us of both kernels with small and large parts: 4 rows 10.5, 11.1; 16 rows 20.1, 14.0; 32 rows
-// 25.5, 16.2 -- the merge reads what the parts leave.  Parts of 4096: 460 rows 76.8 + 10.9 for 66.3 + 7.7.
+// 25.5, 16.2 -- the merge reads what the parts leave.  Parts of 4096: 460 rows 76.8 + 10.9 for 66.3 + 7.7.  All float32; bfloat16 and other vocabularies were not timed for this choice.
 constexpr int kBeamFew = 8, kBeamMany = 32;
 int beam_parts(int vocab, int per) { return (int)(((int64_t)vocab + kBeamThreads * per - 1) / (kBeamThreads * per)); }
 int beam_per(int G, int W, int vocab) { return (int64_t)G * W * beam_parts(vocab, kBeamMany) >= 128 ? kBeamMany : kBeamFew; }
 
 // ---- children ------------------------------------------------------------------------------------------------------------------
-// Bound by their chains, not by their bytes: lengths and parents, the column's ids, what the parts have freed; then the ids of the fresh blocks (one group of 8 beams, 2048 columns, 4.5 + 6.2 us;
-// 64 groups, 1000 columns, 5.0 + 8.6 us).  Two launches over parts of 128 columns of a group's tables, a thread to a column.  k_fork_count finds the blocks that no child holds: in a column, of the old sequences that nobody
+// Bound by their chains, not by their bytes: lengths and parents, the column's ids, what the parts have freed; then the ids of the fresh blocks (one group of 8 beams, 2048 columns, 4.6 + 6.1 us;
+// 64 groups, 1000 columns, 5.1 + 8.8 us).  Over 16 beams by the comparisons of a column's thread, on few CUs (a group of 24, 4096 columns, 32 workgroups, 14.4 + 13.8 us; of 64 50.9 + 27.1).
+// Every workgroup of the second launch adds up the counts of all parts, which counts from thousands of parts on: 31264 of them (32 groups of 2, 125000 columns) 28 + 1295 us.  Two launches over parts of 128 columns of a group's tables, a thread to a column.  k_fork_count finds the blocks that no child holds: in a column, of the old sequences that nobody
 // continues, the ids that none of the continued ones names.  k_fork_write adds up the parts before its own, enters the freed ids, and writes the children's tables.
 struct ForkParts {
     int32_t *freed_n;  // [G * parts]
